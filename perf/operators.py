@@ -186,7 +186,7 @@ def prepare(case, seed):
         st["meta0"] = meta.clone()
         if own:
             st["cca"] = _handle(hk, hk, dh)
-            st["ws"] = st["cca"].alloc_cache4_workspace(B, S)
+            st["ws"] = st["cca"].alloc_qcache_workspace(B, S)
         return st
 
     hq = case["hq"]
@@ -207,7 +207,7 @@ def prepare(case, seed):
     cache["len"].copy_(torch.tensor(_lens(case), dtype=torch.int32, device="cuda"))
     if own:
         st["cca"] = _handle(hq, hk, dh)
-        st["ws"] = st["cca"].alloc_cache4_workspace(B, S)
+        st["ws"] = st["cca"].alloc_qcache_workspace(B, S)
     return st
 
 
@@ -224,7 +224,7 @@ def _attend(st):
     """The new tokens' queries over the cached rows; every row's weight grows by what it was given."""
     q, cache, case = st["q"], st["cache"], st["case"]
     if own:
-        o = st["cca"].cache4_attention(q, cache, case["S"], st["ws"])
+        o = st["cca"].qcache_attention(q, cache, case["S"], st["ws"])
         return {"o": o, "weight": cache["weight"]}
     hk, dh, S = case["hk"], case["dh"], case["S"]
     k, v = (_values(c, s) for c, s in zip(st["codes"], st["scales"]))
@@ -241,8 +241,8 @@ def _append(st):
     """New rows into the cache, and the values that it now holds for them."""
     cache, case = st["cache"], st["case"]
     if own:
-        st["cca"].cache4_append(cache, st["k"], st["v"], st["position"])
-        k, v = st["cca"].cache4_read(cache, case["n"])
+        st["cca"].qcache_append(cache, st["k"], st["v"], st["position"])
+        k, v = st["cca"].qcache_read(cache, case["n"])
         return {"k": k, "v": v, "weight": cache["weight"], "position": cache["position"]}
     n, hk, dev = case["n"], case["hk"], st["k"].device
     row = (cache["len"].view(-1, 1) + torch.arange(n, device=dev)).long()                  # [B, n]
@@ -265,7 +265,7 @@ def _evict(st):
     cache, case = st["cache"], st["case"]
     st["meta"].copy_(st["meta0"])            # weights, positions and lengths as the steps before left them
     if own:
-        st["cca"].cache4_evict(cache, case["keep"], case["recent"], st["next"], case["S"], st["ws"])
+        st["cca"].qcache_evict(cache, case["keep"], case["recent"], st["next"], case["S"], st["ws"])
         return cache
     S, keep = case["S"], case["keep"]
     weight, position, length = cache["weight"], cache["position"], cache["len"]
@@ -291,7 +291,7 @@ def _linear(st):
     """Tokens through a layer with 4-bit weights."""
     dtype = getattr(torch, st["case"]["out"])
     if own:
-        return st["cca"].linear4(st["packed"], st["x"], out_dtype=dtype)
+        return st["cca"].qlinear(st["packed"], st["x"], out_dtype=dtype)
     return (st["x"].float() @ _values(st["codes"], st["scales"]).t()).to(dtype)
 
 
