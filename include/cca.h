@@ -271,6 +271,105 @@ int cca_mla_workspace_size(const cca_handle* h, const cca_mla_dims* m, int64_t B
 int cca_mla_forward(cca_handle* h, const cca_mla_dims* m, const cca_mla_weights* w, const void* x, void* out, void* workspace,
                     size_t workspace_bytes, int64_t B, int64_t S, void* cuda_stream);
 
+/* ---- Cache and weights in 4 bits (serving) ---------------------------------------------------------
+ * The paper's decode keeps 2 B S E / C2 cached numbers and reads every weight once per token; here both take 4.5 bits a
+ * number.  Format, for cache rows and weight rows alike: groups of 32 channels share a bf16 scale s = bf16(max|x| / 7) (division in
+ * fp32, round to nearest); a channel is c * s with the whole number c = clamp(rint(x / s), -7, 7), 0 where s is 0 (a group of
+ * zeros, or one whose s would be below the smallest normal number).  An infinity or NaN makes its whole group NaN.  The kernels take
+ * values up to 2^60 in magnitude.  A code is 4 bits in sign and magnitude, two to a byte: bit 7 | bits 0-2 and bit 6 | bits 3-5.
+ * A row of d channels is cut into blocks of min(d, 128) channels = G groups, 16 G bytes: byte 2 G i + 2 grp + j (i < 8, j < 2) holds
+ * channel 32 grp + 4 i + j (bits 7, 0-2) and channel 32 grp + 4 i + 2 + j (bits 6, 3-5).
+ *
+ * No call here allocates or synchronises; every call may be captured into a graph.  Calls that share a cache or a workspace are
+ * ordered by the caller.  The caller's current device is left as it was. */
+typedef struct {
+  void* k_codes;        /* uint8 [B, h_k, S_max, d_h / 2]: keys after norm, temperature and RoPE (Eq. 11)            */
+  void* v_codes;        /* uint8 [B, h_k, S_max, d_h / 2]: values (Eq. 10)                                           */
+  void* k_scales;       /* bf16 [B, h_k, S_max, d_h / 32]                                                            */
+  void* v_scales;       /* bf16 [B, h_k, S_max, d_h / 32]                                                            */
+  float* weight;        /* fp32 [B, h_k, S_max]: attention weight each row has gathered; may be null (then no eviction) */
+  int32_t* position;    /* int32 [B, h_k, S_max]: position of each row's token; may be null (then no eviction)       */
+  int32_t* len;         /* int32 [B]: rows held, the same for every head; cca_qcache_evict alone writes it           */
+  int64_t S_max;        /* capacity in rows                                                                          */
+} cca_qcache;
+
+/* Puts n new tokens of every sequence into the cache: k, v device bf16 [B, n, h_k, d_h]; row len[b] + i gets token i, weight 0 and
+ * position position[b] + i (its row's index where `position` is null).  count (device int32 [B], may be null): sequence b has
+ * only the first min(count[b], n) of them, a padded batch.  len is not advanced: the caller does that, as with pos of a decode
+ * step.  A sequence whose rows would pass S_max, or whose length or position is negative, is left as it is, and the device status
+ * word becomes 121.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int cca_qcache_append(cca_handle* h, const void* k, const void* v, const int32_t* position, const int32_t* count,
+                      const cca_qcache* cache, int64_t B, int64_t n, void* cuda_stream);
+
+/* The values that rows first[b] .. first[b] + n - 1 (len[b] .. where `first` is null) stand for: k, v device fp32 [B, n, h_k, d_h];
+ * zeros for rows outside the capacity.  Errors as above. */
+int cca_qcache_read(cca_handle* h, const cca_qcache* cache, const int32_t* first, float* k, float* v, int64_t B, int64_t n,
+                    void* cuda_stream);
+
+/* Bytes of device workspace that one cca_qcache_attention or cca_qcache_evict call needs (one size for both) for caches of at most
+ * max_len rows.  Depends on the device's SM count as cca_decode_workspace_size does.  B <= 65535, B * max_len <= 2^30. */
+int cca_qcache_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
+
+/* softmax(q k^T / sqrt(d_h)) v (Eq. 11, third line) of one query token per sequence over its len[b] rows: q, o device bf16
+ * [B, h_q, d_h].  accumulate != 0: weight[b, j, r] grows by what row r got of the attention, summed over the query heads of kv head
+ * j; each row's sum is formed in a fixed order.  A sequence without rows gets zeros.  max_len: host-side bound, len[b] <= max_len <=
+ * S_max; a sequence outside it is skipped (its output is left as it is) and the status word becomes 121.
+ * Rows behind len[b] may hold anything.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE_TOO_SMALL, CUDA. */
+int cca_qcache_attention(cca_handle* h, const void* q, void* o, const cca_qcache* cache, int64_t max_len, int accumulate,
+                         void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream);
+
+/* Cuts every sequence with more than `keep` rows down to `keep`, for each kv head on its own.  The rows that stay are the first
+ * `keep` in this order: rows whose position is at least next_position[b] - recent, then by falling weight (a NaN counts as
+ * lowest), and among equals the lower row first.  A row behind the first `keep` that stays moves into the place of one that goes, both taken in
+ * ascending order; nothing else moves, so the order of the rows is not that of their positions.  Writes len[b] = keep for those
+ * sequences; what lies behind is left as it is.  next_position: device int32 [B].  0 <= recent <= keep.
+ * len[b] <= max_len <= S_max as above.  Errors as above. */
+int cca_qcache_evict(cca_handle* h, const cca_qcache* cache, int64_t keep, int64_t recent, const int32_t* next_position,
+                     int64_t max_len, void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream);
+
+/* A weight matrix [N, K] (K a multiple of 32): tiles of 16 rows by 128 columns, padded with zeros; codes uint8 [ceil(N / 16),
+ * ceil(K / 128), 16, 64], scales bf16 [ceil(N / 16), ceil(K / 128), 16, 4], a tile's row being one block of the format. */
+typedef struct {
+  const void* codes;
+  const void* scales;
+  int64_t N, K;
+} cca_qlinear_weights;
+int cca_qlinear_sizes(int64_t N, int64_t K, size_t* code_bytes, size_t* scale_bytes);
+/* Quantises w (device bf16 [N, K]) into out->codes, out->scales, whose sizes cca_qlinear_sizes gives. */
+int cca_qlinear_pack(cca_handle* h, const void* w, const cca_qlinear_weights* out, void* cuda_stream);
+/* out = x W^T for M tokens: x device bf16 [M, K], out device [M, N], fp32 if out_f32 else bf16.  fp32 accumulation, one rounding at
+ * the end.  Meant for the tokens of a decode step; M <= 65535.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int cca_qlinear(cca_handle* h, const cca_qlinear_weights* w, const void* x, void* out, int out_f32, int64_t M, void* cuda_stream);
+
+/* The decode step on 4-bit projections and a 4-bit cache. */
+typedef struct {
+  cca_qlinear_weights w_qkv;   /* [L + L_k/2, E]: rows of w_qk, then of w_v1 (Eq. 7, 10)                             */
+  cca_qlinear_weights w_vp;    /* [L_k/2, E]: w_v2, the value projection of x_{t-1}                                  */
+  cca_qlinear_weights w_o;     /* [E, L_q]                                                                           */
+  const void* conv0_w;         /* as in cca_weights                                                                  */
+  const void* conv1_w;
+  const float* temp;
+} cca_q_weights;
+typedef struct {
+  cca_qcache cache;
+  void* qk0_hist;       /* as in cca_decode_state                                                                    */
+  void* x_prev;
+  const int32_t* pos;   /* int32 [B], device: position of each sequence's new token.  After an eviction it is larger than the
+                           number of cached rows, and may be larger than S_max                                       */
+} cca_q_decode_state;
+int cca_decode_workspace_size_q(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
+/* cca_decode_step with the new key and value quantised into row len[b] and attention over len[b] + 1 rows (the new one as it is
+ * cached); the weights are gathered where cache.weight is set.  The caller advances pos and len after the step.  max_len: len[b] + 1
+ * <= max_len <= S_max.  A sequence outside it, or with a negative position, is skipped: nothing of its state is written, its output
+ * row is undefined, and the status word becomes 121.  Limits and errors as cca_decode_step, except that every number of query heads
+ * per kv head is covered. */
+int cca_decode_step_q(cca_handle* h, const cca_q_weights* w, const void* x, void* out, const cca_q_decode_state* state,
+                      int64_t max_len, void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream);
+/* cca_decode_state_from_prefill for a 4-bit cache: appends the S keys and values (positions = row indexes; len must be 0 for
+ * them to be the tokens' own) and fills the history and previous input.  The caller then sets len = pos = S. */
+int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B,
+                                    int64_t S, const cca_q_decode_state* state, void* cuda_stream);
+
 /* Select kernel implementations: 0 = plain SIMT kernels, 1 = tcgen05/TMA kernels where they
  * exist (default).  Returns the previous value. */
 int cca_set_impl(cca_handle* h, int impl);
@@ -302,7 +401,7 @@ int64_t cca_launch_count(const cca_handle* h);
 
 /* After the caller has synchronised the stream: copies the device status word.  0 = no error;
  * otherwise the code written by a kernel whose bounded wait expired (101..105 by role, 109 from
- * cca_wait_selftest; or 120: a decode step met a position outside its cache).  Returns
+ * cca_wait_selftest; 120: a decode step met a position outside its cache; 121: a sequence's rows do not fit its 4-bit cache).  Returns
  * CCA_ERR_DEVICE_TIMEOUT if it is non-zero, and clears the word. */
 int cca_last_status(cca_handle* h, int* device_status);
 

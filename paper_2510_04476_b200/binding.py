@@ -61,6 +61,26 @@ class cca_decode_state(C.Structure):
                 ("pos", C.c_void_p), ("S_max", C.c_int64)]
 
 
+QCACHE_TENSORS = ("k_codes", "v_codes", "k_scales", "v_scales", "weight", "position", "len")
+
+
+class cca_qcache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in QCACHE_TENSORS] + [("S_max", C.c_int64)]
+
+
+class cca_qlinear_weights(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("N", C.c_int64), ("K", C.c_int64)]
+
+
+class cca_q_weights(C.Structure):
+    _fields_ = [(n, cca_qlinear_weights) for n in ("w_qkv", "w_vp", "w_o")] + \
+               [(n, C.c_void_p) for n in ("conv0_w", "conv1_w", "temp")]
+
+
+class cca_q_decode_state(C.Structure):
+    _fields_ = [("cache", cca_qcache), ("qk0_hist", C.c_void_p), ("x_prev", C.c_void_p), ("pos", C.c_void_p)]
+
+
 # name -> (restype, argtypes); also the list of symbols the header declares
 SYMBOLS = {
     "cca_init": (C.c_int, [C.POINTER(cca_config), C.c_int, C.POINTER(C.c_void_p)]),
@@ -87,6 +107,23 @@ SYMBOLS = {
     "cca_mla_workspace_size": (C.c_int, [C.c_void_p, C.POINTER(cca_mla_dims), C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
     "cca_mla_forward": (C.c_int, [C.c_void_p, C.POINTER(cca_mla_dims), C.POINTER(cca_mla_weights), C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_size_t, C.c_int64, C.c_int64, C.c_void_p]),
+    "cca_qcache_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(cca_qcache), C.c_int64,
+                                    C.c_int64, C.c_void_p]),
+    "cca_qcache_read": (C.c_int, [C.c_void_p, C.POINTER(cca_qcache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
+                                  C.c_void_p]),
+    "cca_qcache_workspace_size": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "cca_qcache_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(cca_qcache), C.c_int64, C.c_int, C.c_void_p,
+                                       C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_qcache_evict": (C.c_int, [C.c_void_p, C.POINTER(cca_qcache), C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                   C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_qlinear_sizes": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "cca_qlinear_pack": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(cca_qlinear_weights), C.c_void_p]),
+    "cca_qlinear": (C.c_int, [C.c_void_p, C.POINTER(cca_qlinear_weights), C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]),
+    "cca_decode_workspace_size_q": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "cca_decode_step_q": (C.c_int, [C.c_void_p, C.POINTER(cca_q_weights), C.c_void_p, C.c_void_p, C.POINTER(cca_q_decode_state),
+                                    C.c_int64, C.c_void_p, C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_decode_state_from_prefill_q": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64, C.c_int64,
+                                                  C.POINTER(cca_q_decode_state), C.c_void_p]),
     "cca_set_impl": (C.c_int, [C.c_void_p, C.c_int]),
     "cca_set_attention_events": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "cca_set_stage_events": (C.c_int, [C.c_void_p, C.POINTER(C.c_void_p), C.c_int]),
@@ -367,6 +404,205 @@ class CCA:
         st = C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
         _check(self.lib, self.lib.cca_decode_state_from_prefill(self.handle, _ptr(x), wp, wn, B, S, C.byref(ds), st),
                self.handle, "cca_decode_state_from_prefill")
+
+    # ---- cache and weights in 4 bits ------------------------------------------------------
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _need(self, t, name: str, dtype, shape):
+        """Argument check of the 4-bit entry points: a contiguous tensor of this type and shape on the handle's device."""
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            raise CcaError(f"{name}: wants a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, got {t.dtype} "
+                           f"{tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _q_ws(self, ws: torch.Tensor):
+        if ws.device != self.device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+            raise CcaError(f"workspace: wants a contiguous uint8 tensor on {self.device}, got {ws.dtype} on {ws.device}")
+        return self._ws_ptr(ws)
+
+    def new_qcache(self, B: int, S_max: int) -> Dict[str, torch.Tensor]:
+        """Caller-owned tensors of cca_qcache for B empty sequences."""
+        hk, dh, dev = self.cfg.n_kv_heads, self.cfg.head_dim, self.device
+        cache = {"weight": torch.zeros(B, hk, S_max, dtype=torch.float32, device=dev),
+                 "position": torch.zeros(B, hk, S_max, dtype=torch.int32, device=dev),
+                 "len": torch.zeros(B, dtype=torch.int32, device=dev)}
+        for n in ("k", "v"):
+            cache[n + "_codes"] = torch.zeros(B, hk, S_max, dh // 2, dtype=torch.uint8, device=dev)
+            cache[n + "_scales"] = torch.zeros(B, hk, S_max, dh // 32, dtype=torch.bfloat16, device=dev)
+        return cache
+
+    def _qcache(self, cache: Dict[str, torch.Tensor]):
+        """(cca_qcache, B) of a dict as new_qcache makes it; "weight" and "position" may be absent."""
+        hk, dh = self.cfg.n_kv_heads, self.cfg.head_dim
+        B, S = cache["len"].shape[0], cache["k_codes"].shape[2]
+        c = cca_qcache()
+        rows = (B, hk, S)
+        codes, scales = rows + (dh // 2,), rows + (dh // 32,)
+        c.k_codes = self._need(cache["k_codes"], "k_codes", torch.uint8, codes)
+        c.v_codes = self._need(cache["v_codes"], "v_codes", torch.uint8, codes)
+        c.k_scales = self._need(cache["k_scales"], "k_scales", torch.bfloat16, scales)
+        c.v_scales = self._need(cache["v_scales"], "v_scales", torch.bfloat16, scales)
+        if cache.get("weight") is not None:
+            c.weight = self._need(cache["weight"], "weight", torch.float32, rows)
+        if cache.get("position") is not None:
+            c.position = self._need(cache["position"], "position", torch.int32, rows)
+        c.len = self._need(cache["len"], "len", torch.int32, (B,))
+        c.S_max = S
+        return c, B
+
+    def qcache_append(self, cache, k: torch.Tensor, v: torch.Tensor, position: Optional[torch.Tensor] = None,
+                      count: Optional[torch.Tensor] = None):
+        """cca_qcache_append: k, v [B, n, h_k, d_h] into rows len[b] .. ; `len` is the caller's to advance."""
+        c, B = self._qcache(cache)
+        n = k.shape[1]
+        shape = (B, n, self.cfg.n_kv_heads, self.cfg.head_dim)
+        _check(self.lib, self.lib.cca_qcache_append(
+            self.handle, self._need(k, "k", torch.bfloat16, shape), self._need(v, "v", torch.bfloat16, shape),
+            None if position is None else self._need(position, "position", torch.int32, (B,)),
+            None if count is None else self._need(count, "count", torch.int32, (B,)), C.byref(c), B, n, self._stream()),
+            self.handle, "cca_qcache_append")
+
+    def qcache_read(self, cache, n: int, first: Optional[torch.Tensor] = None):
+        """cca_qcache_read: the values (k, v), fp32 [B, n, h_k, d_h], of rows first[b] .. (default: len[b] ..)."""
+        c, B = self._qcache(cache)
+        k = torch.empty(B, n, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=torch.float32, device=self.device)
+        v = torch.empty_like(k)
+        _check(self.lib, self.lib.cca_qcache_read(
+            self.handle, C.byref(c), None if first is None else self._need(first, "first", torch.int32, (B,)), k.data_ptr(),
+            v.data_ptr(), B, n, self._stream()), self.handle, "cca_qcache_read")
+        return k, v
+
+    def qcache_workspace_size(self, B: int, max_len: int) -> int:
+        n = C.c_size_t()
+        _check(self.lib, self.lib.cca_qcache_workspace_size(self.handle, B, max_len, C.byref(n)), self.handle,
+               "cca_qcache_workspace_size")
+        return int(n.value)
+
+    def alloc_qcache_workspace(self, B: int, max_len: int) -> torch.Tensor:
+        return torch.empty(self.qcache_workspace_size(B, max_len) + 256, dtype=torch.uint8, device=self.device)
+
+    def qcache_attention(self, q: torch.Tensor, cache, max_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None,
+                         accumulate: Optional[bool] = None):
+        """cca_qcache_attention: q [B, h_q, d_h] -> o over each sequence's len[b] rows.  accumulate=None: gather the weights
+        if the cache has them."""
+        c, B = self._qcache(cache)
+        shape = (B, self.cfg.n_q_heads, self.cfg.head_dim)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        if accumulate is None:
+            accumulate = cache.get("weight") is not None
+        wp, wn = self._q_ws(workspace)
+        _check(self.lib, self.lib.cca_qcache_attention(
+            self.handle, self._need(q, "q", torch.bfloat16, shape), self._need(out, "out", torch.bfloat16, shape), C.byref(c),
+            max_len, int(accumulate), wp, wn, B, self._stream()), self.handle, "cca_qcache_attention")
+        return out
+
+    def qcache_evict(self, cache, keep: int, recent: int, next_position: torch.Tensor, max_len: int, workspace: torch.Tensor):
+        """cca_qcache_evict: in place, `len` included."""
+        c, B = self._qcache(cache)
+        wp, wn = self._q_ws(workspace)
+        _check(self.lib, self.lib.cca_qcache_evict(
+            self.handle, C.byref(c), keep, recent, self._need(next_position, "next_position", torch.int32, (B,)), max_len, wp, wn, B,
+            self._stream()), self.handle, "cca_qcache_evict")
+
+    def qlinear_pack(self, w: torch.Tensor) -> Dict[str, object]:
+        """A bf16 weight matrix [N, K] in the 4-bit tiles of cca_qlinear_weights."""
+        N, K = w.shape
+        code_bytes, scale_bytes = C.c_size_t(), C.c_size_t()
+        _check(self.lib, self.lib.cca_qlinear_sizes(N, K, C.byref(code_bytes), C.byref(scale_bytes)), None, "cca_qlinear_sizes")
+        shape = ((N + 15) // 16, (K + 127) // 128, 16)
+        out = {"codes": torch.empty(shape + (64,), dtype=torch.uint8, device=self.device),
+               "scales": torch.empty(shape + (4,), dtype=torch.bfloat16, device=self.device), "N": N, "K": K}
+        assert out["codes"].numel() == code_bytes.value and 2 * out["scales"].numel() == scale_bytes.value
+        cw = self._qlinear(out)
+        _check(self.lib, self.lib.cca_qlinear_pack(self.handle, self._need(w, "w", torch.bfloat16, (N, K)), C.byref(cw), self._stream()),
+               self.handle, "cca_qlinear_pack")
+        return out
+
+    def _qlinear(self, w) -> cca_qlinear_weights:
+        N, K = w["N"], w["K"]
+        shape = ((N + 15) // 16, (K + 127) // 128, 16)
+        return cca_qlinear_weights(self._need(w["codes"], "codes", torch.uint8, shape + (64,)),
+                                   self._need(w["scales"], "scales", torch.bfloat16, shape + (4,)), N, K)
+
+    def qlinear(self, w, x: torch.Tensor, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16):
+        """cca_qlinear: x [M, K] bf16 -> [M, N] (bf16 or fp32, that of `out` where it is given)."""
+        M = x.shape[0]
+        if out is None:
+            out = torch.empty(M, w["N"], dtype=out_dtype, device=self.device)
+        if out.dtype not in (torch.bfloat16, torch.float32):
+            raise CcaError(f"cca_qlinear: output type {out.dtype}")
+        cw = self._qlinear(w)
+        _check(self.lib, self.lib.cca_qlinear(self.handle, C.byref(cw), self._need(x, "x", torch.bfloat16, (M, w["K"])),
+                                              self._need(out, "out", out.dtype, (M, w["N"])), int(out.dtype is torch.float32), M,
+                                              self._stream()), self.handle, "cca_qlinear")
+        return out
+
+    def pack_weights_q(self, w: Dict[str, torch.Tensor]) -> Dict[str, object]:
+        """The block's weights for decode_step_q: projections in 4 bits, the rest as it is."""
+        return {"w_qkv": self.qlinear_pack(torch.cat([w["w_qk"], w["w_v1"]], dim=0)), "w_vp": self.qlinear_pack(w["w_v2"]),
+                "w_o": self.qlinear_pack(w["w_o"]), **{n: w.get(n) for n in ("conv0_w", "conv1_w", "temp")}}
+
+    def _q_weights(self, w) -> cca_q_weights:
+        cw = cca_q_weights()
+        for n in ("w_qkv", "w_vp", "w_o"):
+            setattr(cw, n, self._qlinear(w[n]))
+        c = self.cfg
+        L = (c.n_q_heads + c.n_kv_heads) * c.head_dim
+        shapes = {"conv0_w": (L, c.k_seq), "conv1_w": (L, c.head_dim, c.k_ch), "temp": (c.n_kv_heads,)}
+        for n, shape in shapes.items():
+            if w.get(n) is not None:
+                setattr(cw, n, self._need(w[n], n, torch.float32 if n == "temp" else torch.bfloat16, shape))
+        return cw
+
+    def new_decode_state_q(self, B: int, S_max: int) -> Dict[str, object]:
+        """Caller-owned tensors of cca_q_decode_state for B empty sequences: "cache" (new_qcache), history, previous input, "pos"."""
+        s = self.new_decode_state(B, 1)
+        return {"cache": self.new_qcache(B, S_max), **{n: s[n] for n in ("qk0_hist", "x_prev", "pos")}}
+
+    def _decode_state_q(self, state):
+        s = cca_q_decode_state()
+        s.cache, B = self._qcache(state["cache"])
+        c = self.cfg
+        pad, L = c.k_seq + c.k_ch - 2, (c.n_q_heads + c.n_kv_heads) * c.head_dim
+        if pad:
+            s.qk0_hist = self._need(state["qk0_hist"], "qk0_hist", torch.float32, (B, pad, L))
+        s.x_prev = self._need(state["x_prev"], "x_prev", torch.bfloat16, (B, c.d_model))
+        s.pos = self._need(state["pos"], "pos", torch.int32, (B,))
+        return s, B
+
+    def decode_workspace_size_q(self, B: int, max_len: int) -> int:
+        n = C.c_size_t()
+        _check(self.lib, self.lib.cca_decode_workspace_size_q(self.handle, B, max_len, C.byref(n)), self.handle,
+               "cca_decode_workspace_size_q")
+        return int(n.value)
+
+    def alloc_decode_workspace_q(self, B: int, max_len: int) -> torch.Tensor:
+        return torch.empty(self.decode_workspace_size_q(B, max_len) + 256, dtype=torch.uint8, device=self.device)
+
+    def decode_step_q(self, w, x: torch.Tensor, state, max_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None):
+        """cca_decode_step_q: x [B, E] -> out [B, E]; the state is updated in place except `pos` and the cache's `len`, which the
+        caller advances.  w: pack_weights_q."""
+        ds, B = self._decode_state_q(state)
+        shape = (B, self.cfg.d_model)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        cw = self._q_weights(w)
+        wp, wn = self._q_ws(workspace)
+        _check(self.lib, self.lib.cca_decode_step_q(
+            self.handle, C.byref(cw), self._need(x, "x", torch.bfloat16, shape), self._need(out, "out", torch.bfloat16, shape),
+            C.byref(ds), max_len, wp, wn, B, self._stream()), self.handle, "cca_decode_step_q")
+        return out
+
+    def decode_state_from_prefill_q(self, x: torch.Tensor, workspace: torch.Tensor, state):
+        """cca_decode_state_from_prefill_q: the keys and values a forward of x left in `workspace` go into the 4-bit cache."""
+        ds, B = self._decode_state_q(state)
+        S = x.shape[1]
+        wp, wn = self._q_ws(workspace)
+        _check(self.lib, self.lib.cca_decode_state_from_prefill_q(
+            self.handle, self._need(x, "x", torch.bfloat16, (B, S, self.cfg.d_model)), wp, wn, B, S, C.byref(ds), self._stream()),
+            self.handle, "cca_decode_state_from_prefill_q")
 
     def backward(self, w, x: torch.Tensor, d_out: torch.Tensor, workspace: torch.Tensor, separate_grads: bool = False):
         """Returns (d_x bf16, dict of fp32 parameter gradients).  separate_grads: give every gradient a buffer of

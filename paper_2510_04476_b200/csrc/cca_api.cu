@@ -7,6 +7,8 @@
 #include "../../include/cca.h"
 #include "common.cuh"
 #include "decode.cuh"
+#include "qcache.cuh"
+#include "qlinear.cuh"
 #include "tc_kernels.cuh"
 #include "tc_ptx.cuh"
 
@@ -439,6 +441,26 @@ int cca_decode_step(cca_handle* h, const cca_weights* w, const void* x, void* ou
   return CCA_OK;
 }
 
+namespace {
+// What a decode step needs of the tokens before it besides their keys and values, from a forward's input and workspace.
+int copy_token_state(cca_handle* h, const CcaDims& d, const Layout& l, const void* x, const char* ws, int64_t B, int64_t S,
+                     void* x_prev, void* qk0_hist, cudaStream_t st) {
+  const int pad = d.k_seq + d.k_ch - 2;
+  // previous input: the last token of every sequence (rows S-1 of x, one strided copy)
+  CU(cudaMemcpy2DAsync(x_prev, (size_t)d.E * 2, (const char*)x + (size_t)(S - 1) * d.E * 2, (size_t)S * d.E * 2,
+                       (size_t)d.E * 2, (size_t)B, cudaMemcpyDeviceToDevice, st));
+  if (pad > 0) {
+    const size_t row = (size_t)d.L * 4;
+    const int64_t n = S < pad ? S : pad;
+    CU(cudaMemsetAsync(qk0_hist, 0, (size_t)B * pad * row, st));
+    CU(cudaMemcpy2DAsync((char*)qk0_hist + (size_t)(pad - n) * row, (size_t)pad * row,
+                         ws + l.qk0 + (size_t)(S - n) * row, (size_t)S * row, (size_t)n * row, (size_t)B,
+                         cudaMemcpyDeviceToDevice, st));
+  }
+  return CCA_OK;
+}
+}  // namespace
+
 int cca_decode_state_from_prefill(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes,
                                   int64_t B, int64_t S, const cca_decode_state* s, void* cuda_stream) {
   int r = check_sizes(h, B, S, true);
@@ -463,18 +485,7 @@ int cca_decode_state_from_prefill(cca_handle* h, const void* x, const void* work
     CU(cudaMemcpyAsync((char*)s->v_cache + (size_t)b * s->S_max * row_k, ws + l.v + (size_t)b * S * row_k, (size_t)S * row_k,
                        cudaMemcpyDeviceToDevice, st));
   }
-  // previous input: the last token of every sequence (rows S-1 of x, one strided copy)
-  CU(cudaMemcpy2DAsync(s->x_prev, (size_t)d.E * 2, (const char*)x + (size_t)(S - 1) * d.E * 2, (size_t)S * d.E * 2,
-                       (size_t)d.E * 2, (size_t)B, cudaMemcpyDeviceToDevice, st));
-  if (pad > 0) {
-    const size_t row = (size_t)d.L * 4;
-    const int64_t n = S < pad ? S : pad;
-    CU(cudaMemsetAsync(s->qk0_hist, 0, (size_t)B * pad * row, st));
-    CU(cudaMemcpy2DAsync((char*)s->qk0_hist + (size_t)(pad - n) * row, (size_t)pad * row,
-                         ws + l.qk0 + (size_t)(S - n) * row, (size_t)S * row, (size_t)n * row, (size_t)B,
-                         cudaMemcpyDeviceToDevice, st));
-  }
-  return CCA_OK;
+  return copy_token_state(h, d, l, x, ws, B, S, s->x_prev, s->qk0_hist, st);
 }
 
 int cca_forward(cca_handle* h, const cca_weights* w, const void* x, void* out, void* workspace,
@@ -1128,6 +1139,226 @@ int cca_forward_static(cca_handle* h, const cca_weights* w, const void* x, void*
   // Every region of the forward workspace is written in full before it is read, so the previous call's
   // contents need no clearing.  Passing exactly the forward-only size keeps the fp32 copy of o off.
   return cca_forward(h, w, x, out, ws, l.saved_end, B, S, 0, cuda_stream);
+}
+
+// ---- 4-bit cache and weights -------------------------------------------------------------------
+namespace {
+// The caller's current device is left as it was.
+struct OnDevice {
+  int before = -1;
+  cudaError_t enter(int device) {
+    int now = 0;
+    cudaError_t e = cudaGetDevice(&now);
+    if (e != cudaSuccess || now == device) return e;
+    e = cudaSetDevice(device);
+    if (e == cudaSuccess) before = now;
+    return e;
+  }
+  ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
+constexpr int64_t Q_MAX_BATCH = 65535;          // a grid dimension
+
+int check_qcache(const cca_handle* h, const cca_qcache* c, int64_t B) {
+  if (!h || !c || B < 1 || h->device < 0) return CCA_ERR_INVALID_ARG;
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !c->len || c->S_max < 1) return CCA_ERR_INVALID_ARG;
+  if (B > Q_MAX_BATCH || c->S_max > (int64_t)1 << 24) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_scales) || !aligned16(c->v_scales)) return CCA_ERR_ALIGNMENT;
+  return CCA_OK;
+}
+QCache make_qcache(const cca_qcache* c) {
+  return QCache{(uint8_t*)c->k_codes, (uint8_t*)c->v_codes, (bf16*)c->k_scales, (bf16*)c->v_scales, c->weight, c->position, c->len, c->S_max};
+}
+int check_qrows(int64_t B, int64_t max_len) {   // B sequences of up to max_len rows
+  if (B < 1 || max_len < 1) return CCA_ERR_INVALID_ARG;
+  if (B > Q_MAX_BATCH || max_len > (int64_t)1 << 24 || B * max_len > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
+  return CCA_OK;
+}
+int enqueued(cca_handle* h, int r) {
+  if (r < 0) { h->last_cuda = -r; return CCA_ERR_CUDA; }
+  return r > 0 ? CCA_ERR_UNSUPPORTED : CCA_OK;
+}
+int check_qlinear(const cca_qlinear_weights* w) {
+  if (!w || !w->codes || !w->scales) return CCA_ERR_INVALID_ARG;
+  if (!aligned16(w->codes) || !aligned16(w->scales)) return CCA_ERR_ALIGNMENT;
+  return CCA_OK;
+}
+int check_qlinear_size(int64_t N, int64_t K) {
+  if (N < 1 || K < 1) return CCA_ERR_INVALID_ARG;
+  if (K % 32 || N > (int64_t)1 << 24 || K > (int64_t)1 << 20) return CCA_ERR_UNSUPPORTED;
+  return CCA_OK;
+}
+}  // namespace
+
+int cca_qcache_append(cca_handle* h, const void* k, const void* v, const int32_t* position, const int32_t* count,
+                      const cca_qcache* c, int64_t B, int64_t n, void* cuda_stream) {
+  int r = check_qcache(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!k || !v || n < 1) return CCA_ERR_INVALID_ARG;
+  if (n > c->S_max) return CCA_ERR_INVALID_ARG;
+  if (B * n > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v)) return CCA_ERR_ALIGNMENT;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qcache_append(make_dims(h->cfg, B, 1), (const bf16*)k, (const bf16*)v, position, count, make_qcache(c), n,
+                                          c->S_max, h->d_status, &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_qcache_read(cca_handle* h, const cca_qcache* c, const int32_t* first, float* k, float* v, int64_t B, int64_t n, void* cuda_stream) {
+  int r = check_qcache(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!k || !v || n < 1) return CCA_ERR_INVALID_ARG;
+  if (n > (int64_t)1 << 24 || B * n > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v)) return CCA_ERR_ALIGNMENT;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qcache_read(make_dims(h->cfg, B, 1), make_qcache(c), first, k, v, n, &h->launches,
+                                        (cudaStream_t)cuda_stream));
+}
+
+int cca_qcache_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
+  if (!h || !bytes) return CCA_ERR_INVALID_ARG;
+  const int r = check_qrows(B, max_len);
+  if (r != CCA_OK) return r;
+  *bytes = qcache_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
+  return CCA_OK;
+}
+
+int cca_qcache_attention(cca_handle* h, const void* q, void* o, const cca_qcache* c, int64_t max_len, int accumulate, void* workspace,
+                         size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  int r = check_qcache(h, c, B);
+  if (r != CCA_OK) return r;
+  if ((r = check_qrows(B, max_len)) != CCA_OK) return r;
+  if (!q || !o || !workspace || max_len > c->S_max || (accumulate && !c->weight)) return CCA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(o) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CCA_ERR_ALIGNMENT;
+  const CcaDims d = make_dims(h->cfg, B, 1);
+  if (workspace_bytes < qcache_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qcache_attention(d, (const bf16*)q, nullptr, (bf16*)o, make_qcache(c), nullptr, 0, (int)max_len, accumulate,
+                                             workspace, h->sm_count, h->d_status, &h->launches, h->ev_attn_begin,
+                                             h->ev_attn_end, (cudaStream_t)cuda_stream));
+}
+
+int cca_qcache_evict(cca_handle* h, const cca_qcache* c, int64_t keep, int64_t recent, const int32_t* next_position, int64_t max_len,
+                     void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  int r = check_qcache(h, c, B);
+  if (r != CCA_OK) return r;
+  if ((r = check_qrows(B, max_len)) != CCA_OK) return r;
+  if (!c->weight || !c->position || !next_position || !workspace || max_len > c->S_max) return CCA_ERR_INVALID_ARG;
+  if (keep < 0 || recent < 0 || recent > keep || keep > ((int64_t)1 << 24)) return CCA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return CCA_ERR_ALIGNMENT;
+  const CcaDims d = make_dims(h->cfg, B, 1);
+  if (workspace_bytes < qcache_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qcache_evict(d, make_qcache(c), (int)keep, (int)recent, next_position, (int)max_len, workspace, h->d_status,
+                                         &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_qlinear_sizes(int64_t N, int64_t K, size_t* code_bytes, size_t* scale_bytes) {
+  if (!code_bytes || !scale_bytes) return CCA_ERR_INVALID_ARG;
+  const int r = check_qlinear_size(N, K);
+  if (r != CCA_OK) return r;
+  *code_bytes = qlinear_code_bytes(N, K);
+  *scale_bytes = qlinear_scale_bytes(N, K);
+  return CCA_OK;
+}
+
+int cca_qlinear_pack(cca_handle* h, const void* w, const cca_qlinear_weights* out, void* cuda_stream) {
+  if (!h || h->device < 0 || !w) return CCA_ERR_INVALID_ARG;
+  int r = check_qlinear(out);
+  if (r != CCA_OK) return r;
+  if ((r = check_qlinear_size(out->N, out->K)) != CCA_OK) return r;
+  if (!aligned16(w)) return CCA_ERR_ALIGNMENT;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qlinear_pack((const bf16*)w, (uint8_t*)out->codes, (bf16*)out->scales, (int)out->N, (int)out->K,
+                                         &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_qlinear(cca_handle* h, const cca_qlinear_weights* w, const void* x, void* out, int out_f32, int64_t M, void* cuda_stream) {
+  if (!h || h->device < 0 || !x || !out || M < 1) return CCA_ERR_INVALID_ARG;
+  int r = check_qlinear(w);
+  if (r != CCA_OK) return r;
+  if ((r = check_qlinear_size(w->N, w->K)) != CCA_OK) return r;
+  if (M > 65535) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(x) || !aligned16(out)) return CCA_ERR_ALIGNMENT;
+  QLinArgs a;
+  memset(&a, 0, sizeof(a));
+  a.n_seg = 1;
+  a.seg[0] = QLinSeg{(const uint8_t*)w->codes, (const bf16*)w->scales, (const bf16*)x, (int)w->N, 0};
+  a.K = (int)w->K; a.M = (int)M; a.ldo = (int)w->N;
+  if (out_f32) a.out_f32 = (float*)out;
+  else a.out_bf16 = (bf16*)out;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_qlinear(a, h->sm_count, &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_decode_workspace_size_q(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
+  if (!h || !bytes) return CCA_ERR_INVALID_ARG;
+  const int r = check_qrows(B, max_len);
+  if (r != CCA_OK) return r;
+  *bytes = decode_q_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
+  return CCA_OK;
+}
+
+int cca_decode_step_q(cca_handle* h, const cca_q_weights* w, const void* x, void* out, const cca_q_decode_state* s, int64_t max_len,
+                      void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  if (!w || !s) return CCA_ERR_INVALID_ARG;
+  int r = check_qcache(h, &s->cache, B);
+  if (r != CCA_OK) return r;
+  if ((r = check_qrows(B, max_len)) != CCA_OK) return r;
+  const cca_config& c = h->cfg;
+  const CcaDims d = make_dims(c, B, 1);
+  if (!x || !out || !workspace || !s->x_prev || !s->pos || max_len > s->cache.S_max) return CCA_ERR_INVALID_ARG;
+  if (c.k_seq + c.k_ch > 2 && !s->qk0_hist) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_CONV1) && !w->conv0_w) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_CONV2) && !w->conv1_w) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_QK_NORM) && !w->temp) return CCA_ERR_INVALID_ARG;
+  if (!c.causal || d.Lk % 8 || d.E % 32 || d.Lq % 32) return CCA_ERR_UNSUPPORTED;
+  if ((r = check_qlinear(&w->w_qkv)) != CCA_OK || (r = check_qlinear(&w->w_vp)) != CCA_OK || (r = check_qlinear(&w->w_o)) != CCA_OK)
+    return r;
+  if (w->w_qkv.N != d.L + d.Lk / 2 || w->w_qkv.K != d.E || w->w_vp.N != d.Lk / 2 || w->w_vp.K != d.E || w->w_o.N != d.E ||
+      w->w_o.K != d.Lq)
+    return CCA_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(out) || !aligned16(s->x_prev) || ((c.flags & CCA_CONV2) && !aligned16(w->conv1_w)) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return CCA_ERR_ALIGNMENT;
+  if (workspace_bytes < decode_q_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  const DecodeQWeights dw{(const uint8_t*)w->w_qkv.codes, (const uint8_t*)w->w_vp.codes, (const uint8_t*)w->w_o.codes,
+                          (const bf16*)w->w_qkv.scales, (const bf16*)w->w_vp.scales, (const bf16*)w->w_o.scales,
+                          (const bf16*)w->conv0_w, (const bf16*)w->conv1_w, w->temp};
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_decode_step_q(d, dw, (const bf16*)x, (bf16*)out, make_qcache(&s->cache), (float*)s->qk0_hist,
+                                          (bf16*)s->x_prev, s->pos, (int)max_len, workspace, h->sm_count, h->d_status,
+                                          &h->launches, h->ev_attn_begin, h->ev_attn_end, (cudaStream_t)cuda_stream));
+}
+
+int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B, int64_t S,
+                                    const cca_q_decode_state* s, void* cuda_stream) {
+  if (!s) return CCA_ERR_INVALID_ARG;
+  int r = check_qcache(h, &s->cache, B);
+  if (r != CCA_OK) return r;
+  if ((r = check_sizes(h, B, S, true)) != CCA_OK) return r;
+  const cca_config& c = h->cfg;
+  const int pad = c.k_seq + c.k_ch - 2;
+  if (!x || !workspace || !s->x_prev || (pad > 0 && !s->qk0_hist) || S > s->cache.S_max) return CCA_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(s->x_prev) || (pad > 0 && !aligned16(s->qk0_hist)) || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return CCA_ERR_ALIGNMENT;
+  const Layout l = make_layout(c, B, S);
+  if (workspace_bytes < l.saved_end) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  OnDevice on;
+  CU(on.enter(h->device));
+  const CcaDims d = make_dims(c, B, S);
+  const char* ws = (const char*)workspace;
+  r = enqueued(h, launch_qcache_append(make_dims(c, B, 1), (const bf16*)(ws + l.k), (const bf16*)(ws + l.v), nullptr, nullptr,
+                                       make_qcache(&s->cache), S, s->cache.S_max, h->d_status, &h->launches,
+                                       (cudaStream_t)cuda_stream));
+  if (r != CCA_OK) return r;
+  return copy_token_state(h, d, l, x, ws, B, S, s->x_prev, s->qk0_hist, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

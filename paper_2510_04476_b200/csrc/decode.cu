@@ -18,31 +18,11 @@
 
 #include "common.cuh"
 #include "decode.cuh"
+#include "pdl.cuh"
+#include "qcache.cuh"
+#include "qlinear.cuh"
 
 namespace {
-
-// Programmatic dependent launch: every kernel of the step lets the next one be scheduled as soon as all of its own
-// CTAs have started, and waits for the kernel before it (completion and visibility of its writes) before it touches
-// global memory.  The wait comes first in every CTA, also in those that return early, so that "kernel N complete"
-// always implies "kernel N - 1 complete".
-CCA_DEVINL void pdl_enter() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-template <typename... KArgs, typename... Args>
-cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t st, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = 0;
-  cfg.stream = st;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
 
 constexpr unsigned F_CONV1 = 1, F_CONV2 = 2, F_QK_MEAN = 4, F_V_SHIFT = 8, F_QK_NORM = 16, F_ROPE = 32;
 constexpr int ST_DECODE_BAD_POSITION = 120;
@@ -158,6 +138,19 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) decode_proj_kernel(ProjArgs a) 
 // ------------------------------------------------------------------------------------------------ transforms
 // Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
 // the history for the next token and the input the next step's value shift needs.
+// Where a step's new key and value go: row pos[b] of the bf16 caches or, on a 4-bit cache (qlen set), row b of a staging area
+// from which they are quantised.  False: this sequence's position or length does not fit its cache.
+CCA_DEVINL bool new_row(const int* pos, const int* qlen, long long S_max, int max_len, int b, int& t, size_t& row) {
+  t = pos[b];
+  if (qlen != nullptr) {
+    const int n = qlen[b];
+    row = (size_t)b;
+    return t >= 0 && n >= 0 && n < S_max && n < max_len;
+  }
+  row = (size_t)b * S_max + t;
+  return t >= 0 && t < S_max && t < max_len;
+}
+
 struct C1Args {
   CcaDims d;
   const float* lat;      // [B, L + Lk]: q0 | k0 | v1 | v2 of the new token
@@ -169,6 +162,7 @@ struct C1Args {
   float* hist;           // [B, pad, L]
   bf16* x_prev;          // [B, E]
   const int* pos;
+  const int* qlen;       // rows of the 4-bit cache, or null
   long long S_max;
   int max_len;
   int* status;
@@ -178,9 +172,10 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
   pdl_enter();
   const CcaDims& d = a.d;
   const int b = blockIdx.y, tid = threadIdx.x;
-  const int t = a.pos[b];
-  if (t < 0 || t >= a.S_max || t >= a.max_len) {
-    if (tid == 0 && blockIdx.x == 0) atomicCAS(a.status, 0, ST_DECODE_BAD_POSITION);
+  int t;
+  size_t row;
+  if (!new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)) {
+    if (tid == 0 && blockIdx.x == 0) atomicCAS(a.status, 0, a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
     return;
   }
   const int ld_lat = d.L + d.Lk;
@@ -197,13 +192,13 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
       if (r < pad) win[r] = a.hist[((size_t)b * pad + r) * d.L + ch];
     win[pad] = lat_b[ch];
     for (int r = 0; r < kc; ++r) {
-      const int row = pad - (kc - 1) + r;
+      const int at = pad - (kc - 1) + r;
       float acc;
       if (d.flags & F_CONV1) {
         acc = 0.f;
-        for (int j = 0; j < ks; ++j) acc = fmaf(__bfloat162float(a.w0[(size_t)ch * d.k_seq + j]), win[row - (ks - 1) + j], acc);
+        for (int j = 0; j < ks; ++j) acc = fmaf(__bfloat162float(a.w0[(size_t)ch * d.k_seq + j]), win[at - (ks - 1) + j], acc);
       } else {
-        acc = win[row];
+        acc = win[at];
       }
       if (d.flags & F_CONV2) a.y1s[((size_t)b * d.L + ch) * kc + r] = __float2bfloat16(acc);
       else a.y2[(size_t)b * d.L + ch] = acc;
@@ -213,7 +208,7 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
       if (r < pad) a.hist[((size_t)b * pad + r) * d.L + ch] = win[r + 1];
   }
   for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256)
-    a.v_cache[((size_t)b * a.S_max + t) * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
+    a.v_cache[row * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
   for (int c = blockIdx.x * 256 + tid; c < d.E / 8; c += gridDim.x * 256)
     reinterpret_cast<uint4*>(a.x_prev + (size_t)b * d.E)[c] = reinterpret_cast<const uint4*>(a.x + (size_t)b * d.E)[c];
 }
@@ -228,6 +223,7 @@ struct FnArgs {
   float* q;              // [B, Lq]
   bf16* k_cache;
   const int* pos;
+  const int* qlen;       // as in C1Args
   long long S_max;
   int max_len;
 };
@@ -241,8 +237,9 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
   const CcaDims& d = a.d;
   const int b = blockIdx.y, head = blockIdx.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int t = a.pos[b];
-  if (t < 0 || t >= a.S_max || t >= a.max_len) return;      // reported by the conv1 kernel
+  int t;
+  size_t row;
+  if (!new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)) return;      // reported by the conv1 kernel
   const bool is_q = head < d.hq;
   const int ch0 = head * DH;                   // first channel of the head in the q0|k0 latent
   const float* lat_b = a.lat + (size_t)b * (d.L + d.Lk);
@@ -286,7 +283,7 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
     v = c < DH / 2 ? xh[c] * (float)cs - xh[c + DH / 2] * (float)sn : xh[c] * (float)cs + xh[c - DH / 2] * (float)sn;
   }
   if (is_q) a.q[(size_t)b * d.Lq + ch0 + c] = v;
-  else a.k_cache[((size_t)b * a.S_max + t) * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
+  else a.k_cache[row * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -576,6 +573,16 @@ cudaError_t launch_attn_dh(const AtArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+cudaError_t launch_finalize_dh(const FnArgs& fa, cudaStream_t st) {
+  const dim3 grid((unsigned)(fa.d.hq + fa.d.hk), (unsigned)fa.d.B);
+  switch (fa.d.dh) {
+    case 32: return launch_pdl(decode_finalize_kernel<32>, grid, dim3(128), st, fa);
+    case 64: return launch_pdl(decode_finalize_kernel<64>, grid, dim3(128), st, fa);
+    case 128: return launch_pdl(decode_finalize_kernel<128>, grid, dim3(128), st, fa);
+    default: return launch_pdl(decode_finalize_kernel<256>, grid, dim3(256), st, fa);
+  }
+}
+
 }  // namespace
 
 void decode_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
@@ -645,7 +652,7 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   const int kc = (d.flags & F_CONV2) ? d.k_ch : 1;
   C1Args c1;
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = s.v_cache;
-  c1.hist = s.qk0_hist; c1.x_prev = s.x_prev; c1.pos = s.pos; c1.S_max = s.S_max; c1.max_len = max_len; c1.status = status;
+  c1.hist = s.qk0_hist; c1.x_prev = s.x_prev; c1.pos = s.pos; c1.qlen = nullptr; c1.S_max = s.S_max; c1.max_len = max_len; c1.status = status;
   if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
   ++*launches;
@@ -660,18 +667,9 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   }
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = s.k_cache; fa.pos = s.pos;
-  fa.S_max = s.S_max; fa.max_len = max_len;
-  {
-    dim3 grid((unsigned)(d.hq + d.hk), (unsigned)d.B);
-    switch (d.dh) {
-      case 32: e = launch_pdl(decode_finalize_kernel<32>, grid, dim3(128), st, fa); break;
-      case 64: e = launch_pdl(decode_finalize_kernel<64>, grid, dim3(128), st, fa); break;
-      case 128: e = launch_pdl(decode_finalize_kernel<128>, grid, dim3(128), st, fa); break;
-      default: e = launch_pdl(decode_finalize_kernel<256>, grid, dim3(256), st, fa); break;
-    }
-    if (e != cudaSuccess) return -(int)e;
-    ++*launches;
-  }
+  fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len;
+  if ((e = launch_finalize_dh(fa, st)) != cudaSuccess) return -(int)e;
+  ++*launches;
   AtArgs aa;
   aa.d = d; aa.q = q; aa.k_cache = s.k_cache; aa.v_cache = s.v_cache;
   aa.temp = (d.flags & F_QK_NORM) ? w.temp : nullptr;
@@ -712,4 +710,76 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   if ((e = launch_proj(pb, st)) != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
+}
+
+namespace {
+struct QStepLayout { size_t lat, q, k_new, v_new, o, y1s, y2, cache, end; };
+QStepLayout qstep_layout(const CcaDims& d, int max_len, int sm_count) {
+  QStepLayout l;
+  size_t off = 0;
+  auto take = [&](size_t n) { const size_t o = off; off += (n + 255) / 256 * 256; return o; };
+  l.lat = take((size_t)d.B * (d.L + d.Lk) * 4);
+  l.q = take((size_t)d.B * d.Lq * 4);
+  l.k_new = take((size_t)d.B * d.Lk * 2);
+  l.v_new = take((size_t)d.B * d.Lk * 2);
+  l.o = take((size_t)d.B * d.Lq * 2);
+  l.y1s = take((size_t)d.B * d.L * d.k_ch * 2);
+  l.y2 = take((size_t)d.B * d.L * 4);
+  l.cache = take(qcache_workspace_bytes(d, max_len, sm_count));
+  l.end = off;
+  return l;
+}
+}  // namespace
+
+size_t decode_q_workspace_bytes(const CcaDims& d, int max_len, int sm_count) { return qstep_layout(d, max_len, sm_count).end; }
+
+// The step of launch_decode_step with the projections' weights in 4 bits and the new key and value quantised into a 4-bit cache.
+int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* x, bf16* out, const QCache& cache, float* hist,
+                         bf16* x_prev, const int* pos, int max_len, void* workspace, int sm_count, int* status,
+                         long long* launches, cudaEvent_t ev_attn_begin, cudaEvent_t ev_attn_end, cudaStream_t st) {
+  const QStepLayout l = qstep_layout(d, max_len, sm_count);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  float *lat = reinterpret_cast<float*>(ws + l.lat), *q = reinterpret_cast<float*>(ws + l.q), *y2 = reinterpret_cast<float*>(ws + l.y2);
+  bf16 *k_new = reinterpret_cast<bf16*>(ws + l.k_new), *v_new = reinterpret_cast<bf16*>(ws + l.v_new);
+  bf16 *o = reinterpret_cast<bf16*>(ws + l.o), *y1s = reinterpret_cast<bf16*>(ws + l.y1s);
+  cudaError_t e;
+  int r;
+  QLinArgs pa;
+  memset(&pa, 0, sizeof(pa));
+  pa.n_seg = 2;
+  pa.seg[0] = QLinSeg{w.qkv1_codes, w.qkv1_scales, x, d.L + d.Lk / 2, 0};
+  pa.seg[1] = QLinSeg{w.v2_codes, w.v2_scales, (d.flags & F_V_SHIFT) ? x_prev : x, d.Lk / 2, d.L + d.Lk / 2};
+  pa.K = d.E; pa.M = d.B; pa.out_f32 = lat; pa.ldo = d.L + d.Lk;
+  if ((r = launch_qlinear(pa, sm_count, launches, st)) != 0) return r;
+  const int kc = (d.flags & F_CONV2) ? d.k_ch : 1;
+  C1Args c1;
+  c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = v_new; c1.hist = hist; c1.x_prev = x_prev;
+  c1.pos = pos; c1.qlen = cache.len; c1.S_max = cache.S_max; c1.max_len = max_len; c1.status = status;
+  if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
+    return -(int)e;
+  ++*launches;
+  if (d.flags & F_CONV2) {
+    ProjArgs pc;
+    memset(&pc, 0, sizeof(pc));
+    pc.n_seg = 1;
+    pc.seg[0] = ProjSeg{w.conv1_w, y1s, d.L, 0};
+    pc.K = d.dh * kc; pc.B = d.B; pc.ldx = d.L * kc; pc.x_head_rows = d.dh; pc.out_f32 = y2; pc.ldo = d.L;
+    if ((e = launch_proj(pc, st)) != cudaSuccess) return -(int)e;
+    ++*launches;
+  }
+  FnArgs fa;
+  fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = k_new; fa.pos = pos; fa.qlen = cache.len;
+  fa.S_max = cache.S_max; fa.max_len = max_len;
+  if ((e = launch_finalize_dh(fa, st)) != cudaSuccess) return -(int)e;
+  ++*launches;
+  if ((r = launch_qcache_append(d, k_new, v_new, pos, nullptr, cache, 1, max_len, status, launches, st)) != 0) return r;
+  if ((r = launch_qcache_attention(d, nullptr, q, o, cache, pos, 1, max_len, cache.weight != nullptr, ws + l.cache, sm_count, status,
+                                   launches, ev_attn_begin, ev_attn_end, st)) != 0)
+    return r;
+  QLinArgs pb;
+  memset(&pb, 0, sizeof(pb));
+  pb.n_seg = 1;
+  pb.seg[0] = QLinSeg{w.o_codes, w.o_scales, o, d.E, 0};
+  pb.K = d.Lq; pb.M = d.B; pb.out_bf16 = out; pb.ldo = d.E;
+  return launch_qlinear(pb, sm_count, launches, st);
 }

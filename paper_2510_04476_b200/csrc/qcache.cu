@@ -1,0 +1,786 @@
+// The latent cache in 4 bits: rows put in (quantised), read back, attended to by one new token per sequence, and evicted by the
+// attention weight that they have gathered.  The format is that of qformat.cuh.
+//
+// All of it is bound by memory traffic.  Per (sequence, kv head) the cache is one contiguous run of rows, so that a head's rows
+// stream as whole lines and a row moves without touching its neighbours' heads.
+#include <cstring>
+
+#include "pdl.cuh"
+#include "qcache.cuh"
+#include "qformat.cuh"
+
+namespace {
+
+using namespace q4;
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <int DH>
+struct Row {                                       // a cache row of one head
+  static constexpr int BLK = DH < 128 ? DH : 128;  // channels of a block
+  static constexpr int NB = DH / BLK;              // blocks
+  static constexpr int NG = BLK / GROUP;           // scale groups of a block
+  static constexpr int CODES = DH / 2;             // bytes of codes
+  static constexpr int SCALES = DH / GROUP;        // scales
+  static constexpr int SW = (SCALES + 1) / 2;      // 32-bit words that hold the scales
+};
+
+// A row's scales as words; d_h = 32 has a single 16-bit scale.
+template <int DH>
+CCA_DEVINL void load_scales(uint32_t (&w)[Row<DH>::SW], const bf16* p) {
+  if constexpr (DH == 32) w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
+  else load_words<Row<DH>::SW>(w, p);
+}
+
+// ------------------------------------------------------------------------------------------------ rows in and out
+struct IoArgs {
+  const bf16 *k, *v;             // [B, n, hk, dh]
+  float *k_out, *v_out;          // the same, fp32
+  const int *position, *count, *first;
+  QCache c;
+  long long n, limit;            // rows a sequence may hold
+  int B, hk;
+  int* status;
+};
+
+// Eight neighbouring lanes take one block of one row (quantise_block); units run over (sequence, new row, head, block, key | value)
+// with the last fastest, so that a warp reads whole token rows.  Bound by traffic at a prompt's length, by the launch at a step's.
+template <int DH>
+__global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
+  pdl_enter();
+  using R = Row<DH>;
+  const int lane8 = threadIdx.x & 7;
+  const long long per_seq = a.n * a.hk * R::NB * 2, units = per_seq * a.B;
+  // whole warps stay in the loop: the shuffles need every lane
+  const long long step = (long long)gridDim.x * 32;
+  for (long long u0 = (long long)blockIdx.x * 32 + (threadIdx.x >> 5) * 4; u0 < units; u0 += step) {
+    const long long u = u0 + ((threadIdx.x & 31) >> 3);
+    bool ok = u < units;
+    const int b = ok ? (int)(u / per_seq) : 0;
+    const long long in_seq = ok ? u % per_seq : 0;
+    const int kv = (int)(in_seq & 1);
+    const int blk = (int)((in_seq >> 1) % R::NB);
+    const long long ih = (in_seq >> 1) / R::NB;             // (new row, head)
+    const int h = (int)(ih % a.hk);
+    const long long i = ih / a.hk;
+    const long long len = a.c.len[b];
+    long long cnt = a.n;
+    if (a.count) cnt = max(0, min(a.count[b], (int)min(a.n, (long long)0x7fffffff)));
+    // a sequence whose rows do not fit, or whose position is none: nothing of it is written
+    if (len < 0 || len + cnt > a.limit || (a.position && a.position[b] < 0)) {
+      if (ok && in_seq == 0 && lane8 == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+      ok = false;
+    }
+    ok = ok && i < cnt;
+    const bf16* src = (kv ? a.v : a.k) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
+    uint8_t code[2 * R::NG];
+    bf16 scale[R::NG];
+    quantise_block<R::NG>([&](int grp) { return ok ? __ldcs(reinterpret_cast<const uint2*>(src + grp * GROUP)) : make_uint2(0, 0); },
+                          code, scale);
+    if (!ok) continue;
+    const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + len + i;
+    uint8_t* dst = (kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + blk * (R::BLK / 2) + lane8 * 2 * R::NG;
+    if constexpr (R::NG == 4) {
+      uint2 w;
+      w.x = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
+      w.y = code[4] | (code[5] << 8) | (code[6] << 16) | ((uint32_t)code[7] << 24);
+      *reinterpret_cast<uint2*>(dst) = w;
+    } else if constexpr (R::NG == 2) {
+      *reinterpret_cast<uint32_t*>(dst) = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
+    } else {
+      *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(code[0] | (code[1] << 8));
+    }
+    bf16* sc = (kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + blk * R::NG;
+#pragma unroll
+    for (int grp = 0; grp < R::NG; ++grp)
+      if (lane8 == grp) sc[grp] = scale[grp];
+    if (kv == 0 && blk == 0 && lane8 == 0) {
+      if (a.c.weight) a.c.weight[row] = 0.f;
+      if (a.c.position) a.c.position[row] = a.position ? a.position[b] + (int)i : (int)(len + i);
+    }
+  }
+}
+
+template <int DH>
+__global__ void __launch_bounds__(256) qcache_read_kernel(IoArgs a) {
+  pdl_enter();
+  using R = Row<DH>;
+  const int lane8 = threadIdx.x & 7;
+  const long long per_seq = a.n * a.hk * R::NB * 2, units = per_seq * a.B;
+  for (long long u = (long long)blockIdx.x * 32 + (threadIdx.x >> 3); u < units; u += (long long)gridDim.x * 32) {
+    const int b = (int)(u / per_seq);
+    const long long in_seq = u % per_seq;
+    const int kv = (int)(in_seq & 1);
+    const int blk = (int)((in_seq >> 1) % R::NB);
+    const long long ih = (in_seq >> 1) / R::NB;
+    const int h = (int)(ih % a.hk);
+    const long long i = ih / a.hk;
+    const long long r = (long long)(a.first ? a.first[b] : a.c.len[b]) + i;
+    const bool there = r >= 0 && r < a.c.S_max;
+    const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + (there ? r : 0);
+    const uint8_t* src = (kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + blk * (R::BLK / 2) + lane8 * 2 * R::NG;
+    const bf16* sc = (kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + blk * R::NG;
+    float* dst = (kv ? a.v_out : a.k_out) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
+#pragma unroll
+    for (int grp = 0; grp < R::NG; ++grp) {
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (there) {
+        const uint32_t pair = *reinterpret_cast<const uint16_t*>(src + 2 * grp);
+        const float s = __bfloat162float(sc[grp]);
+        o = make_float4(s * value_e0(pair & 255u), s * value_e0(pair >> 8), s * value_e1(pair & 255u), s * value_e1(pair >> 8));
+      }
+      __stcs(reinterpret_cast<float4*>(dst + grp * GROUP), o);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+struct QaArgs {
+  CcaDims d;
+  const bf16* q;             // [B, Lq], one of the two
+  const float* q32;
+  QCache c;
+  const int* pos;            // decode step: a sequence whose position is negative is skipped; else null
+  int extra, max_len, chunk, splits;
+  float* part_o;             // [B, hq, splits, DH]
+  float* part_ml;            // [B, hq, splits, 2]
+  float* scores;             // [B, hk, max_len, g]: logits times log2(e), where the weights are gathered; else null
+  bf16* o;
+  int* status;
+};
+
+CCA_DEVINL int rows_of(const QaArgs& a, int b) {          // -1: does not fit
+  const int len = a.c.len[b];
+  const long long n = (long long)len + a.extra;
+  return (len < 0 || n > a.max_len || n > a.c.S_max || (a.pos && a.pos[b] < 0)) ? -1 : (int)n;
+}
+
+// The row of a 16-row tile that operand row r (of 8) stands for: with this order the four lanes t of a quad read four
+// neighbouring value rows at a time, and the eight lane groups still read eight neighbouring key rows.
+CCA_DEVINL int tile_row(int r) { return (r >> 1) + 4 * (r & 1); }
+
+template <int DH>
+struct Tile {                                              // what a lane holds of 16 rows
+  using R = Row<DH>;
+  static constexpr int KW = R::NB * R::NG;                 // words of codes of a key row per lane: 2 channel octets of every group
+  static constexpr int VB = 2 * R::NG;                     // bytes of codes of a value row per lane and block
+  static constexpr int VW = (VB + 3) / 4;
+  uint32_t k[2][KW], v[4][R::NB * VW], ks[2][R::SW], vs[2][R::SW];
+
+  CCA_DEVINL void load(const uint8_t* kc, const uint8_t* vc, const bf16* ksc, const bf16* vsc, int r0, int r_end, int g, int t) {
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+      const int r = r0 + 8 * hi + tile_row(g);
+      zero_words(k[hi]); zero_words(ks[hi]); zero_words(vs[hi]);
+      if (r < r_end) {
+#pragma unroll
+        for (int blk = 0; blk < R::NB; ++blk) {
+          uint32_t w[R::NG];
+          load_words<R::NG>(w, kc + (size_t)r * R::CODES + blk * (R::BLK / 2) + t * 4 * R::NG);
+#pragma unroll
+          for (int i = 0; i < R::NG; ++i) k[hi][blk * R::NG + i] = w[i];
+        }
+        load_scales<DH>(ks[hi], ksc + (size_t)r * R::SCALES);
+        load_scales<DH>(vs[hi], vsc + (size_t)r * R::SCALES);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                          // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
+      const int r = r0 + 4 * i + t;
+      zero_words(v[i]);
+      if (r < r_end) {
+#pragma unroll
+        for (int blk = 0; blk < R::NB; ++blk) {
+          const uint8_t* p = vc + (size_t)r * R::CODES + blk * (R::BLK / 2) + g * VB;
+          if constexpr (VB == 2) {
+            v[i][0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
+          } else {
+            uint32_t w[VW];
+            load_words<VW>(w, p);
+#pragma unroll
+            for (int x = 0; x < VW; ++x) v[i][blk * VW + x] = w[x];
+          }
+        }
+      }
+    }
+  }
+};
+
+constexpr int QA_WARPS = 4;
+
+// One CTA: rows [split * chunk, ...) of sequence b, kv head j, up to 8 NHT of its query heads; its four warps take 16 rows each in
+// turn.  S^T = K Q^T has the rows as the 16 and the heads as the 8 of m16n8k16, so that up to 8 heads cost one instruction per
+// 256 codes; O^T = V^T P^T has the channels as the 16.  Both read the codes from the registers that they were loaded into.  A
+// group's scale multiplies the group's partial logit in fp32; a value row's scale is multiplied into the probability, once
+// per group, before that is rounded to bf16 as the operand (the only rounding of the probabilities; the sums are taken before it).
+template <int DH, int NHT>
+__global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
+  pdl_enter();
+  using R = Row<DH>;
+  using T = Tile<DH>;
+  constexpr int MT = DH / 16;                              // 16-channel tiles of O^T
+  const CcaDims& d = a.d;
+  const int split = blockIdx.x, b = blockIdx.z;
+  const int n_grp = (d.g + 8 * NHT - 1) / (8 * NHT);
+  const int j = blockIdx.y / n_grp, h0 = (blockIdx.y % n_grp) * 8 * NHT;
+  const int nh = min(8 * NHT, d.g - h0);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  const int n_rows = rows_of(a, b);
+  if (n_rows < 0) {
+    if (threadIdx.x == 0 && split == 0 && blockIdx.y == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+    return;
+  }
+  const int r_begin = split * a.chunk, r_end = min(n_rows, r_begin + a.chunk);
+
+  // query operand: head h0 + g (+ 8), channels grp * 32 + 8 t .. + 7 of every group, times 2^64 (e0 lanes) or 2^60 (e1 lanes)
+  uint32_t qb[NHT][R::NB * R::NG][4];
+#pragma unroll
+  for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+    for (int gi = 0; gi < R::NB * R::NG; ++gi) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (g + 8 * ht < nh) {
+        const size_t off = (size_t)b * d.Lq + (size_t)(j * d.g + h0 + g + 8 * ht) * DH + gi * GROUP + t * 8;
+        if (a.q32) {
+          const float4 x = *reinterpret_cast<const float4*>(a.q32 + off), y = *reinterpret_cast<const float4*>(a.q32 + off + 4);
+          w = make_uint4(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+        } else {
+          w = *reinterpret_cast<const uint4*>(a.q + off);
+        }
+      }
+      qb[ht][gi][0] = mul_bf16x2(w.x, MUL_E0); qb[ht][gi][1] = mul_bf16x2(w.y, MUL_E1);
+      qb[ht][gi][2] = mul_bf16x2(w.z, MUL_E0); qb[ht][gi][3] = mul_bf16x2(w.w, MUL_E1);
+    }
+  const float c_scale = rsqrtf((float)DH) * LOG2E * TWO_69;
+
+  // softmax state of heads 2t, 2t + 1 (+ 8 ht): the maximum is the same in all lanes of a column, the sums are per lane.
+  // Probabilities carry 2^64, which the bf16 subnormals of the value codes need.
+  float mx[NHT][2], off[NHT][2], sum[NHT][2];
+  float o[NHT][MT][4];
+#pragma unroll
+  for (int ht = 0; ht < NHT; ++ht) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) { mx[ht][c] = -INFINITY; off[ht][c] = 64.f; sum[ht][c] = 0.f; }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[ht][mt][c] = 0.f;
+  }
+
+  const size_t base = ((size_t)b * d.hk + j) * a.c.S_max;
+  const uint8_t *kc = a.c.k_codes + base * R::CODES, *vc = a.c.v_codes + base * R::CODES;
+  const bf16 *ksc = a.c.k_scales + base * R::SCALES, *vsc = a.c.v_scales + base * R::SCALES;
+  float* sco = a.scores ? a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g + h0 : nullptr;
+
+  T cur, nxt;
+  int r0 = r_begin + warp * 16;
+  if (r0 < r_end) cur.load(kc, vc, ksc, vsc, r0, r_end, g, t);
+  for (; r0 < r_end; r0 += QA_WARPS * 16) {
+    if (r0 + QA_WARPS * 16 < r_end) nxt.load(kc, vc, ksc, vsc, r0 + QA_WARPS * 16, r_end, g, t);
+    // ---- logits (times log2 e) of rows tile_row(g), 8 + tile_row(g), heads 2t, 2t + 1
+    float s[NHT][4];
+#pragma unroll
+    for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[ht][c] = 0.f;
+#pragma unroll
+    for (int gi = 0; gi < R::NB * R::NG; ++gi) {
+      const float s_lo = scale_at(cur.ks[0], gi), s_hi = scale_at(cur.ks[1], gi);
+      float part[NHT][4];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {                        // channel octets of lanes 2t and 2t + 1
+        const int blk = gi / R::NG, byte = c * 2 * R::NG + (gi % R::NG) * 2;
+        const uint32_t sel = (byte & 2) ? 0x3322u : 0x1100u;
+        const uint32_t p0 = __byte_perm(cur.k[0][blk * R::NG + byte / 4], 0, sel), p1 = __byte_perm(cur.k[1][blk * R::NG + byte / 4], 0, sel);
+        const uint32_t ka[4] = {code_e0(p0), code_e0(p1), code_e1(p0), code_e1(p1)};
+#pragma unroll
+        for (int ht = 0; ht < NHT; ++ht) {
+          if (c == 0) mma_16816_zero(part[ht], ka, qb[ht][gi][0], qb[ht][gi][1]);
+          else mma_16816(part[ht], ka, qb[ht][gi][2], qb[ht][gi][3]);
+        }
+      }
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht) {
+        s[ht][0] = fmaf(s_lo, part[ht][0], s[ht][0]); s[ht][1] = fmaf(s_lo, part[ht][1], s[ht][1]);
+        s[ht][2] = fmaf(s_hi, part[ht][2], s[ht][2]); s[ht][3] = fmaf(s_hi, part[ht][3], s[ht][3]);
+      }
+    }
+    const int r_lo = r0 + tile_row(g), r_hi = r_lo + 8;
+    bool grow = false;
+#pragma unroll
+    for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[ht][c] = (c < 2 ? r_lo : r_hi) < r_end ? s[ht][c] * c_scale : -INFINITY;
+        grow = grow || s[ht][c] > mx[ht][c & 1] + 8.f;     // probabilities may pass 1 by 2^8 before the maximum is moved
+      }
+    if (sco) {
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int r = c < 2 ? r_lo : r_hi, h = 8 * ht + 2 * t + (c & 1);
+          if (r < r_end && h < nh) sco[(size_t)r * d.g + h] = s[ht][c];
+        }
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float m = fmaxf(s[ht][c], s[ht][2 + c]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+          if (m > mx[ht][c]) {
+            const float al = exp2f(mx[ht][c] - m);         // 0 while nothing has been seen
+            mx[ht][c] = m; off[ht][c] = 64.f - m;
+            sum[ht][c] *= al;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) { o[ht][mt][c] *= al; o[ht][mt][2 + c] *= al; }
+          }
+        }
+    }
+#pragma unroll
+    for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[ht][c] = exp2f(s[ht][c] + off[ht][c & 1]);
+        sum[ht][c & 1] += s[ht][c];
+      }
+    // ---- O^T += V^T P^T
+#pragma unroll
+    for (int gi = 0; gi < R::NB * R::NG; ++gi) {
+      const float s_lo = scale_at(cur.vs[0], gi), s_hi = scale_at(cur.vs[1], gi);
+      uint32_t pb[NHT][2];
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht) {
+        pb[ht][0] = transpose_8x8(pack_bf16x2(s[ht][0] * s_lo, s[ht][1] * s_lo));
+        pb[ht][1] = transpose_8x8(pack_bf16x2(s[ht][2] * s_hi, s[ht][3] * s_hi));
+      }
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        const int blk = gi / R::NG, byte = (gi % R::NG) * 2 + jj, w = blk * T::VW + byte / 4;
+        const uint32_t sel = (byte & 3) * 0x11u + ((byte & 3) + 4) * 0x1100u;
+        const uint32_t p0 = __byte_perm(cur.v[0][w], cur.v[1][w], sel), p1 = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
+        const uint32_t va[4] = {code_e0(p0), code_e1(p0), code_e0(p1), code_e1(p1)};
+#pragma unroll
+        for (int ht = 0; ht < NHT; ++ht) mma_16816(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
+      }
+    }
+    cur = nxt;
+  }
+#pragma unroll
+  for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) sum[ht][c] += __shfl_xor_sync(0xffffffffu, sum[ht][c], x);
+  // merge the warps through shared memory
+  __shared__ float sm_o[QA_WARPS][8 * NHT][DH + 1];
+  __shared__ float sm_ml[QA_WARPS][8 * NHT][2];
+#pragma unroll
+  for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        sm_o[warp][8 * ht + 2 * t + (c & 1)][(mt >> 1) * GROUP + 4 * g + (mt & 1) + 2 * (c >> 1)] =
+            o[ht][mt][c] * (c < 2 ? TWO_69 : TWO_65);
+  if (g == 0) {
+#pragma unroll
+    for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        sm_ml[warp][8 * ht + 2 * t + c][0] = mx[ht][c];
+        sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c] * TWO_M64;
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nh * DH; i += QA_WARPS * 32) {
+    const int h = i / DH, c = i % DH;
+    float mn = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < QA_WARPS; ++w) mn = fmaxf(mn, sm_ml[w][h][0]);
+    float lo = 0.f, oo = 0.f;
+#pragma unroll
+    for (int w = 0; w < QA_WARPS; ++w) {
+      const float al = (sm_ml[w][h][0] == -INFINITY) ? 0.f : exp2f(sm_ml[w][h][0] - mn);
+      lo += sm_ml[w][h][1] * al;
+      oo += sm_o[w][h][c] * al;
+    }
+    const size_t pidx = ((size_t)b * d.hq + j * d.g + h0 + h) * a.splits + split;
+    a.part_o[pidx * DH + c] = oo;
+    if (c == 0) { a.part_ml[pidx * 2] = mn; a.part_ml[pidx * 2 + 1] = lo; }
+  }
+}
+
+// Joins the chunks' partial results of one (sequence, kv head) and, where the weights are gathered, adds to every row what its
+// heads gave it: 2^(logit - logsumexp), from the logits that the first kernel left (exact in fp32 whatever maximum a chunk used).
+template <int DH>
+__global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
+  pdl_enter();
+  __shared__ float sm_m[64], sm_l[64], red[256];
+  const CcaDims& d = a.d;
+  const int j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n_rows = rows_of(a, b);
+  if (n_rows < 0) return;
+  const size_t p0 = ((size_t)b * d.hq + j * d.g) * a.splits;
+  const int used = (n_rows + a.chunk - 1) / a.chunk;       // chunks that hold rows
+  for (int h = warp; h < d.g; h += 8) {
+    float m = -INFINITY, l = 0.f;
+    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[(p0 + (size_t)h * a.splits + s) * 2]);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    for (int s = lane; s < used; s += 32) {
+      const float ms = a.part_ml[(p0 + (size_t)h * a.splits + s) * 2];
+      l += ms == -INFINITY ? 0.f : a.part_ml[(p0 + (size_t)h * a.splits + s) * 2 + 1] * exp2f(ms - m);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (lane == 0) { sm_m[h] = m; sm_l[h] = l; }
+  }
+  __syncthreads();
+  constexpr int PAR = 256 / DH > 0 ? 256 / DH : 1;          // threads that share an output channel, each with its chunks
+  for (int h = blockIdx.x; h < d.g; h += gridDim.x) {
+    const int c = tid % DH, part = tid / DH;
+    float acc = 0.f;
+    for (int s = part; s < used; s += PAR) {
+      const size_t p = p0 + (size_t)h * a.splits + s;
+      const float ms = a.part_ml[p * 2];
+      if (ms != -INFINITY) acc += a.part_o[p * DH + c] * exp2f(ms - sm_m[h]);
+    }
+    red[tid] = acc;
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+      for (int x = 1; x < PAR; ++x) acc += red[x * DH + c];
+      a.o[(size_t)b * d.Lq + (size_t)(j * d.g + h) * DH + c] = __float2bfloat16(n_rows > 0 ? acc / sm_l[h] : 0.f);
+    }
+    __syncthreads();
+  }
+  if (!a.scores || n_rows == 0) return;
+  if (tid < d.g) sm_m[tid] += __log2f(sm_l[tid]);
+  __syncthreads();
+  const float* sc = a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g;
+  float* w = a.c.weight + ((size_t)b * d.hk + j) * a.c.S_max;
+  for (int r = blockIdx.x * 256 + tid; r < n_rows; r += gridDim.x * 256) {
+    float acc = 0.f;
+    for (int h = 0; h < d.g; ++h) acc += exp2f(sc[(size_t)r * d.g + h] - sm_m[h]);
+    w[r] += acc;
+  }
+}
+
+int heads_per_cta(const CcaDims& d) { return d.g <= 8 || d.dh == 256 ? 8 : 16; }
+
+// Rows per CTA and number of chunks for sequences of up to max_len rows.
+void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
+  const int n_grp = (d.g + heads_per_cta(d) - 1) / heads_per_cta(d);
+  const long long base = (long long)d.B * d.hk * n_grp;
+  long long want = (12LL * sm_count + base - 1) / base;
+  if (want < 1) want = 1;
+  if (want > 256) want = 256;
+  int ch = (int)((max_len + want - 1) / want);
+  ch = (ch + 63) / 64 * 64;                                // the four warps of a CTA take 16 rows each per round
+  if (ch < 64) ch = 64;
+  *chunk = ch;
+  *splits = (max_len + ch - 1) / ch;
+}
+
+template <int DH>
+cudaError_t attn_dh(const QaArgs& a, cudaStream_t st) {
+  const CcaDims& d = a.d;
+  const int per = heads_per_cta(d);
+  dim3 grid((unsigned)a.splits, (unsigned)(d.hk * ((d.g + per - 1) / per)), (unsigned)d.B);
+  if constexpr (DH <= 128)
+    if (per == 16) return launch_pdl(qcache_attn_kernel<DH, 2>, grid, dim3(QA_WARPS * 32), st, a);
+  return launch_pdl(qcache_attn_kernel<DH, 1>, grid, dim3(QA_WARPS * 32), st, a);
+}
+
+// ------------------------------------------------------------------------------------------------ eviction
+struct EvArgs {
+  QCache c;
+  int hk, keep, recent, max_len;
+  const int* next;               // [B] position of the next token
+  int* count;                    // [B * hk] rows to move
+  int* new_len;                  // [B]: keep, or -1 where nothing goes
+  int* list;                     // [B * hk][2][cap]: destinations (rows that go, ascending), sources (rows that come, ascending)
+  long long cap;
+  int* status;
+};
+
+constexpr int EV_THREADS = 1024, EV_BINS = 2048;
+
+// The order of eviction as an unsigned number, larger = kept: 0xffffffff for the newest, else the weight's order (a NaN is lowest).
+CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
+  if ((long long)pos >= first_recent) return 0xffffffffu;
+  uint32_t u = __float_as_uint(w);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
+  if ((u << 1) == 0u) u = 0u;
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// Exclusive sum over the 32 warps of a value that lane 0 of each holds; every thread gets its warp's.
+CCA_DEVINL int warp_offsets(int v, int* sm, int warp, int lane) {
+  __syncthreads();
+  if (lane == 0) sm[warp] = v;
+  __syncthreads();
+  int x = sm[lane], inc = x;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, s);
+    if (lane >= s) inc += y;
+  }
+  return __shfl_sync(0xffffffffu, inc - x, warp);
+}
+
+// One CTA per (sequence, head): the keep-th largest key by three counting passes over its digits (11, 11, 10 bits), then, in
+// ascending order of rows, the rows below `keep` that go and the rows behind it that stay.  Each warp takes a contiguous run of rows,
+// 32 at a time, so ranks come from ballots and one sum over the warps.  IN_SMEM: the keys are kept in shared memory after
+// the first reading; longer caches read weight and position again (from L2).
+template <bool IN_SMEM>
+__global__ void __launch_bounds__(EV_THREADS) qcache_select_kernel(EvArgs a) {
+  pdl_enter();
+  extern __shared__ uint32_t keys[];
+  __shared__ int hist[EV_BINS];
+  __shared__ int sm[32];
+  __shared__ int found[2];
+  const int b = blockIdx.y, j = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int bj = b * a.hk + j;
+  const int n = a.c.len[b];
+  const bool bad = n < 0 || n > a.max_len || n > a.c.S_max;
+  if (bad && tid == 0 && j == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+  if (bad || n <= a.keep || a.keep == 0) {
+    if (tid == 0) {
+      a.count[bj] = 0;
+      if (j == 0) a.new_len[b] = (!bad && n > a.keep) ? a.keep : -1;
+    }
+    return;
+  }
+  const float* w = a.c.weight + (size_t)bj * a.c.S_max;
+  const int* pos = a.c.position + (size_t)bj * a.c.S_max;
+  const long long first_recent = (long long)a.next[b] - a.recent;
+  auto key_of = [&](int r) { return IN_SMEM ? keys[r] : keep_key(w[r], pos[r], first_recent); };
+
+  uint32_t prefix = 0;
+  int left = a.keep;                                       // how many of the rows that share the prefix are kept
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
+    __syncthreads();
+    for (int r = tid; r < n; r += EV_THREADS) {
+      uint32_t k;
+      if (IN_SMEM && pass > 0) k = keys[r];
+      else {
+        k = keep_key(w[r], pos[r], first_recent);
+        if (IN_SMEM) keys[r] = k;
+      }
+      if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1);
+    }
+    __syncthreads();
+    // bins from the top: thread i has bins BINS - 1 - 2i and BINS - 2 - 2i
+    const int c0 = hist[EV_BINS - 1 - 2 * tid], c1 = hist[EV_BINS - 2 - 2 * tid];
+    int inc = c0 + c1;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, s);
+      if (lane >= s) inc += y;
+    }
+    const int tot = __shfl_sync(0xffffffffu, inc, 31);
+    const int before = warp_offsets(tot, sm, warp, lane) + inc - c0 - c1;
+    if (before < left && left <= before + c0) { found[0] = EV_BINS - 1 - 2 * tid; found[1] = left - before; }
+    if (before + c0 < left && left <= before + c0 + c1) { found[0] = EV_BINS - 2 - 2 * tid; found[1] = left - before - c0; }
+    __syncthreads();
+    prefix = (prefix << bits) | (uint32_t)found[0];
+    left = found[1];
+    __syncthreads();
+  }
+  const uint32_t lowest = prefix;                          // keys above it stay, and the first `left` rows that equal it
+  const int run = (n + EV_THREADS - 1) / EV_THREADS * 32;  // rows of a warp
+  const int r_begin = min(n, warp * run), r_end = min(n, r_begin + run);
+  int eq = 0;
+  for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+    const int r = r0 + lane;
+    eq += __popc(__ballot_sync(0xffffffffu, r < r_end && key_of(r) == lowest));
+  }
+  const int eq0 = warp_offsets(eq, sm, warp, lane);
+  int go = 0, come = 0;
+  int go0 = 0, come0 = 0;
+  int* dst = a.list + (size_t)bj * 2 * a.cap;
+  int* src = dst + a.cap;
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {                   // count, then write
+    int e = eq0;
+    go = come = 0;
+    for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+      const int r = r0 + lane;
+      const uint32_t k = r < r_end ? key_of(r) : 0u;
+      const unsigned below = (1u << lane) - 1u;
+      const unsigned beq = __ballot_sync(0xffffffffu, r < r_end && k == lowest);
+      const bool stays = r < r_end && (k > lowest || (k == lowest && e + __popc(beq & below) < left));
+      const unsigned bgo = __ballot_sync(0xffffffffu, r < r_end && r < a.keep && !stays);
+      const unsigned bco = __ballot_sync(0xffffffffu, r >= a.keep && stays);
+      if (pass == 1) {
+        if (bgo >> lane & 1u) dst[go0 + go + __popc(bgo & below)] = r;
+        if (bco >> lane & 1u) src[come0 + come + __popc(bco & below)] = r;
+      }
+      e += __popc(beq); go += __popc(bgo); come += __popc(bco);
+    }
+    if (pass == 0) {
+      go0 = warp_offsets(go, sm, warp, lane);
+      come0 = warp_offsets(come, sm, warp, lane);
+      if (warp == 31 && lane == 0) {
+        a.count[bj] = come0 + come;
+        if (j == 0) a.new_len[b] = a.keep;
+      }
+    }
+  }
+}
+
+// Moves the listed rows: DH / 16 lanes take the 16-byte pieces of a row's codes, the first lanes its scales, weight and position.
+// A destination is below `keep` and a source is not, so no order matters.
+template <int DH>
+__global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
+  pdl_enter();
+  using R = Row<DH>;
+  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = 256 / LANES;
+  const int j = blockIdx.y, b = blockIdx.z, bj = b * a.hk + j;
+  if (blockIdx.x == 0 && j == 0 && threadIdx.x == 0 && a.new_len[b] >= 0) a.c.len[b] = a.new_len[b];
+  const int n = a.count[bj];
+  const int* dst = a.list + (size_t)bj * 2 * a.cap;
+  const int* src = dst + a.cap;
+  const size_t base = (size_t)bj * a.c.S_max;
+  const int l = threadIdx.x % LANES, piece = l % PIECES;
+  uint8_t* codes = (l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES;
+  bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES;
+  for (int i = blockIdx.x * ROWS + threadIdx.x / LANES; i < n; i += gridDim.x * ROWS) {
+    const size_t from = (size_t)src[i], to = (size_t)dst[i];
+    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(codes + from * R::CODES) + piece);
+    const bf16 s = scales[from * R::SCALES + piece];       // as many scales as 16-byte pieces: 32 channels each
+    reinterpret_cast<uint4*>(codes + to * R::CODES)[piece] = u;
+    scales[to * R::SCALES + piece] = s;
+    if (l == 0) a.c.weight[base + to] = a.c.weight[base + from];
+    if (l == PIECES) a.c.position[base + to] = a.c.position[base + from];
+  }
+}
+
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+constexpr int EV_SMEM_ROWS = 49152;                        // 192 KB of keys
+constexpr int MAX_DEVICES = 64;
+
+}  // namespace
+
+#define QC_BY_HEAD(call)           \
+  switch (d.dh) {                  \
+    case 32: { constexpr int DH = 32; e = call; break; }    \
+    case 64: { constexpr int DH = 64; e = call; break; }    \
+    case 128: { constexpr int DH = 128; e = call; break; }  \
+    case 256: { constexpr int DH = 256; e = call; break; }  \
+    default: return 1;             \
+  }
+
+int launch_qcache_append(const CcaDims& d, const bf16* k, const bf16* v, const int* position, const int* count, const QCache& c,
+                         long long n, long long limit, int* status, long long* launches, cudaStream_t st) {
+  IoArgs a;
+  memset(&a, 0, sizeof(a));
+  a.k = k; a.v = v; a.position = position; a.count = count; a.c = c; a.n = n; a.limit = limit; a.B = d.B; a.hk = d.hk;
+  a.status = status;
+  const long long units = (long long)d.B * n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2;
+  const long long want = (units + 31) / 32;
+  const unsigned grid = (unsigned)(want < 4736 ? want : 4736);      // 32 CTAs for each of 148 SMs, then around again
+  cudaError_t e;
+  QC_BY_HEAD((launch_pdl(qcache_append_kernel<DH>, dim3(grid), dim3(256), st, a)))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+int launch_qcache_read(const CcaDims& d, const QCache& c, const int* first, float* k, float* v, long long n, long long* launches,
+                       cudaStream_t st) {
+  IoArgs a;
+  memset(&a, 0, sizeof(a));
+  a.k_out = k; a.v_out = v; a.first = first; a.c = c; a.n = n; a.B = d.B; a.hk = d.hk;
+  const long long units = (long long)d.B * n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2;
+  const long long want = (units + 31) / 32;
+  const unsigned grid = (unsigned)(want < 4736 ? want : 4736);
+  cudaError_t e;
+  QC_BY_HEAD((launch_pdl(qcache_read_kernel<DH>, dim3(grid), dim3(256), st, a)))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+size_t qcache_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
+  int chunk, splits;
+  attn_plan(d, max_len, sm_count, &chunk, &splits);
+  const size_t attn = up256((size_t)d.B * d.hq * splits * d.dh * 4) + up256((size_t)d.B * d.hq * splits * 2 * 4) +
+                      up256((size_t)d.B * d.hq * max_len * 4);
+  const size_t ev = up256((size_t)d.B * d.hk * 4) + up256((size_t)d.B * 4) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
+  return attn > ev ? attn : ev;
+}
+
+int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, bf16* o, const QCache& c, const int* pos, int extra,
+                            int max_len, int accumulate, void* workspace, int sm_count, int* status, long long* launches,
+                            cudaEvent_t ev_begin, cudaEvent_t ev_end, cudaStream_t st) {
+  QaArgs a;
+  memset(&a, 0, sizeof(a));
+  a.d = d; a.q = q; a.q32 = q32; a.c = c; a.pos = pos; a.extra = extra; a.max_len = max_len; a.o = o; a.status = status;
+  attn_plan(d, max_len, sm_count, &a.chunk, &a.splits);
+  unsigned char* p = static_cast<unsigned char*>(workspace);
+  a.part_o = reinterpret_cast<float*>(p); p += up256((size_t)d.B * d.hq * a.splits * d.dh * 4);
+  a.part_ml = reinterpret_cast<float*>(p); p += up256((size_t)d.B * d.hq * a.splits * 2 * 4);
+  a.scores = accumulate ? reinterpret_cast<float*>(p) : nullptr;
+  cudaError_t e;
+  if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
+  QC_BY_HEAD(attn_dh<DH>(a, st))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  if (ev_end && (e = cudaEventRecord(ev_end, st)) != cudaSuccess) return -(int)e;
+  // one CTA per head at least; with weights to gather, one per 1024 rows
+  int nx = d.g;
+  if (accumulate && (max_len + 1023) / 1024 > nx) nx = (max_len + 1023) / 1024;
+  QC_BY_HEAD((launch_pdl(qcache_join_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent, const int* next_position, int max_len,
+                        void* workspace, int* status, long long* launches, cudaStream_t st) {
+  EvArgs a;
+  memset(&a, 0, sizeof(a));
+  a.c = c; a.hk = d.hk; a.keep = keep; a.recent = recent; a.max_len = max_len; a.next = next_position; a.status = status;
+  a.cap = max_len / 2 + 1;                                 // as many rows go below `keep` as come from behind it
+  unsigned char* p = static_cast<unsigned char*>(workspace);
+  a.count = reinterpret_cast<int*>(p); p += up256((size_t)d.B * d.hk * 4);
+  a.new_len = reinterpret_cast<int*>(p); p += up256((size_t)d.B * 4);
+  a.list = reinterpret_cast<int*>(p);
+  cudaError_t e;
+  const dim3 grid((unsigned)d.hk, (unsigned)d.B);
+  if (max_len <= EV_SMEM_ROWS) {
+    const int smem = (max_len > 1 ? max_len : 1) * 4;
+    if (smem > 32 * 1024) {
+      static bool opted[MAX_DEVICES];                      // the opt-in to more shared memory is per device
+      int dev = 0;
+      if ((e = cudaGetDevice(&dev)) != cudaSuccess) return -(int)e;
+      if (dev >= MAX_DEVICES || !opted[dev]) {
+        e = cudaFuncSetAttribute(qcache_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_SMEM_ROWS * 4);
+        if (e != cudaSuccess) return -(int)e;
+        if (dev < MAX_DEVICES) opted[dev] = true;
+      }
+    }
+    e = launch_pdl_smem(qcache_select_kernel<true>, grid, dim3(EV_THREADS), (size_t)smem, st, a);
+  } else {
+    e = launch_pdl(qcache_select_kernel<false>, grid, dim3(EV_THREADS), st, a);
+  }
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  const int most = keep < max_len - keep ? keep : max_len - keep;      // rows that can move
+  int nx = (most * (d.dh / 16) + 1023) / 1024;
+  if (nx < 1) nx = 1;
+  QC_BY_HEAD((launch_pdl(qcache_move_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}

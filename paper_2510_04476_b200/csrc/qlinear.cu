@@ -1,0 +1,162 @@
+// y = x W^T for a few tokens, W in the 4-bit format of qformat.cuh.  Bound by reading W at few tokens.
+#include "pdl.cuh"
+#include "qformat.cuh"
+#include "qlinear.cuh"
+
+namespace {
+
+using namespace q4;
+constexpr int QL_WARPS = 8, QL_UNR = 4;
+
+struct PackArgs {
+  const bf16* w;
+  uint8_t* codes;
+  bf16* scales;
+  int N, K, n16, k128;
+};
+
+// Eight neighbouring lanes take one block of 128 columns of one row; four rows of a warp are neighbours in the tile.
+__global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
+  const int lane8 = threadIdx.x & 7;
+  const long long units = (long long)a.n16 * a.k128 * 16;          // (row tile, column tile, row)
+  for (long long u0 = (long long)blockIdx.x * 32 + (threadIdx.x >> 5) * 4; u0 < units; u0 += (long long)gridDim.x * 32) {
+    const long long u = u0 + ((threadIdx.x & 31) >> 3);            // units is a multiple of 16: every lane has one
+    const int r = (int)(u & 15);
+    const long long tile = u >> 4;
+    const int kb = (int)(tile % a.k128);
+    const long long row = tile / a.k128 * 16 + r;
+    uint8_t code[8];
+    bf16 scale[4];
+    quantise_block<4>([&](int grp) {
+      const int col = kb * 128 + grp * GROUP;
+      return row < a.N && col < a.K ? __ldcs(reinterpret_cast<const uint2*>(a.w + (size_t)row * a.K + col + lane8 * 4)) : make_uint2(0, 0);
+    }, code, scale);
+    uint2 w;
+    w.x = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
+    w.y = code[4] | (code[5] << 8) | (code[6] << 16) | ((uint32_t)code[7] << 24);
+    *reinterpret_cast<uint2*>(a.codes + (size_t)u * 64 + lane8 * 8) = w;
+#pragma unroll
+    for (int grp = 0; grp < 4; ++grp)
+      if (lane8 == grp) a.scales[(size_t)u * 4 + grp] = scale[grp];
+  }
+}
+
+// 16 weight rows per CTA, 8 NT tokens, the inner dimension split over the 8 warps and summed through shared memory in a fixed
+// order.  A lane's 16 bytes of a weight row are 8 channels of each of 4 groups: two instructions per group, whose sum is multiplied
+// by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.
+template <int NT>
+__global__ void __launch_bounds__(QL_WARPS * 32) qlinear_kernel(QLinArgs a) {
+  pdl_enter();
+  __shared__ float red[QL_WARPS][16][NT * 8 + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int tok0 = blockIdx.y * (NT * 8);
+  const int k128 = (a.K + 127) / 128;
+  int tile = blockIdx.x;
+  QLinSeg sg = a.seg[0];
+  if (a.n_seg > 1) {
+    const int t0 = (a.seg[0].N + 15) / 16;
+    if (tile >= t0) { sg = a.seg[1]; tile -= t0; }
+  }
+  const uint8_t* codes = sg.codes + (size_t)tile * k128 * 1024 + lane * 16;
+  const bf16* scales = sg.scales + (size_t)tile * k128 * 64 + g * 4;
+  const bf16* x = sg.X + t * 8;
+  float acc[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[nt][c] = 0.f;
+  for (int kb0 = warp; kb0 < k128; kb0 += QL_WARPS * QL_UNR) {
+    uint32_t wl[QL_UNR][4], wh[QL_UNR][4], sl[QL_UNR][2], sh[QL_UNR][2];
+#pragma unroll
+    for (int u = 0; u < QL_UNR; ++u) {
+      const int kb = kb0 + u * QL_WARPS;
+      zero_words(wl[u]); zero_words(wh[u]); zero_words(sl[u]); zero_words(sh[u]);
+      if (kb < k128) {
+        load_words<4>(wl[u], codes + (size_t)kb * 1024);
+        load_words<4>(wh[u], codes + (size_t)kb * 1024 + 512);
+        load_words<2>(sl[u], scales + (size_t)kb * 64);
+        load_words<2>(sh[u], scales + (size_t)kb * 64 + 32);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < QL_UNR; ++u) {
+      const int kb = kb0 + u * QL_WARPS;
+      if (kb >= k128) break;
+#pragma unroll
+      for (int gi = 0; gi < 4; ++gi) {
+        const int col = kb * 128 + gi * GROUP;
+        uint32_t ka[2][4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int byte = c * 8 + gi * 2;
+          const uint32_t sel = (byte & 2) ? 0x3322u : 0x1100u;
+          const uint32_t p0 = __byte_perm(wl[u][byte / 4], 0, sel), p1 = __byte_perm(wh[u][byte / 4], 0, sel);
+          ka[c][0] = code_e0(p0); ka[c][1] = code_e0(p1); ka[c][2] = code_e1(p0); ka[c][3] = code_e1(p1);
+        }
+        const float s_lo = scale_at(sl[u], gi), s_hi = scale_at(sh[u], gi);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int tok = tok0 + nt * 8 + g;
+          uint4 xv = make_uint4(0, 0, 0, 0);
+          if (tok < a.M && col < a.K) xv = __ldg(reinterpret_cast<const uint4*>(x + (size_t)tok * a.K + col));
+          float part[4];
+          mma_16816_zero(part, ka[0], mul_bf16x2(xv.x, MUL_E0), mul_bf16x2(xv.y, MUL_E1));
+          mma_16816(part, ka[1], mul_bf16x2(xv.z, MUL_E0), mul_bf16x2(xv.w, MUL_E1));
+          acc[nt][0] = fmaf(s_lo, part[0], acc[nt][0]); acc[nt][1] = fmaf(s_lo, part[1], acc[nt][1]);
+          acc[nt][2] = fmaf(s_hi, part[2], acc[nt][2]); acc[nt][3] = fmaf(s_hi, part[3], acc[nt][3]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) red[warp][g + 8 * (c >> 1)][nt * 8 + 2 * t + (c & 1)] = acc[nt][c];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * NT * 8; i += QL_WARPS * 32) {
+    const int row = i % 16, tok = i / 16;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < QL_WARPS; ++w) v += red[w][row][tok];
+    v *= TWO_69;
+    const int r = tile * 16 + row;
+    if (r < sg.N && tok0 + tok < a.M) {
+      const size_t o = (size_t)(tok0 + tok) * a.ldo + sg.out_off + r;
+      if (a.out_f32) a.out_f32[o] = v;
+      else a.out_bf16[o] = __float2bfloat16(v);
+    }
+  }
+}
+
+template <int NT>
+cudaError_t run_nt(const QLinArgs& a, int tiles, cudaStream_t st) {
+  return launch_pdl(qlinear_kernel<NT>, dim3((unsigned)tiles, (unsigned)((a.M + NT * 8 - 1) / (NT * 8))), dim3(QL_WARPS * 32), st, a);
+}
+
+}  // namespace
+
+size_t qlinear_code_bytes(long long N, long long K) { return (size_t)((N + 15) / 16) * ((K + 127) / 128) * 1024; }
+size_t qlinear_scale_bytes(long long N, long long K) { return (size_t)((N + 15) / 16) * ((K + 127) / 128) * 128; }
+
+int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int K, long long* launches, cudaStream_t st) {
+  PackArgs a{w, codes, scales, N, K, (N + 15) / 16, (K + 127) / 128};
+  const long long ctas = ((long long)a.n16 * a.k128 * 16 + 31) / 32;
+  qlinear_pack_kernel<<<(unsigned)(ctas < 4736 ? ctas : 4736), 256, 0, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+int launch_qlinear(const QLinArgs& a, int sm_count, long long* launches, cudaStream_t st) {
+  int tiles = 0;
+  for (int s = 0; s < a.n_seg; ++s) tiles += (a.seg[s].N + 15) / 16;
+  cudaError_t e;
+  if (a.M <= 8) e = run_nt<1>(a, tiles, st);
+  else if (a.M <= 16) e = run_nt<2>(a, tiles, st);
+  else if (a.M <= 32) e = run_nt<4>(a, tiles, st);
+  else e = run_nt<8>(a, tiles, st);
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
