@@ -407,19 +407,22 @@ class CCA:
 
     # ---- cache and weights in 4 bits ------------------------------------------------------
     def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def _need(self, t, name: str, dtype, shape):
-        """Argument check of the 4-bit entry points: a contiguous tensor of this type and shape on the handle's device."""
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
-            raise CcaError(f"{name}: wants a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, got {t.dtype} "
-                           f"{tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+        """Argument check of the 4-bit entry points: a contiguous tensor of this type and shape on the handle's device.  Cheap
+        attribute reads only: at a decode step's sizes a call is bound by what the host does for it."""
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self.device.index and t.is_contiguous():
+            return t.data_ptr()
+        raise CcaError(f"{name}: wants a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, got {t.dtype} "
+                       f"{tuple(t.shape)} on {t.device}")
 
     def _q_ws(self, ws: torch.Tensor):
-        if ws.device != self.device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        if ws.get_device() != self.device.index or ws.dtype is not torch.uint8 or not ws.is_contiguous():
             raise CcaError(f"workspace: wants a contiguous uint8 tensor on {self.device}, got {ws.dtype} on {ws.device}")
-        return self._ws_ptr(ws)
+        p = ws.data_ptr()
+        a = (p + 255) // 256 * 256
+        return a, ws.numel() - (a - p)
 
     def new_qcache(self, B: int, S_max: int) -> Dict[str, torch.Tensor]:
         """Caller-owned tensors of cca_qcache for B empty sequences."""
@@ -436,20 +439,15 @@ class CCA:
         """(cca_qcache, B) of a dict as new_qcache makes it; "weight" and "position" may be absent."""
         hk, dh = self.cfg.n_kv_heads, self.cfg.head_dim
         B, S = cache["len"].shape[0], cache["k_codes"].shape[2]
-        c = cca_qcache()
         rows = (B, hk, S)
-        codes, scales = rows + (dh // 2,), rows + (dh // 32,)
-        c.k_codes = self._need(cache["k_codes"], "k_codes", torch.uint8, codes)
-        c.v_codes = self._need(cache["v_codes"], "v_codes", torch.uint8, codes)
-        c.k_scales = self._need(cache["k_scales"], "k_scales", torch.bfloat16, scales)
-        c.v_scales = self._need(cache["v_scales"], "v_scales", torch.bfloat16, scales)
-        if cache.get("weight") is not None:
-            c.weight = self._need(cache["weight"], "weight", torch.float32, rows)
-        if cache.get("position") is not None:
-            c.position = self._need(cache["position"], "position", torch.int32, rows)
-        c.len = self._need(cache["len"], "len", torch.int32, (B,))
-        c.S_max = S
-        return c, B
+        codes, scales = (B, hk, S, dh // 2), (B, hk, S, dh // 32)
+        need, weight, position = self._need, cache.get("weight"), cache.get("position")
+        return cca_qcache(need(cache["k_codes"], "k_codes", torch.uint8, codes), need(cache["v_codes"], "v_codes", torch.uint8, codes),
+                          need(cache["k_scales"], "k_scales", torch.bfloat16, scales),
+                          need(cache["v_scales"], "v_scales", torch.bfloat16, scales),
+                          None if weight is None else need(weight, "weight", torch.float32, rows),
+                          None if position is None else need(position, "position", torch.int32, rows),
+                          need(cache["len"], "len", torch.int32, (B,)), S), B
 
     def qcache_append(self, cache, k: torch.Tensor, v: torch.Tensor, position: Optional[torch.Tensor] = None,
                       count: Optional[torch.Tensor] = None):

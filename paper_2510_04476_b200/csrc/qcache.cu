@@ -13,6 +13,7 @@ namespace {
 
 using namespace q4;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int MAX_DEVICES = 64;
 
 template <int DH>
 struct Row {                                       // a cache row of one head
@@ -154,58 +155,125 @@ CCA_DEVINL int rows_of(const QaArgs& a, int b) {          // -1: does not fit
   return (len < 0 || n > a.max_len || n > a.c.S_max || (a.pos && a.pos[b] < 0)) ? -1 : (int)n;
 }
 
-// The row of a 16-row tile that operand row r (of 8) stands for: with this order the four lanes t of a quad read four
-// neighbouring value rows at a time, and the eight lane groups still read eight neighbouring key rows.
-CCA_DEVINL int tile_row(int r) { return (r >> 1) + 4 * (r & 1); }
+// The row of a 16-row tile that operand row r (of 8) stands for.  With this order the key rows of lane groups 2i, 2i + 1 and the
+// four value rows of a quad are spread evenly over the two halves of a 128-byte line of shared memory.
+CCA_DEVINL int tile_row(int r) { return r ^ ((r >> 1) & 1); }
 
+template <int BYTES>
+CCA_DEVINL void cp_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+template <int BYTES>
+CCA_DEVINL void cp_async_or_zero(uint32_t dst, const void* src, bool ok) {       // not ok: zeros, nothing is read
+  const int n = ok ? BYTES : 0;
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
+}
+CCA_DEVINL void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+CCA_DEVINL void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A warp's stage of the cache: SR rows' codes and scales as they lie in global memory.  Each warp copies its own (asynchronously,
+// 16 bytes a lane, whole lines) and reads it alone, so no barrier but the warp's own stands between them.
 template <int DH>
-struct Tile {                                              // what a lane holds of 16 rows
+struct Stage {
   using R = Row<DH>;
+  static constexpr int SR = DH == 256 ? 16 : 32;           // rows
+  static constexpr int SB = R::SCALES * 2;                 // bytes of scales of a row
+  static constexpr int K = 0, V = SR * R::CODES, KS = 2 * SR * R::CODES, VS = KS + SR * SB, BYTES = VS + SR * SB;
+  static constexpr int N = 2;                              // stages of a warp: one in flight while the other is worked on
   static constexpr int KW = R::NB * R::NG;                 // words of codes of a key row per lane: 2 channel octets of every group
   static constexpr int VB = 2 * R::NG;                     // bytes of codes of a value row per lane and block
   static constexpr int VW = (VB + 3) / 4;
-  uint32_t k[2][KW], v[4][R::NB * VW], ks[2][R::SW], vs[2][R::SW];
 
-  CCA_DEVINL void load(const uint8_t* kc, const uint8_t* vc, const bf16* ksc, const bf16* vsc, int r0, int r_end, int g, int t) {
+  static constexpr int PER_ROW = R::CODES / 16, PIECES = SR * PER_ROW / 32;
+
+  // Copies rows r0 .. r0 + SR - 1; the pointers are this lane's places in them: byte 16 lane of the codes, row `lane` of the scales.
+  CCA_DEVINL static void fill(uint32_t dst, const uint8_t* kp, const uint8_t* vp, const bf16* ksp, const bf16* vsp, int lane) {
 #pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-      const int r = r0 + 8 * hi + tile_row(g);
-      zero_words(k[hi]); zero_words(ks[hi]); zero_words(vs[hi]);
-      if (r < r_end) {
-#pragma unroll
-        for (int blk = 0; blk < R::NB; ++blk) {
-          uint32_t w[R::NG];
-          load_words<R::NG>(w, kc + (size_t)r * R::CODES + blk * (R::BLK / 2) + t * 4 * R::NG);
-#pragma unroll
-          for (int i = 0; i < R::NG; ++i) k[hi][blk * R::NG + i] = w[i];
-        }
-        load_scales<DH>(ks[hi], ksc + (size_t)r * R::SCALES);
-        load_scales<DH>(vs[hi], vsc + (size_t)r * R::SCALES);
+    for (int i = 0; i < PIECES; ++i) {
+      cp_async<16>(dst + K + i * 512 + lane * 16, kp + i * 512);
+      cp_async<16>(dst + V + i * 512 + lane * 16, vp + i * 512);
+    }
+    if constexpr (SB >= 4) {                               // d_h = 32: 2 bytes a row are too few for a copy (see Rows)
+      if (SR == 32 || lane < SR) {
+        cp_async<SB>(dst + KS + lane * SB, ksp);
+        cp_async<SB>(dst + VS + lane * SB, vsp);
       }
     }
+  }
+  // The same for the first `rows` < SR rows alone; the others' places are filled with zeros.
+  CCA_DEVINL static void fill_part(uint32_t dst, const uint8_t* kp, const uint8_t* vp, const bf16* ksp, const bf16* vsp, int lane, int rows) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                          // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
-      const int r = r0 + 4 * i + t;
-      zero_words(v[i]);
-      if (r < r_end) {
-#pragma unroll
-        for (int blk = 0; blk < R::NB; ++blk) {
-          const uint8_t* p = vc + (size_t)r * R::CODES + blk * (R::BLK / 2) + g * VB;
-          if constexpr (VB == 2) {
-            v[i][0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
-          } else {
-            uint32_t w[VW];
-            load_words<VW>(w, p);
-#pragma unroll
-            for (int x = 0; x < VW; ++x) v[i][blk * VW + x] = w[x];
-          }
-        }
+    for (int i = 0; i < PIECES; ++i) {
+      const bool ok = lane / PER_ROW + i * (32 / PER_ROW) < rows;
+      cp_async_or_zero<16>(dst + K + i * 512 + lane * 16, ok ? kp + i * 512 : kp - lane * 16, ok);
+      cp_async_or_zero<16>(dst + V + i * 512 + lane * 16, ok ? vp + i * 512 : vp - lane * 16, ok);
+    }
+    if constexpr (SB >= 4) {
+      if (lane < SR) {
+        const bool ok = lane < rows;
+        cp_async_or_zero<SB>(dst + KS + lane * SB, ok ? ksp : ksp - lane * R::SCALES, ok);
+        cp_async_or_zero<SB>(dst + VS + lane * SB, ok ? vsp : vsp - lane * R::SCALES, ok);
       }
     }
   }
 };
 
-constexpr int QA_WARPS = 4;
+// What a lane takes of 16 rows of a stage: key rows tile_row(g) and 8 more, value rows tile_row(2t), tile_row(2t + 1) and 8 more of each.
+template <int DH>
+struct Rows {
+  using R = Row<DH>;
+  using S = Stage<DH>;
+  uint32_t k[2][S::KW], v[4][R::NB * S::VW], ks[2][R::SW], vs[2][R::SW];
+
+  template <int NW>
+  CCA_DEVINL static void take(uint32_t* dst, const unsigned char* p) {
+    if constexpr (NW == 1) dst[0] = *reinterpret_cast<const uint32_t*>(p);
+    else if constexpr (NW == 2) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      dst[0] = u.x; dst[1] = u.y;
+    } else {
+      const uint4 u = *reinterpret_cast<const uint4*>(p);
+      dst[0] = u.x; dst[1] = u.y; dst[2] = u.z; dst[3] = u.w;
+    }
+  }
+  // `st`: the first of the 16 rows' place in the stage, for codes; `row`: its number in the stage; r0: its number in the sequence
+  CCA_DEVINL void read_keys(const unsigned char* st, int row, int r0, int last, const bf16* ksc, int g, int t) {
+    const unsigned char* kp = st + S::K + (row + tile_row(g)) * R::CODES + t * 4 * R::NG;
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+#pragma unroll
+      for (int blk = 0; blk < R::NB; ++blk) take<R::NG>(k[hi] + blk * R::NG, kp + 8 * hi * R::CODES + blk * (R::BLK / 2));
+      read_scales(ks[hi], st + S::KS, row + 8 * hi + tile_row(g), ksc, min(r0 + 8 * hi + tile_row(g), last));
+    }
+  }
+  CCA_DEVINL void read_values(const unsigned char* st, int row, int r0, int last, const bf16* vsc, int g, int t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                          // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
+      const unsigned char* vp = st + S::V + (row + 8 * (i >> 1) + tile_row(2 * t + (i & 1))) * R::CODES + g * S::VB;
+#pragma unroll
+      for (int blk = 0; blk < R::NB; ++blk) {
+        if constexpr (S::VB == 2) v[i][0] = *reinterpret_cast<const unsigned short*>(vp);
+        else take<S::VW>(v[i] + blk * S::VW, vp + blk * (R::BLK / 2));
+      }
+    }
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi)
+      read_scales(vs[hi], st + S::VS, row + 8 * hi + tile_row(g), vsc, min(r0 + 8 * hi + tile_row(g), last));
+  }
+  CCA_DEVINL static void read_scales(uint32_t (&w)[R::SW], const unsigned char* st, int row, const bf16* sc, int r) {
+    if constexpr (DH == 32) w[0] = *reinterpret_cast<const unsigned short*>(sc + r);
+    else take<R::SW>(w, st + row * S::SB);
+  }
+};
+
+constexpr int QA_WARPS = 4, QA_MAX_SPLITS = 128;
+// CTAs of the attention kernel that an SM holds; registers are given out accordingly.
+__host__ __device__ constexpr int qa_resident(int dh, int nht) {
+  return nht == 1 ? (dh == 32 ? 7 : dh == 64 ? 6 : dh == 128 ? 4 : 3) : (dh == 32 ? 5 : dh == 64 ? 4 : 3);
+}
 
 // One CTA: rows [split * chunk, ...) of sequence b, kv head j, up to 8 NHT of its query heads; its four warps take 16 rows each in
 // turn.  S^T = K Q^T has the rows as the 16 and the heads as the 8 of m16n8k16, so that up to 8 heads cost one instruction per
@@ -213,10 +281,10 @@ constexpr int QA_WARPS = 4;
 // group's scale multiplies the group's partial logit in fp32; a value row's scale is multiplied into the probability, once
 // per group, before that is rounded to bf16 as the operand (the only rounding of the probabilities; the sums are taken before it).
 template <int DH, int NHT>
-__global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
+__global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_attn_kernel(QaArgs a) {
   pdl_enter();
   using R = Row<DH>;
-  using T = Tile<DH>;
+  using S = Stage<DH>;
   constexpr int MT = DH / 16;                              // 16-channel tiles of O^T
   const CcaDims& d = a.d;
   const int split = blockIdx.x, b = blockIdx.z;
@@ -233,34 +301,32 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
   const int r_begin = split * a.chunk, r_end = min(n_rows, r_begin + a.chunk);
 
   // query operand: head h0 + g (+ 8), channels grp * 32 + 8 t .. + 7 of every group, times 2^64 (e0 lanes) or 2^60 (e1 lanes)
-  uint32_t qb[NHT][R::NB * R::NG][4];
+  __shared__ uint4 qs[NHT][R::NB * R::NG][32];
 #pragma unroll
-  for (int ht = 0; ht < NHT; ++ht)
-#pragma unroll
-    for (int gi = 0; gi < R::NB * R::NG; ++gi) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (g + 8 * ht < nh) {
-        const size_t off = (size_t)b * d.Lq + (size_t)(j * d.g + h0 + g + 8 * ht) * DH + gi * GROUP + t * 8;
-        if (a.q32) {
-          const float4 x = *reinterpret_cast<const float4*>(a.q32 + off), y = *reinterpret_cast<const float4*>(a.q32 + off + 4);
-          w = make_uint4(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
-        } else {
-          w = *reinterpret_cast<const uint4*>(a.q + off);
-        }
+  for (int x = warp; x < NHT * R::NB * R::NG; x += QA_WARPS) {
+    const int ht = x / (R::NB * R::NG), gi = x % (R::NB * R::NG);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (g + 8 * ht < nh) {
+      const size_t off = (size_t)b * d.Lq + (size_t)(j * d.g + h0 + g + 8 * ht) * DH + gi * GROUP + t * 8;
+      if (a.q32) {
+        const float4 x = *reinterpret_cast<const float4*>(a.q32 + off), y = *reinterpret_cast<const float4*>(a.q32 + off + 4);
+        w = make_uint4(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+      } else {
+        w = *reinterpret_cast<const uint4*>(a.q + off);
       }
-      qb[ht][gi][0] = mul_bf16x2(w.x, MUL_E0); qb[ht][gi][1] = mul_bf16x2(w.y, MUL_E1);
-      qb[ht][gi][2] = mul_bf16x2(w.z, MUL_E0); qb[ht][gi][3] = mul_bf16x2(w.w, MUL_E1);
     }
+    qs[ht][gi][lane] = make_uint4(mul_bf16x2(w.x, MUL_E0), mul_bf16x2(w.y, MUL_E1), mul_bf16x2(w.z, MUL_E0), mul_bf16x2(w.w, MUL_E1));
+  }
   const float c_scale = rsqrtf((float)DH) * LOG2E * TWO_69;
 
-  // softmax state of heads 2t, 2t + 1 (+ 8 ht): the maximum is the same in all lanes of a column, the sums are per lane.
-  // Probabilities carry 2^64, which the bf16 subnormals of the value codes need.
-  float mx[NHT][2], off[NHT][2], sum[NHT][2];
+  // softmax state of heads 2t, 2t + 1 (+ 8 ht): off = 64 - maximum, the same in all lanes of a column; the sums are per lane.
+  // Probabilities carry 2^64, which the bf16 subnormals of the value codes need, and may pass that by 2^8 before the maximum is moved.
+  float off[NHT][2], sum[NHT][2];
   float o[NHT][MT][4];
 #pragma unroll
   for (int ht = 0; ht < NHT; ++ht) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) { mx[ht][c] = -INFINITY; off[ht][c] = 64.f; sum[ht][c] = 0.f; }
+    for (int c = 0; c < 2; ++c) { off[ht][c] = INFINITY; sum[ht][c] = 0.f; }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -272,11 +338,12 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
   const bf16 *ksc = a.c.k_scales + base * R::SCALES, *vsc = a.c.v_scales + base * R::SCALES;
   float* sco = a.scores ? a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g + h0 : nullptr;
 
-  T cur, nxt;
-  int r0 = r_begin + warp * 16;
-  if (r0 < r_end) cur.load(kc, vc, ksc, vsc, r0, r_end, g, t);
-  for (; r0 < r_end; r0 += QA_WARPS * 16) {
-    if (r0 + QA_WARPS * 16 < r_end) nxt.load(kc, vc, ksc, vsc, r0 + QA_WARPS * 16, r_end, g, t);
+  const int last = r_end - 1, g8 = 8 * d.g;
+  const bool even_heads = d.g % 2 == 0;
+  auto tile = [&](const unsigned char* st, int row, int r0) {
+    Rows<DH> cur;
+    cur.read_keys(st, row, r0, last, ksc, g, t);
+    const bool masked = r0 + 15 > last;
     // ---- logits (times log2 e) of rows tile_row(g), 8 + tile_row(g), heads 2t, 2t + 1
     float s[NHT][4];
 #pragma unroll
@@ -287,6 +354,9 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
     for (int gi = 0; gi < R::NB * R::NG; ++gi) {
       const float s_lo = scale_at(cur.ks[0], gi), s_hi = scale_at(cur.ks[1], gi);
       float part[NHT][4];
+      uint4 qb[NHT];
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht) qb[ht] = qs[ht][gi][lane];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {                        // channel octets of lanes 2t and 2t + 1
         const int blk = gi / R::NG, byte = c * 2 * R::NG + (gi % R::NG) * 2;
@@ -295,8 +365,8 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
         const uint32_t ka[4] = {code_e0(p0), code_e0(p1), code_e1(p0), code_e1(p1)};
 #pragma unroll
         for (int ht = 0; ht < NHT; ++ht) {
-          if (c == 0) mma_16816_zero(part[ht], ka, qb[ht][gi][0], qb[ht][gi][1]);
-          else mma_16816(part[ht], ka, qb[ht][gi][2], qb[ht][gi][3]);
+          if (c == 0) mma_16816_zero(part[ht], ka, qb[ht].x, qb[ht].y);
+          else mma_16816(part[ht], ka, qb[ht].z, qb[ht].w);
         }
       }
 #pragma unroll
@@ -306,23 +376,37 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
       }
     }
     const int r_lo = r0 + tile_row(g), r_hi = r_lo + 8;
+#pragma unroll
+    for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[ht][c] *= c_scale;
+    if (sco) {
+      float* sp = sco + (uint32_t)(r_lo * d.g + 2 * t);
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht) {
+        const bool ok_lo = 8 * ht + 2 * t < nh && (!masked || r_lo <= last), ok_hi = ok_lo && (!masked || r_hi <= last);
+        if (even_heads) {
+          if (ok_lo) *reinterpret_cast<float2*>(sp + 8 * ht) = make_float2(s[ht][0], s[ht][1]);
+          if (ok_hi) *reinterpret_cast<float2*>(sp + 8 * ht + g8) = make_float2(s[ht][2], s[ht][3]);
+        } else {
+          const bool two = 8 * ht + 2 * t + 1 < nh;
+          if (ok_lo) { sp[8 * ht] = s[ht][0]; if (two) sp[8 * ht + 1] = s[ht][1]; }
+          if (ok_hi) { sp[8 * ht + g8] = s[ht][2]; if (two) sp[8 * ht + g8 + 1] = s[ht][3]; }
+        }
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int ht = 0; ht < NHT; ++ht)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if ((c < 2 ? r_lo : r_hi) > last) s[ht][c] = -INFINITY;
+    }
     bool grow = false;
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        s[ht][c] = (c < 2 ? r_lo : r_hi) < r_end ? s[ht][c] * c_scale : -INFINITY;
-        grow = grow || s[ht][c] > mx[ht][c & 1] + 8.f;     // probabilities may pass 1 by 2^8 before the maximum is moved
-      }
-    if (sco) {
-#pragma unroll
-      for (int ht = 0; ht < NHT; ++ht)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int r = c < 2 ? r_lo : r_hi, h = 8 * ht + 2 * t + (c & 1);
-          if (r < r_end && h < nh) sco[(size_t)r * d.g + h] = s[ht][c];
-        }
-    }
+      for (int c = 0; c < 4; ++c) grow = grow || s[ht][c] + off[ht][c & 1] > 72.f;
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht)
@@ -331,9 +415,9 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
           float m = fmaxf(s[ht][c], s[ht][2 + c]);
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-          if (m > mx[ht][c]) {
-            const float al = exp2f(mx[ht][c] - m);         // 0 while nothing has been seen
-            mx[ht][c] = m; off[ht][c] = 64.f - m;
+          if (m + off[ht][c] > 64.f) {
+            const float al = exp2f(64.f - off[ht][c] - m); // 0 while nothing has been seen
+            off[ht][c] = 64.f - m;
             sum[ht][c] *= al;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) { o[ht][mt][c] *= al; o[ht][mt][2 + c] *= al; }
@@ -348,6 +432,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
         sum[ht][c & 1] += s[ht][c];
       }
     // ---- O^T += V^T P^T
+    cur.read_values(st, row, r0, last, vsc, g, t);
 #pragma unroll
     for (int gi = 0; gi < R::NB * R::NG; ++gi) {
       const float s_lo = scale_at(cur.vs[0], gi), s_hi = scale_at(cur.vs[1], gi);
@@ -359,7 +444,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
       }
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
-        const int blk = gi / R::NG, byte = (gi % R::NG) * 2 + jj, w = blk * T::VW + byte / 4;
+        const int blk = gi / R::NG, byte = (gi % R::NG) * 2 + jj, w = blk * S::VW + byte / 4;
         const uint32_t sel = (byte & 3) * 0x11u + ((byte & 3) + 4) * 0x1100u;
         const uint32_t p0 = __byte_perm(cur.v[0][w], cur.v[1][w], sel), p1 = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
         const uint32_t va[4] = {code_e0(p0), code_e1(p0), code_e0(p1), code_e1(p1)};
@@ -367,8 +452,38 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
         for (int ht = 0; ht < NHT; ++ht) mma_16816(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
       }
     }
-    cur = nxt;
+  };
+  // warp w takes stages w, w + 4, ... of the chunk
+  constexpr int STEP = QA_WARPS * S::SR;
+  extern __shared__ __align__(128) unsigned char ring[];
+  unsigned char* mine = ring + warp * (S::N * S::BYTES);
+  const uint32_t mine_u32 = (uint32_t)__cvta_generic_to_shared(mine);
+  int r0 = r_begin + warp * S::SR, slot = 0;
+  int ahead = r0;                                          // first row of the next stage to be filled
+  auto fill_next = [&](int into) {
+    const uint32_t dst = mine_u32 + into * S::BYTES;
+    const uint32_t at = (uint32_t)ahead * R::CODES + lane * 16, sat = (uint32_t)(ahead + lane) * R::SCALES;   // 2^31 bytes at most
+    if (ahead + S::SR <= r_end) S::fill(dst, kc + at, vc + at, ksc + sat, vsc + sat, lane);
+    else if (ahead < r_end) S::fill_part(dst, kc + at, vc + at, ksc + sat, vsc + sat, lane, r_end - ahead);
+    cp_async_commit();
+    ahead += STEP;
+  };
+#pragma unroll
+  for (int i = 0; i < S::N; ++i) fill_next(i);
+  __syncthreads();                                         // the query operand
+  for (; r0 < r_end; r0 += STEP) {
+    cp_async_wait<S::N - 1>();
+    __syncwarp();
+#pragma unroll
+    for (int half = 0; half < S::SR / 16; ++half) {
+      if (half > 0 && r0 + half * 16 > last) break;
+      tile(mine + slot * S::BYTES, half * 16, r0 + half * 16);
+    }
+    __syncwarp();
+    fill_next(slot);
+    slot = slot + 1 == S::N ? 0 : slot + 1;
   }
+  cp_async_wait<0>();
 #pragma unroll
   for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
@@ -376,22 +491,24 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) sum[ht][c] += __shfl_xor_sync(0xffffffffu, sum[ht][c], x);
   // merge the warps through shared memory
-  __shared__ float sm_o[QA_WARPS][8 * NHT][DH + 1];
+  static_assert(8 * NHT * (DH + 1) * 4 <= S::N * S::BYTES, "a warp's partial result takes the place of its stages");
   __shared__ float sm_ml[QA_WARPS][8 * NHT][2];
+  float* my_o = reinterpret_cast<float*>(mine);
+  __syncwarp();
 #pragma unroll
   for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        sm_o[warp][8 * ht + 2 * t + (c & 1)][(mt >> 1) * GROUP + 4 * g + (mt & 1) + 2 * (c >> 1)] =
+        my_o[(8 * ht + 2 * t + (c & 1)) * (DH + 1) + (mt >> 1) * GROUP + 4 * g + (mt & 1) + 2 * (c >> 1)] =
             o[ht][mt][c] * (c < 2 ? TWO_69 : TWO_65);
   if (g == 0) {
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        sm_ml[warp][8 * ht + 2 * t + c][0] = mx[ht][c];
+        sm_ml[warp][8 * ht + 2 * t + c][0] = 64.f - off[ht][c];
         sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c] * TWO_M64;
       }
   }
@@ -406,7 +523,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
     for (int w = 0; w < QA_WARPS; ++w) {
       const float al = (sm_ml[w][h][0] == -INFINITY) ? 0.f : exp2f(sm_ml[w][h][0] - mn);
       lo += sm_ml[w][h][1] * al;
-      oo += sm_o[w][h][c] * al;
+      oo += reinterpret_cast<const float*>(ring + w * (S::N * S::BYTES))[h * (DH + 1) + c] * al;
     }
     const size_t pidx = ((size_t)b * d.hq + j * d.g + h0 + h) * a.splits + split;
     a.part_o[pidx * DH + c] = oo;
@@ -416,84 +533,149 @@ __global__ void __launch_bounds__(QA_WARPS * 32) qcache_attn_kernel(QaArgs a) {
 
 // Joins the chunks' partial results of one (sequence, kv head) and, where the weights are gathered, adds to every row what its
 // heads gave it: 2^(logit - logsumexp), from the logits that the first kernel left (exact in fp32 whatever maximum a chunk used).
+// Its time is latency: the logits and weights of its rows are asked for before the logsumexps that they wait for are formed.
+constexpr int QJ_ROWS = 4;                                 // rows of a thread, where the weights are gathered
 template <int DH>
 __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
   pdl_enter();
-  __shared__ float sm_m[64], sm_l[64], red[256];
+  __shared__ float sm_lse[64], sm_inv[64], fac[QA_MAX_SPLITS];
+  __shared__ float4 red[256];
   const CcaDims& d = a.d;
   const int j = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_rows = rows_of(a, b);
   if (n_rows < 0) return;
   const size_t p0 = ((size_t)b * d.hq + j * d.g) * a.splits;
   const int used = (n_rows + a.chunk - 1) / a.chunk;       // chunks that hold rows
+  const float* sc = a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g;
+  float* w = a.c.weight + ((size_t)b * d.hk + j) * a.c.S_max;
+  const int r_first = blockIdx.x * (256 * QJ_ROWS) + tid;
+  float4 s4[QJ_ROWS];
+  float wr[QJ_ROWS];
+  if (a.scores) {
+#pragma unroll
+    for (int i = 0; i < QJ_ROWS; ++i) {
+      const int r = r_first + i * 256;
+      wr[i] = 0.f; s4[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < n_rows) {
+        wr[i] = w[r];
+        if (d.g % 4 == 0) s4[i] = *reinterpret_cast<const float4*>(sc + (size_t)r * d.g);
+      }
+    }
+  }
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   for (int h = warp; h < d.g; h += 8) {
+    float2 v[QA_MAX_SPLITS / 32];
     float m = -INFINITY, l = 0.f;
-    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[(p0 + (size_t)h * a.splits + s) * 2]);
+#pragma unroll
+    for (int i = 0; i < QA_MAX_SPLITS / 32; ++i) {
+      v[i] = make_float2(-INFINITY, 0.f);
+      if (lane + 32 * i < used) v[i] = ml[p0 + (size_t)h * a.splits + lane + 32 * i];
+    }
+#pragma unroll
+    for (int i = 0; i < QA_MAX_SPLITS / 32; ++i) m = fmaxf(m, v[i].x);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    for (int s = lane; s < used; s += 32) {
-      const float ms = a.part_ml[(p0 + (size_t)h * a.splits + s) * 2];
-      l += ms == -INFINITY ? 0.f : a.part_ml[(p0 + (size_t)h * a.splits + s) * 2 + 1] * exp2f(ms - m);
+#pragma unroll
+    for (int i = 0; i < QA_MAX_SPLITS / 32; ++i) {
+      const float f = v[i].x == -INFINITY ? 0.f : exp2f(v[i].x - m);
+      if (h == (int)blockIdx.x && lane + 32 * i < used) fac[lane + 32 * i] = f;
+      l += v[i].y * f;
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) { sm_m[h] = m; sm_l[h] = l; }
+    if (lane == 0) { sm_lse[h] = m + __log2f(l); sm_inv[h] = n_rows > 0 ? 1.f / l : 0.f; }
   }
   __syncthreads();
-  constexpr int PAR = 256 / DH > 0 ? 256 / DH : 1;          // threads that share an output channel, each with its chunks
-  for (int h = blockIdx.x; h < d.g; h += gridDim.x) {
-    const int c = tid % DH, part = tid / DH;
-    float acc = 0.f;
+  if ((int)blockIdx.x < d.g) {                             // CTA x joins head x: 256 / (DH / 4) threads share 4 channels
+    constexpr int LANES = DH / 4, PAR = 256 / LANES;
+    const int h = blockIdx.x, c = tid % LANES, part = tid / LANES;
+    const float4* po = reinterpret_cast<const float4*>(a.part_o + (p0 + (size_t)h * a.splits) * DH) + c;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int s = part; s < used; s += PAR) {
-      const size_t p = p0 + (size_t)h * a.splits + s;
-      const float ms = a.part_ml[p * 2];
-      if (ms != -INFINITY) acc += a.part_o[p * DH + c] * exp2f(ms - sm_m[h]);
+      const float4 v = po[(size_t)s * LANES];
+      const float f = fac[s];
+      acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y); acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
     }
     red[tid] = acc;
     __syncthreads();
     if (part == 0) {
-#pragma unroll
-      for (int x = 1; x < PAR; ++x) acc += red[x * DH + c];
-      a.o[(size_t)b * d.Lq + (size_t)(j * d.g + h) * DH + c] = __float2bfloat16(n_rows > 0 ? acc / sm_l[h] : 0.f);
+      for (int x = 1; x < PAR; ++x) {
+        const float4 v = red[x * LANES + c];
+        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+      }
+      const float inv = sm_inv[h];
+      const uint2 u = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+      reinterpret_cast<uint2*>(a.o + (size_t)b * d.Lq + (size_t)(j * d.g + h) * DH)[c] = u;
     }
-    __syncthreads();
   }
-  if (!a.scores || n_rows == 0) return;
-  if (tid < d.g) sm_m[tid] += __log2f(sm_l[tid]);
-  __syncthreads();
-  const float* sc = a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g;
-  float* w = a.c.weight + ((size_t)b * d.hk + j) * a.c.S_max;
-  for (int r = blockIdx.x * 256 + tid; r < n_rows; r += gridDim.x * 256) {
+  if (!a.scores) return;
+#pragma unroll
+  for (int i = 0; i < QJ_ROWS; ++i) {
+    const int r = r_first + i * 256;
+    if (r >= n_rows) break;
     float acc = 0.f;
-    for (int h = 0; h < d.g; ++h) acc += exp2f(sc[(size_t)r * d.g + h] - sm_m[h]);
-    w[r] += acc;
+    if (d.g % 4 == 0) {
+      acc = exp2f(s4[i].x - sm_lse[0]) + exp2f(s4[i].y - sm_lse[1]) + exp2f(s4[i].z - sm_lse[2]) + exp2f(s4[i].w - sm_lse[3]);
+      for (int h = 4; h < d.g; h += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(sc + (size_t)r * d.g + h);
+        acc += exp2f(v.x - sm_lse[h]) + exp2f(v.y - sm_lse[h + 1]) + exp2f(v.z - sm_lse[h + 2]) + exp2f(v.w - sm_lse[h + 3]);
+      }
+    } else {
+      for (int h = 0; h < d.g; ++h) acc += exp2f(sc[(size_t)r * d.g + h] - sm_lse[h]);
+    }
+    w[r] = wr[i] + acc;
   }
 }
 
 int heads_per_cta(const CcaDims& d) { return d.g <= 8 || d.dh == 256 ? 8 : 16; }
 
-// Rows per CTA and number of chunks for sequences of up to max_len rows.
+// Rows per CTA and number of chunks for sequences of up to max_len rows.  A chunk costs its rows plus what a CTA costs whatever its
+// rows (the way to its first loads, the merge of its warps, its share of the join: about as long as FIXED rows take); of one to four
+// full waves of resident CTAs the one with the least is taken.
 void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
   const int n_grp = (d.g + heads_per_cta(d) - 1) / heads_per_cta(d);
   const long long base = (long long)d.B * d.hk * n_grp;
-  long long want = (12LL * sm_count + base - 1) / base;
-  if (want < 1) want = 1;
-  if (want > 256) want = 256;
-  int ch = (int)((max_len + want - 1) / want);
-  ch = (ch + 63) / 64 * 64;                                // the four warps of a CTA take 16 rows each per round
-  if (ch < 64) ch = 64;
-  *chunk = ch;
-  *splits = (max_len + ch - 1) / ch;
+  const int resident = sm_count * qa_resident(d.dh, heads_per_cta(d) / 8);
+  constexpr int FIXED = 192;
+  long long best = -1;
+  for (int waves = 1; waves <= 4; ++waves) {
+    long long n = (long long)resident * waves / base;
+    if (n < 1) n = 1;
+    if (n > QA_MAX_SPLITS) n = QA_MAX_SPLITS;
+    long long ch = (max_len + n - 1) / n;
+    ch = (ch + 63) / 64 * 64;                              // the four warps of a CTA take 16 rows each per round
+    const long long used = (max_len + ch - 1) / ch;
+    const long long cost = (base * used + resident - 1) / resident * (ch + FIXED);
+    if (best < 0 || cost < best) { best = cost; *chunk = (int)ch; *splits = (int)used; }
+  }
 }
 
+// The opt-in to more than 48 KB of dynamic shared memory, per device and kernel (`done`: one flag per device).
+template <typename K>
+cudaError_t opt_in(K kernel, int bytes, bool* done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < MAX_DEVICES && done[dev])) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < MAX_DEVICES) done[dev] = true;
+  return e;
+}
+
+template <int DH, int NHT>
+cudaError_t attn_run(const QaArgs& a, dim3 grid, cudaStream_t st) {
+  constexpr int smem = QA_WARPS * Stage<DH>::N * Stage<DH>::BYTES;
+  static_assert(smem <= 48 * 1024, "no opt-in needed");
+  return launch_pdl_smem(qcache_attn_kernel<DH, NHT>, grid, dim3(QA_WARPS * 32), smem, st, a);
+}
 template <int DH>
 cudaError_t attn_dh(const QaArgs& a, cudaStream_t st) {
   const CcaDims& d = a.d;
   const int per = heads_per_cta(d);
   dim3 grid((unsigned)a.splits, (unsigned)(d.hk * ((d.g + per - 1) / per)), (unsigned)d.B);
   if constexpr (DH <= 128)
-    if (per == 16) return launch_pdl(qcache_attn_kernel<DH, 2>, grid, dim3(QA_WARPS * 32), st, a);
-  return launch_pdl(qcache_attn_kernel<DH, 1>, grid, dim3(QA_WARPS * 32), st, a);
+    if (per == 16) return attn_run<DH, 2>(a, grid, st);
+  return attn_run<DH, 1>(a, grid, st);
 }
 
 // ------------------------------------------------------------------------------------------------ eviction
@@ -667,7 +849,6 @@ __global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 constexpr int EV_SMEM_ROWS = 49152;                        // 192 KB of keys
-constexpr int MAX_DEVICES = 64;
 
 }  // namespace
 
@@ -737,9 +918,9 @@ int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, b
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   if (ev_end && (e = cudaEventRecord(ev_end, st)) != cudaSuccess) return -(int)e;
-  // one CTA per head at least; with weights to gather, one per 1024 rows
-  int nx = d.g;
-  if (accumulate && (max_len + 1023) / 1024 > nx) nx = (max_len + 1023) / 1024;
+  int nx = d.g;                                            // a CTA per head at least
+  const int by_rows = (max_len + 256 * QJ_ROWS - 1) / (256 * QJ_ROWS);
+  if (accumulate && by_rows > nx) nx = by_rows;
   QC_BY_HEAD((launch_pdl(qcache_join_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
@@ -761,14 +942,8 @@ int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent,
   if (max_len <= EV_SMEM_ROWS) {
     const int smem = (max_len > 1 ? max_len : 1) * 4;
     if (smem > 32 * 1024) {
-      static bool opted[MAX_DEVICES];                      // the opt-in to more shared memory is per device
-      int dev = 0;
-      if ((e = cudaGetDevice(&dev)) != cudaSuccess) return -(int)e;
-      if (dev >= MAX_DEVICES || !opted[dev]) {
-        e = cudaFuncSetAttribute(qcache_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_SMEM_ROWS * 4);
-        if (e != cudaSuccess) return -(int)e;
-        if (dev < MAX_DEVICES) opted[dev] = true;
-      }
+      static bool done[MAX_DEVICES];
+      if ((e = opt_in(qcache_select_kernel<true>, EV_SMEM_ROWS * 4, done)) != cudaSuccess) return -(int)e;
     }
     e = launch_pdl_smem(qcache_select_kernel<true>, grid, dim3(EV_THREADS), (size_t)smem, st, a);
   } else {
