@@ -1293,7 +1293,7 @@ int cca_qlinear(cca_handle* h, const cca_qlinear_weights* w, const void* x, void
   else a.out_bf16 = (bf16*)out;
   OnDevice on;
   CU(on.enter(h->device));
-  return enqueued(h, launch_qlinear(a, h->sm_count, &h->launches, (cudaStream_t)cuda_stream));
+  return enqueued(h, launch_qlinear(a, h->impl >= 1 ? h->tc : nullptr, h->d_status, &h->launches, (cudaStream_t)cuda_stream));
 }
 
 int cca_decode_workspace_size_q(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
@@ -1333,8 +1333,9 @@ int cca_decode_step_q(cca_handle* h, const cca_q_weights* w, const void* x, void
   OnDevice on;
   CU(on.enter(h->device));
   return enqueued(h, launch_decode_step_q(d, dw, (const bf16*)x, (bf16*)out, make_qcache(&s->cache), (float*)s->qk0_hist,
-                                          (bf16*)s->x_prev, s->pos, (int)max_len, workspace, h->sm_count, h->d_status,
-                                          &h->launches, h->ev_attn_begin, h->ev_attn_end, (cudaStream_t)cuda_stream));
+                                          (bf16*)s->x_prev, s->pos, (int)max_len, workspace, h->sm_count,
+                                          h->impl >= 1 ? h->tc : nullptr, h->d_status, &h->launches, h->ev_attn_begin, h->ev_attn_end,
+                                          (cudaStream_t)cuda_stream));
 }
 
 int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B, int64_t S,

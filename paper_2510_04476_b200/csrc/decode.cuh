@@ -2,6 +2,7 @@
 #pragma once
 #include "common.cuh"
 #include "qcache.cuh"
+#include "tc_kernels.cuh"
 
 struct DecodeWeights {
   const bf16 *w_qk, *w_v1, *w_v2, *w_o, *conv0_w, *conv1_w;
@@ -35,5 +36,5 @@ struct DecodeQWeights {
 };
 size_t decode_q_workspace_bytes(const CcaDims& d, int max_len, int sm_count);
 int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* x, bf16* out, const QCache& cache, float* hist,
-                         bf16* x_prev, const int* pos, int max_len, void* workspace, int sm_count, int* status,
+                         bf16* x_prev, const int* pos, int max_len, void* workspace, int sm_count, TcState* tc, int* status,
                          long long* launches, cudaEvent_t ev_attn_begin, cudaEvent_t ev_attn_end, cudaStream_t st);

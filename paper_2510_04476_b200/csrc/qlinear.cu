@@ -148,7 +148,15 @@ int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int 
   return 0;
 }
 
-int launch_qlinear(const QLinArgs& a, int sm_count, long long* launches, cudaStream_t st) {
+#ifndef QL_TC_M
+#define QL_TC_M 8
+#endif
+int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st) {
+  if (tc && a.M > QL_TC_M) {
+    const int r = tc_qlinear(tc, a, status, st);
+    if (r < 0) return r;
+    if (r == 0) { ++*launches; return 0; }
+  }
   int tiles = 0;
   for (int s = 0; s < a.n_seg; ++s) tiles += (a.seg[s].N + 15) / 16;
   cudaError_t e;
