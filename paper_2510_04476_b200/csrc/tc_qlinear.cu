@@ -1,6 +1,6 @@
 // y = x W^T for up to 64 tokens at a time on the tensor cores of this architecture, W in the 4-bit format of qformat.cuh.
 //
-//   warp 0       : TMA producer (one lane)            -- x tiles, up to 64 tokens x 128 channels, 4 stages
+//   warp 0       : TMA producer (one lane)            -- x tiles, up to 64 tokens x 128 channels, 6 stages
 //   warp 1       : TMEM owner + MMA issuer (one lane) -- 128 weight rows x tokens x 16 channels per instruction
 //   warps 2..13  : three groups of four, a thread per weight row: a block of 128 channels from its 64 bytes of codes into tensor
 //                  memory, as the MMA's A operand; the groups take the blocks in turn
@@ -23,20 +23,25 @@ using namespace q4;
 namespace {
 
 constexpr int TQ_GROUPS = 3, TQ_WARPS = 2 + 4 * TQ_GROUPS, TQ_THREADS = 32 * TQ_WARPS;
-constexpr int TQ_STAGES = 4, TQ_TOKENS = 64;
+constexpr int TQ_STAGES = 2 * TQ_GROUPS, TQ_TOKENS = 64;
 constexpr int TQ_STAGE_BYTES = TQ_TOKENS * 256;
-constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + 256 + 1024;      // barriers, slack for the 1024-byte alignment
+constexpr int TQ_PART_BYTES = TQ_TOKENS * 512;                        // a cluster's sums: [rank][this rank's tokens][128] fp32
+constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + 256 + 1024;      // barriers, slack for the 1024-byte alignment
 constexpr int TQ_A_COL = 64;                                          // accumulator columns, then the groups' operands
 constexpr uint32_t MUL_96 = 0x6f806f80u, MUL_92 = 0x6d806d80u;        // bf16x2 2^96, 2^92: operands become c s 2^-37
 constexpr float TWO_37 = 137438953472.f;
+constexpr uint32_t IDESC_NEG_A = 1u << 13;                            // instruction descriptor: A is negated
 
+struct TqSeg {
+  const uint8_t* codes;
+  const bf16* scales;
+  int N, out_off;
+};
 struct TqParams {
-  const uint8_t* codes[2];
-  const bf16* scales[2];
-  int N[2], out_off[2];
+  TqSeg seg0, seg1;
   int blocks0;               // row blocks of the first segment
   int K128, M, n_tok;        // n_tok: tokens of a pass, a multiple of 16
-  int per_cta;               // channel blocks of a CTA
+  int per_cta, log_ranks;    // channel blocks of a CTA; log2 of the CTAs that share a row block
   float* out_f32;
   bf16* out_bf16;
   int ldo;
@@ -47,29 +52,27 @@ TC_DEVINL void fail(volatile int* abort_flag, int* status, int code) {
   *abort_flag = 1;
   atomicCAS(status, 0, code);
 }
-CCA_DEVINL uint32_t rest_bf16x2(uint32_t a, uint32_t b, uint32_t ab) {          // a * b - ab
+CCA_DEVINL uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t r;
-  asm("{\n\t.reg .b32 t;\n\tneg.bf16x2 t, %3;\n\tfma.rn.bf16x2 %0, %1, %2, t;\n\t}" : "=r"(r) : "r"(a), "r"(b), "r"(ab));
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
-CCA_DEVINL float ld_cluster_f32(uint32_t addr, uint32_t rank) {
-  uint32_t remote;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-  return v;
+CCA_DEVINL uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
 }
-CCA_DEVINL void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+CCA_DEVINL void st_cluster_f32(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+CCA_DEVINL void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+CCA_DEVINL void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 __global__ void __launch_bounds__(TQ_THREADS, 1)
 tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant__ CUtensorMap tm1, TqParams p) {
   pdl_enter();
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* smem = smem_align1024(smem_dyn);
-  uint64_t* b_full = reinterpret_cast<uint64_t*>(smem + TQ_STAGES * TQ_STAGE_BYTES);
+  float* part = reinterpret_cast<float*>(smem + TQ_STAGES * TQ_STAGE_BYTES);
+  uint64_t* b_full = reinterpret_cast<uint64_t*>(smem + TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES);
   uint64_t* b_empty = b_full + TQ_STAGES;
   uint64_t* a_full = b_empty + TQ_STAGES;
   uint64_t* a_empty = a_full + TQ_GROUPS;
@@ -77,18 +80,48 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done_bar + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x, ranks = gridDim.x;
-  const int seg = (int)blockIdx.y >= p.blocks0 ? 1 : 0;
-  const int row0 = ((int)blockIdx.y - (seg ? p.blocks0 : 0)) * 128, tok0 = (int)blockIdx.z * TQ_TOKENS;
+  const int rank = blockIdx.x, ranks = gridDim.x, lr = p.log_ranks;      // ranks is a power of two
+  const bool second = (int)blockIdx.y >= p.blocks0;
+  const TqSeg sg = second ? p.seg1 : p.seg0;
+  const CUtensorMap* map = second ? &tm1 : &tm0;
+  const int row0 = ((int)blockIdx.y - (second ? p.blocks0 : 0)) * 128, tok0 = (int)blockIdx.z * TQ_TOKENS;
   const int kb_begin = rank * p.per_cta, n_kb = max(0, min(p.K128, kb_begin + p.per_cta) - kb_begin);
+
+  const int sub = p.n_tok * 128;                           // bytes of a 64-channel half of an x tile
+  auto load_x = [&](int i, int st) {
+    unsigned char* dst = smem + st * TQ_STAGE_BYTES;
+    mbar_expect_tx(&b_full[st], 2 * sub);
+    tma_load_2d(dst, map, (kb_begin + i) * 128, tok0, &b_full[st]);
+    tma_load_2d(dst + sub, map, (kb_begin + i) * 128 + 64, tok0, &b_full[st]);
+  };
+  // a dequantising thread's row and its first two blocks, on their way while the barriers and the tensor memory are set up
+  const int gr = (warp - 2) >> 2, q = warp & 3;
+  const int row = row0 + q * 32 + lane;
+  const bool there = warp >= 2 && row < (sg.N + 15) / 16 * 16;      // rows that the tiles hold
+  const size_t tile = (size_t)(row >> 4) * p.K128 + kb_begin;
+  const uint4* codes = reinterpret_cast<const uint4*>(sg.codes + (tile * 16 + (row & 15)) * 64);
+  const uint2* scales = reinterpret_cast<const uint2*>(sg.scales + (tile * 16 + (row & 15)) * 4);
+  struct Block { uint4 c[4]; uint2 s; };
+  Block w0, w1, w2;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w0.c[x] = w1.c[x] = w2.c[x] = make_uint4(0, 0, 0, 0);
+  w0.s = w1.s = w2.s = make_uint2(0, 0);
+  auto load = [&](Block& w, int i) {
+    if (i < n_kb && there) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w.c[x] = __ldg(codes + (size_t)i * 64 + x);
+      w.s = __ldg(scales + (size_t)i * 16);
+    }
+  };
+  load(w0, gr); load(w1, gr + TQ_GROUPS);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < TQ_STAGES; ++s) { mbar_init(&b_full[s], 1); mbar_init(&b_empty[s], 1); }
     for (int s = 0; s < TQ_GROUPS; ++s) { mbar_init(&a_full[s], 4); mbar_init(&a_empty[s], 1); }
     mbar_init(done_bar, 1);
-    wait_ctl_init(abort_flag, p.status);
     fence_barrier_init();
-    prefetch_tmap(seg ? &tm1 : &tm0);
+    for (int i = 0; i < min(n_kb, TQ_STAGES); ++i) load_x(i, i);
+    wait_ctl_init(abort_flag, p.status);
   }
   if (warp == 1) {
     tmem_alloc(tmem_slot, 512);
@@ -97,18 +130,15 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (ranks > 1) cluster_arrive();                         // from here on the others may be written to (see the sums)
   const uint32_t tmem = *tmem_slot;
-  const int sub = p.n_tok * 128;                           // bytes of a 64-channel half of an x tile
 
   if (warp == 0) {
     if (lane == 0) {
-      for (int i = 0; i < n_kb; ++i) {
+      for (int i = TQ_STAGES; i < n_kb; ++i) {
         const int st = i % TQ_STAGES;
         if (!mbar_wait(&b_empty[st], ((i / TQ_STAGES) & 1) ^ 1, abort_flag)) { fail(abort_flag, p.status, ST_TIMEOUT_TMA); break; }
-        unsigned char* dst = smem + st * TQ_STAGE_BYTES;
-        mbar_expect_tx(&b_full[st], 2 * sub);
-        tma_load_2d(dst, seg ? &tm1 : &tm0, (kb_begin + i) * 128, tok0, &b_full[st]);
-        tma_load_2d(dst + sub, seg ? &tm1 : &tm0, (kb_begin + i) * 128 + 64, tok0, &b_full[st]);
+        load_x(i, st);
       }
     }
   } else if (warp == 1) {
@@ -117,62 +147,53 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
     const uint32_t desc_hi = (uint32_t)(smem_desc_sw128(0, 0, 1024) >> 32);
     const uint32_t smem_lo = smem_u32(smem) >> 4;
     bool ok = true;
-    for (int i = 0; i < n_kb; ++i) {
-      const int st = i % TQ_STAGES, gr = i % TQ_GROUPS;
-      ok = __all_sync(0xffffffffu, mbar_wait(&b_full[st], (i / TQ_STAGES) & 1, abort_flag)) &&
-           __all_sync(0xffffffffu, mbar_wait(&a_full[gr], (i / TQ_GROUPS) & 1, abort_flag));
-      if (!ok) { fail(abort_flag, p.status, ST_TIMEOUT_MMA); break; }
-      tc_fence_after();
-      const uint32_t a = tmem + TQ_A_COL + gr * 128;
-      const uint32_t b = (smem_lo + st * (TQ_STAGE_BYTES >> 4)) | (1u << 16);
-      if (leader) {
+    uint32_t sph = 0;
+    for (int i0 = 0; ok && i0 < n_kb; i0 += TQ_STAGES, sph ^= 1) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part)               // hi, lo
+      for (int st = 0; st < TQ_STAGES; ++st) {             // stage and group are constants here, and so are the operands' places
+        const int i = i0 + st, gr = st % TQ_GROUPS;
+        if (i >= n_kb) break;
+        ok = __all_sync(0xffffffffu, mbar_wait(&b_full[st], sph, abort_flag)) &&
+             __all_sync(0xffffffffu, mbar_wait(&a_full[gr], (st / TQ_GROUPS) & 1, abort_flag));
+        if (!ok) { fail(abort_flag, p.status, ST_TIMEOUT_MMA); break; }
+        tc_fence_after();
+        const uint32_t a = tmem + TQ_A_COL + gr * 128;
+        const uint32_t b = (smem_lo + st * (TQ_STAGE_BYTES >> 4)) | (1u << 16);
+        if (leader) {
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            mma_ts_w(tmem, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi, idesc, (i | part | ks) != 0);
-        mma_commit(&a_empty[gr]);
-        mma_commit(&b_empty[st]);
-        if (i == n_kb - 1) mma_commit(done_bar);
+          for (int part = 0; part < 2; ++part)             // hi, then the negated rest
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              mma_ts_w(tmem, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi,
+                       part ? idesc | IDESC_NEG_A : idesc, (i | part | ks) != 0);
+          mma_commit(&a_empty[gr]);
+          mma_commit(&b_empty[st]);
+          if (i == n_kb - 1) mma_commit(done_bar);
+        }
       }
     }
   } else {
-    const int gr = (warp - 2) >> 2, q = warp & 3;
-    const int row = row0 + q * 32 + lane;
-    const bool there = row < (p.N[seg] + 15) / 16 * 16;    // rows that the tiles hold
-    const size_t tile = (size_t)(row >> 4) * p.K128 + kb_begin;
-    const uint4* codes = reinterpret_cast<const uint4*>(p.codes[seg] + (tile * 16 + (row & 15)) * 64);
-    const uint2* scales = reinterpret_cast<const uint2*>(p.scales[seg] + (tile * 16 + (row & 15)) * 4);
     const uint32_t a = tmem + ((uint32_t)(q * 32) << 16) + TQ_A_COL + gr * 128;
-    uint32_t w[16], nw[16];
-    uint2 sc = make_uint2(0, 0), nsc = make_uint2(0, 0);
-    auto load = [&](int i) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint4 u = there ? __ldg(codes + (size_t)i * 64 + x) : make_uint4(0, 0, 0, 0);
-        nw[4 * x] = u.x; nw[4 * x + 1] = u.y; nw[4 * x + 2] = u.z; nw[4 * x + 3] = u.w;
-      }
-      nsc = there ? __ldg(scales + (size_t)i * 16) : make_uint2(0, 0);
-    };
-    if (gr < n_kb) load(gr);
-    for (int i = gr, turn = 0; i < n_kb; i += TQ_GROUPS, ++turn) {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) w[x] = nw[x];
-      sc = nsc;
-      if (i + TQ_GROUPS < n_kb) load(i + TQ_GROUPS);
-      if (!mbar_wait(&a_empty[gr], (turn & 1) ^ 1, abort_flag)) { fail(abort_flag, p.status, ST_TIMEOUT_EPI); break; }
+    // two blocks of the group ahead are on their way while one is worked on
+    uint32_t phase = 1;
+    auto work = [&](const Block& w) -> bool {
+      if (!mbar_wait(&a_empty[gr], phase, abort_flag)) { fail(abort_flag, p.status, ST_TIMEOUT_EPI); return false; }
+      phase ^= 1;
       tc_fence_after();
 #pragma unroll
       for (int grp = 0; grp < 4; ++grp) {
-        const uint32_t s2 = __byte_perm(grp < 2 ? sc.x : sc.y, 0, (grp & 1) ? 0x3232u : 0x1010u);
+        const uint32_t s2 = __byte_perm(grp < 2 ? w.s.x : w.s.y, 0, (grp & 1) ? 0x3232u : 0x1010u);
         const uint32_t m0 = mul_bf16x2(s2, MUL_96), m1 = mul_bf16x2(s2, MUL_92);
+        const uint32_t n0 = m0 ^ 0x80008000u, n1 = m1 ^ 0x80008000u;
         uint32_t hi[16], lo[16];
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
-          const uint32_t pr = __byte_perm(w[g * 2 + (grp >> 1)], 0, (grp & 1) ? 0x3322u : 0x1100u);
+          const uint4 c = w.c[g >> 1];
+          const uint32_t word = (g & 1) ? (grp < 2 ? c.z : c.w) : (grp < 2 ? c.x : c.y);
+          const uint32_t pr = __byte_perm(word, 0, (grp & 1) ? 0x3322u : 0x1100u);
           const uint32_t e0 = code_e0(pr), e1 = code_e1(pr);
           hi[2 * g] = mul_bf16x2(e0, m0); hi[2 * g + 1] = mul_bf16x2(e1, m1);
-          lo[2 * g] = rest_bf16x2(e0, m0, hi[2 * g]); lo[2 * g + 1] = rest_bf16x2(e1, m1, hi[2 * g + 1]);
+          lo[2 * g] = fma_bf16x2(e0, n0, hi[2 * g]); lo[2 * g + 1] = fma_bf16x2(e1, n1, hi[2 * g + 1]);
         }
         tmem_st16(a + grp * 16, hi);
         tmem_st16(a + 64 + grp * 16, lo);
@@ -181,40 +202,52 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&a_full[gr]);
+      return true;
+    };
+    for (int i = gr; i < n_kb; i += 3 * TQ_GROUPS) {
+      load(w2, i + 2 * TQ_GROUPS);
+      if (!work(w0)) break;
+      if (i + TQ_GROUPS >= n_kb) break;
+      load(w0, i + 3 * TQ_GROUPS);
+      if (!work(w1)) break;
+      if (i + 2 * TQ_GROUPS >= n_kb) break;
+      load(w1, i + 4 * TQ_GROUPS);
+      if (!work(w2)) break;
     }
-    // ---- sums: thread = row, one column per token
-    if (gr == 0) {
-      bool ok = true;
+    // ---- sums: thread = row, one column per token.  In a cluster, token t is rank t % ranks's to add up: every CTA writes its
+    // part of it into that rank's shared memory.
+    bool ok = true;
+    if (n_kb > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag));
+      if (!ok) fail(abort_flag, p.status, ST_TIMEOUT_EPI);
+      tc_fence_after();
+    }
+    if (ranks > 1) cluster_wait();
+    const int r = q * 32 + lane, mine = p.n_tok >> lr;
+    const uint32_t to = smem_u32(part) + (uint32_t)(rank * mine * 128 + r) * 4;
+    for (int c = gr; ok && c < p.n_tok / 16; c += TQ_GROUPS) {
+      uint32_t v[16];
+#pragma unroll
+      for (int x = 0; x < 16; ++x) v[x] = 0u;
       if (n_kb > 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag));
-        if (!ok) fail(abort_flag, p.status, ST_TIMEOUT_EPI);
-        tc_fence_after();
+        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c * 16, v);
+        tmem_ld_wait();
       }
-      float* part = reinterpret_cast<float*>(smem);        // [tokens][128] where a cluster joins its sums; the x stages are done with
-      const int r = q * 32 + lane;
-      for (int c = 0; ok && c < p.n_tok / 16; ++c) {
-        uint32_t v[16];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) v[x] = 0u;
-        if (n_kb > 0) {
-          tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c * 16, v);
-          tmem_ld_wait();
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int tok = c * 16 + x;
-          const float y = __uint_as_float(v[x]) * TWO_37;
-          if (ranks > 1) {
-            part[tok * 128 + r] = y;
-          } else if (tok0 + tok < p.M && row < p.N[seg]) {
-            const size_t o = (size_t)(tok0 + tok) * p.ldo + p.out_off[seg] + row;
-            if (p.out_f32) p.out_f32[o] = y;
-            else p.out_bf16[o] = __float2bfloat16(y);
-          }
+      for (int x = 0; x < 16; ++x) {
+        const int tok = c * 16 + x;
+        const float y = __uint_as_float(v[x]) * TWO_37;
+        if (ranks > 1) {
+          st_cluster_f32(cluster_addr(to + (uint32_t)(tok >> lr) * 512, tok & (ranks - 1)), y);
+        } else if (tok0 + tok < p.M && row < sg.N) {
+          const size_t o = (size_t)(tok0 + tok) * p.ldo + sg.out_off + row;
+          if (p.out_f32) p.out_f32[o] = y;
+          else p.out_bf16[o] = __float2bfloat16(y);
         }
       }
     }
   }
+  if (ranks > 1 && warp < 2) { __syncwarp(); cluster_wait(); }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
@@ -228,19 +261,17 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
     tmem_dealloc(tmem, 512);
   }
   if (ranks > 1) {
-    cluster_sync();
-    const uint32_t part = smem_u32(smem);
-    const int n = min(p.n_tok, p.M - tok0);
-    for (int i = threadIdx.x; i < n * 128; i += TQ_THREADS) {
-      const int tok = i >> 7, r = i & 127;
-      if (tok % ranks != rank || row0 + r >= p.N[seg]) continue;
-      float y = 0.f;
-      for (int x = 0; x < ranks; ++x) y += ld_cluster_f32(part + (uint32_t)(tok * 128 + r) * 4, x);
-      const size_t o = (size_t)(tok0 + tok) * p.ldo + p.out_off[seg] + row0 + r;
-      if (p.out_f32) p.out_f32[o] = y;
-      else p.out_bf16[o] = __float2bfloat16(y);
-    }
-    cluster_sync();                                        // nobody leaves while its sums may still be read
+    cluster_arrive();                                      // all parts are written once everybody has come here
+    cluster_wait();
+    const int n = min(p.n_tok, p.M - tok0), r = threadIdx.x & 127, mine = p.n_tok >> lr;
+    if (threadIdx.x < 384 && row0 + r < sg.N)
+      for (int k = threadIdx.x >> 7; (k << lr) + rank < n; k += 3) {
+        float y = 0.f;
+        for (int x = 0; x < ranks; ++x) y += part[(x * mine + k) * 128 + r];
+        const size_t o = (size_t)(tok0 + (k << lr) + rank) * p.ldo + sg.out_off + row0 + r;
+        if (p.out_f32) p.out_f32[o] = y;
+        else p.out_bf16[o] = __float2bfloat16(y);
+      }
   }
 }
 
@@ -248,21 +279,19 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
 
 int tc_qlinear(TcState* tc, const QLinArgs& a, int* status, cudaStream_t st) {
   TqParams p;
-  p.blocks0 = 0;
-  int blocks = 0;
-  for (int s = 0; s < 2; ++s) {
-    const QLinSeg& sg = a.seg[s < a.n_seg ? s : 0];
-    p.codes[s] = sg.codes; p.scales[s] = sg.scales; p.N[s] = sg.N; p.out_off[s] = sg.out_off;
-    if (s < a.n_seg) blocks += (sg.N + 127) / 128;
-    if (s == 0) p.blocks0 = blocks;
-  }
+  const QLinSeg &s0 = a.seg[0], &s1 = a.seg[a.n_seg - 1];
+  p.seg0 = TqSeg{s0.codes, s0.scales, s0.N, s0.out_off};
+  p.seg1 = TqSeg{s1.codes, s1.scales, s1.N, s1.out_off};
+  p.blocks0 = (s0.N + 127) / 128;
+  const int blocks = p.blocks0 + (a.n_seg > 1 ? (s1.N + 127) / 128 : 0);
   p.K128 = (a.K + 127) / 128; p.M = a.M;
   p.n_tok = a.M >= TQ_TOKENS ? TQ_TOKENS : (a.M + 15) / 16 * 16;
   p.out_f32 = a.out_f32; p.out_bf16 = a.out_bf16; p.ldo = a.ldo; p.status = status;
   const int passes = (a.M + TQ_TOKENS - 1) / TQ_TOKENS;
   // the inner dimension over a cluster while that leaves every CTA two blocks and the SMs are not all taken
   int ranks = 1;
-  while (ranks < 8 && (long long)blocks * passes * ranks * 2 <= tc->sm_count && p.K128 >= ranks * 4) ranks *= 2;
+  p.log_ranks = 0;
+  while (ranks < 8 && (long long)blocks * passes * ranks * 2 <= tc->sm_count && p.K128 >= ranks * 4) { ranks *= 2; ++p.log_ranks; }
   p.per_cta = (p.K128 + ranks - 1) / ranks;
   CUtensorMap maps[2];
   for (int s = 0; s < 2; ++s)
