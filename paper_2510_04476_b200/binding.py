@@ -1,4 +1,5 @@
-"""Thin ctypes binding over libcca.so: argument marshalling only.
+"""Thin binding over libcca.so: argument marshalling only, by ctypes and, for the 4-bit entry points, whose calls are a few
+microseconds long, by a small CPython extension (csrc/bind.cpp).
 
 Every step of the block runs inside the library's CUDA kernels; torch is used here for device
 memory and streams.  There is no CPU fallback: if the library cannot be loaded, or a call fails,
@@ -15,6 +16,7 @@ import torch
 from . import build as _build
 
 _LIB = None
+_BIND = None
 
 
 class CcaError(RuntimeError):
@@ -61,11 +63,9 @@ class cca_decode_state(C.Structure):
                 ("pos", C.c_void_p), ("S_max", C.c_int64)]
 
 
-QCACHE_TENSORS = ("k_codes", "v_codes", "k_scales", "v_scales", "weight", "position", "len")
-
-
 class cca_qcache(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in QCACHE_TENSORS] + [("S_max", C.c_int64)]
+    _fields_ = [(n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "weight", "position", "len")] + \
+               [("S_max", C.c_int64)]
 
 
 class cca_qlinear_weights(C.Structure):
@@ -153,6 +153,10 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
+    global _BIND
+    from . import _bind
+    _bind.set_error(CcaError)
+    _BIND = _bind
     _LIB = lib
     return lib
 
@@ -193,6 +197,7 @@ class CCA:
         self.device = torch.device("cuda", device)
         self.handle = C.c_void_p()
         _check(self.lib, self.lib.cca_init(C.byref(self.cfg), device, C.byref(self.handle)), None, "cca_init")
+        self._native = _BIND.new_handle(self.handle.value, d_model, n_q_heads, n_kv_heads, head_dim, k_seq, k_ch, device)
 
     @classmethod
     def from_shape(cls, sh, device=0) -> "CCA":
@@ -201,6 +206,8 @@ class CCA:
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:
+            if getattr(self, "_native", None) is not None:
+                _BIND.close_handle(self._native)
             self.lib.cca_destroy(self.handle)
             self.handle = C.c_void_p()
 
@@ -406,26 +413,10 @@ class CCA:
                self.handle, "cca_decode_state_from_prefill")
 
     # ---- cache and weights in 4 bits ------------------------------------------------------
-    def _stream(self):
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
-
-    def _need(self, t, name: str, dtype, shape):
-        """Argument check of the 4-bit entry points: a contiguous tensor of this type and shape on the handle's device.  Cheap
-        attribute reads only: at a decode step's sizes a call is bound by what the host does for it."""
-        if t.dtype is dtype and t.shape == shape and t.get_device() == self.device.index and t.is_contiguous():
-            return t.data_ptr()
-        raise CcaError(f"{name}: wants a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, got {t.dtype} "
-                       f"{tuple(t.shape)} on {t.device}")
-
-    def _q_ws(self, ws: torch.Tensor):
-        if ws.get_device() != self.device.index or ws.dtype is not torch.uint8 or not ws.is_contiguous():
-            raise CcaError(f"workspace: wants a contiguous uint8 tensor on {self.device}, got {ws.dtype} on {ws.device}")
-        p = ws.data_ptr()
-        a = (p + 255) // 256 * 256
-        return a, ws.numel() - (a - p)
-
+    # Tensors are checked (type, shape, device, contiguous) by the extension; what does not fit raises CcaError.
     def new_qcache(self, B: int, S_max: int) -> Dict[str, torch.Tensor]:
-        """Caller-owned tensors of cca_qcache for B empty sequences."""
+        """Caller-owned tensors of cca_qcache for B empty sequences.  "weight" and "position" may be left out of the dict that
+        the calls are given (then nothing is gathered and nothing can be evicted)."""
         hk, dh, dev = self.cfg.n_kv_heads, self.cfg.head_dim, self.device
         cache = {"weight": torch.zeros(B, hk, S_max, dtype=torch.float32, device=dev),
                  "position": torch.zeros(B, hk, S_max, dtype=torch.int32, device=dev),
@@ -435,41 +426,14 @@ class CCA:
             cache[n + "_scales"] = torch.zeros(B, hk, S_max, dh // 32, dtype=torch.bfloat16, device=dev)
         return cache
 
-    def _qcache(self, cache: Dict[str, torch.Tensor]):
-        """(cca_qcache, B) of a dict as new_qcache makes it; "weight" and "position" may be absent."""
-        hk, dh = self.cfg.n_kv_heads, self.cfg.head_dim
-        B, S = cache["len"].shape[0], cache["k_codes"].shape[2]
-        rows = (B, hk, S)
-        codes, scales = (B, hk, S, dh // 2), (B, hk, S, dh // 32)
-        need, weight, position = self._need, cache.get("weight"), cache.get("position")
-        return cca_qcache(need(cache["k_codes"], "k_codes", torch.uint8, codes), need(cache["v_codes"], "v_codes", torch.uint8, codes),
-                          need(cache["k_scales"], "k_scales", torch.bfloat16, scales),
-                          need(cache["v_scales"], "v_scales", torch.bfloat16, scales),
-                          None if weight is None else need(weight, "weight", torch.float32, rows),
-                          None if position is None else need(position, "position", torch.int32, rows),
-                          need(cache["len"], "len", torch.int32, (B,)), S), B
-
     def qcache_append(self, cache, k: torch.Tensor, v: torch.Tensor, position: Optional[torch.Tensor] = None,
                       count: Optional[torch.Tensor] = None):
         """cca_qcache_append: k, v [B, n, h_k, d_h] into rows len[b] .. ; `len` is the caller's to advance."""
-        c, B = self._qcache(cache)
-        n = k.shape[1]
-        shape = (B, n, self.cfg.n_kv_heads, self.cfg.head_dim)
-        _check(self.lib, self.lib.cca_qcache_append(
-            self.handle, self._need(k, "k", torch.bfloat16, shape), self._need(v, "v", torch.bfloat16, shape),
-            None if position is None else self._need(position, "position", torch.int32, (B,)),
-            None if count is None else self._need(count, "count", torch.int32, (B,)), C.byref(c), B, n, self._stream()),
-            self.handle, "cca_qcache_append")
+        _BIND.qcache_append(self._native, cache, k, v, position, count)
 
     def qcache_read(self, cache, n: int, first: Optional[torch.Tensor] = None):
         """cca_qcache_read: the values (k, v), fp32 [B, n, h_k, d_h], of rows first[b] .. (default: len[b] ..)."""
-        c, B = self._qcache(cache)
-        k = torch.empty(B, n, self.cfg.n_kv_heads, self.cfg.head_dim, dtype=torch.float32, device=self.device)
-        v = torch.empty_like(k)
-        _check(self.lib, self.lib.cca_qcache_read(
-            self.handle, C.byref(c), None if first is None else self._need(first, "first", torch.int32, (B,)), k.data_ptr(),
-            v.data_ptr(), B, n, self._stream()), self.handle, "cca_qcache_read")
-        return k, v
+        return _BIND.qcache_read(self._native, cache, n, first)
 
     def qcache_workspace_size(self, B: int, max_len: int) -> int:
         n = C.c_size_t()
@@ -484,91 +448,30 @@ class CCA:
                          accumulate: Optional[bool] = None):
         """cca_qcache_attention: q [B, h_q, d_h] -> o over each sequence's len[b] rows.  accumulate=None: gather the weights
         if the cache has them."""
-        c, B = self._qcache(cache)
-        shape = (B, self.cfg.n_q_heads, self.cfg.head_dim)
-        if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        if accumulate is None:
-            accumulate = cache.get("weight") is not None
-        wp, wn = self._q_ws(workspace)
-        _check(self.lib, self.lib.cca_qcache_attention(
-            self.handle, self._need(q, "q", torch.bfloat16, shape), self._need(out, "out", torch.bfloat16, shape), C.byref(c),
-            max_len, int(accumulate), wp, wn, B, self._stream()), self.handle, "cca_qcache_attention")
-        return out
+        return _BIND.qcache_attention(self._native, q, cache, max_len, workspace, out, accumulate)
 
     def qcache_evict(self, cache, keep: int, recent: int, next_position: torch.Tensor, max_len: int, workspace: torch.Tensor):
         """cca_qcache_evict: in place, `len` included."""
-        c, B = self._qcache(cache)
-        wp, wn = self._q_ws(workspace)
-        _check(self.lib, self.lib.cca_qcache_evict(
-            self.handle, C.byref(c), keep, recent, self._need(next_position, "next_position", torch.int32, (B,)), max_len, wp, wn, B,
-            self._stream()), self.handle, "cca_qcache_evict")
+        _BIND.qcache_evict(self._native, cache, keep, recent, next_position, max_len, workspace)
 
     def qlinear_pack(self, w: torch.Tensor) -> Dict[str, object]:
         """A bf16 weight matrix [N, K] in the 4-bit tiles of cca_qlinear_weights."""
-        N, K = w.shape
-        code_bytes, scale_bytes = C.c_size_t(), C.c_size_t()
-        _check(self.lib, self.lib.cca_qlinear_sizes(N, K, C.byref(code_bytes), C.byref(scale_bytes)), None, "cca_qlinear_sizes")
-        shape = ((N + 15) // 16, (K + 127) // 128, 16)
-        out = {"codes": torch.empty(shape + (64,), dtype=torch.uint8, device=self.device),
-               "scales": torch.empty(shape + (4,), dtype=torch.bfloat16, device=self.device), "N": N, "K": K}
-        assert out["codes"].numel() == code_bytes.value and 2 * out["scales"].numel() == scale_bytes.value
-        cw = self._qlinear(out)
-        _check(self.lib, self.lib.cca_qlinear_pack(self.handle, self._need(w, "w", torch.bfloat16, (N, K)), C.byref(cw), self._stream()),
-               self.handle, "cca_qlinear_pack")
-        return out
-
-    def _qlinear(self, w) -> cca_qlinear_weights:
-        N, K = w["N"], w["K"]
-        shape = ((N + 15) // 16, (K + 127) // 128, 16)
-        return cca_qlinear_weights(self._need(w["codes"], "codes", torch.uint8, shape + (64,)),
-                                   self._need(w["scales"], "scales", torch.bfloat16, shape + (4,)), N, K)
+        codes, scales = _BIND.qlinear_pack(self._native, w)
+        return {"codes": codes, "scales": scales, "N": w.shape[0], "K": w.shape[1]}
 
     def qlinear(self, w, x: torch.Tensor, out: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16):
         """cca_qlinear: x [M, K] bf16 -> [M, N] (bf16 or fp32, that of `out` where it is given)."""
-        M = x.shape[0]
-        if out is None:
-            out = torch.empty(M, w["N"], dtype=out_dtype, device=self.device)
-        if out.dtype not in (torch.bfloat16, torch.float32):
-            raise CcaError(f"cca_qlinear: output type {out.dtype}")
-        cw = self._qlinear(w)
-        _check(self.lib, self.lib.cca_qlinear(self.handle, C.byref(cw), self._need(x, "x", torch.bfloat16, (M, w["K"])),
-                                              self._need(out, "out", out.dtype, (M, w["N"])), int(out.dtype is torch.float32), M,
-                                              self._stream()), self.handle, "cca_qlinear")
-        return out
+        return _BIND.qlinear(self._native, w, x, out, out_dtype)
 
     def pack_weights_q(self, w: Dict[str, torch.Tensor]) -> Dict[str, object]:
         """The block's weights for decode_step_q: projections in 4 bits, the rest as it is."""
         return {"w_qkv": self.qlinear_pack(torch.cat([w["w_qk"], w["w_v1"]], dim=0)), "w_vp": self.qlinear_pack(w["w_v2"]),
                 "w_o": self.qlinear_pack(w["w_o"]), **{n: w.get(n) for n in ("conv0_w", "conv1_w", "temp")}}
 
-    def _q_weights(self, w) -> cca_q_weights:
-        cw = cca_q_weights()
-        for n in ("w_qkv", "w_vp", "w_o"):
-            setattr(cw, n, self._qlinear(w[n]))
-        c = self.cfg
-        L = (c.n_q_heads + c.n_kv_heads) * c.head_dim
-        shapes = {"conv0_w": (L, c.k_seq), "conv1_w": (L, c.head_dim, c.k_ch), "temp": (c.n_kv_heads,)}
-        for n, shape in shapes.items():
-            if w.get(n) is not None:
-                setattr(cw, n, self._need(w[n], n, torch.float32 if n == "temp" else torch.bfloat16, shape))
-        return cw
-
     def new_decode_state_q(self, B: int, S_max: int) -> Dict[str, object]:
         """Caller-owned tensors of cca_q_decode_state for B empty sequences: "cache" (new_qcache), history, previous input, "pos"."""
         s = self.new_decode_state(B, 1)
         return {"cache": self.new_qcache(B, S_max), **{n: s[n] for n in ("qk0_hist", "x_prev", "pos")}}
-
-    def _decode_state_q(self, state):
-        s = cca_q_decode_state()
-        s.cache, B = self._qcache(state["cache"])
-        c = self.cfg
-        pad, L = c.k_seq + c.k_ch - 2, (c.n_q_heads + c.n_kv_heads) * c.head_dim
-        if pad:
-            s.qk0_hist = self._need(state["qk0_hist"], "qk0_hist", torch.float32, (B, pad, L))
-        s.x_prev = self._need(state["x_prev"], "x_prev", torch.bfloat16, (B, c.d_model))
-        s.pos = self._need(state["pos"], "pos", torch.int32, (B,))
-        return s, B
 
     def decode_workspace_size_q(self, B: int, max_len: int) -> int:
         n = C.c_size_t()
@@ -582,25 +485,11 @@ class CCA:
     def decode_step_q(self, w, x: torch.Tensor, state, max_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None):
         """cca_decode_step_q: x [B, E] -> out [B, E]; the state is updated in place except `pos` and the cache's `len`, which the
         caller advances.  w: pack_weights_q."""
-        ds, B = self._decode_state_q(state)
-        shape = (B, self.cfg.d_model)
-        if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        cw = self._q_weights(w)
-        wp, wn = self._q_ws(workspace)
-        _check(self.lib, self.lib.cca_decode_step_q(
-            self.handle, C.byref(cw), self._need(x, "x", torch.bfloat16, shape), self._need(out, "out", torch.bfloat16, shape),
-            C.byref(ds), max_len, wp, wn, B, self._stream()), self.handle, "cca_decode_step_q")
-        return out
+        return _BIND.decode_step_q(self._native, w, x, state, max_len, workspace, out)
 
     def decode_state_from_prefill_q(self, x: torch.Tensor, workspace: torch.Tensor, state):
         """cca_decode_state_from_prefill_q: the keys and values a forward of x left in `workspace` go into the 4-bit cache."""
-        ds, B = self._decode_state_q(state)
-        S = x.shape[1]
-        wp, wn = self._q_ws(workspace)
-        _check(self.lib, self.lib.cca_decode_state_from_prefill_q(
-            self.handle, self._need(x, "x", torch.bfloat16, (B, S, self.cfg.d_model)), wp, wn, B, S, C.byref(ds), self._stream()),
-            self.handle, "cca_decode_state_from_prefill_q")
+        _BIND.decode_state_from_prefill_q(self._native, x, workspace, state)
 
     def backward(self, w, x: torch.Tensor, d_out: torch.Tensor, workspace: torch.Tensor, separate_grads: bool = False):
         """Returns (d_x bf16, dict of fp32 parameter gradients).  separate_grads: give every gradient a buffer of

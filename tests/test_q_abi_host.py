@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2510_04476_b200 import binding
 from tests.test_abi_host import host_handle
@@ -61,3 +62,26 @@ def test_host_only_handle_refuses_compute(host):
     assert lib.cca_qlinear(h, C.byref(w), one, one, 0, 1, None) == 1
     assert lib.cca_decode_step_q(h, C.byref(qw), one, one, C.byref(s), 16, one, 1 << 30, 1, None) == 1
     assert lib.cca_decode_state_from_prefill_q(h, one, one, 1 << 30, 1, 1, C.byref(s), None) == 1
+
+
+def test_extension_refuses_what_does_not_fit():
+    """The marshalling extension on CPU tensors: every argument is refused by name, nothing reaches the library."""
+    binding.load_library()
+    from paper_2510_04476_b200 import _bind as b
+    h = b.new_handle(0, 256, 4, 2, 64, 2, 2, 0)
+    w = {"codes": torch.zeros(2, 1, 16, 64, dtype=torch.uint8), "scales": torch.zeros(2, 1, 16, 4, dtype=torch.bfloat16), "N": 24, "K": 64}
+    x = torch.zeros(2, 64, dtype=torch.bfloat16)
+    cache = {"len": torch.zeros(1, dtype=torch.int32), "k_codes": torch.zeros(1, 2, 8, 32, dtype=torch.uint8)}
+    for match, call in (("N", lambda: b.qlinear(h, {}, x, None, torch.bfloat16)),
+                        ("codes: wants a contiguous Byte tensor .* on cuda:0, got .* on cpu", lambda: b.qlinear(h, w, x, None, torch.bfloat16)),
+                        ("dict", lambda: b.qlinear(h, 5, x, None, torch.bfloat16)),
+                        ("k_codes", lambda: b.qcache_attention(h, x, cache, 8, x, None, None)),
+                        ("len: wants a tensor", lambda: b.qcache_evict(h, {}, 1, 0, x, 8, x)),
+                        ("cache", lambda: b.decode_step_q(h, {}, x, {}, 8, x, None)),
+                        ("w: wants two", lambda: b.qlinear_pack(h, x[0]))):
+        with pytest.raises(binding.CcaError, match=match):
+            call()
+    with pytest.raises(TypeError):
+        b.qlinear(h)
+    with pytest.raises(ValueError):
+        b.qlinear(3, w, x, None, torch.bfloat16)           # no handle
