@@ -1178,6 +1178,14 @@ int enqueued(cca_handle* h, int r) {
   if (r < 0) { h->last_cuda = -r; return CCA_ERR_CUDA; }
   return r > 0 ? CCA_ERR_UNSUPPORTED : CCA_OK;
 }
+// A number that a call's counters in the caller's workspace are told by: mixed from the handle's address and its count of launches.
+unsigned long long next_tag(const cca_handle* h) {
+  unsigned long long z = reinterpret_cast<uintptr_t>(h) * 0x9e3779b97f4a7c15ull + (unsigned long long)h->launches;
+  z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
+  z = (z ^ (z >> 27)) * 0x94d049bb133111ebull;
+  z = (z ^ (z >> 31)) >> 16;
+  return z ? z : 1;
+}
 int check_qlinear(const cca_qlinear_weights* w) {
   if (!w || !w->codes || !w->scales) return CCA_ERR_INVALID_ARG;
   if (!aligned16(w->codes) || !aligned16(w->scales)) return CCA_ERR_ALIGNMENT;
@@ -1252,7 +1260,8 @@ int cca_qcache_evict(cca_handle* h, const cca_qcache* c, int64_t keep, int64_t r
   if (workspace_bytes < qcache_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
   OnDevice on;
   CU(on.enter(h->device));
-  return enqueued(h, launch_qcache_evict(d, make_qcache(c), (int)keep, (int)recent, next_position, (int)max_len, workspace, h->d_status,
+  return enqueued(h, launch_qcache_evict(d, make_qcache(c), (int)keep, (int)recent, next_position, (int)max_len, workspace,
+                                         next_tag(h), h->sm_count, h->d_status,
                                          &h->launches, (cudaStream_t)cuda_stream));
 }
 

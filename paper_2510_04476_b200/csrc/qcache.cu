@@ -38,8 +38,8 @@ struct IoArgs {
   float *k_out, *v_out;          // the same, fp32
   const int *position, *count, *first;
   QCache c;
-  long long n, limit;            // rows a sequence may hold
-  int B, hk;
+  long long n, limit;            // n * hk * blocks * 2 <= 2^31; limit: rows a sequence may hold
+  int hk;
   int* status;
 };
 
@@ -49,29 +49,22 @@ template <int DH>
 __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
   pdl_enter();
   using R = Row<DH>;
-  const int lane8 = threadIdx.x & 7;
-  const long long per_seq = a.n * a.hk * R::NB * 2, units = per_seq * a.B;
-  // whole warps stay in the loop: the shuffles need every lane
-  const long long step = (long long)gridDim.x * 32;
-  for (long long u0 = (long long)blockIdx.x * 32 + (threadIdx.x >> 5) * 4; u0 < units; u0 += step) {
-    const long long u = u0 + ((threadIdx.x & 31) >> 3);
-    bool ok = u < units;
-    const int b = ok ? (int)(u / per_seq) : 0;
-    const long long in_seq = ok ? u % per_seq : 0;
-    const int kv = (int)(in_seq & 1);
-    const int blk = (int)((in_seq >> 1) % R::NB);
-    const long long ih = (in_seq >> 1) / R::NB;             // (new row, head)
-    const int h = (int)(ih % a.hk);
-    const long long i = ih / a.hk;
-    const long long len = a.c.len[b];
-    long long cnt = a.n;
-    if (a.count) cnt = max(0, min(a.count[b], (int)min(a.n, (long long)0x7fffffff)));
+  const int lane8 = threadIdx.x & 7, b = blockIdx.y;
+  const uint32_t units = (uint32_t)a.n * a.hk * R::NB * 2;
+  const int len = a.c.len[b], first_pos = a.position ? a.position[b] : 0;
+  const int cnt = a.count ? max(0, min(a.count[b], (int)a.n)) : (int)a.n;
+  if (len < 0 || (long long)len + cnt > a.limit || first_pos < 0) {
     // a sequence whose rows do not fit, or whose position is none: nothing of it is written
-    if (len < 0 || len + cnt > a.limit || (a.position && a.position[b] < 0)) {
-      if (ok && in_seq == 0 && lane8 == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
-      ok = false;
-    }
-    ok = ok && i < cnt;
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+    return;
+  }
+  // whole warps stay in the loop: the shuffles need every lane
+  for (uint32_t u0 = blockIdx.x * 32 + (threadIdx.x >> 5) * 4; u0 < units; u0 += gridDim.x * 32) {
+    const uint32_t u = u0 + ((threadIdx.x & 31) >> 3);
+    const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
+    const uint32_t ih = (u >> 1) / R::NB;                  // (new row, head)
+    const int i = (int)(ih / a.hk), h = (int)(ih - (uint32_t)i * a.hk);
+    const bool ok = i < cnt;                               // false behind the last unit too
     const bf16* src = (kv ? a.v : a.k) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
     uint8_t code[2 * R::NG];
     bf16 scale[R::NG];
@@ -96,7 +89,7 @@ __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
       if (lane8 == grp) sc[grp] = scale[grp];
     if (kv == 0 && blk == 0 && lane8 == 0) {
       if (a.c.weight) a.c.weight[row] = 0.f;
-      if (a.c.position) a.c.position[row] = a.position ? a.position[b] + (int)i : (int)(len + i);
+      if (a.c.position) a.c.position[row] = (a.position ? first_pos : len) + i;
     }
   }
 }
@@ -105,17 +98,14 @@ template <int DH>
 __global__ void __launch_bounds__(256) qcache_read_kernel(IoArgs a) {
   pdl_enter();
   using R = Row<DH>;
-  const int lane8 = threadIdx.x & 7;
-  const long long per_seq = a.n * a.hk * R::NB * 2, units = per_seq * a.B;
-  for (long long u = (long long)blockIdx.x * 32 + (threadIdx.x >> 3); u < units; u += (long long)gridDim.x * 32) {
-    const int b = (int)(u / per_seq);
-    const long long in_seq = u % per_seq;
-    const int kv = (int)(in_seq & 1);
-    const int blk = (int)((in_seq >> 1) % R::NB);
-    const long long ih = (in_seq >> 1) / R::NB;
-    const int h = (int)(ih % a.hk);
-    const long long i = ih / a.hk;
-    const long long r = (long long)(a.first ? a.first[b] : a.c.len[b]) + i;
+  const int lane8 = threadIdx.x & 7, b = blockIdx.y;
+  const uint32_t units = (uint32_t)a.n * a.hk * R::NB * 2;
+  const long long first = a.first ? a.first[b] : a.c.len[b];
+  for (uint32_t u = blockIdx.x * 32 + (threadIdx.x >> 3); u < units; u += gridDim.x * 32) {
+    const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
+    const uint32_t ih = (u >> 1) / R::NB;
+    const int i = (int)(ih / a.hk), h = (int)(ih - (uint32_t)i * a.hk);
+    const long long r = first + i;
     const bool there = r >= 0 && r < a.c.S_max;
     const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + (there ? r : 0);
     const uint8_t* src = (kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + blk * (R::BLK / 2) + lane8 * 2 * R::NG;
@@ -682,9 +672,10 @@ cudaError_t attn_dh(const QaArgs& a, cudaStream_t st) {
 struct EvArgs {
   QCache c;
   int hk, keep, recent, max_len;
+  int per_cta;                   // rows of a CTA, a multiple of 32
   const int* next;               // [B] position of the next token
-  int* count;                    // [B * hk] rows to move
-  int* new_len;                  // [B]: keep, or -1 where nothing goes
+  unsigned long long* arrived;   // [B] heads that are done with a sequence
+  unsigned long long tag;        // of this call, 48 bits, not 0
   int* list;                     // [B * hk][2][cap]: destinations (rows that go, ascending), sources (rows that come, ascending)
   long long cap;
   int* status;
@@ -701,148 +692,230 @@ CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Exclusive sum over the 32 warps of a value that lane 0 of each holds; every thread gets its warp's.
-CCA_DEVINL int warp_offsets(int v, int* sm, int warp, int lane) {
+CCA_DEVINL uint32_t cluster_u32(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return r;
+}
+CCA_DEVINL int cluster_load(const int* p, int rank) {
+  int v;
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(cluster_u32(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL int2 cluster_load2(const int* p, int rank) {
+  int2 v;
+  asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_u32(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL void all_sync(int ranks) {                      // the CTAs that share a head
+  if (ranks == 1) { __syncthreads(); return; }
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Exclusive sum over the 32 warps of a value that is the same in a warp's lanes; `total`: over all of them.
+CCA_DEVINL int warp_offsets(int v, int* sm, int warp, int lane, int& total) {
   __syncthreads();
   if (lane == 0) sm[warp] = v;
   __syncthreads();
-  int x = sm[lane], inc = x;
+  const int x = sm[lane];
+  int inc = x;
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, inc, s);
     if (lane >= s) inc += y;
   }
+  total = __shfl_sync(0xffffffffu, inc, 31);
   return __shfl_sync(0xffffffffu, inc - x, warp);
 }
 
-// One CTA per (sequence, head): the keep-th largest key by three counting passes over its digits (11, 11, 10 bits), then, in
-// ascending order of rows, the rows below `keep` that go and the rows behind it that stay.  Each warp takes a contiguous run of rows,
-// 32 at a time, so ranks come from ballots and one sum over the warps.  IN_SMEM: the keys are kept in shared memory after
-// the first reading; longer caches read weight and position again (from L2).
-template <bool IN_SMEM>
-__global__ void __launch_bounds__(EV_THREADS) qcache_select_kernel(EvArgs a) {
-  pdl_enter();
-  extern __shared__ uint32_t keys[];
-  __shared__ int hist[EV_BINS];
-  __shared__ int sm[32];
-  __shared__ int found[2];
-  const int b = blockIdx.y, j = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int bj = b * a.hk + j;
-  const int n = a.c.len[b];
-  const bool bad = n < 0 || n > a.max_len || n > a.c.S_max;
-  if (bad && tid == 0 && j == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
-  if (bad || n <= a.keep || a.keep == 0) {
-    if (tid == 0) {
-      a.count[bj] = 0;
-      if (j == 0) a.new_len[b] = (!bad && n > a.keep) ? a.keep : -1;
-    }
-    return;
-  }
-  const float* w = a.c.weight + (size_t)bj * a.c.S_max;
-  const int* pos = a.c.position + (size_t)bj * a.c.S_max;
-  const long long first_recent = (long long)a.next[b] - a.recent;
-  auto key_of = [&](int r) { return IN_SMEM ? keys[r] : keep_key(w[r], pos[r], first_recent); };
-
-  uint32_t prefix = 0;
-  int left = a.keep;                                       // how many of the rows that share the prefix are kept
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int r = tid; r < n; r += EV_THREADS) {
-      uint32_t k;
-      if (IN_SMEM && pass > 0) k = keys[r];
-      else {
-        k = keep_key(w[r], pos[r], first_recent);
-        if (IN_SMEM) keys[r] = k;
-      }
-      if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1u)], 1);
-    }
-    __syncthreads();
-    // bins from the top: thread i has bins BINS - 1 - 2i and BINS - 2 - 2i
-    const int c0 = hist[EV_BINS - 1 - 2 * tid], c1 = hist[EV_BINS - 2 - 2 * tid];
-    int inc = c0 + c1;
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, inc, s);
-      if (lane >= s) inc += y;
-    }
-    const int tot = __shfl_sync(0xffffffffu, inc, 31);
-    const int before = warp_offsets(tot, sm, warp, lane) + inc - c0 - c1;
-    if (before < left && left <= before + c0) { found[0] = EV_BINS - 1 - 2 * tid; found[1] = left - before; }
-    if (before + c0 < left && left <= before + c0 + c1) { found[0] = EV_BINS - 2 - 2 * tid; found[1] = left - before - c0; }
-    __syncthreads();
-    prefix = (prefix << bits) | (uint32_t)found[0];
-    left = found[1];
-    __syncthreads();
-  }
-  const uint32_t lowest = prefix;                          // keys above it stay, and the first `left` rows that equal it
-  const int run = (n + EV_THREADS - 1) / EV_THREADS * 32;  // rows of a warp
-  const int r_begin = min(n, warp * run), r_end = min(n, r_begin + run);
-  int eq = 0;
-  for (int r0 = r_begin; r0 < r_end; r0 += 32) {
-    const int r = r0 + lane;
-    eq += __popc(__ballot_sync(0xffffffffu, r < r_end && key_of(r) == lowest));
-  }
-  const int eq0 = warp_offsets(eq, sm, warp, lane);
-  int go = 0, come = 0;
-  int go0 = 0, come0 = 0;
-  int* dst = a.list + (size_t)bj * 2 * a.cap;
-  int* src = dst + a.cap;
-#pragma unroll
-  for (int pass = 0; pass < 2; ++pass) {                   // count, then write
-    int e = eq0;
-    go = come = 0;
-    for (int r0 = r_begin; r0 < r_end; r0 += 32) {
-      const int r = r0 + lane;
-      const uint32_t k = r < r_end ? key_of(r) : 0u;
-      const unsigned below = (1u << lane) - 1u;
-      const unsigned beq = __ballot_sync(0xffffffffu, r < r_end && k == lowest);
-      const bool stays = r < r_end && (k > lowest || (k == lowest && e + __popc(beq & below) < left));
-      const unsigned bgo = __ballot_sync(0xffffffffu, r < r_end && r < a.keep && !stays);
-      const unsigned bco = __ballot_sync(0xffffffffu, r >= a.keep && stays);
-      if (pass == 1) {
-        if (bgo >> lane & 1u) dst[go0 + go + __popc(bgo & below)] = r;
-        if (bco >> lane & 1u) src[come0 + come + __popc(bco & below)] = r;
-      }
-      e += __popc(beq); go += __popc(bgo); come += __popc(bco);
-    }
-    if (pass == 0) {
-      go0 = warp_offsets(go, sm, warp, lane);
-      come0 = warp_offsets(come, sm, warp, lane);
-      if (warp == 31 && lane == 0) {
-        a.count[bj] = come0 + come;
-        if (j == 0) a.new_len[b] = a.keep;
-      }
-    }
-  }
-}
-
-// Moves the listed rows: DH / 16 lanes take the 16-byte pieces of a row's codes, the first lanes its scales, weight and position.
-// A destination is below `keep` and a source is not, so no order matters.
-template <int DH>
-__global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
+// One cluster of 1 to 8 CTAs per (sequence, head), each with a contiguous run of rows: the keep-th largest key by three counting
+// passes over its digits (11, 11, 10 bits; the CTAs read each other's counts), then, in ascending order of rows, the rows below `keep` that go and
+// the rows behind it that stay, and their moves.  A warp takes a contiguous run of rows, 32 at a time, so ranks come
+// from ballots and sums over warps and CTAs.  IN_SMEM: the keys are kept in shared memory after the first reading; longer caches
+// read weight and position again (from L2).  A destination is below `keep` and a source is not, so the moves need no order.
+// Its time is latency (barriers, one pass after the other) where little moves, else the rows' traffic.
+template <int DH, bool IN_SMEM>
+__global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
   pdl_enter();
   using R = Row<DH>;
-  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = 256 / LANES;
-  const int j = blockIdx.y, b = blockIdx.z, bj = b * a.hk + j;
-  if (blockIdx.x == 0 && j == 0 && threadIdx.x == 0 && a.new_len[b] >= 0) a.c.len[b] = a.new_len[b];
-  const int n = a.count[bj];
-  const int* dst = a.list + (size_t)bj * 2 * a.cap;
-  const int* src = dst + a.cap;
+  extern __shared__ uint32_t keys[];
+  __shared__ __align__(8) int hist[3][EV_BINS];
+  __shared__ int sm[32];
+  __shared__ int found[3];
+  __shared__ int mine[4];                                  // this CTA's counts, read by the others: equal keys, rows that go, that come
+  const int rank = blockIdx.x, ranks = gridDim.x, j = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int bj = b * a.hk + j;
+  const int n = *reinterpret_cast<volatile int*>(a.c.len + b);
+  if (n < 0 || n > a.max_len || n > a.c.S_max) {
+    if (tid == 0 && j == 0 && rank == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+    return;
+  }
+  if (n <= a.keep) return;
   const size_t base = (size_t)bj * a.c.S_max;
-  const int l = threadIdx.x % LANES, piece = l % PIECES;
+  int moves = 0;
+  int* dst = a.list + (size_t)bj * 2 * a.cap;
+  int* src = dst + a.cap;
+  if (a.keep > 0) {
+    const float* w = a.c.weight + base;
+    const int* pos = a.c.position + base;
+    const long long first_recent = (long long)a.next[b] - a.recent;
+    const int row0 = min(n, rank * a.per_cta), row1 = min(n, row0 + a.per_cta);
+    auto key_of = [&](int r) { return IN_SMEM ? keys[r - row0] : keep_key(w[r], pos[r], first_recent); };
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[0][i] = hist[1][i] = hist[2][i] = 0;
+    __syncthreads();
+    uint32_t prefix = 0;
+    int left = a.keep, equal = 0;                          // how many of the rows that share the prefix are kept, and there are
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+#pragma unroll 4
+      for (int r = row0 + tid; r < row1; r += EV_THREADS) {
+        uint32_t k;
+        if (IN_SMEM && pass > 0) k = keys[r - row0];
+        else {
+          k = keep_key(w[r], pos[r], first_recent);
+          if (IN_SMEM) keys[r - row0] = k;
+        }
+        if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[pass][(k >> shift) & ((1u << bits) - 1u)], 1);
+      }
+      all_sync(ranks);
+      // bins from the top: thread i has bins BINS - 1 - 2i and BINS - 2 - 2i
+      const int* mybins = &hist[pass][EV_BINS - 2 - 2 * tid];
+      int c0 = 0, c1 = 0;
+      if (ranks == 1) { c0 = mybins[1]; c1 = mybins[0]; }
+      else
+        for (int x = 0; x < ranks; ++x) {
+          const int2 v = cluster_load2(mybins, x);
+          c0 += v.y; c1 += v.x;
+        }
+      int inc = c0 + c1;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, s);
+        if (lane >= s) inc += y;
+      }
+      int all;
+      const int before = warp_offsets(__shfl_sync(0xffffffffu, inc, 31), sm, warp, lane, all) + inc - c0 - c1;
+      if (before < left && left <= before + c0) { found[0] = EV_BINS - 1 - 2 * tid; found[1] = left - before; found[2] = c0; }
+      if (before + c0 < left && left <= before + c0 + c1) { found[0] = EV_BINS - 2 - 2 * tid; found[1] = left - before - c0; found[2] = c1; }
+      __syncthreads();
+      prefix = (prefix << bits) | (uint32_t)found[0];
+      left = found[1];
+      equal = found[2];
+    }
+    const uint32_t lowest = prefix;                        // keys above it stay, and the first `left` rows that equal it
+    const int run = (a.per_cta + EV_THREADS - 1) / EV_THREADS * 32;    // rows of a warp
+    const int r_begin = min(row1, row0 + warp * run), r_end = min(row1, r_begin + run);
+    // what this CTA's and the lower CTAs' warps before this one have counted
+    auto place = [&](int v, int slot) {
+      int total;
+      int at = warp_offsets(v, sm, warp, lane, total);
+      if (ranks > 1) {
+        if (tid == 0) mine[slot] = total;
+        all_sync(ranks);
+        for (int x = 0; x < rank; ++x) at += cluster_load(&mine[slot], x);
+      }
+      return at;
+    };
+    int eq0 = 0;
+    if (equal > left) {                                    // the same in every CTA of the cluster
+      int eq = 0;
+      for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+        const int r = r0 + lane;
+        eq += __popc(__ballot_sync(0xffffffffu, r < r_end && key_of(r) == lowest));
+      }
+      eq0 = place(eq, 0);
+    }
+    int go0 = 0, come0 = 0;
+    const unsigned below = (1u << lane) - 1u;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {                 // count, then write
+      int e = eq0, go = 0, come = 0;
+      for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+        const int r = r0 + lane;
+        const uint32_t k = r < r_end ? key_of(r) : 0u;
+        bool stays = k > lowest;
+        if (equal <= left) stays = stays || k == lowest;
+        else {
+          const unsigned beq = __ballot_sync(0xffffffffu, r < r_end && k == lowest);
+          stays = stays || (k == lowest && e + __popc(beq & below) < left);
+          e += __popc(beq);
+        }
+        const unsigned bgo = __ballot_sync(0xffffffffu, r < r_end && r < a.keep && !stays);
+        const unsigned bco = __ballot_sync(0xffffffffu, r < r_end && r >= a.keep && stays);
+        if (pass == 1) {
+          if (bgo >> lane & 1u) dst[go0 + go + __popc(bgo & below)] = r;
+          if (bco >> lane & 1u) src[come0 + come + __popc(bco & below)] = r;
+        }
+        go += __popc(bgo); come += __popc(bco);
+      }
+      if (pass == 0) {
+        int tg, tc;
+        go0 = warp_offsets(go, sm, warp, lane, tg);
+        come0 = warp_offsets(come, sm, warp, lane, tc);
+        moves = tg;
+        if (ranks > 1) {
+          if (tid == 0) { mine[1] = tg; mine[2] = tc; }
+          all_sync(ranks);
+          moves = 0;
+          for (int x = 0; x < ranks; ++x) {
+            const int xg = cluster_load(&mine[1], x), xc = cluster_load(&mine[2], x);
+            moves += xg;
+            if (x < rank) { go0 += xg; come0 += xc; }
+          }
+        }
+      }
+    }
+    all_sync(ranks);                                       // the lists are whole, and nobody reads weights or positions any more
+  }
+  // ---- moves: DH / 16 lanes take the 16-byte pieces of a row's codes; as many scales as 16-byte pieces
+  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = EV_THREADS / LANES, U = 4;
+  const int l = tid % LANES, piece = l % PIECES;
   uint8_t* codes = (l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES;
   bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES;
-  for (int i = blockIdx.x * ROWS + threadIdx.x / LANES; i < n; i += gridDim.x * ROWS) {
-    const size_t from = (size_t)src[i], to = (size_t)dst[i];
-    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(codes + from * R::CODES) + piece);
-    const bf16 s = scales[from * R::SCALES + piece];       // as many scales as 16-byte pieces: 32 channels each
-    reinterpret_cast<uint4*>(codes + to * R::CODES)[piece] = u;
-    scales[to * R::SCALES + piece] = s;
-    if (l == 0) a.c.weight[base + to] = a.c.weight[base + from];
-    if (l == PIECES) a.c.position[base + to] = a.c.position[base + from];
+  for (int i0 = rank * ROWS * U + tid / LANES; i0 < moves; i0 += ranks * ROWS * U) {
+    size_t from[U], to[U];
+    uint4 u[U];
+    bf16 s[U];
+    float wt[U];
+    int ps[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) { from[x] = (size_t)src[i0 + x * ROWS]; to[x] = (size_t)dst[i0 + x * ROWS]; }
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) {
+        u[x] = __ldcs(reinterpret_cast<const uint4*>(codes + from[x] * R::CODES) + piece);
+        s[x] = scales[from[x] * R::SCALES + piece];
+        if (l == 0) wt[x] = a.c.weight[base + from[x]];
+        if (l == PIECES) ps[x] = a.c.position[base + from[x]];
+      }
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) {
+        reinterpret_cast<uint4*>(codes + to[x] * R::CODES)[piece] = u[x];
+        scales[to[x] * R::SCALES + piece] = s[x];
+        if (l == 0) a.c.weight[base + to[x]] = wt[x];
+        if (l == PIECES) a.c.position[base + to[x]] = ps[x];
+      }
+  }
+  // The length is written by the last head to be done with it, so that every CTA, early or late, reads the length from before.  The
+  // workspace comes as it is: a count is one only under this call's tag (48 bits), and the last head leaves a zero, so that a
+  // replayed call finds none of its own.
+  if (a.keep == 0) all_sync(ranks);                        // (else: every CTA of the cluster has read it before the lists were whole)
+  if (rank == 0 && tid == 0) {
+    unsigned long long seen = a.arrived[b], now;
+    bool last;
+    do {
+      now = seen;
+      const int heads = (now >> 16) == a.tag ? (int)(now & 0xffffu) + 1 : 1;
+      last = heads == a.hk;
+      seen = atomicCAS(a.arrived + b, now, last ? 0ull : (a.tag << 16 | (unsigned long long)heads));
+    } while (seen != now);
+    if (last) a.c.len[b] = a.keep;
   }
 }
 
@@ -861,17 +934,26 @@ constexpr int EV_SMEM_ROWS = 49152;                        // 192 KB of keys
     default: return 1;             \
   }
 
+namespace {
+long long io_units(const CcaDims& d, long long n) { return n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2; }
+// 32 units a CTA and the sequences side by side; at most about 32 CTAs for each of 148 SMs, then around again
+dim3 io_grid(const CcaDims& d, long long n) {
+  long long x = (io_units(d, n) + 31) / 32, most = 4736 / d.B;
+  if (most < 1) most = 1;
+  return dim3((unsigned)(x < most ? x : most), (unsigned)d.B);
+}
+}  // namespace
+
 int launch_qcache_append(const CcaDims& d, const bf16* k, const bf16* v, const int* position, const int* count, const QCache& c,
                          long long n, long long limit, int* status, long long* launches, cudaStream_t st) {
   IoArgs a;
   memset(&a, 0, sizeof(a));
-  a.k = k; a.v = v; a.position = position; a.count = count; a.c = c; a.n = n; a.limit = limit; a.B = d.B; a.hk = d.hk;
+  a.k = k; a.v = v; a.position = position; a.count = count; a.c = c; a.n = n; a.limit = limit; a.hk = d.hk;
   a.status = status;
-  const long long units = (long long)d.B * n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2;
-  const long long want = (units + 31) / 32;
-  const unsigned grid = (unsigned)(want < 4736 ? want : 4736);      // 32 CTAs for each of 148 SMs, then around again
+  if (io_units(d, n) > 1LL << 31) return 1;
+  const dim3 grid = io_grid(d, n);
   cudaError_t e;
-  QC_BY_HEAD((launch_pdl(qcache_append_kernel<DH>, dim3(grid), dim3(256), st, a)))
+  QC_BY_HEAD((launch_pdl(qcache_append_kernel<DH>, grid, dim3(256), st, a)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
@@ -881,12 +963,11 @@ int launch_qcache_read(const CcaDims& d, const QCache& c, const int* first, floa
                        cudaStream_t st) {
   IoArgs a;
   memset(&a, 0, sizeof(a));
-  a.k_out = k; a.v_out = v; a.first = first; a.c = c; a.n = n; a.B = d.B; a.hk = d.hk;
-  const long long units = (long long)d.B * n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2;
-  const long long want = (units + 31) / 32;
-  const unsigned grid = (unsigned)(want < 4736 ? want : 4736);
+  a.k_out = k; a.v_out = v; a.first = first; a.c = c; a.n = n; a.hk = d.hk;
+  if (io_units(d, n) > 1LL << 31) return 1;
+  const dim3 grid = io_grid(d, n);
   cudaError_t e;
-  QC_BY_HEAD((launch_pdl(qcache_read_kernel<DH>, dim3(grid), dim3(256), st, a)))
+  QC_BY_HEAD((launch_pdl(qcache_read_kernel<DH>, grid, dim3(256), st, a)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
@@ -897,7 +978,7 @@ size_t qcache_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
   attn_plan(d, max_len, sm_count, &chunk, &splits);
   const size_t attn = up256((size_t)d.B * d.hq * splits * d.dh * 4) + up256((size_t)d.B * d.hq * splits * 2 * 4) +
                       up256((size_t)d.B * d.hq * max_len * 4);
-  const size_t ev = up256((size_t)d.B * d.hk * 4) + up256((size_t)d.B * 4) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
+  const size_t ev = up256((size_t)d.B * 8) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
   return attn > ev ? attn : ev;
 }
 
@@ -927,34 +1008,47 @@ int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, b
   return 0;
 }
 
+namespace {
+template <int DH, bool IN_SMEM>
+cudaError_t evict_run(const EvArgs& a, int ranks, int B, int smem, cudaStream_t st) {
+  static bool done[MAX_DEVICES];
+  if (IN_SMEM) {
+    const cudaError_t e = opt_in(qcache_evict_kernel<DH, IN_SMEM>, EV_SMEM_ROWS * 4, done);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ranks, (unsigned)a.hk, (unsigned)B);
+  cfg.blockDim = dim3(EV_THREADS);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)ranks; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, qcache_evict_kernel<DH, IN_SMEM>, a);
+}
+}  // namespace
+
 int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent, const int* next_position, int max_len,
-                        void* workspace, int* status, long long* launches, cudaStream_t st) {
+                        void* workspace, unsigned long long tag, int sm_count, int* status, long long* launches, cudaStream_t st) {
   EvArgs a;
   memset(&a, 0, sizeof(a));
   a.c = c; a.hk = d.hk; a.keep = keep; a.recent = recent; a.max_len = max_len; a.next = next_position; a.status = status;
   a.cap = max_len / 2 + 1;                                 // as many rows go below `keep` as come from behind it
-  unsigned char* p = static_cast<unsigned char*>(workspace);
-  a.count = reinterpret_cast<int*>(p); p += up256((size_t)d.B * d.hk * 4);
-  a.new_len = reinterpret_cast<int*>(p); p += up256((size_t)d.B * 4);
-  a.list = reinterpret_cast<int*>(p);
+  a.arrived = static_cast<unsigned long long*>(workspace);
+  a.tag = tag;
+  a.list = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + up256((size_t)d.B * 8));
+  // more CTAs a head while there are SMs for them and each keeps 2048 rows or more (fewer cost more in barriers than they save)
+  int ranks = 1;
+  while (ranks < 8 && (long long)d.B * d.hk * ranks * 2 <= sm_count && max_len >= ranks * 4096) ranks *= 2;
+  a.per_cta = ((max_len + ranks - 1) / ranks + 31) / 32 * 32;
+  const bool in_smem = a.per_cta <= EV_SMEM_ROWS;
   cudaError_t e;
-  const dim3 grid((unsigned)d.hk, (unsigned)d.B);
-  if (max_len <= EV_SMEM_ROWS) {
-    const int smem = (max_len > 1 ? max_len : 1) * 4;
-    if (smem > 32 * 1024) {
-      static bool done[MAX_DEVICES];
-      if ((e = opt_in(qcache_select_kernel<true>, EV_SMEM_ROWS * 4, done)) != cudaSuccess) return -(int)e;
-    }
-    e = launch_pdl_smem(qcache_select_kernel<true>, grid, dim3(EV_THREADS), (size_t)smem, st, a);
-  } else {
-    e = launch_pdl(qcache_select_kernel<false>, grid, dim3(EV_THREADS), st, a);
-  }
-  if (e != cudaSuccess) return -(int)e;
-  ++*launches;
-  const int most = keep < max_len - keep ? keep : max_len - keep;      // rows that can move
-  int nx = (most * (d.dh / 16) + 1023) / 1024;
-  if (nx < 1) nx = 1;
-  QC_BY_HEAD((launch_pdl(qcache_move_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
+  if (in_smem) QC_BY_HEAD((evict_run<DH, true>(a, ranks, d.B, a.per_cta * 4, st)))
+  else QC_BY_HEAD((evict_run<DH, false>(a, ranks, d.B, 0, st)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;

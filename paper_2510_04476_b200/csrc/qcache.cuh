@@ -25,5 +25,7 @@ size_t qcache_workspace_bytes(const CcaDims& d, int max_len, int sm_count);
 int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, bf16* o, const QCache& c, const int* pos, int extra,
                             int max_len, int accumulate, void* workspace, int sm_count, int* status, long long* launches,
                             cudaEvent_t ev_begin, cudaEvent_t ev_end, cudaStream_t st);
+// tag: a number below 2^48, not 0, that no memory is expected to hold by chance, another one for every call.
 int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent, const int* next_position, int max_len,
-                        void* workspace, int* status, long long* launches, cudaStream_t st);
+                        void* workspace, unsigned long long tag, int sm_count, int* status, long long* launches,
+                        cudaStream_t st);

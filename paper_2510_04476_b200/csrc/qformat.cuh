@@ -92,10 +92,13 @@ CCA_DEVINL bf16 group_scale(float amax) {
   const bf16 s = __float2bfloat16_rn(__fdiv_rn(amax, 7.f));
   return __bfloat162float(s) < 1.17549435e-38f ? __ushort_as_bfloat16((unsigned short)0) : s;
 }
-CCA_DEVINL int code_of(float x, float s) {
+// x / s correctly rounded from r = 1 / s (correctly rounded): one Newton step on the quotient.  It holds while nothing over- or
+// underflows on the way; a scale below 2^-96 takes the division itself.
+CCA_DEVINL int code_of(float x, float s, float r) {
   if (!(s > 0.f)) return 0;
-  const float r = rintf(__fdiv_rn(x, s));
-  return (int)fminf(fmaxf(r, -7.f), 7.f);
+  float q = x * r;
+  q = s < 1.2621774e-29f ? __fdiv_rn(x, s) : fmaf(fmaf(-s, q, x), r, q);
+  return (int)fminf(fmaxf(rintf(q), -7.f), 7.f);
 }
 CCA_DEVINL uint32_t code_byte(int c0, int c1) {
   return (c0 < 0 ? 0x80u : 0u) | (uint32_t)(c0 < 0 ? -c0 : c0) | (c1 < 0 ? 0x40u : 0u) | ((uint32_t)(c1 < 0 ? -c1 : c1) << 3);
@@ -119,9 +122,9 @@ CCA_DEVINL void quantise_block(F x, uint8_t (&code)[2 * NG], bf16 (&scale)[NG]) 
 #pragma unroll
     for (int s = 1; s < 8; s <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
     scale[grp] = group_scale(__uint_as_float(m));
-    const float sf = __bfloat162float(scale[grp]);
-    code[2 * grp] = (uint8_t)code_byte(code_of(v[0], sf), code_of(v[2], sf));
-    code[2 * grp + 1] = (uint8_t)code_byte(code_of(v[1], sf), code_of(v[3], sf));
+    const float sf = __bfloat162float(scale[grp]), r = __frcp_rn(sf);
+    code[2 * grp] = (uint8_t)code_byte(code_of(v[0], sf, r), code_of(v[2], sf, r));
+    code[2 * grp + 1] = (uint8_t)code_byte(code_of(v[1], sf, r), code_of(v[3], sf, r));
   }
 }
 
