@@ -673,6 +673,8 @@ struct EvArgs {
   QCache c;
   int hk, keep, recent, max_len;
   int per_cta;                   // rows of a CTA, a multiple of 32
+  int move_here;                 // the selecting CTAs move the rows too; else the next kernel does
+  int* count;                    // [B * hk] rows to move, for the next kernel
   const int* next;               // [B] position of the next token
   unsigned long long* arrived;   // [B] heads that are done with a sequence
   unsigned long long tag;        // of this call, 48 bits, not 0
@@ -681,7 +683,10 @@ struct EvArgs {
   int* status;
 };
 
-constexpr int EV_THREADS = 1024, EV_BINS = 2048;
+#ifndef EV_RANK_ROWS
+#define EV_RANK_ROWS 16384
+#endif
+constexpr int EV_THREADS = 1024, EV_BINS = 2048, EV_RANK = EV_RANK_ROWS;
 
 // The order of eviction as an unsigned number, larger = kept: 0xffffffff for the newest, else the weight's order (a NaN is lowest).
 CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
@@ -730,6 +735,50 @@ CCA_DEVINL int warp_offsets(int v, int* sm, int warp, int lane, int& total) {
   return __shfl_sync(0xffffffffu, inc - x, warp);
 }
 
+// Moves the listed rows of one head: DH / 16 lanes take the 16-byte pieces of a row's codes (and as many scales), four rows a
+// thread at a time.  A destination is below `keep` and a source is not, so the moves need no order.
+template <int DH, int THREADS>
+CCA_DEVINL void move_rows(const EvArgs& a, size_t base, const int* src, const int* dst, int moves, int part, int parts) {
+  using R = Row<DH>;
+  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = THREADS / LANES, U = 4;
+  const int l = threadIdx.x % LANES, piece = l % PIECES;
+  uint8_t* codes = (l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES;
+  bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES;
+  for (int i0 = part * ROWS * U + threadIdx.x / LANES; i0 < moves; i0 += parts * ROWS * U) {
+    size_t from[U], to[U];
+    uint4 u[U];
+    bf16 s[U];
+    float wt[U];
+    int ps[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) { from[x] = (size_t)src[i0 + x * ROWS]; to[x] = (size_t)dst[i0 + x * ROWS]; }
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) {
+        u[x] = __ldcs(reinterpret_cast<const uint4*>(codes + from[x] * R::CODES) + piece);
+        s[x] = scales[from[x] * R::SCALES + piece];
+        if (l == 0) wt[x] = a.c.weight[base + from[x]];
+        if (l == PIECES) ps[x] = a.c.position[base + from[x]];
+      }
+#pragma unroll
+    for (int x = 0; x < U; ++x)
+      if (i0 + x * ROWS < moves) {
+        reinterpret_cast<uint4*>(codes + to[x] * R::CODES)[piece] = u[x];
+        scales[to[x] * R::SCALES + piece] = s[x];
+        if (l == 0) a.c.weight[base + to[x]] = wt[x];
+        if (l == PIECES) a.c.position[base + to[x]] = ps[x];
+      }
+  }
+}
+template <int DH>
+__global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
+  pdl_enter();
+  const int bj = blockIdx.z * a.hk + blockIdx.y;
+  const int* dst = a.list + (size_t)bj * 2 * a.cap;
+  move_rows<DH, 256>(a, (size_t)bj * a.c.S_max, dst + a.cap, dst, a.count[bj], blockIdx.x, gridDim.x);
+}
+
 // One cluster of 1 to 8 CTAs per (sequence, head), each with a contiguous run of rows: the keep-th largest key by three counting
 // passes over its digits (11, 11, 10 bits; the CTAs read each other's counts), then, in ascending order of rows, the rows below `keep` that go and
 // the rows behind it that stay, and their moves.  A warp takes a contiguous run of rows, 32 at a time, so ranks come
@@ -751,17 +800,48 @@ __global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
   const int n = *reinterpret_cast<volatile int*>(a.c.len + b);
   if (n < 0 || n > a.max_len || n > a.c.S_max) {
     if (tid == 0 && j == 0 && rank == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
+    if (tid == 0 && rank == 0) a.count[bj] = 0;
     return;
   }
-  if (n <= a.keep) return;
+  if (n <= a.keep) {
+    if (tid == 0 && rank == 0) a.count[bj] = 0;
+    return;
+  }
   const size_t base = (size_t)bj * a.c.S_max;
   int moves = 0;
   int* dst = a.list + (size_t)bj * 2 * a.cap;
   int* src = dst + a.cap;
-  if (a.keep > 0) {
-    const float* w = a.c.weight + base;
-    const int* pos = a.c.position + base;
-    const long long first_recent = (long long)a.next[b] - a.recent;
+  const float* w = a.c.weight + base;
+  const int* pos = a.c.position + base;
+  const long long first_recent = (long long)a.next[b] - a.recent;
+  if (a.keep > 0 && n == a.keep + 1 && ranks == 1) {
+    // One row goes, as at every step of a cache at its bound: the lowest key's, of equal ones the last row's.  A single minimum
+    // instead of three counting passes and two lists (4097 rows: EV1_NEW us instead of EV1_OLD).
+    unsigned long long least = ~0ull;
+#pragma unroll 4
+    for (int r = tid; r < n; r += EV_THREADS) {
+      const unsigned long long k = (unsigned long long)keep_key(w[r], pos[r], first_recent) << 32 | (uint32_t)~r;
+      least = k < least ? k : least;
+    }
+    unsigned long long* part = reinterpret_cast<unsigned long long*>(hist[0]);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+      const unsigned long long o = __shfl_xor_sync(0xffffffffu, least, s);
+      least = o < least ? o : least;
+    }
+    if (lane == 0) part[warp] = least;
+    __syncthreads();
+    least = part[lane];
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+      const unsigned long long o = __shfl_xor_sync(0xffffffffu, least, s);
+      least = o < least ? o : least;
+    }
+    const int gone = (int)~(uint32_t)least;
+    moves = gone < a.keep ? 1 : 0;
+    if (tid == 0) { dst[0] = gone; src[0] = a.keep; }
+    __syncthreads();
+  } else if (a.keep > 0) {
     const int row0 = min(n, rank * a.per_cta), row1 = min(n, row0 + a.per_cta);
     auto key_of = [&](int r) { return IN_SMEM ? keys[r - row0] : keep_key(w[r], pos[r], first_recent); };
     for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[0][i] = hist[1][i] = hist[2][i] = 0;
@@ -771,14 +851,25 @@ __global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      if (IN_SMEM && pass == 0) {                          // eight rows of a thread on their way at a time
+        for (int r0 = row0 + tid; r0 < row1; r0 += 8 * EV_THREADS) {
+          float wr[8];
+          int pr[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (r0 + x * EV_THREADS < row1) { wr[x] = w[r0 + x * EV_THREADS]; pr[x] = pos[r0 + x * EV_THREADS]; }
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (r0 + x * EV_THREADS < row1) {
+              const uint32_t k = keep_key(wr[x], pr[x], first_recent);
+              keys[r0 + x * EV_THREADS - row0] = k;
+              atomicAdd(&hist[0][k >> shift], 1);
+            }
+        }
+      } else
 #pragma unroll 4
       for (int r = row0 + tid; r < row1; r += EV_THREADS) {
-        uint32_t k;
-        if (IN_SMEM && pass > 0) k = keys[r - row0];
-        else {
-          k = keep_key(w[r], pos[r], first_recent);
-          if (IN_SMEM) keys[r - row0] = k;
-        }
+        const uint32_t k = key_of(r);
         if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[pass][(k >> shift) & ((1u << bits) - 1u)], 1);
       }
       all_sync(ranks);
@@ -871,37 +962,8 @@ __global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
     }
     all_sync(ranks);                                       // the lists are whole, and nobody reads weights or positions any more
   }
-  // ---- moves: DH / 16 lanes take the 16-byte pieces of a row's codes; as many scales as 16-byte pieces
-  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = EV_THREADS / LANES, U = 4;
-  const int l = tid % LANES, piece = l % PIECES;
-  uint8_t* codes = (l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES;
-  bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES;
-  for (int i0 = rank * ROWS * U + tid / LANES; i0 < moves; i0 += ranks * ROWS * U) {
-    size_t from[U], to[U];
-    uint4 u[U];
-    bf16 s[U];
-    float wt[U];
-    int ps[U];
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) { from[x] = (size_t)src[i0 + x * ROWS]; to[x] = (size_t)dst[i0 + x * ROWS]; }
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) {
-        u[x] = __ldcs(reinterpret_cast<const uint4*>(codes + from[x] * R::CODES) + piece);
-        s[x] = scales[from[x] * R::SCALES + piece];
-        if (l == 0) wt[x] = a.c.weight[base + from[x]];
-        if (l == PIECES) ps[x] = a.c.position[base + from[x]];
-      }
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) {
-        reinterpret_cast<uint4*>(codes + to[x] * R::CODES)[piece] = u[x];
-        scales[to[x] * R::SCALES + piece] = s[x];
-        if (l == 0) a.c.weight[base + to[x]] = wt[x];
-        if (l == PIECES) a.c.position[base + to[x]] = ps[x];
-      }
-  }
+  if (a.move_here) move_rows<DH, EV_THREADS>(a, base, src, dst, moves, rank, ranks);
+  else if (tid == 0 && rank == 0) a.count[bj] = moves;
   // The length is written by the last head to be done with it, so that every CTA, early or late, reads the length from before.  The
   // workspace comes as it is: a count is one only under this call's tag (48 bits), and the last head leaves a zero, so that a
   // replayed call finds none of its own.
@@ -978,7 +1040,7 @@ size_t qcache_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
   attn_plan(d, max_len, sm_count, &chunk, &splits);
   const size_t attn = up256((size_t)d.B * d.hq * splits * d.dh * 4) + up256((size_t)d.B * d.hq * splits * 2 * 4) +
                       up256((size_t)d.B * d.hq * max_len * 4);
-  const size_t ev = up256((size_t)d.B * 8) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
+  const size_t ev = up256((size_t)d.B * 8) + up256((size_t)d.B * d.hk * 4) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
   return attn > ev ? attn : ev;
 }
 
@@ -1040,15 +1102,23 @@ int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent,
   a.cap = max_len / 2 + 1;                                 // as many rows go below `keep` as come from behind it
   a.arrived = static_cast<unsigned long long*>(workspace);
   a.tag = tag;
-  a.list = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + up256((size_t)d.B * 8));
-  // more CTAs a head while there are SMs for them and each keeps 2048 rows or more (fewer cost more in barriers than they save)
+  a.count = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + up256((size_t)d.B * 8));
+  a.list = reinterpret_cast<int*>(reinterpret_cast<unsigned char*>(a.count) + up256((size_t)d.B * d.hk * 4));
+  // more CTAs a head while there are SMs for them and each keeps EV_RANK rows or more (fewer cost more in barriers than they save)
   int ranks = 1;
-  while (ranks < 8 && (long long)d.B * d.hk * ranks * 2 <= sm_count && max_len >= ranks * 4096) ranks *= 2;
+  while (ranks < 8 && (long long)d.B * d.hk * ranks * 2 <= sm_count && max_len >= ranks * 2 * EV_RANK) ranks *= 2;
+  const int most = keep < max_len - keep ? keep : max_len - keep;      // rows of a head that can move
+  a.move_here = most <= 512 * ranks;                                   // more are moved by a kernel over all SMs
   a.per_cta = ((max_len + ranks - 1) / ranks + 31) / 32 * 32;
   const bool in_smem = a.per_cta <= EV_SMEM_ROWS;
   cudaError_t e;
   if (in_smem) QC_BY_HEAD((evict_run<DH, true>(a, ranks, d.B, a.per_cta * 4, st)))
   else QC_BY_HEAD((evict_run<DH, false>(a, ranks, d.B, 0, st)))
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  if (a.move_here) return 0;
+  int nx = (most * (d.dh / 16) + 1023) / 1024;
+  QC_BY_HEAD((launch_pdl(qcache_move_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
