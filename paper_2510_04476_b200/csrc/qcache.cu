@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
     const uint32_t u = u0 + ((threadIdx.x & 31) >> 3);
     const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
     const uint32_t ih = (u >> 1) / R::NB;                  // (new row, head)
-    const int i = (int)(ih / a.hk), h = (int)(ih - (uint32_t)i * a.hk);
+    const int i = (int)(ih / (uint32_t)a.hk), h = (int)(ih - (uint32_t)i * a.hk);
     const bool ok = i < cnt;                               // false behind the last unit too
     const bf16* src = (kv ? a.v : a.k) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
     uint8_t code[2 * R::NG];
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(256) qcache_read_kernel(IoArgs a) {
   for (uint32_t u = blockIdx.x * 32 + (threadIdx.x >> 3); u < units; u += gridDim.x * 32) {
     const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
     const uint32_t ih = (u >> 1) / R::NB;
-    const int i = (int)(ih / a.hk), h = (int)(ih - (uint32_t)i * a.hk);
+    const int i = (int)(ih / (uint32_t)a.hk), h = (int)(ih - (uint32_t)i * a.hk);
     const long long r = first + i;
     const bool there = r >= 0 && r < a.c.S_max;
     const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + (there ? r : 0);

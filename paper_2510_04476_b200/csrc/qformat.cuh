@@ -84,24 +84,17 @@ CCA_DEVINL void zero_words(uint32_t (&w)[NW]) {
   for (int i = 0; i < NW; ++i) w[i] = 0u;
 }
 
-// The scale of a group from the largest magnitude in it, and a channel's code.  IEEE division, so that the result does not
-// depend on the build's fast-math setting; an infinity or NaN in the group makes the scale NaN (and every code 0), a scale
-// below the smallest normal number counts as zero.
-CCA_DEVINL bf16 group_scale(float amax) {
-  if (!(amax <= 3.3895313892515355e38f)) return __ushort_as_bfloat16((unsigned short)0x7fc0);
-  const bf16 s = __float2bfloat16_rn(__fdiv_rn(amax, 7.f));
-  return __bfloat162float(s) < 1.17549435e-38f ? __ushort_as_bfloat16((unsigned short)0) : s;
+CCA_DEVINL float divide(float a, float b) {                // to nearest, subnormal numbers as they are whatever the build's setting
+  float r;
+  asm("div.rn.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
-// x / s correctly rounded from r = 1 / s (correctly rounded): one Newton step on the quotient.  It holds while nothing over- or
-// underflows on the way; a scale below 2^-96 takes the division itself.
-CCA_DEVINL int code_of(float x, float s, float r) {
-  if (!(s > 0.f)) return 0;
-  float q = x * r;
-  q = s < 1.2621774e-29f ? __fdiv_rn(x, s) : fmaf(fmaf(-s, q, x), r, q);
-  return (int)fminf(fmaxf(rintf(q), -7.f), 7.f);
-}
+// The whole number nearest to q (ties to even), |q| < 2^21: what adding 1.5 * 2^23 leaves in the low bits.  No clamp to -7 .. 7 is
+// needed: a scale rounded down by its 2^-9 still leaves the largest quotient below 7.02.
+CCA_DEVINL int nearest(float q) { return __float_as_int(__fadd_rn(q, 12582912.f)) - 0x4b400000; }
+// Codes as a byte, in sign and magnitude; no negative zero.
 CCA_DEVINL uint32_t code_byte(int c0, int c1) {
-  return (c0 < 0 ? 0x80u : 0u) | (uint32_t)(c0 < 0 ? -c0 : c0) | (c1 < 0 ? 0x40u : 0u) | ((uint32_t)(c1 < 0 ? -c1 : c1) << 3);
+  return (uint32_t)abs(c0) | ((uint32_t)abs(c1) << 3) | (((uint32_t)c0 >> 24) & 0x80u) | (((uint32_t)c1 >> 25) & 0x40u);
 }
 CCA_DEVINL int value_e0(uint32_t byte) { const int m = (int)(byte & 7u); return (byte & 0x80u) ? -m : m; }
 CCA_DEVINL int value_e1(uint32_t byte) { const int m = (int)((byte >> 3) & 7u); return (byte & 0x40u) ? -m : m; }
@@ -111,20 +104,49 @@ CCA_DEVINL int value_e1(uint32_t byte) { const int m = (int)((byte >> 3) & 7u); 
 // (the same in all eight lanes).  All 32 lanes call it.
 template <int NG, typename F>
 CCA_DEVINL void quantise_block(F x, uint8_t (&code)[2 * NG], bf16 (&scale)[NG]) {
+  uint2 u[NG];
+#pragma unroll
+  for (int grp = 0; grp < NG; ++grp) u[grp] = x(grp);
 #pragma unroll
   for (int grp = 0; grp < NG; ++grp) {
-    const uint2 u = x(grp);
-    const float v[4] = {bf_lo(u.x), bf_hi(u.x), bf_lo(u.y), bf_hi(u.y)};
-    // a NaN must win the maximum: compare the magnitudes' bit patterns
-    uint32_t m = 0;
+    // magnitudes compared as 16-bit patterns, two at a time: their order is the numbers', and a NaN wins
+    uint32_t m = __vmaxu2(u[grp].x & 0x7fff7fffu, u[grp].y & 0x7fff7fffu);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int s = 1; s < 8; s <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, s));
+    const float amax = __uint_as_float(max(m << 16, m & 0xffff0000u));
+    const float v[4] = {bf_lo(u[grp].x), bf_hi(u[grp].x), bf_lo(u[grp].y), bf_hi(u[grp].y)};
+    float sf;
+    int c[4];
+    if (__any_sync(0xffffffffu, amax > 0.f && amax < 1.0097420e-28f)) {
+      // Below 2^-93 (in any of the warp's groups) the steps of the other branch would underflow.  A scale below the smallest
+      // normal number counts as zero.
+      const bf16 s = __float2bfloat16_rn(divide(amax, 7.f));
+      sf = __bfloat162float(s);
+      if (sf < 1.17549435e-38f) sf = 0.f;
+      if (amax >= 1.0097420e-28f && !(amax <= 3.3895314e38f)) sf = __uint_as_float(0x7fc00000u);
 #pragma unroll
-    for (int s = 1; s < 8; s <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
-    scale[grp] = group_scale(__uint_as_float(m));
-    const float sf = __bfloat162float(scale[grp]), r = __frcp_rn(sf);
-    code[2 * grp] = (uint8_t)code_byte(code_of(v[0], sf, r), code_of(v[2], sf, r));
-    code[2 * grp + 1] = (uint8_t)code_byte(code_of(v[1], sf, r), code_of(v[3], sf, r));
+      for (int i = 0; i < 4; ++i) c[i] = nearest(divide(v[i], sf));
+    } else {
+      // Quotients by one Newton step, so that nothing depends on the build's fast-math setting.  amax / 7 comes out correctly
+      // rounded (the reciprocal of 7 is).  x / s comes out exact where it is half way between two whole numbers: then the
+      // residual is exact and the correction off by less than a last place; elsewhere it is at least 2^-12 of itself away from
+      // half way (x and s have 8 significant bits each), a thousand times what is left of the error.  An infinity or a NaN in the
+      // group gives a NaN scale by itself (inf - inf).
+      constexpr float R7 = 1.f / 7.f;
+      const float q7 = amax * R7;
+      sf = __bfloat162float(__float2bfloat16_rn(fmaf(fmaf(-7.f, q7, amax), R7, q7)));
+      float r;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sf));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float q = v[i] * r;
+        c[i] = nearest(fmaf(fmaf(-sf, q, v[i]), r, q));
+      }
+    }
+    scale[grp] = __float2bfloat16_rn(sf);
+    const uint32_t two = sf > 0.f ? code_byte(c[0], c[2]) | (code_byte(c[1], c[3]) << 8) : 0u;
+    code[2 * grp] = (uint8_t)two;
+    code[2 * grp + 1] = (uint8_t)(two >> 8);
   }
 }
 

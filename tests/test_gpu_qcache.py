@@ -93,6 +93,29 @@ def test_append_and_read(hk, dh, B, n, S):
     cca.close()
 
 
+def test_append_of_every_quotient():
+    """Every pair of an 8-bit significand over an 8-bit scale that a group can hold: 128 largest values (each with another scale)
+    against all numbers up to them, halves between two codes among them; and the same far down and far up in the range."""
+    cca = _cca(1, 1, 64)
+    mant = torch.arange(128, 256, dtype=torch.float64)
+    top = mant.repeat_interleave(128 * 8)                            # the largest of a group
+    x = mant.repeat(128)[:, None] * 2.0 ** -torch.arange(8, dtype=torch.float64)
+    x = torch.minimum(x.reshape(-1), top)                            # 1024 numbers for each of 128 scales
+    g = x.view(-1, 16)
+    rows = torch.zeros(g.shape[0], 32, dtype=torch.float64)
+    rows[:, :16] = g
+    rows[:, 16:31] = -g[:, :15]
+    rows[:, 31] = top.view(-1, 16)[:, 0]
+    for scale in (1.0, 2.0 ** -90, 2.0 ** -104, 2.0 ** -130, 2.0 ** 52, 2.0 ** 119):
+        k = (rows * scale).bfloat16().view(1, -1, 1, 64)
+        cache = cca.new_qcache(1, k.shape[1])
+        cca.qcache_append(cache, k.cuda(), k.cuda())
+        c, s = Q.quantise(k)
+        assert torch.equal(cache["k_scales"][0, 0].cpu().double(), s[0, :, 0]), scale
+        assert torch.equal(cache["k_codes"][0, 0].cpu(), Q.pack(c[0, :, 0])), scale
+    cca.close()
+
+
 def test_append_of_a_padded_batch_and_rows_that_do_not_fit():
     cca = _cca(2, 2, 64)
     B, n, S = 5, 4, 10
