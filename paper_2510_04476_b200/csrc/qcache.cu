@@ -134,7 +134,8 @@ struct QaArgs {
   int extra, max_len, chunk, splits;
   float* part_o;             // [B, hq, splits, DH]
   float* part_ml;            // [B, hq, splits, 2]
-  float* scores;             // [B, hk, max_len, g]: logits times log2(e), where the weights are gathered; else null
+  int gather;                // add what each row is given to its weight
+  float* scores;             // [B, hk, max_len, g]: logits times log2(e), where the weights are gathered by the second kernel
   bf16* o;
   int* status;
 };
@@ -259,7 +260,40 @@ struct Rows {
   }
 };
 
-constexpr int QA_WARPS = 4, QA_MAX_SPLITS = 128;
+constexpr int QA_WARPS = 4, QA_MAX_SPLITS = 128, QA_FIXED = 192;
+constexpr int QA_FUSED_SPLITS = 8, QA_FUSED_ROWS = 512, QA_FUSED_LOGITS = 32 * 1024;    // chunks, rows of one, bytes of its logits
+
+CCA_DEVINL uint32_t cluster_place(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return r;
+}
+CCA_DEVINL float cluster_float(const float* p, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL float2 cluster_float2(const float2* p, int rank) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+CCA_DEVINL void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+CCA_DEVINL void cluster_barrier() { cluster_arrive(); cluster_wait(); }
+
+template <int DH, int H>
+struct FusedShare {                                        // what the CTAs of a cluster read of each other, and what they make of it
+  float o[H * DH];
+  float2 ml[H];
+  float fac[H][8], lse[H];
+};
 // CTAs of the attention kernel that an SM holds; registers are given out accordingly.
 __host__ __device__ constexpr int qa_resident(int dh, int nht) {
   return nht == 1 ? (dh == 32 ? 7 : dh == 64 ? 6 : dh == 128 ? 4 : 3) : (dh == 32 ? 5 : dh == 64 ? 4 : 3);
@@ -270,7 +304,10 @@ __host__ __device__ constexpr int qa_resident(int dh, int nht) {
 // 256 codes; O^T = V^T P^T has the channels as the 16.  Both read the codes from the registers that they were loaded into.  A
 // group's scale multiplies the group's partial logit in fp32; a value row's scale is multiplied into the probability, once
 // per group, before that is rounded to bf16 as the operand (the only rounding of the probabilities; the sums are taken before it).
-template <int DH, int NHT>
+//
+// FUSED: a cluster is all of a (sequence, kv head)'s chunks (8 at most); its CTAs join their results through each other's shared
+// memory, keep their logits in their own, and finish the whole call: one launch instead of two.
+template <int DH, int NHT, bool FUSED>
 __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_attn_kernel(QaArgs a) {
   pdl_enter();
   using R = Row<DH>;
@@ -326,7 +363,13 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   const size_t base = ((size_t)b * d.hk + j) * a.c.S_max;
   const uint8_t *kc = a.c.k_codes + base * R::CODES, *vc = a.c.v_codes + base * R::CODES;
   const bf16 *ksc = a.c.k_scales + base * R::SCALES, *vsc = a.c.v_scales + base * R::SCALES;
-  float* sco = a.scores ? a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g + h0 : nullptr;
+  extern __shared__ __align__(128) unsigned char ring[];
+  float* sco = nullptr;                                    // logits of this CTA's rows, from the sequence's row 0 on
+  if (FUSED) {
+    if (a.gather) sco = reinterpret_cast<float*>(ring + QA_WARPS * S::N * S::BYTES) - r_begin * d.g;
+  } else if (a.gather) {
+    sco = a.scores + ((size_t)b * d.hk + j) * a.max_len * d.g + h0;
+  }
 
   const int last = r_end - 1, g8 = 8 * d.g;
   const bool even_heads = d.g % 2 == 0;
@@ -371,7 +414,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[ht][c] *= c_scale;
     if (sco) {
-      float* sp = sco + (uint32_t)(r_lo * d.g + 2 * t);
+      float* sp = sco + (r_lo * d.g + 2 * t);
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht) {
         const bool ok_lo = 8 * ht + 2 * t < nh && (!masked || r_lo <= last), ok_hi = ok_lo && (!masked || r_hi <= last);
@@ -445,7 +488,6 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   };
   // warp w takes stages w, w + 4, ... of the chunk
   constexpr int STEP = QA_WARPS * S::SR;
-  extern __shared__ __align__(128) unsigned char ring[];
   unsigned char* mine = ring + warp * (S::N * S::BYTES);
   const uint32_t mine_u32 = (uint32_t)__cvta_generic_to_shared(mine);
   int r0 = r_begin + warp * S::SR, slot = 0;
@@ -483,6 +525,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   // merge the warps through shared memory
   static_assert(8 * NHT * (DH + 1) * 4 <= S::N * S::BYTES, "a warp's partial result takes the place of its stages");
   __shared__ float sm_ml[QA_WARPS][8 * NHT][2];
+  __shared__ FusedShare<FUSED ? DH : 1, FUSED ? 8 * NHT : 1> fz;
   float* my_o = reinterpret_cast<float*>(mine);
   __syncwarp();
 #pragma unroll
@@ -515,9 +558,51 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
       lo += sm_ml[w][h][1] * al;
       oo += reinterpret_cast<const float*>(ring + w * (S::N * S::BYTES))[h * (DH + 1) + c] * al;
     }
-    const size_t pidx = ((size_t)b * d.hq + j * d.g + h0 + h) * a.splits + split;
-    a.part_o[pidx * DH + c] = oo;
-    if (c == 0) { a.part_ml[pidx * 2] = mn; a.part_ml[pidx * 2 + 1] = lo; }
+    if constexpr (FUSED) {
+      fz.o[h * DH + c] = oo;
+      if (c == 0) fz.ml[h] = make_float2(mn, lo);
+    } else {
+      const size_t pidx = ((size_t)b * d.hq + j * d.g + h0 + h) * a.splits + split;
+      a.part_o[pidx * DH + c] = oo;
+      if (c == 0) { a.part_ml[pidx * 2] = mn; a.part_ml[pidx * 2 + 1] = lo; }
+    }
+  }
+  if constexpr (FUSED) {
+    const int ranks = gridDim.x;
+    cluster_barrier();
+    for (int h = warp; h < nh; h += QA_WARPS) {            // lane = chunk
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < ranks) ml = cluster_float2(&fz.ml[h], lane);
+      float m = ml.x;
+#pragma unroll
+      for (int x = 4; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
+      float l = ml.y * f;
+#pragma unroll
+      for (int x = 4; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+      if (lane < 8) fz.fac[h][lane] = n_rows > 0 ? f / l : 0.f;
+      if (lane == 0) fz.lse[h] = m + __log2f(l);
+    }
+    __syncthreads();
+    // the output's channels are shared out among the CTAs
+    for (int i = split * (QA_WARPS * 32) + threadIdx.x; i < nh * DH; i += ranks * (QA_WARPS * 32)) {
+      float part[8], acc = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) part[x] = x < ranks ? cluster_float(&fz.o[i], x) : 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) acc = fmaf(part[x], x < ranks ? fz.fac[i / DH][x] : 0.f, acc);
+      a.o[(size_t)b * d.Lq + (size_t)(j * d.g) * DH + i] = __float2bfloat16(acc);
+    }
+    cluster_arrive();                                      // this CTA reads no other's memory any more
+    if (sco) {
+      float* w = a.c.weight + ((size_t)b * d.hk + j) * a.c.S_max;
+      for (int r = r_begin + threadIdx.x; r < r_end; r += QA_WARPS * 32) {
+        float acc = 0.f;
+        for (int h = 0; h < d.g; ++h) acc += exp2f(sco[r * d.g + h] - fz.lse[h]);
+        atomicAdd(w + r, acc);                             // the row's only one: no order to depend on, and nothing to wait for
+      }
+    }
+    cluster_wait();                                        // nobody leaves while its memory may be read
   }
 }
 
@@ -541,7 +626,7 @@ __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
   const int r_first = blockIdx.x * (256 * QJ_ROWS) + tid;
   float4 s4[QJ_ROWS];
   float wr[QJ_ROWS];
-  if (a.scores) {
+  if (a.gather) {
 #pragma unroll
     for (int i = 0; i < QJ_ROWS; ++i) {
       const int r = r_first + i * 256;
@@ -599,7 +684,7 @@ __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
       reinterpret_cast<uint2*>(a.o + (size_t)b * d.Lq + (size_t)(j * d.g + h) * DH)[c] = u;
     }
   }
-  if (!a.scores) return;
+  if (!a.gather) return;
 #pragma unroll
   for (int i = 0; i < QJ_ROWS; ++i) {
     const int r = r_first + i * 256;
@@ -621,13 +706,12 @@ __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
 int heads_per_cta(const CcaDims& d) { return d.g <= 8 || d.dh == 256 ? 8 : 16; }
 
 // Rows per CTA and number of chunks for sequences of up to max_len rows.  A chunk costs its rows plus what a CTA costs whatever its
-// rows (the way to its first loads, the merge of its warps, its share of the join: about as long as FIXED rows take); of one to four
+// rows (the way to its first loads, the merge of its warps, its share of the join: about as long as QA_FIXED rows take); of one to four
 // full waves of resident CTAs the one with the least is taken.
 void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
   const int n_grp = (d.g + heads_per_cta(d) - 1) / heads_per_cta(d);
   const long long base = (long long)d.B * d.hk * n_grp;
   const int resident = sm_count * qa_resident(d.dh, heads_per_cta(d) / 8);
-  constexpr int FIXED = 192;
   long long best = -1;
   for (int waves = 1; waves <= 4; ++waves) {
     long long n = (long long)resident * waves / base;
@@ -636,9 +720,25 @@ void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* spl
     long long ch = (max_len + n - 1) / n;
     ch = (ch + 63) / 64 * 64;                              // the four warps of a CTA take 16 rows each per round
     const long long used = (max_len + ch - 1) / ch;
-    const long long cost = (base * used + resident - 1) / resident * (ch + FIXED);
+    const long long cost = (base * used + resident - 1) / resident * (ch + QA_FIXED);
     if (best < 0 || cost < best) { best = cost; *chunk = (int)ch; *splits = (int)used; }
   }
+}
+
+// One launch does where 8 chunks of 512 rows hold the sequence (what a longer chunk takes more is then less than the second launch:
+// 1 x 1024 rows FUSED_NEW us instead of FUSED_OLD, 1 x 4096 FUSED4_NEW instead of FUSED4_OLD), one CTA has all of a kv head's query
+// heads, and a chunk's logits find room.  Chunks of 128 rows: a stage for each warp.
+bool attn_fused(const CcaDims& d, int max_len, int sm_count, int gather, int* chunk, int* splits) {
+  if (d.g > heads_per_cta(d)) return false;
+  const long long base = (long long)d.B * d.hk, resident = (long long)sm_count * qa_resident(d.dh, heads_per_cta(d) / 8);
+  long long best = -1;
+  for (int n = 1; n <= QA_FUSED_SPLITS; n *= 2) {
+    const int ch = ((max_len + n - 1) / n + 127) / 128 * 128;
+    if (ch > QA_FUSED_ROWS || (gather && ch * d.g * 4 > QA_FUSED_LOGITS)) continue;
+    const long long cost = (base * n + resident - 1) / resident * (ch + QA_FIXED);
+    if (best < 0 || cost < best) { best = cost; *chunk = ch; *splits = n; }
+  }
+  return best >= 0;
 }
 
 // The opt-in to more than 48 KB of dynamic shared memory, per device and kernel (`done`: one flag per device).
@@ -653,19 +753,35 @@ cudaError_t opt_in(K kernel, int bytes, bool* done) {
 }
 
 template <int DH, int NHT>
-cudaError_t attn_run(const QaArgs& a, dim3 grid, cudaStream_t st) {
+cudaError_t attn_run(const QaArgs& a, dim3 grid, bool fused, cudaStream_t st) {
   constexpr int smem = QA_WARPS * Stage<DH>::N * Stage<DH>::BYTES;
   static_assert(smem <= 48 * 1024, "no opt-in needed");
-  return launch_pdl_smem(qcache_attn_kernel<DH, NHT>, grid, dim3(QA_WARPS * 32), smem, st, a);
+  if (!fused) return launch_pdl_smem(qcache_attn_kernel<DH, NHT, false>, grid, dim3(QA_WARPS * 32), smem, st, a);
+  static bool done[MAX_DEVICES];
+  const cudaError_t e = opt_in(qcache_attn_kernel<DH, NHT, true>, smem + QA_FUSED_LOGITS, done);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(QA_WARPS * 32);
+  cfg.dynamicSmemBytes = (size_t)(smem + (a.gather ? a.chunk * a.d.g * 4 : 0));
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = grid.x; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, qcache_attn_kernel<DH, NHT, true>, a);
 }
 template <int DH>
-cudaError_t attn_dh(const QaArgs& a, cudaStream_t st) {
+cudaError_t attn_dh(const QaArgs& a, bool fused, cudaStream_t st) {
   const CcaDims& d = a.d;
   const int per = heads_per_cta(d);
   dim3 grid((unsigned)a.splits, (unsigned)(d.hk * ((d.g + per - 1) / per)), (unsigned)d.B);
   if constexpr (DH <= 128)
-    if (per == 16) return attn_run<DH, 2>(a, grid, st);
-  return attn_run<DH, 1>(a, grid, st);
+    if (per == 16) return attn_run<DH, 2>(a, grid, fused, st);
+  return attn_run<DH, 1>(a, grid, fused, st);
 }
 
 // ------------------------------------------------------------------------------------------------ eviction
@@ -697,26 +813,19 @@ CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-CCA_DEVINL uint32_t cluster_u32(const void* p, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-  return r;
-}
 CCA_DEVINL int cluster_load(const int* p, int rank) {
   int v;
-  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(cluster_u32(p, rank)) : "memory");
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(cluster_place(p, rank)) : "memory");
   return v;
 }
 CCA_DEVINL int2 cluster_load2(const int* p, int rank) {
   int2 v;
-  asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_u32(p, rank)) : "memory");
+  asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_place(p, rank)) : "memory");
   return v;
 }
 CCA_DEVINL void all_sync(int ranks) {                      // the CTAs that share a head
-  if (ranks == 1) { __syncthreads(); return; }
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (ranks == 1) __syncthreads();
+  else cluster_barrier();
 }
 
 // Exclusive sum over the 32 warps of a value that is the same in a warp's lanes; `total`: over all of them.
@@ -1054,13 +1163,16 @@ int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, b
   unsigned char* p = static_cast<unsigned char*>(workspace);
   a.part_o = reinterpret_cast<float*>(p); p += up256((size_t)d.B * d.hq * a.splits * d.dh * 4);
   a.part_ml = reinterpret_cast<float*>(p); p += up256((size_t)d.B * d.hq * a.splits * 2 * 4);
-  a.scores = accumulate ? reinterpret_cast<float*>(p) : nullptr;
+  a.scores = reinterpret_cast<float*>(p);
+  a.gather = accumulate != 0;
+  const bool fused = attn_fused(d, max_len, sm_count, a.gather, &a.chunk, &a.splits);
   cudaError_t e;
   if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
-  QC_BY_HEAD(attn_dh<DH>(a, st))
+  QC_BY_HEAD(attn_dh<DH>(a, fused, st))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   if (ev_end && (e = cudaEventRecord(ev_end, st)) != cudaSuccess) return -(int)e;
+  if (fused) return 0;
   int nx = d.g;                                            // a CTA per head at least
   const int by_rows = (max_len + 256 * QJ_ROWS - 1) / (256 * QJ_ROWS);
   if (accumulate && by_rows > nx) nx = by_rows;
