@@ -165,6 +165,9 @@ CCA_DEVINL void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "m
 template <int N>
 CCA_DEVINL void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+template <int V>
+struct Int { static constexpr int value = V; };
+
 // A warp's stage of the cache: SR rows' codes and scales as they lie in global memory.  Each warp copies its own (asynchronously,
 // 16 bytes a lane, whole lines) and reads it alone, so no barrier but the warp's own stands between them.
 template <int DH>
@@ -219,49 +222,62 @@ struct Rows {
   using S = Stage<DH>;
   uint32_t k[2][S::KW], v[4][R::NB * S::VW], ks[2][R::SW], vs[2][R::SW];
 
-  template <int NW>
-  CCA_DEVINL static void take(uint32_t* dst, const unsigned char* p) {
-    if constexpr (NW == 1) dst[0] = *reinterpret_cast<const uint32_t*>(p);
-    else if constexpr (NW == 2) {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
-      dst[0] = u.x; dst[1] = u.y;
+  // This lane's places in a stage, relative to its start: key row tile_row(g), value rows tile_row(2t) and tile_row(2t + 1), scale
+  // row tile_row(g).  Everything else lies at constant distances.
+  struct Places {
+    uint32_t k, v0, v1, s;
+    CCA_DEVINL Places(uint32_t stage, int g, int t)
+        : k(stage + S::K + tile_row(g) * R::CODES + t * 4 * R::NG), v0(stage + S::V + tile_row(2 * t) * R::CODES + g * S::VB),
+          v1(stage + S::V + tile_row(2 * t + 1) * R::CODES + g * S::VB), s(stage + S::KS + tile_row(g) * S::SB) {}
+  };
+  template <int NW, int OFF>
+  CCA_DEVINL static void take(uint32_t* w, uint32_t at) {
+    if constexpr (NW == 1) asm volatile("ld.shared.u32 %0, [%1+%2];" : "=r"(w[0]) : "r"(at), "n"(OFF));
+    else if constexpr (NW == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2+%3];" : "=r"(w[0]), "=r"(w[1]) : "r"(at), "n"(OFF));
+    else
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4+%5];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at), "n"(OFF));
+  }
+  // ROW: the 16 rows' number in the stage; r0: the first one's number in the sequence
+  template <int ROW>
+  CCA_DEVINL void read_keys(const Places& p, int r0, int last, const bf16* ksc, int g) {
+    take<R::NG, ROW * R::CODES>(k[0], p.k);
+    take<R::NG, (ROW + 8) * R::CODES>(k[1], p.k);
+    if constexpr (R::NB == 2) {
+      take<R::NG, ROW * R::CODES + R::BLK / 2>(k[0] + R::NG, p.k);
+      take<R::NG, (ROW + 8) * R::CODES + R::BLK / 2>(k[1] + R::NG, p.k);
+    }
+    if constexpr (DH == 32) single_scales(ks, r0, last, ksc, g);
+    else { take<R::SW, ROW * S::SB>(ks[0], p.s); take<R::SW, (ROW + 8) * S::SB>(ks[1], p.s); }
+  }
+  template <int OFF>
+  CCA_DEVINL static void take_v(uint32_t* w, uint32_t at) {
+    if constexpr (S::VB == 2) {
+      unsigned short h;
+      asm volatile("ld.shared.u16 %0, [%1+%2];" : "=h"(h) : "r"(at), "n"(OFF));
+      w[0] = h;
     } else {
-      const uint4 u = *reinterpret_cast<const uint4*>(p);
-      dst[0] = u.x; dst[1] = u.y; dst[2] = u.z; dst[3] = u.w;
+      take<S::VW, OFF>(w, at);
+      if constexpr (R::NB == 2) take<S::VW, OFF + R::BLK / 2>(w + S::VW, at);
     }
   }
-  // `st`: the first of the 16 rows' place in the stage, for codes; `row`: its number in the stage; r0: its number in the sequence
-  CCA_DEVINL void read_keys(const unsigned char* st, int row, int r0, int last, const bf16* ksc, int g, int t) {
-    const unsigned char* kp = st + S::K + (row + tile_row(g)) * R::CODES + t * 4 * R::NG;
-#pragma unroll
-    for (int hi = 0; hi < 2; ++hi) {
-#pragma unroll
-      for (int blk = 0; blk < R::NB; ++blk) take<R::NG>(k[hi] + blk * R::NG, kp + 8 * hi * R::CODES + blk * (R::BLK / 2));
-      read_scales(ks[hi], st + S::KS, row + 8 * hi + tile_row(g), ksc, min(r0 + 8 * hi + tile_row(g), last));
-    }
+  template <int ROW>
+  CCA_DEVINL void read_values(const Places& p, int r0, int last, const bf16* vsc, int g) {
+    take_v<ROW * R::CODES>(v[0], p.v0);                    // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
+    take_v<ROW * R::CODES>(v[1], p.v1);
+    take_v<(ROW + 8) * R::CODES>(v[2], p.v0);
+    take_v<(ROW + 8) * R::CODES>(v[3], p.v1);
+    if constexpr (DH == 32) single_scales(vs, r0, last, vsc, g);
+    else { take<R::SW, S::VS - S::KS + ROW * S::SB>(vs[0], p.s); take<R::SW, S::VS - S::KS + (ROW + 8) * S::SB>(vs[1], p.s); }
   }
-  CCA_DEVINL void read_values(const unsigned char* st, int row, int r0, int last, const bf16* vsc, int g, int t) {
+  CCA_DEVINL static void single_scales(uint32_t (&w)[2][R::SW], int r0, int last, const bf16* sc, int g) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                          // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
-      const unsigned char* vp = st + S::V + (row + 8 * (i >> 1) + tile_row(2 * t + (i & 1))) * R::CODES + g * S::VB;
-#pragma unroll
-      for (int blk = 0; blk < R::NB; ++blk) {
-        if constexpr (S::VB == 2) v[i][0] = *reinterpret_cast<const unsigned short*>(vp);
-        else take<S::VW>(v[i] + blk * S::VW, vp + blk * (R::BLK / 2));
-      }
-    }
-#pragma unroll
-    for (int hi = 0; hi < 2; ++hi)
-      read_scales(vs[hi], st + S::VS, row + 8 * hi + tile_row(g), vsc, min(r0 + 8 * hi + tile_row(g), last));
-  }
-  CCA_DEVINL static void read_scales(uint32_t (&w)[R::SW], const unsigned char* st, int row, const bf16* sc, int r) {
-    if constexpr (DH == 32) w[0] = *reinterpret_cast<const unsigned short*>(sc + r);
-    else take<R::SW>(w, st + row * S::SB);
+    for (int hi = 0; hi < 2; ++hi) w[hi][0] = *reinterpret_cast<const unsigned short*>(sc + min(r0 + 8 * hi + tile_row(g), last));
   }
 };
 
 constexpr int QA_WARPS = 4, QA_MAX_SPLITS = 128, QA_FIXED = 192;
-constexpr int QA_FUSED_SPLITS = 8, QA_FUSED_ROWS = 512, QA_FUSED_LOGITS = 32 * 1024;    // chunks, rows of one, bytes of its logits
+constexpr int QA_FUSED_SPLITS = 8, QA_FUSED_ROWS = 256, QA_FUSED_LOGITS = 32 * 1024;    // chunks, rows of one, bytes of its logits
 
 CCA_DEVINL uint32_t cluster_place(const void* p, int rank) {
   uint32_t r;
@@ -373,10 +389,12 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 
   const int last = r_end - 1, g8 = 8 * d.g;
   const bool even_heads = d.g % 2 == 0;
-  auto tile = [&](const unsigned char* st, int row, int r0) {
+  const bool put = sco != nullptr && 2 * t < nh;
+  auto tile = [&](const typename Rows<DH>::Places& at, int r0, float* sp, auto row_t, auto masked_t) {
+    constexpr int ROW = decltype(row_t)::value;
+    constexpr bool masked = decltype(masked_t)::value != 0;
     Rows<DH> cur;
-    cur.read_keys(st, row, r0, last, ksc, g, t);
-    const bool masked = r0 + 15 > last;
+    cur.template read_keys<ROW>(at, r0, last, ksc, g);
     // ---- logits (times log2 e) of rows tile_row(g), 8 + tile_row(g), heads 2t, 2t + 1
     float s[NHT][4];
 #pragma unroll
@@ -413,11 +431,10 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[ht][c] *= c_scale;
-    if (sco) {
-      float* sp = sco + (r_lo * d.g + 2 * t);
+    if (put) {
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht) {
-        const bool ok_lo = 8 * ht + 2 * t < nh && (!masked || r_lo <= last), ok_hi = ok_lo && (!masked || r_hi <= last);
+        const bool ok_lo = (ht == 0 || 8 * ht + 2 * t < nh) && (!masked || r_lo <= last), ok_hi = ok_lo && (!masked || r_hi <= last);
         if (even_heads) {
           if (ok_lo) *reinterpret_cast<float2*>(sp + 8 * ht) = make_float2(s[ht][0], s[ht][1]);
           if (ok_hi) *reinterpret_cast<float2*>(sp + 8 * ht + g8) = make_float2(s[ht][2], s[ht][3]);
@@ -428,7 +445,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         }
       }
     }
-    if (masked) {
+    if constexpr (masked) {
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
@@ -465,7 +482,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         sum[ht][c & 1] += s[ht][c];
       }
     // ---- O^T += V^T P^T
-    cur.read_values(st, row, r0, last, vsc, g, t);
+    cur.template read_values<ROW>(at, r0, last, vsc, g);
 #pragma unroll
     for (int gi = 0; gi < R::NB * R::NG; ++gi) {
       const float s_lo = scale_at(cur.vs[0], gi), s_hi = scale_at(cur.vs[1], gi);
@@ -493,7 +510,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   int r0 = r_begin + warp * S::SR, slot = 0;
   int ahead = r0;                                          // first row of the next stage to be filled
   auto fill_next = [&](int into) {
-    const uint32_t dst = mine_u32 + into * S::BYTES;
+    const uint32_t dst = mine_u32 + into;
     const uint32_t at = (uint32_t)ahead * R::CODES + lane * 16, sat = (uint32_t)(ahead + lane) * R::SCALES;   // 2^31 bytes at most
     if (ahead + S::SR <= r_end) S::fill(dst, kc + at, vc + at, ksc + sat, vsc + sat, lane);
     else if (ahead < r_end) S::fill_part(dst, kc + at, vc + at, ksc + sat, vsc + sat, lane, r_end - ahead);
@@ -501,19 +518,27 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
     ahead += STEP;
   };
 #pragma unroll
-  for (int i = 0; i < S::N; ++i) fill_next(i);
+  for (int i = 0; i < S::N; ++i) fill_next(i * S::BYTES);
+  static_assert(S::N == 2, "the stages' places alternate");
   __syncthreads();                                         // the query operand
+  float* sp = sco + (r0 + tile_row(g)) * d.g + 2 * t;
+  const int g16 = 16 * d.g;
   for (; r0 < r_end; r0 += STEP) {
     cp_async_wait<S::N - 1>();
     __syncwarp();
-#pragma unroll
-    for (int half = 0; half < S::SR / 16; ++half) {
-      if (half > 0 && r0 + half * 16 > last) break;
-      tile(mine + slot * S::BYTES, half * 16, r0 + half * 16);
+    const typename Rows<DH>::Places at(mine_u32 + slot, g, t);
+    if (r0 + S::SR <= r_end) {
+      tile(at, r0, sp, Int<0>{}, Int<0>{});
+      if constexpr (S::SR == 32) tile(at, r0 + 16, sp + g16, Int<16>{}, Int<0>{});
+    } else {
+      tile(at, r0, sp, Int<0>{}, Int<1>{});
+      if constexpr (S::SR == 32)
+        if (r0 + 16 < r_end) tile(at, r0 + 16, sp + g16, Int<16>{}, Int<1>{});
     }
     __syncwarp();
     fill_next(slot);
-    slot = slot + 1 == S::N ? 0 : slot + 1;
+    slot ^= S::BYTES;
+    sp += STEP * d.g;
   }
   cp_async_wait<0>();
 #pragma unroll
@@ -725,16 +750,17 @@ void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* spl
   }
 }
 
-// One launch does where 8 chunks of 512 rows hold the sequence (what a longer chunk takes more is then less than the second launch:
-// 1 x 1024 rows FUSED_NEW us instead of FUSED_OLD, 1 x 4096 FUSED4_NEW instead of FUSED4_OLD), one CTA has all of a kv head's query
-// heads, and a chunk's logits find room.  Chunks of 128 rows: a stage for each warp.
-bool attn_fused(const CcaDims& d, int max_len, int sm_count, int gather, int* chunk, int* splits) {
+// One launch does where 8 chunks hold the sequence that have no more rows than 256 or than the plan above gives a chunk (d_h 128, h_q 8,
+// h_k 2, in a graph: 1 x 1024 rows 5.1 us against 6.2 in two launches, 1 x 2048 6.3 against 6.0, 1 x 4096 8.4 against 6.5, 32 x 4096
+// 16.9 against 18.3; called one by one, 5.7 against 8.5 us of host time), one CTA has all of a kv head's query heads, and a chunk's logits
+// find room.  Chunks of 128 rows: a stage for each warp.
+bool attn_fused(const CcaDims& d, int max_len, int sm_count, int gather, int plan_chunk, int* chunk, int* splits) {
   if (d.g > heads_per_cta(d)) return false;
   const long long base = (long long)d.B * d.hk, resident = (long long)sm_count * qa_resident(d.dh, heads_per_cta(d) / 8);
   long long best = -1;
   for (int n = 1; n <= QA_FUSED_SPLITS; n *= 2) {
     const int ch = ((max_len + n - 1) / n + 127) / 128 * 128;
-    if (ch > QA_FUSED_ROWS || (gather && ch * d.g * 4 > QA_FUSED_LOGITS)) continue;
+    if ((ch > QA_FUSED_ROWS && ch > plan_chunk) || (gather && ch * d.g * 4 > QA_FUSED_LOGITS)) continue;
     const long long cost = (base * n + resident - 1) / resident * (ch + QA_FIXED);
     if (best < 0 || cost < best) { best = cost; *chunk = ch; *splits = n; }
   }
@@ -1165,7 +1191,7 @@ int launch_qcache_attention(const CcaDims& d, const bf16* q, const float* q32, b
   a.part_ml = reinterpret_cast<float*>(p); p += up256((size_t)d.B * d.hq * a.splits * 2 * 4);
   a.scores = reinterpret_cast<float*>(p);
   a.gather = accumulate != 0;
-  const bool fused = attn_fused(d, max_len, sm_count, a.gather, &a.chunk, &a.splits);
+  const bool fused = attn_fused(d, max_len, sm_count, a.gather, a.chunk, &a.chunk, &a.splits);
   cudaError_t e;
   if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
   QC_BY_HEAD(attn_dh<DH>(a, fused, st))
