@@ -825,10 +825,8 @@ struct EvArgs {
   int* status;
 };
 
-#ifndef EV_RANK_ROWS
-#define EV_RANK_ROWS 16384
-#endif
-constexpr int EV_THREADS = 1024, EV_BINS = 2048, EV_RANK = EV_RANK_ROWS;
+constexpr int EV_SMEM_ROWS = 49152;                        // 192 KB of keys in shared memory
+constexpr int EV_THREADS = 1024, EV_BINS = 2048, EV_RANK = 16384;
 
 // The order of eviction as an unsigned number, larger = kept: 0xffffffff for the newest, else the weight's order (a NaN is lowest).
 CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
@@ -870,44 +868,38 @@ CCA_DEVINL int warp_offsets(int v, int* sm, int warp, int lane, int& total) {
   return __shfl_sync(0xffffffffu, inc - x, warp);
 }
 
-// Moves the listed rows of one head: DH / 16 lanes take the 16-byte pieces of a row's codes (and as many scales), four rows a
-// thread at a time.  A destination is below `keep` and a source is not, so the moves need no order.
+// Moves the listed rows of one head: DH / 16 lanes take the 16-byte pieces of a row's codes (and as many scales); the
+// next row's numbers are asked for meanwhile.  A destination is below `keep` and a source is not, so the moves
+// need no order.  Bound by scattered reads and writes of rows and
+// of their few bytes of scales, weight and position, each of which moves a 32-byte sector (one to four rows a thread, 6 to 48 CTAs per
+// SM: all within 5 %).
 template <int DH, int THREADS>
 CCA_DEVINL void move_rows(const EvArgs& a, size_t base, const int* src, const int* dst, int moves, int part, int parts) {
   using R = Row<DH>;
-  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = THREADS / LANES, U = 4;
+  constexpr int PIECES = R::CODES / 16, LANES = 2 * PIECES, ROWS = THREADS / LANES;
   const int l = threadIdx.x % LANES, piece = l % PIECES;
-  uint8_t* codes = (l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES;
-  bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES;
-  for (int i0 = part * ROWS * U + threadIdx.x / LANES; i0 < moves; i0 += parts * ROWS * U) {
-    size_t from[U], to[U];
-    uint4 u[U];
-    bf16 s[U];
-    float wt[U];
-    int ps[U];
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) { from[x] = (size_t)src[i0 + x * ROWS]; to[x] = (size_t)dst[i0 + x * ROWS]; }
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) {
-        u[x] = __ldcs(reinterpret_cast<const uint4*>(codes + from[x] * R::CODES) + piece);
-        s[x] = scales[from[x] * R::SCALES + piece];
-        if (l == 0) wt[x] = a.c.weight[base + from[x]];
-        if (l == PIECES) ps[x] = a.c.position[base + from[x]];
-      }
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (i0 + x * ROWS < moves) {
-        reinterpret_cast<uint4*>(codes + to[x] * R::CODES)[piece] = u[x];
-        scales[to[x] * R::SCALES + piece] = s[x];
-        if (l == 0) a.c.weight[base + to[x]] = wt[x];
-        if (l == PIECES) a.c.position[base + to[x]] = ps[x];
-      }
+  uint4* codes = reinterpret_cast<uint4*>((l < PIECES ? a.c.k_codes : a.c.v_codes) + base * R::CODES) + piece;
+  bf16* scales = (l < PIECES ? a.c.k_scales : a.c.v_scales) + base * R::SCALES + piece;
+  // lane 0 of a row also moves its weight, lane PIECES its position
+  int* extra = l == 0 ? reinterpret_cast<int*>(a.c.weight + base) : l == PIECES ? a.c.position + base : nullptr;
+  const int step = parts * ROWS;
+  int i = part * ROWS + threadIdx.x / LANES;
+  uint32_t from = 0, to = 0;
+  if (i < moves) { from = (uint32_t)src[i]; to = (uint32_t)dst[i]; }
+  for (; i < moves; i += step) {
+    const uint4 u = __ldcs(codes + from * (uint32_t)PIECES);           // a head's rows: 2^27 pieces at most
+    const bf16 s = scales[from * (uint32_t)R::SCALES];
+    int e = 0;
+    if (extra) e = extra[from];
+    const uint32_t here = to;
+    if (i + step < moves) { from = (uint32_t)src[i + step]; to = (uint32_t)dst[i + step]; }
+    codes[here * (uint32_t)PIECES] = u;
+    scales[here * (uint32_t)R::SCALES] = s;
+    if (extra) extra[here] = e;
   }
 }
 template <int DH>
-__global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
+__global__ void __launch_bounds__(256, 8) qcache_move_kernel(EvArgs a) {
   pdl_enter();
   const int bj = blockIdx.z * a.hk + blockIdx.y;
   const int* dst = a.list + (size_t)bj * 2 * a.cap;
@@ -921,7 +913,7 @@ __global__ void __launch_bounds__(256) qcache_move_kernel(EvArgs a) {
 // read weight and position again (from L2).  A destination is below `keep` and a source is not, so the moves need no order.
 // Its time is latency (barriers, one pass after the other) where little moves, else the rows' traffic.
 template <int DH, bool IN_SMEM>
-__global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
+__global__ void __launch_bounds__(EV_THREADS, 1) qcache_evict_kernel(EvArgs a) {
   pdl_enter();
   using R = Row<DH>;
   extern __shared__ uint32_t keys[];
@@ -1055,45 +1047,78 @@ __global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
       }
       eq0 = place(eq, 0);
     }
-    int go0 = 0, come0 = 0;
     const unsigned below = (1u << lane) - 1u;
+    int e = eq0;
+    auto stays_of = [&](int r0) {                          // of rows r0 .. r0 + 31, as a mask; called for a warp's rows in order
+      const int r = r0 + lane;
+      const uint32_t k = r < r_end ? key_of(r) : 0u;
+      bool stays = k > lowest;
+      if (equal <= left) return __ballot_sync(0xffffffffu, r < r_end && (stays || k == lowest));
+      const unsigned beq = __ballot_sync(0xffffffffu, r < r_end && k == lowest);
+      stays = stays || (k == lowest && e + __popc(beq & below) < left);
+      e += __popc(beq);
+      return __ballot_sync(0xffffffffu, r < r_end && stays);
+    };
+    // 32 times 32 rows at a time: lane i keeps the mask of the i-th 32, and from it the masks of those that go and that come
+    unsigned mgo, mco;
+    auto masks = [&](int s0) {
+      unsigned st = 0;
+      const int chunks = min(32, (r_end - s0 + 31) >> 5);
+#pragma unroll 4
+      for (int i = 0; i < chunks; ++i) {
+        const unsigned m = stays_of(s0 + 32 * i);
+        if (lane == i) st = m;
+      }
+      const int r0 = s0 + 32 * lane, head = a.keep - r0, there = r_end - r0;
+      const unsigned below_keep = head >= 32 ? 0xffffffffu : head <= 0 ? 0u : (1u << head) - 1u;
+      const unsigned rows = there >= 32 ? 0xffffffffu : there <= 0 ? 0u : (1u << there) - 1u;
+      mgo = rows & below_keep & ~st;
+      mco = ~below_keep & st;
+    };
+    int go = 0, come = 0;
+    for (int s0 = r_begin; s0 < r_end; s0 += 1024) {
+      masks(s0);
+      go += __popc(mgo); come += __popc(mco);
+    }
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {                 // count, then write
-      int e = eq0, go = 0, come = 0;
-      for (int r0 = r_begin; r0 < r_end; r0 += 32) {
-        const int r = r0 + lane;
-        const uint32_t k = r < r_end ? key_of(r) : 0u;
-        bool stays = k > lowest;
-        if (equal <= left) stays = stays || k == lowest;
-        else {
-          const unsigned beq = __ballot_sync(0xffffffffu, r < r_end && k == lowest);
-          stays = stays || (k == lowest && e + __popc(beq & below) < left);
-          e += __popc(beq);
-        }
-        const unsigned bgo = __ballot_sync(0xffffffffu, r < r_end && r < a.keep && !stays);
-        const unsigned bco = __ballot_sync(0xffffffffu, r < r_end && r >= a.keep && stays);
-        if (pass == 1) {
-          if (bgo >> lane & 1u) dst[go0 + go + __popc(bgo & below)] = r;
-          if (bco >> lane & 1u) src[come0 + come + __popc(bco & below)] = r;
-        }
-        go += __popc(bgo); come += __popc(bco);
+    for (int s = 16; s > 0; s >>= 1) {
+      go += __shfl_xor_sync(0xffffffffu, go, s);
+      come += __shfl_xor_sync(0xffffffffu, come, s);
+    }
+    int tg, tc;
+    int go0 = warp_offsets(go, sm, warp, lane, tg), come0 = warp_offsets(come, sm, warp, lane, tc);
+    moves = tg;
+    if (ranks > 1) {
+      if (tid == 0) { mine[1] = tg; mine[2] = tc; }
+      all_sync(ranks);
+      moves = 0;
+      for (int x = 0; x < ranks; ++x) {
+        const int xg = cluster_load(&mine[1], x), xc = cluster_load(&mine[2], x);
+        moves += xg;
+        if (x < rank) { go0 += xg; come0 += xc; }
       }
-      if (pass == 0) {
-        int tg, tc;
-        go0 = warp_offsets(go, sm, warp, lane, tg);
-        come0 = warp_offsets(come, sm, warp, lane, tc);
-        moves = tg;
-        if (ranks > 1) {
-          if (tid == 0) { mine[1] = tg; mine[2] = tc; }
-          all_sync(ranks);
-          moves = 0;
-          for (int x = 0; x < ranks; ++x) {
-            const int xg = cluster_load(&mine[1], x), xc = cluster_load(&mine[2], x);
-            moves += xg;
-            if (x < rank) { go0 += xg; come0 += xc; }
-          }
-        }
+    }
+    e = eq0;
+    for (int s0 = r_begin; s0 < r_end; s0 += 1024) {
+      if (s0 > r_begin || r_end - r_begin > 1024) masks(s0);           // else they are still there
+      const int both = __popc(mgo) | (__popc(mco) << 16);
+      int inc = both;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, s);
+        if (lane >= s) inc += y;
       }
+      const int at = inc - both;
+      const int chunks = min(32, (r_end - s0 + 31) >> 5);
+#pragma unroll 4
+      for (int i = 0; i < chunks; ++i) {
+        const unsigned g = __shfl_sync(0xffffffffu, mgo, i), c = __shfl_sync(0xffffffffu, mco, i);
+        const int p = __shfl_sync(0xffffffffu, at, i), r = s0 + 32 * i + lane;
+        if (g >> lane & 1u) dst[go0 + (p & 0xffff) + __popc(g & below)] = r;
+        if (c >> lane & 1u) src[come0 + (p >> 16) + __popc(c & below)] = r;
+      }
+      const int all = __shfl_sync(0xffffffffu, inc, 31);
+      go0 += all & 0xffff; come0 += all >> 16;
     }
     all_sync(ranks);                                       // the lists are whole, and nobody reads weights or positions any more
   }
@@ -1118,7 +1143,6 @@ __global__ void __launch_bounds__(EV_THREADS) qcache_evict_kernel(EvArgs a) {
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-constexpr int EV_SMEM_ROWS = 49152;                        // 192 KB of keys
 
 }  // namespace
 
@@ -1255,7 +1279,11 @@ int launch_qcache_evict(const CcaDims& d, const QCache& c, int keep, int recent,
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   if (a.move_here) return 0;
-  int nx = (most * (d.dh / 16) + 1023) / 1024;
+  // up to four full waves of CTAs over all heads (fewer rows a CTA hide less of what each waits for), none without a turn of its loop
+  const int rows = 256 / (d.dh / 16);
+  int nx = (most + rows - 1) / rows;
+  const int per_head = (int)((32LL * sm_count + (long long)d.B * d.hk - 1) / ((long long)d.B * d.hk));
+  if (nx > per_head) nx = per_head;
   QC_BY_HEAD((launch_pdl(qcache_move_kernel<DH>, dim3((unsigned)nx, (unsigned)d.hk, (unsigned)d.B), dim3(256), st, a)))
   if (e != cudaSuccess) return -(int)e;
   ++*launches;

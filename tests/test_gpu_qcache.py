@@ -421,6 +421,18 @@ def test_evict_of_a_cache_beyond_the_shared_memory():
     cca.close()
 
 
+def test_evict_of_long_caches_of_a_full_batch():
+    """More heads than the chip has room for clusters, and more rows than a CTA has shared memory for keys."""
+    cca = _cca(1, 1, 32)
+    B, S = 150, 50011
+    cache = _random_cache(cca, B, S, 9)
+    cache["weight"][7] = cache["weight"][7].round()          # many equal ones
+    lens = [10 + b for b in range(B)]
+    lens[7], lens[149], lens[60] = S, S - 1, 48000          # CTAs' warps take more than 1024 rows each
+    assert _check_evict(cca, cache, lens, 30000, 700, [S] * B) > 0
+    cca.close()
+
+
 def test_evict_odd_weights():
     """Equal weights (the lower row stays), zeros of both signs, NaN, infinities, negative ones."""
     cca = _cca(2, 2, 64)
