@@ -211,13 +211,14 @@ int cca_init(const cca_config* cfg, int device, cca_handle** out) {
   *out = nullptr;
   int v = validate_config(cfg);
   if (v != CCA_OK) return v;
-  cudaDeviceProp prop;
-  prop.multiProcessorCount = 0;
+  int sm_count = 0, major = 0;      // single attributes: the whole property struct takes milliseconds
   if (device >= 0) {
     int ndev = 0;
     if (cudaGetDeviceCount(&ndev) != cudaSuccess || device >= ndev) return CCA_ERR_CUDA;
-    if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) return CCA_ERR_CUDA;
-    if (prop.major != 10) return CCA_ERR_UNSUPPORTED;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+      return CCA_ERR_CUDA;
+    if (major != 10) return CCA_ERR_UNSUPPORTED;
     if (cudaSetDevice(device) != cudaSuccess) return CCA_ERR_CUDA;
   } else if (device != -1) {
     return CCA_ERR_INVALID_ARG;
@@ -227,7 +228,7 @@ int cca_init(const cca_config* cfg, int device, cca_handle** out) {
   h->cfg = *cfg;
   h->device = device;
   h->impl = 1;
-  h->sm_count = prop.multiProcessorCount;
+  h->sm_count = sm_count;
   h->last_cuda = 0;
   h->launches = 0;
   h->d_status = nullptr;
