@@ -1303,7 +1303,7 @@ int cca_qlinear(cca_handle* h, const cca_qlinear_weights* w, const void* x, void
   else a.out_bf16 = (bf16*)out;
   OnDevice on;
   CU(on.enter(h->device));
-  return enqueued(h, launch_qlinear(a, h->impl >= 1 ? h->tc : nullptr, h->sm_count, h->d_status, &h->launches, (cudaStream_t)cuda_stream));
+  return enqueued(h, launch_qlinear(a, h->impl >= 1 ? h->tc : nullptr, h->d_status, &h->launches, (cudaStream_t)cuda_stream));
 }
 
 int cca_decode_workspace_size_q(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {

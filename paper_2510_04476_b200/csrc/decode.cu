@@ -750,7 +750,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   pa.seg[0] = QLinSeg{w.qkv1_codes, w.qkv1_scales, x, d.L + d.Lk / 2, 0};
   pa.seg[1] = QLinSeg{w.v2_codes, w.v2_scales, (d.flags & F_V_SHIFT) ? x_prev : x, d.Lk / 2, d.L + d.Lk / 2};
   pa.K = d.E; pa.M = d.B; pa.out_f32 = lat; pa.ldo = d.L + d.Lk;
-  if ((r = launch_qlinear(pa, tc, sm_count, status, launches, st)) != 0) return r;
+  if ((r = launch_qlinear(pa, tc, status, launches, st)) != 0) return r;
   const int kc = (d.flags & F_CONV2) ? d.k_ch : 1;
   C1Args c1;
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = v_new; c1.hist = hist; c1.x_prev = x_prev;
@@ -781,5 +781,5 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   pb.n_seg = 1;
   pb.seg[0] = QLinSeg{w.o_codes, w.o_scales, o, d.E, 0};
   pb.K = d.Lq; pb.M = d.B; pb.out_bf16 = out; pb.ldo = d.E;
-  return launch_qlinear(pb, tc, sm_count, status, launches, st);
+  return launch_qlinear(pb, tc, status, launches, st);
 }

@@ -41,24 +41,26 @@ __global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
   }
 }
 
-// 16 MT weight rows per CTA, 8 NT tokens, the inner dimension split over the 8 warps and summed through shared memory in a fixed
+// 16 weight rows per CTA, 8 NT tokens, the inner dimension split over the 8 warps and summed through shared memory in a fixed
 // order.  A lane's 16 bytes of a weight row are 8 channels of each of 4 groups: two instructions per group, whose sum is multiplied
 // by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.
-template <int NT, int MT>
-__global__ void __launch_bounds__(QL_WARPS * 32) qlinear_kernel(QLinArgs a) {
+// At few tokens it is bound by the 200 instructions that a block of 16 rows by 128 columns takes, and what hides their latency is
+// warps: four CTAs per SM with one block of each warp on its way take 18.4 us for 5 x 16383 x 8192 (75 MB: 64 % of the measured copy
+// rate), three with two or three 20.1 to 21.2, two with four 21.1; rings of asynchronous copies under CTAs that stay (16 or 32 warps, x in
+// registers or in shared memory, one row tile or two) 22.6 to 24.3.
+template <int NT>
+__global__ void __launch_bounds__(QL_WARPS * 32, NT == 1 ? 4 : 1) qlinear_kernel(QLinArgs a) {
   pdl_enter();
-  constexpr int UNR = MT == 1 ? 4 : 2;                     // blocks of 128 columns on their way at a time
-  __shared__ float red[QL_WARPS][16 * MT][NT * 8 + 1];
+  __shared__ float red[QL_WARPS][16][NT * 8 + 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int tok0 = blockIdx.y * (NT * 8);
   const int k128 = (a.K + 127) / 128;
-  int tile = blockIdx.x * MT;
+  int tile = blockIdx.x;
   QLinSeg sg = a.seg[0];
-  if (a.n_seg > 1) {                                       // a CTA's tiles are of one segment: their number is rounded up to MT
-    const int t0 = ((a.seg[0].N + 15) / 16 + MT - 1) / MT * MT;
+  if (a.n_seg > 1) {
+    const int t0 = (a.seg[0].N + 15) / 16;
     if (tile >= t0) { sg = a.seg[1]; tile -= t0; }
   }
-  const int n16 = (sg.N + 15) / 16;
   const uint8_t* codes = sg.codes + (size_t)tile * k128 * 1024 + lane * 16;
   const bf16* scales = sg.scales + (size_t)tile * k128 * 64 + g * 4;
   bool ok_tok[NT];
@@ -69,76 +71,48 @@ __global__ void __launch_bounds__(QL_WARPS * 32) qlinear_kernel(QLinArgs a) {
     ok_tok[nt] = tok < a.M;
     xp[nt] = sg.X + (size_t)(ok_tok[nt] ? tok : 0) * a.K + t * 8;
   }
-  float acc[MT][NT][4];
+  float acc[NT][4];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int c = 0; c < 4; ++c) acc[nt][c] = 0.f;
+  for (int kb = warp; kb < k128; kb += QL_WARPS) {
+    uint32_t wl[4], wh[4], sl[2], sh[2];
+    load_words<4>(wl, codes + (size_t)kb * 1024);
+    load_words<4>(wh, codes + (size_t)kb * 1024 + 512);
+    load_words<2>(sl, scales + (size_t)kb * 64);
+    load_words<2>(sh, scales + (size_t)kb * 64 + 32);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[mt][nt][c] = 0.f;
-  for (int kb0 = warp; kb0 < k128; kb0 += QL_WARPS * UNR) {
-    uint32_t wl[UNR][MT][4], wh[UNR][MT][4], sl[UNR][MT][2], sh[UNR][MT][2];
+    for (int gi = 0; gi < 4; ++gi) {
+      const int col = kb * 128 + gi * GROUP;
+      uint32_t ka[2][4];
 #pragma unroll
-    for (int u = 0; u < UNR; ++u) {
-      const int kb = kb0 + u * QL_WARPS;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        zero_words(wl[u][mt]); zero_words(wh[u][mt]); zero_words(sl[u][mt]); zero_words(sh[u][mt]);
-        if (kb < k128 && (MT == 1 || tile + mt < n16)) {
-          const size_t at = (size_t)mt * k128 + kb;
-          load_words<4>(wl[u][mt], codes + at * 1024);
-          load_words<4>(wh[u][mt], codes + at * 1024 + 512);
-          load_words<2>(sl[u][mt], scales + at * 64);
-          load_words<2>(sh[u][mt], scales + at * 64 + 32);
-        }
+      for (int c = 0; c < 2; ++c) {
+        const int byte = c * 8 + gi * 2;
+        const uint32_t sel = (byte & 2) ? 0x3322u : 0x1100u;
+        const uint32_t p0 = __byte_perm(wl[byte / 4], 0, sel), p1 = __byte_perm(wh[byte / 4], 0, sel);
+        ka[c][0] = code_e0(p0); ka[c][1] = code_e0(p1); ka[c][2] = code_e1(p0); ka[c][3] = code_e1(p1);
       }
-    }
+      const float s_lo = scale_at(sl, gi), s_hi = scale_at(sh, gi);
 #pragma unroll
-    for (int u = 0; u < UNR; ++u) {
-      const int kb = kb0 + u * QL_WARPS;
-      if (kb >= k128) break;
-#pragma unroll
-      for (int gi = 0; gi < 4; ++gi) {
-        const int col = kb * 128 + gi * GROUP;
-        uint32_t ka[MT][2][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int byte = c * 8 + gi * 2;
-            const uint32_t sel = (byte & 2) ? 0x3322u : 0x1100u;
-            const uint32_t p0 = __byte_perm(wl[u][mt][byte / 4], 0, sel), p1 = __byte_perm(wh[u][mt][byte / 4], 0, sel);
-            ka[mt][c][0] = code_e0(p0); ka[mt][c][1] = code_e0(p1); ka[mt][c][2] = code_e1(p0); ka[mt][c][3] = code_e1(p1);
-          }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          uint4 xv = make_uint4(0, 0, 0, 0);
-          if (ok_tok[nt] && col < a.K) xv = __ldg(reinterpret_cast<const uint4*>(xp[nt] + col));
-          xv.x = mul_bf16x2(xv.x, MUL_E0); xv.y = mul_bf16x2(xv.y, MUL_E1);
-          xv.z = mul_bf16x2(xv.z, MUL_E0); xv.w = mul_bf16x2(xv.w, MUL_E1);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            float part[4];
-            mma_16816_zero(part, ka[mt][0], xv.x, xv.y);
-            mma_16816(part, ka[mt][1], xv.z, xv.w);
-            const float s_lo = scale_at(sl[u][mt], gi), s_hi = scale_at(sh[u][mt], gi);
-            float (&ac)[4] = acc[mt][nt];
-            ac[0] = fmaf(s_lo, part[0], ac[0]); ac[1] = fmaf(s_lo, part[1], ac[1]);
-            ac[2] = fmaf(s_hi, part[2], ac[2]); ac[3] = fmaf(s_hi, part[3], ac[3]);
-          }
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        uint4 xv = make_uint4(0, 0, 0, 0);
+        if (ok_tok[nt] && col < a.K) xv = __ldg(reinterpret_cast<const uint4*>(xp[nt] + col));
+        float part[4];
+        mma_16816_zero(part, ka[0], mul_bf16x2(xv.x, MUL_E0), mul_bf16x2(xv.y, MUL_E1));
+        mma_16816(part, ka[1], mul_bf16x2(xv.z, MUL_E0), mul_bf16x2(xv.w, MUL_E1));
+        acc[nt][0] = fmaf(s_lo, part[0], acc[nt][0]); acc[nt][1] = fmaf(s_lo, part[1], acc[nt][1]);
+        acc[nt][2] = fmaf(s_hi, part[2], acc[nt][2]); acc[nt][3] = fmaf(s_hi, part[3], acc[nt][3]);
       }
     }
   }
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) red[warp][mt * 16 + g + 8 * (c >> 1)][nt * 8 + 2 * t + (c & 1)] = acc[mt][nt][c];
+    for (int c = 0; c < 4; ++c) red[warp][g + 8 * (c >> 1)][nt * 8 + 2 * t + (c & 1)] = acc[nt][c];
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * MT * NT * 8; i += QL_WARPS * 32) {
-    const int row = i % (16 * MT), tok = i / (16 * MT);
+  for (int i = threadIdx.x; i < 16 * NT * 8; i += QL_WARPS * 32) {
+    const int row = i % 16, tok = i / 16;
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < QL_WARPS; ++w) v += red[w][row][tok];
@@ -152,11 +126,11 @@ __global__ void __launch_bounds__(QL_WARPS * 32) qlinear_kernel(QLinArgs a) {
   }
 }
 
-template <int NT, int MT>
+template <int NT>
 cudaError_t run_nt(const QLinArgs& a, cudaStream_t st) {
-  int ctas = 0;
-  for (int s = 0; s < a.n_seg; ++s) ctas += ((a.seg[s].N + 15) / 16 + MT - 1) / MT;
-  return launch_pdl(qlinear_kernel<NT, MT>, dim3((unsigned)ctas, (unsigned)((a.M + NT * 8 - 1) / (NT * 8))), dim3(QL_WARPS * 32), st, a);
+  int tiles = 0;
+  for (int s = 0; s < a.n_seg; ++s) tiles += (a.seg[s].N + 15) / 16;
+  return launch_pdl(qlinear_kernel<NT>, dim3((unsigned)tiles, (unsigned)((a.M + NT * 8 - 1) / (NT * 8))), dim3(QL_WARPS * 32), st, a);
 }
 
 }  // namespace
@@ -174,19 +148,15 @@ int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int 
   return 0;
 }
 
-int launch_qlinear(const QLinArgs& a, TcState* tc, int sm_count, int* status, long long* launches, cudaStream_t st) {
+int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st) {
+  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.6 us against 7.7, 64 x 8192 x 8192: 22.7
+  // against 95.6), unless the handle has the tensor-core kernels switched off
   if (tc && a.M > 8) {
     const int r = tc_qlinear(tc, a, status, st);
     if (r < 0) return r;
     if (r == 0) { ++*launches; return 0; }
   }
-  int tiles = 0;
-  for (int s = 0; s < a.n_seg; ++s) tiles += (a.seg[s].N + 15) / 16;
-  cudaError_t e;
-  if (a.M <= 8) e = tiles >= 4 * sm_count ? run_nt<1, 2>(a, st) : run_nt<1, 1>(a, st);
-  else if (a.M <= 16) e = run_nt<2, 1>(a, st);
-  else if (a.M <= 32) e = run_nt<4, 1>(a, st);
-  else e = run_nt<8, 1>(a, st);
+  const cudaError_t e = a.M <= 8 ? run_nt<1>(a, st) : run_nt<4>(a, st);
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;

@@ -23,5 +23,5 @@ size_t qlinear_code_bytes(long long N, long long K);
 size_t qlinear_scale_bytes(long long N, long long K);
 int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int K, long long* launches, cudaStream_t st);
 // tc: the handle's tensor-map state, or null (then only the warp-level kernel is used)
-int launch_qlinear(const QLinArgs& a, TcState* tc, int sm_count, int* status, long long* launches, cudaStream_t st);
+int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st);
 int tc_qlinear(TcState* tc, const QLinArgs& a, int* status, cudaStream_t st);     // tc_qlinear.cu

@@ -71,12 +71,36 @@ def test_product_of_a_layer(cca, M, N, K):
     assert torch.equal(y, cca.qlinear(packed, x.cuda(), out_dtype=torch.float32))
 
 
+@pytest.mark.parametrize("M", [1, 5, 8, 9])
+@pytest.mark.parametrize("N,K", [(9473, 32), (9500, 160), (9487, 1024), (10001, 2080), (9600, 3136), (9472, 5120), (9473, 8192), (9473, 8224)])
+def test_product_of_many_rows(cca, M, N, K):
+    """Many rows and long inner dimensions, ragged ends."""
+    w, gen = _weights(N, K, N + K)
+    packed = cca.qlinear_pack(w.cuda())
+    x = torch.randn(M, K, generator=gen).bfloat16()
+    w64 = Q.values(*Q.quantise(w))
+    for dtype in (torch.float32, torch.bfloat16):
+        _check(cca.qlinear(packed, x.cuda(), out_dtype=dtype), x, w64, K)
+
+
 @pytest.mark.parametrize("scale", [1e-12, 1e12])
 def test_product_of_small_and_large_inputs(cca, scale):
     w, gen = _weights(64, 512, 6)
     packed = cca.qlinear_pack(w.cuda())
     x = (scale * torch.randn(3, 512, generator=gen)).bfloat16()
     _check(cca.qlinear(packed, x.cuda(), out_dtype=torch.float32), x, Q.values(*Q.quantise(w)), 512)
+
+
+@pytest.mark.parametrize("M", [3, 9, 40])
+def test_product_without_the_tensor_core_kernels(cca, M):
+    w, gen = _weights(100, 1056, 8)
+    packed = cca.qlinear_pack(w.cuda())
+    x = torch.randn(M, 1056, generator=gen).bfloat16()
+    before = cca.set_impl(0)
+    try:
+        _check(cca.qlinear(packed, x.cuda(), out_dtype=torch.float32), x, Q.values(*Q.quantise(w)), 1056)
+    finally:
+        cca.set_impl(before)
 
 
 def test_a_nan_input_touches_its_own_token_alone(cca):
@@ -158,6 +182,7 @@ STEPS = [
     S_("q_no_shift", 2, 5, 512, 8, 2, 64, flags=63 & ~8),
     S_("q_no_conv2", 2, 5, 512, 8, 2, 64, flags=63 & ~2),
     S_("q_batch_over_32", 37, 4, 256, 4, 2, 64),
+    S_("q_wide", 2, 3, 4096, 32, 32, 128),
 ]
 
 
