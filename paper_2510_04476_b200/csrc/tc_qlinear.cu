@@ -5,12 +5,14 @@
 //   warps 2..13  : three groups of four, a thread per weight row: a block of 128 channels from its 64 bytes of codes into tensor
 //                  memory, as the MMA's A operand; the groups take the blocks in turn
 //
-// A weight c * s has up to 11 significant bits, which one bf16 operand cannot hold.  It becomes two: hi = bf16(c * s) by
-// a product and lo = c * s - hi by one fused multiply-add, both exact, so that the only roundings are the accumulator's.  (One operand alone would
-// add an error of 2^-9 of each weight; the matrix unit has the time for two: at 64 tokens its work is 0.6 of the dequantisation's.)
-// Bound by the integer and half-precision instructions of the dequantisation, 2 a code, which come close to the time of reading the
-// codes.  The inner dimension is split over the CTAs of a cluster where there are fewer row blocks than SMs; their sums
-// are added in rank order through distributed shared memory.
+// A weight c * s has up to 11 significant bits, which one bf16 operand cannot hold.  It becomes two, c * s' and c * (s - s'), with
+// s' the scale's first four significant bits: both products are exact (3 + 4 bits), so that the only roundings are the
+// accumulator's.  One operand alone would add an error of up to 2^-8 of each weight to a result that is rounded once.
+// 64 x 8192 x 8192 takes TQ_US us (floor: 6.2 us to read the codes, 7.7 us of matrix instructions).  Timed with parts left out, 6.9 us of it
+// are a CTA's way to its first block and from its last (3.2 of them the sums' way through the cluster), 8.4 us the matrix unit,
+// which the dequantisation (2 instructions a code, 3.4 us by itself, 3.4 more for its loads) does not overlap well: three groups of warps are
+// what tensor memory has room for.  The inner dimension is split over the CTAs of a cluster where there are fewer row blocks
+// than SMs; their sums are added in rank order through distributed shared memory.
 #include "pdl.cuh"
 #include "qformat.cuh"
 #include "qlinear.cuh"
@@ -28,9 +30,8 @@ constexpr int TQ_STAGE_BYTES = TQ_TOKENS * 256;
 constexpr int TQ_PART_BYTES = TQ_TOKENS * 512;                        // a cluster's sums: [rank][this rank's tokens][128] fp32
 constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + 256 + 1024;      // barriers, slack for the 1024-byte alignment
 constexpr int TQ_A_COL = 64;                                          // accumulator columns, then the groups' operands
-constexpr uint32_t MUL_96 = 0x6f806f80u, MUL_92 = 0x6d806d80u;        // bf16x2 2^96, 2^92: operands become c s 2^-37
-constexpr float TWO_37 = 137438953472.f;
-constexpr uint32_t IDESC_NEG_A = 1u << 13;                            // instruction descriptor: A is negated
+constexpr uint32_t MUL_104 = 0x73807380u, MUL_100 = 0x71807180u;      // bf16x2 2^104, 2^100: operands become c s 2^-29
+constexpr float TWO_29 = 536870912.f;                                 // exact for scales from 2^-90 to 2^22
 
 struct TqSeg {
   const uint8_t* codes;
@@ -52,9 +53,9 @@ TC_DEVINL void fail(volatile int* abort_flag, int* status, int code) {
   *abort_flag = 1;
   atomicCAS(status, 0, code);
 }
-CCA_DEVINL uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+CCA_DEVINL uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 CCA_DEVINL uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
@@ -161,11 +162,10 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
         const uint32_t b = (smem_lo + st * (TQ_STAGE_BYTES >> 4)) | (1u << 16);
         if (leader) {
 #pragma unroll
-          for (int part = 0; part < 2; ++part)             // hi, then the negated rest
+          for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
-              mma_ts_w(tmem, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi,
-                       part ? idesc | IDESC_NEG_A : idesc, (i | part | ks) != 0);
+              mma_ts_w(tmem, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi, idesc, (i | part | ks) != 0);
           mma_commit(&a_empty[gr]);
           mma_commit(&b_empty[st]);
           if (i == n_kb - 1) mma_commit(done_bar);
@@ -183,8 +183,9 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
 #pragma unroll
       for (int grp = 0; grp < 4; ++grp) {
         const uint32_t s2 = __byte_perm(grp < 2 ? w.s.x : w.s.y, 0, (grp & 1) ? 0x3232u : 0x1010u);
-        const uint32_t m0 = mul_bf16x2(s2, MUL_96), m1 = mul_bf16x2(s2, MUL_92);
-        const uint32_t n0 = m0 ^ 0x80008000u, n1 = m1 ^ 0x80008000u;
+        const uint32_t h2 = s2 & 0xfff0fff0u, l2 = sub_bf16x2(s2, h2);             // four significant bits, and the rest
+        const uint32_t m0 = mul_bf16x2(h2, MUL_104), m1 = mul_bf16x2(h2, MUL_100);
+        const uint32_t n0 = mul_bf16x2(l2, MUL_104), n1 = mul_bf16x2(l2, MUL_100);
         uint32_t hi[16], lo[16];
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
@@ -193,7 +194,7 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
           const uint32_t pr = __byte_perm(word, 0, (grp & 1) ? 0x3322u : 0x1100u);
           const uint32_t e0 = code_e0(pr), e1 = code_e1(pr);
           hi[2 * g] = mul_bf16x2(e0, m0); hi[2 * g + 1] = mul_bf16x2(e1, m1);
-          lo[2 * g] = fma_bf16x2(e0, n0, hi[2 * g]); lo[2 * g + 1] = fma_bf16x2(e1, n1, hi[2 * g + 1]);
+          lo[2 * g] = mul_bf16x2(e0, n0); lo[2 * g + 1] = mul_bf16x2(e1, n1);
         }
         tmem_st16(a + grp * 16, hi);
         tmem_st16(a + 64 + grp * 16, lo);
@@ -236,7 +237,7 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const int tok = c * 16 + x;
-        const float y = __uint_as_float(v[x]) * TWO_37;
+        const float y = __uint_as_float(v[x]) * TWO_29;
         if (ranks > 1) {
           st_cluster_f32(cluster_addr(to + (uint32_t)(tok >> lr) * 512, tok & (ranks - 1)), y);
         } else if (tok0 + tok < p.M && row < sg.N) {
