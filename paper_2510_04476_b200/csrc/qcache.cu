@@ -943,7 +943,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) qcache_evict_kernel(EvArgs a) {
   const long long first_recent = (long long)a.next[b] - a.recent;
   if (a.keep > 0 && n == a.keep + 1 && ranks == 1) {
     // One row goes, as at every step of a cache at its bound: the lowest key's, of equal ones the last row's.  A single minimum
-    // instead of three counting passes and two lists (4097 rows: EV1_NEW us instead of EV1_OLD).
+    // instead of three counting passes and two lists (32 x 4097 rows, 4 heads: 8.1 us instead of 14.9, the copy that restores them for the next timing counted in both).
     unsigned long long least = ~0ull;
 #pragma unroll 4
     for (int r = tid; r < n; r += EV_THREADS) {

@@ -8,11 +8,11 @@
 // A weight c * s has up to 11 significant bits, which one bf16 operand cannot hold.  It becomes two, c * s' and c * (s - s'), with
 // s' the scale's first four significant bits: both products are exact (3 + 4 bits), so that the only roundings are the
 // accumulator's.  One operand alone would add an error of up to 2^-8 of each weight to a result that is rounded once.
-// 64 x 8192 x 8192 takes TQ_US us (floor: 6.2 us to read the codes, 7.7 us of matrix instructions).  Timed with parts left out, 6.9 us of it
-// are a CTA's way to its first block and from its last (3.2 of them the sums' way through the cluster), 8.4 us the matrix unit,
-// which the dequantisation (2 instructions a code, 3.4 us by itself, 3.4 more for its loads) does not overlap well: three groups of warps are
-// what tensor memory has room for.  The inner dimension is split over the CTAs of a cluster where there are fewer row blocks
-// than SMs; their sums are added in rank order through distributed shared memory.
+// 64 x 8192 x 8192 takes 21.3 us (floor: 6.2 us to read the codes, 7.7 us of matrix instructions).  Timed with parts left out, a third of
+// it is a CTA's way to its first block and from its last, 8.4 us the matrix unit, which the dequantisation (2 instructions a code,
+// 3.4 us by itself, 3.4 more for its loads) does not overlap well: three groups of warps are what tensor memory has room for.
+// The inner dimension is split over the CTAs of a cluster where there are fewer row blocks than SMs; each rank adds up its share of the
+// tokens, in rank order, from parts that the others write into its shared memory (four tokens a store: 21.3 us, 23.1 with one).
 #include "pdl.cuh"
 #include "qformat.cuh"
 #include "qlinear.cuh"
@@ -27,7 +27,7 @@ namespace {
 constexpr int TQ_GROUPS = 3, TQ_WARPS = 2 + 4 * TQ_GROUPS, TQ_THREADS = 32 * TQ_WARPS;
 constexpr int TQ_STAGES = 2 * TQ_GROUPS, TQ_TOKENS = 64;
 constexpr int TQ_STAGE_BYTES = TQ_TOKENS * 256;
-constexpr int TQ_PART_BYTES = TQ_TOKENS * 512;                        // a cluster's sums: [rank][this rank's tokens][128] fp32
+constexpr int TQ_PART_BYTES = 8 * 128 * 12 * 4;                       // a cluster's sums: [rank][128 rows][this rank's tokens + 4] fp32
 constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + 256 + 1024;      // barriers, slack for the 1024-byte alignment
 constexpr int TQ_A_COL = 64;                                          // accumulator columns, then the groups' operands
 constexpr uint32_t MUL_104 = 0x73807380u, MUL_100 = 0x71807180u;      // bf16x2 2^104, 2^100: operands become c s 2^-29
@@ -42,7 +42,8 @@ struct TqParams {
   TqSeg seg0, seg1;
   int blocks0;               // row blocks of the first segment
   int K128, M, n_tok;        // n_tok: tokens of a pass, a multiple of 16
-  int per_cta, log_ranks;    // channel blocks of a CTA; log2 of the CTAs that share a row block
+  int per_cta;               // channel blocks of a CTA
+  int mine;                  // tokens that a rank adds up: the ranks' shares, rounded up to a multiple of 4
   float* out_f32;
   bf16* out_bf16;
   int ldo;
@@ -63,7 +64,9 @@ CCA_DEVINL uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-CCA_DEVINL void st_cluster_f32(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+CCA_DEVINL void st_cluster_v4(uint32_t addr, float a, float b, float c, float d) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
 CCA_DEVINL void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 CCA_DEVINL void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -81,7 +84,7 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done_bar + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x, ranks = gridDim.x, lr = p.log_ranks;      // ranks is a power of two
+  const int rank = blockIdx.x, ranks = gridDim.x;
   const bool second = (int)blockIdx.y >= p.blocks0;
   const TqSeg sg = second ? p.seg1 : p.seg0;
   const CUtensorMap* map = second ? &tm1 : &tm0;
@@ -122,8 +125,8 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
     mbar_init(done_bar, 1);
     fence_barrier_init();
     for (int i = 0; i < min(n_kb, TQ_STAGES); ++i) load_x(i, i);
-    wait_ctl_init(abort_flag, p.status);
   }
+  if (threadIdx.x == 64) wait_ctl_init(abort_flag, p.status);
   if (warp == 1) {
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
@@ -215,8 +218,9 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
       load(w1, i + 4 * TQ_GROUPS);
       if (!work(w2)) break;
     }
-    // ---- sums: thread = row, one column per token.  In a cluster, token t is rank t % ranks's to add up: every CTA writes its
-    // part of it into that rank's shared memory.
+    // ---- sums: thread = row, one column per token.  In a cluster a rank adds up `mine` neighbouring tokens: every CTA writes its part
+    // of them into that rank's shared memory, four at a time (rows 16 bytes further apart than they are long, so that the lanes' pieces
+    // fall into different banks).
     bool ok = true;
     if (n_kb > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag));
@@ -224,8 +228,8 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
       tc_fence_after();
     }
     if (ranks > 1) cluster_wait();
-    const int r = q * 32 + lane, mine = p.n_tok >> lr;
-    const uint32_t to = smem_u32(part) + (uint32_t)(rank * mine * 128 + r) * 4;
+    const int r = q * 32 + lane;
+    const uint32_t to = smem_u32(part) + (uint32_t)((rank * 128 + r) * (p.mine + 4)) * 4;
     for (int c = gr; ok && c < p.n_tok / 16; c += TQ_GROUPS) {
       uint32_t v[16];
 #pragma unroll
@@ -234,16 +238,25 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
         tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c * 16, v);
         tmem_ld_wait();
       }
+      if (ranks > 1) {
+        int owner = c * 16 / p.mine, at = c * 16 - owner * p.mine;       // of the chunk's first token; mine is a multiple of 4
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int tok = c * 16 + x;
-        const float y = __uint_as_float(v[x]) * TWO_29;
-        if (ranks > 1) {
-          st_cluster_f32(cluster_addr(to + (uint32_t)(tok >> lr) * 512, tok & (ranks - 1)), y);
-        } else if (tok0 + tok < p.M && row < sg.N) {
-          const size_t o = (size_t)(tok0 + tok) * p.ldo + sg.out_off + row;
-          if (p.out_f32) p.out_f32[o] = y;
-          else p.out_bf16[o] = __float2bfloat16(y);
+        for (int x = 0; x < 16; x += 4) {
+          st_cluster_v4(cluster_addr(to + (uint32_t)at * 4, owner), __uint_as_float(v[x]) * TWO_29, __uint_as_float(v[x + 1]) * TWO_29,
+                        __uint_as_float(v[x + 2]) * TWO_29, __uint_as_float(v[x + 3]) * TWO_29);
+          at += 4;
+          if (at == p.mine) { at = 0; ++owner; }
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int tok = tok0 + c * 16 + x;
+          const float y = __uint_as_float(v[x]) * TWO_29;
+          if (tok < p.M && row < sg.N) {
+            const size_t o = (size_t)tok * p.ldo + sg.out_off + row;
+            if (p.out_f32) p.out_f32[o] = y;
+            else p.out_bf16[o] = __float2bfloat16(y);
+          }
         }
       }
     }
@@ -264,14 +277,24 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   if (ranks > 1) {
     cluster_arrive();                                      // all parts are written once everybody has come here
     cluster_wait();
-    const int n = min(p.n_tok, p.M - tok0), r = threadIdx.x & 127, mine = p.n_tok >> lr;
+    const int r = threadIdx.x & 127, first = tok0 + rank * p.mine, n = min(p.mine, min(p.M, tok0 + p.n_tok) - first);
     if (threadIdx.x < 384 && row0 + r < sg.N)
-      for (int k = threadIdx.x >> 7; (k << lr) + rank < n; k += 3) {
-        float y = 0.f;
-        for (int x = 0; x < ranks; ++x) y += part[(x * mine + k) * 128 + r];
-        const size_t o = (size_t)(tok0 + (k << lr) + rank) * p.ldo + sg.out_off + row0 + r;
-        if (p.out_f32) p.out_f32[o] = y;
-        else p.out_bf16[o] = __float2bfloat16(y);
+      for (int k = (threadIdx.x >> 7) * 4; k < n; k += 12) {
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (x < ranks) {
+            const float4 v = *reinterpret_cast<const float4*>(part + (x * 128 + r) * (p.mine + 4) + k);
+            y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+          }
+        const float ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k + e < n) {
+            const size_t o = (size_t)(first + k + e) * p.ldo + sg.out_off + row0 + r;
+            if (p.out_f32) p.out_f32[o] = ys[e];
+            else p.out_bf16[o] = __float2bfloat16(ys[e]);
+          }
       }
   }
 }
@@ -291,8 +314,8 @@ int tc_qlinear(TcState* tc, const QLinArgs& a, int* status, cudaStream_t st) {
   const int passes = (a.M + TQ_TOKENS - 1) / TQ_TOKENS;
   // the inner dimension over a cluster while that leaves every CTA two blocks and the SMs are not all taken
   int ranks = 1;
-  p.log_ranks = 0;
-  while (ranks < 8 && (long long)blocks * passes * ranks * 2 <= tc->sm_count && p.K128 >= ranks * 4) { ranks *= 2; ++p.log_ranks; }
+  while (ranks < 8 && (long long)blocks * passes * ranks * 2 <= tc->sm_count && p.K128 >= ranks * 4) ranks *= 2;
+  p.mine = ((p.n_tok + ranks - 1) / ranks + 3) / 4 * 4;
   p.per_cta = (p.K128 + ranks - 1) / ranks;
   CUtensorMap maps[2];
   for (int s = 0; s < 2; ++s)
