@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
 // order.  A lane's 16 bytes of a weight row are 8 channels of each of 4 groups: two instructions per group, whose sum is multiplied
 // by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.
 // At few tokens it is bound by the 200 instructions that a block of 16 rows by 128 columns takes, and what hides their latency is
-// warps: four CTAs per SM with one block of each warp on its way take 18.4 us for 5 x 16383 x 8192 (75 MB: 64 % of the measured copy
+// warps: four CTAs per SM with one block of each warp on its way take 18.7 us for 5 x 16383 x 8192 (75 MB: 64 % of the measured copy
 // rate), three with two or three 20.1 to 21.2, two with four 21.1; rings of asynchronous copies under CTAs that stay (16 or 32 warps, x in
 // registers or in shared memory, one row tile or two) 22.6 to 24.3.
 template <int NT>
@@ -149,7 +149,7 @@ int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int 
 }
 
 int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st) {
-  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.6 us against 7.7, 64 x 8192 x 8192: 22.7
+  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.6 us against 7.7, 64 x 8192 x 8192: 21.3
   // against 95.6), unless the handle has the tensor-core kernels switched off
   if (tc && a.M > 8) {
     const int r = tc_qlinear(tc, a, status, st);

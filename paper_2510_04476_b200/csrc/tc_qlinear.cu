@@ -308,6 +308,7 @@ int tc_qlinear(TcState* tc, const QLinArgs& a, int* status, cudaStream_t st) {
   p.seg1 = TqSeg{s1.codes, s1.scales, s1.N, s1.out_off};
   p.blocks0 = (s0.N + 127) / 128;
   const int blocks = p.blocks0 + (a.n_seg > 1 ? (s1.N + 127) / 128 : 0);
+  if (blocks > 65535) return 1;                            // a grid dimension
   p.K128 = (a.K + 127) / 128; p.M = a.M;
   p.n_tok = a.M >= TQ_TOKENS ? TQ_TOKENS : (a.M + 15) / 16 * 16;
   p.out_f32 = a.out_f32; p.out_bf16 = a.out_bf16; p.ldo = a.ldo; p.status = status;

@@ -2,7 +2,13 @@
 
 Tolerance of a product: the codes are exact operands and every product of one with a bf16 number is exact in fp32; an output is a sum of 32
 products per group, one scaling per group, and a chain of at most K / 256 + 1 groups per warp and 8 warps, each add off by at
-most 2^-23 of the terms' magnitudes (adds may truncate): |err| <= 2^-23 (K / 256 + 48) sum |x w|, plus 2^-8 |y| for a bf16 output."""
+most 2^-23 of the terms' magnitudes (adds may truncate): |err| <= 2^-23 (K / 256 + 48) sum |x w|, plus 2^-8 |y| for a bf16 output.
+
+From 9 tokens on an output is one chain of 2 K / 16 adds (two exact parts of each weight, 16 products an add), each off by at most
+2^-23 of the sum so far.  With inputs of random signs that sum is a random walk: products of standard deviation d have, four
+deviations out, |sum after i of the K / 8 adds| <= 4 d sqrt(8 i), so all adds together are off by at most
+2^-23 * 4 d sqrt(8) (2/3) (K / 8)^(3/2) = 2^-23 K^(3/2) d / 3; with sum |x w| = (2 / pi) d K for normal numbers that is
+2^-23 * 0.53 sqrt(K) sum |x w|, and 0.53 sqrt(K) < K / 256 + 48 for every K (K / 256 + 48 >= 2 sqrt(48 K / 256) = 0.86 sqrt(K))."""
 import pytest
 import torch
 
@@ -101,6 +107,17 @@ def test_product_without_the_tensor_core_kernels(cca, M):
         _check(cca.qlinear(packed, x.cuda(), out_dtype=torch.float32), x, Q.values(*Q.quantise(w)), 1056)
     finally:
         cca.set_impl(before)
+
+
+def test_product_of_more_rows_than_a_grid_dimension_has_blocks(cca):
+    N, K, M = 65535 * 128 + 1, 32, 9
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.randn(N, K, generator=gen, device="cuda").bfloat16()
+    x = torch.randn(M, K, generator=gen, device="cuda").bfloat16()
+    y = cca.qlinear(cca.qlinear_pack(w), x, out_dtype=torch.float32)
+    for part in (slice(0, 200), slice(N - 200, N)):
+        _check(y[:, part], x.cpu(), Q.values(*Q.quantise(w[part].cpu())), K)
+    assert cca.last_status() == 0
 
 
 def test_a_nan_input_touches_its_own_token_alone(cca):
