@@ -275,8 +275,10 @@ int cca_mla_forward(cca_handle* h, const cca_mla_dims* m, const cca_mla_weights*
  * The paper's decode keeps 2 B S E / C2 cached numbers and reads every weight once per token; here both take 4.5 bits a
  * number.  Format, for cache rows and weight rows alike: groups of 32 channels share a bf16 scale s = bf16(max|x| / 7) (division in
  * fp32, round to nearest); a channel is c * s with the whole number c = clamp(rint(x / s), -7, 7), 0 where s is 0 (a group of
- * zeros, or one whose s would be below the smallest normal number).  An infinity or NaN makes its whole group NaN.  The kernels take
- * values up to 2^60 in magnitude.  A code is 4 bits in sign and magnitude, two to a byte: bit 7 | bits 0-2 and bit 6 | bits 3-5.
+ * zeros, or one whose s would be below the smallest normal number).  An infinity or NaN makes its whole group NaN.  The format
+ * holds any bf16 number; the kernels that compute with it keep their accuracy for queries and inputs of magnitude 2^-30 .. 2^60,
+ * cached numbers up to 2^50 and weights whose groups' largest magnitude is 2^-87 .. 2^24 (or 0); above that results overflow,
+ * below it they lose bits as numbers do that underflow.  A code is 4 bits in sign and magnitude, two to a byte: bit 7 | bits 0-2 and bit 6 | bits 3-5.
  * A row of d channels is cut into blocks of min(d, 128) channels = G groups, 16 G bytes: byte 2 G i + 2 grp + j (i < 8, j < 2) holds
  * channel 32 grp + 4 i + j (bits 7, 0-2) and channel 32 grp + 4 i + 2 + j (bits 6, 3-5).
  *
@@ -296,7 +298,7 @@ typedef struct {
 /* Puts n new tokens of every sequence into the cache: k, v device bf16 [B, n, h_k, d_h]; row len[b] + i gets token i, weight 0 and
  * position position[b] + i (its row's index where `position` is null).  count (device int32 [B], may be null): sequence b has
  * only the first min(count[b], n) of them, a padded batch.  len is not advanced: the caller does that, as with pos of a decode
- * step.  A sequence whose rows would pass S_max, or whose length or position is negative, is left as it is, and the device status
+ * step.  A sequence whose rows would pass S_max, whose length or position is negative, or whose last position would pass 2^31 - 1, is left as it is, and the device status
  * word becomes 121.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
 int cca_qcache_append(cca_handle* h, const void* k, const void* v, const int32_t* position, const int32_t* count,
                       const cca_qcache* cache, int64_t B, int64_t n, void* cuda_stream);
@@ -338,7 +340,8 @@ int cca_qlinear_sizes(int64_t N, int64_t K, size_t* code_bytes, size_t* scale_by
 /* Quantises w (device bf16 [N, K]) into out->codes, out->scales, whose sizes cca_qlinear_sizes gives. */
 int cca_qlinear_pack(cca_handle* h, const void* w, const cca_qlinear_weights* out, void* cuda_stream);
 /* out = x W^T for M tokens: x device bf16 [M, K], out device [M, N], fp32 if out_f32 else bf16.  fp32 accumulation, one rounding at
- * the end.  Meant for the tokens of a decode step; M <= 65535.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+ * the end.  Meant for the tokens of a decode step; M <= 65535; out does not
+ * overlap x.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
 int cca_qlinear(cca_handle* h, const cca_qlinear_weights* w, const void* x, void* out, int out_f32, int64_t M, void* cuda_stream);
 
 /* The decode step on 4-bit projections and a 4-bit cache. */

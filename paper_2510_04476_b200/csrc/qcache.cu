@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
   const uint32_t units = (uint32_t)a.n * a.hk * R::NB * 2;
   const int len = a.c.len[b], first_pos = a.position ? a.position[b] : 0;
   const int cnt = a.count ? max(0, min(a.count[b], (int)a.n)) : (int)a.n;
-  if (len < 0 || (long long)len + cnt > a.limit || first_pos < 0) {
-    // a sequence whose rows do not fit, or whose position is none: nothing of it is written
+  if (len < 0 || (long long)len + cnt > a.limit || first_pos < 0 || (long long)first_pos + cnt > 0x80000000ll) {
+    // a sequence whose rows do not fit, or whose positions are none: nothing of it is written
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(a.status, 0, ST_QCACHE_BAD_LEN);
     return;
   }
@@ -943,7 +943,8 @@ __global__ void __launch_bounds__(EV_THREADS, 1) qcache_evict_kernel(EvArgs a) {
   const long long first_recent = (long long)a.next[b] - a.recent;
   if (a.keep > 0 && n == a.keep + 1 && ranks == 1) {
     // One row goes, as at every step of a cache at its bound: the lowest key's, of equal ones the last row's.  A single minimum
-    // instead of three counting passes and two lists (32 x 4097 rows, 4 heads: 8.1 us instead of 14.9, the copy that restores them for the next timing counted in both).
+    // instead of three counting passes and two lists (32 x 4097 rows,
+    // 2 heads: 8.1 us instead of 14.9, both with the copy that restores the lengths).
     unsigned long long least = ~0ull;
 #pragma unroll 4
     for (int r = tid; r < n; r += EV_THREADS) {

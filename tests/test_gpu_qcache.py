@@ -148,6 +148,14 @@ def test_append_of_a_padded_batch_and_rows_that_do_not_fit():
     torch.cuda.synchronize()
     assert cca.last_status() == 121
     assert torch.equal(cache["k_codes"][2], before[2]) and not torch.equal(cache["k_codes"][1], before[1])
+    # positions up to the last that 32 bits hold, and one further
+    before = cache["k_codes"].clone()
+    top = (1 << 31) - 1
+    cca.qcache_append(cache, k, v, torch.tensor([0, top - 3, top - 2, 3, 4], dtype=torch.int32).cuda())
+    torch.cuda.synchronize()
+    assert cca.last_status() == 121
+    assert torch.equal(cache["k_codes"][2], before[2]) and not torch.equal(cache["k_codes"][1], before[1])
+    assert cache["position"][1, 0, 6:].tolist() == [top - 3, top - 2, top - 1, top]
     cca.close()
 
 
