@@ -40,17 +40,44 @@ struct IoArgs {
   QCache c;
   long long n, limit;            // n * hk * blocks * 2 <= 2^31; limit: rows a sequence may hold
   int hk;
+  uint32_t hk_inv;               // 2^32 / hk rounded down, 2^32 - 1 for one head
   int* status;
 };
 
 // Eight neighbouring lanes take one block of one row (quantise_block); units run over (sequence, new row, head, block, key | value)
-// with the last fastest, so that a warp reads whole token rows.  Bound by traffic at a prompt's length, by the launch at a step's.
+// with the last fastest, so that a warp reads whole token rows.  1 x 16384 rows of 2 heads x 128 and their reading back take 13.9 us
+// (8.6 us of traffic, the rest two launches; 16.9 with the groups quantised one by one: 503 instructions a warp instead of 342), one row
+// of each of 32 sequences and its reading back 3.0.
+struct IoUnit { int kv, blk, i, h; };
+template <int DH>
+CCA_DEVINL IoUnit io_unit(const IoArgs& a, uint32_t u) {
+  constexpr int NB = Row<DH>::NB;
+  IoUnit w;
+  w.kv = (int)(u & 1); w.blk = (int)((u >> 1) % NB);
+  const uint32_t ih = (u >> 1) / NB;                       // (new row, head)
+  w.i = (int)__umulhi(ih, a.hk_inv); w.h = (int)ih - w.i * a.hk;       // the quotient, or one less
+  if (w.h >= a.hk) { w.h -= a.hk; ++w.i; }
+  return w;
+}
+
 template <int DH>
 __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
   pdl_enter();
   using R = Row<DH>;
+  constexpr int NG = R::NG;
   const int lane8 = threadIdx.x & 7, b = blockIdx.y;
   const uint32_t units = (uint32_t)a.n * a.hk * R::NB * 2;
+  uint2 x[NG];
+  IoUnit w;
+  auto fetch = [&](uint32_t u) {
+    w = io_unit<DH>(a, u);
+    const bf16* src = (w.kv ? a.v : a.k) + (((size_t)b * a.n + w.i) * a.hk + w.h) * DH + w.blk * R::BLK + lane8 * 4;
+#pragma unroll
+    for (int grp = 0; grp < NG; ++grp) x[grp] = u < units ? __ldcs(reinterpret_cast<const uint2*>(src + grp * GROUP)) : make_uint2(0, 0);
+  };
+  uint32_t u0 = blockIdx.x * 32 + (threadIdx.x >> 5) * 4;
+  const uint32_t mine = (threadIdx.x & 31) >> 3;
+  fetch(u0 + mine);                                        // on its way while the length is asked for
   const int len = a.c.len[b], first_pos = a.position ? a.position[b] : 0;
   const int cnt = a.count ? max(0, min(a.count[b], (int)a.n)) : (int)a.n;
   if (len < 0 || (long long)len + cnt > a.limit || first_pos < 0 || (long long)first_pos + cnt > 0x80000000ll) {
@@ -59,67 +86,71 @@ __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
     return;
   }
   // whole warps stay in the loop: the shuffles need every lane
-  for (uint32_t u0 = blockIdx.x * 32 + (threadIdx.x >> 5) * 4; u0 < units; u0 += gridDim.x * 32) {
-    const uint32_t u = u0 + ((threadIdx.x & 31) >> 3);
-    const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
-    const uint32_t ih = (u >> 1) / R::NB;                  // (new row, head)
-    const int i = (int)(ih / (uint32_t)a.hk), h = (int)(ih - (uint32_t)i * a.hk);
-    const bool ok = i < cnt;                               // false behind the last unit too
-    const bf16* src = (kv ? a.v : a.k) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
-    uint8_t code[2 * R::NG];
-    bf16 scale[R::NG];
-    quantise_block<R::NG>([&](int grp) { return ok ? __ldcs(reinterpret_cast<const uint2*>(src + grp * GROUP)) : make_uint2(0, 0); },
-                          code, scale);
+  while (u0 < units) {
+    const IoUnit o = w;
+    const bool ok = u0 + mine < units && o.i < cnt;
+    uint32_t code[(NG + 1) / 2], scale[(NG + 1) / 2];
+    // rows behind `count` may hold anything: as zeros they leave their neighbours in the warp on the short way
+    quantise_block<NG>([&](int grp) { return ok ? x[grp] : make_uint2(0, 0); }, code, scale);
+    u0 += gridDim.x * 32;
+    if (u0 < units) fetch(u0 + mine);
     if (!ok) continue;
-    const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + len + i;
-    uint8_t* dst = (kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + blk * (R::BLK / 2) + lane8 * 2 * R::NG;
-    if constexpr (R::NG == 4) {
-      uint2 w;
-      w.x = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
-      w.y = code[4] | (code[5] << 8) | (code[6] << 16) | ((uint32_t)code[7] << 24);
-      *reinterpret_cast<uint2*>(dst) = w;
-    } else if constexpr (R::NG == 2) {
-      *reinterpret_cast<uint32_t*>(dst) = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
+    const size_t row = ((size_t)b * a.hk + o.h) * a.c.S_max + len + o.i;
+    uint8_t* dst = (o.kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + o.blk * (R::BLK / 2) + lane8 * 2 * NG;
+    bf16* sc = (o.kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + o.blk * NG;
+    if constexpr (NG == 4) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(code[0], code[1]);
+      if (lane8 == 0) *reinterpret_cast<uint2*>(sc) = make_uint2(scale[0], scale[1]);
+    } else if constexpr (NG == 2) {
+      *reinterpret_cast<uint32_t*>(dst) = code[0];
+      if (lane8 == 0) *reinterpret_cast<uint32_t*>(sc) = scale[0];
     } else {
-      *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(code[0] | (code[1] << 8));
+      *reinterpret_cast<uint16_t*>(dst) = (uint16_t)code[0];
+      if (lane8 == 0) *reinterpret_cast<uint16_t*>(sc) = (uint16_t)scale[0];
     }
-    bf16* sc = (kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + blk * R::NG;
-#pragma unroll
-    for (int grp = 0; grp < R::NG; ++grp)
-      if (lane8 == grp) sc[grp] = scale[grp];
-    if (kv == 0 && blk == 0 && lane8 == 0) {
+    if (o.kv == 0 && o.blk == 0 && lane8 == 0) {
       if (a.c.weight) a.c.weight[row] = 0.f;
-      if (a.c.position) a.c.position[row] = (a.position ? first_pos : len) + i;
+      if (a.c.position) a.c.position[row] = (a.position ? first_pos : len) + o.i;
     }
   }
 }
 
+// The same units.  A code becomes a number exactly: the bf16 subnormal that its bits are, times powers of two.
 template <int DH>
 __global__ void __launch_bounds__(256) qcache_read_kernel(IoArgs a) {
   pdl_enter();
   using R = Row<DH>;
+  constexpr int NG = R::NG, NP = (NG + 1) / 2;
+  constexpr uint32_t UP_E0 = 0x7b807b80u, UP_E1 = 0x79807980u, UP = 0x46004600u;      // bf16x2 2^120, 2^116, 2^13
   const int lane8 = threadIdx.x & 7, b = blockIdx.y;
   const uint32_t units = (uint32_t)a.n * a.hk * R::NB * 2;
   const long long first = a.first ? a.first[b] : a.c.len[b];
   for (uint32_t u = blockIdx.x * 32 + (threadIdx.x >> 3); u < units; u += gridDim.x * 32) {
-    const int kv = (int)(u & 1), blk = (int)((u >> 1) % R::NB);
-    const uint32_t ih = (u >> 1) / R::NB;
-    const int i = (int)(ih / (uint32_t)a.hk), h = (int)(ih - (uint32_t)i * a.hk);
-    const long long r = first + i;
+    const IoUnit o = io_unit<DH>(a, u);
+    const long long r = first + o.i;
     const bool there = r >= 0 && r < a.c.S_max;
-    const size_t row = ((size_t)b * a.hk + h) * a.c.S_max + (there ? r : 0);
-    const uint8_t* src = (kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + blk * (R::BLK / 2) + lane8 * 2 * R::NG;
-    const bf16* sc = (kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + blk * R::NG;
-    float* dst = (kv ? a.v_out : a.k_out) + (((size_t)b * a.n + i) * a.hk + h) * DH + blk * R::BLK + lane8 * 4;
+    const size_t row = ((size_t)b * a.hk + o.h) * a.c.S_max + (there ? r : 0);
+    const uint8_t* src = (o.kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + o.blk * (R::BLK / 2) + lane8 * 2 * NG;
+    const bf16* sc = (o.kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + o.blk * NG;
+    float* dst = (o.kv ? a.v_out : a.k_out) + (((size_t)b * a.n + o.i) * a.hk + o.h) * DH + o.blk * R::BLK + lane8 * 4;
+    uint32_t code[NP], scale[NP];
+    if constexpr (NG == 1) {
+      code[0] = *reinterpret_cast<const uint16_t*>(src);
+      scale[0] = *reinterpret_cast<const uint16_t*>(sc);
+    } else {
 #pragma unroll
-    for (int grp = 0; grp < R::NG; ++grp) {
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (there) {
-        const uint32_t pair = *reinterpret_cast<const uint16_t*>(src + 2 * grp);
-        const float s = __bfloat162float(sc[grp]);
-        o = make_float4(s * value_e0(pair & 255u), s * value_e0(pair >> 8), s * value_e1(pair & 255u), s * value_e1(pair >> 8));
+      for (int p = 0; p < NP; ++p) {
+        code[p] = reinterpret_cast<const uint32_t*>(src)[p];
+        scale[p] = reinterpret_cast<const uint32_t*>(sc)[p];
       }
-      __stcs(reinterpret_cast<float4*>(dst + grp * GROUP), o);
+    }
+#pragma unroll
+    for (int grp = 0; grp < NG; ++grp) {
+      const uint32_t pr = __byte_perm(code[grp / 2], 0, (grp & 1) ? 0x3322u : 0x1100u);
+      const uint32_t lo = mul_bf16x2(mul_bf16x2(code_e0(pr), UP_E0), UP), hi = mul_bf16x2(mul_bf16x2(code_e1(pr), UP_E1), UP);
+      const float s = scale_at(scale, grp);
+      const float4 v = make_float4(s * bf_lo(lo), s * bf_hi(lo), s * bf_lo(hi), s * bf_hi(hi));
+      __stcs(reinterpret_cast<float4*>(dst + grp * GROUP), there ? v : make_float4(0.f, 0.f, 0.f, 0.f));
     }
   }
 }
@@ -1157,6 +1188,7 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
   }
 
 namespace {
+uint32_t head_inverse(int hk) { return hk == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / (unsigned)hk); }
 long long io_units(const CcaDims& d, long long n) { return n * d.hk * (d.dh > 128 ? d.dh / 128 : 1) * 2; }
 // 32 units a CTA and the sequences side by side; at most about 32 CTAs for each of 148 SMs, then around again
 dim3 io_grid(const CcaDims& d, long long n) {
@@ -1171,6 +1203,7 @@ int launch_qcache_append(const CcaDims& d, const bf16* k, const bf16* v, const i
   IoArgs a;
   memset(&a, 0, sizeof(a));
   a.k = k; a.v = v; a.position = position; a.count = count; a.c = c; a.n = n; a.limit = limit; a.hk = d.hk;
+  a.hk_inv = head_inverse(d.hk);
   a.status = status;
   if (io_units(d, n) > 1LL << 31) return 1;
   const dim3 grid = io_grid(d, n);
@@ -1185,7 +1218,7 @@ int launch_qcache_read(const CcaDims& d, const QCache& c, const int* first, floa
                        cudaStream_t st) {
   IoArgs a;
   memset(&a, 0, sizeof(a));
-  a.k_out = k; a.v_out = v; a.first = first; a.c = c; a.n = n; a.hk = d.hk;
+  a.k_out = k; a.v_out = v; a.first = first; a.c = c; a.n = n; a.hk = d.hk; a.hk_inv = head_inverse(d.hk);
   if (io_units(d, n) > 1LL << 31) return 1;
   const dim3 grid = io_grid(d, n);
   cudaError_t e;

@@ -96,57 +96,99 @@ CCA_DEVINL int nearest(float q) { return __float_as_int(__fadd_rn(q, 12582912.f)
 CCA_DEVINL uint32_t code_byte(int c0, int c1) {
   return (uint32_t)abs(c0) | ((uint32_t)abs(c1) << 3) | (((uint32_t)c0 >> 24) & 0x80u) | (((uint32_t)c1 >> 25) & 0x40u);
 }
-CCA_DEVINL int value_e0(uint32_t byte) { const int m = (int)(byte & 7u); return (byte & 0x80u) ? -m : m; }
-CCA_DEVINL int value_e1(uint32_t byte) { const int m = (int)((byte >> 3) & 7u); return (byte & 0x40u) ? -m : m; }
 
 // One thread's share of quantising a block: 4 channels 4 g .. 4 g + 3 of each of its NG groups, the eight threads g of a block
-// being eight neighbouring lanes.  `x(grp)` returns the 4 channels as bf16x2 pairs; out: 2 NG code bytes and the NG scales
-// (the same in all eight lanes).  All 32 lanes call it.
+// being eight neighbouring lanes.  `x(grp)` returns the 4 channels as bf16x2 pairs; out, two groups to a word: the code bytes in
+// order and the scales (the same in all eight lanes).  All 32 lanes call it.  What bounds it is instructions: two groups go
+// through the maximum and the scale as halves of one register, the eight lanes share the groups out while they find their maxima,
+// and magnitude and sign of a code are put in place for four bytes at a time.
 template <int NG, typename F>
-CCA_DEVINL void quantise_block(F x, uint8_t (&code)[2 * NG], bf16 (&scale)[NG]) {
-  uint2 u[NG];
+CCA_DEVINL void quantise_block(F x, uint32_t (&code)[(NG + 1) / 2], uint32_t (&scale)[(NG + 1) / 2]) {
+  constexpr int NP = (NG + 1) / 2;                         // pairs of groups
+  const bool odd = threadIdx.x & 1;
+  uint2 u[2 * NP];
 #pragma unroll
-  for (int grp = 0; grp < NG; ++grp) u[grp] = x(grp);
+  for (int grp = 0; grp < 2 * NP; ++grp) u[grp] = grp < NG ? x(grp) : make_uint2(0, 0);
+  // magnitudes compared as 16-bit patterns: their order is the numbers', and a NaN wins
+  uint32_t m[NP];
 #pragma unroll
-  for (int grp = 0; grp < NG; ++grp) {
-    // magnitudes compared as 16-bit patterns, two at a time: their order is the numbers', and a NaN wins
-    uint32_t m = __vmaxu2(u[grp].x & 0x7fff7fffu, u[grp].y & 0x7fff7fffu);
-#pragma unroll
-    for (int s = 1; s < 8; s <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, s));
-    const float amax = __uint_as_float(max(m << 16, m & 0xffff0000u));
-    const float v[4] = {bf_lo(u[grp].x), bf_hi(u[grp].x), bf_lo(u[grp].y), bf_hi(u[grp].y)};
-    float sf;
-    int c[4];
-    if (__any_sync(0xffffffffu, amax > 0.f && amax < 1.0097420e-28f)) {
-      // Below 2^-93 (in any of the warp's groups) the steps of the other branch would underflow.  A scale below the smallest
-      // normal number counts as zero.
-      const bf16 s = __float2bfloat16_rn(divide(amax, 7.f));
-      sf = __bfloat162float(s);
-      if (sf < 1.17549435e-38f) sf = 0.f;
-      if (amax >= 1.0097420e-28f && !(amax <= 3.3895314e38f)) sf = __uint_as_float(0x7fc00000u);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = nearest(divide(v[i], sf));
+  for (int p = 0; p < NP; ++p) {
+    const uint32_t a = __vmaxu2(u[2 * p].x & 0x7fff7fffu, u[2 * p].y & 0x7fff7fffu);
+    const uint32_t b = __vmaxu2(u[2 * p + 1].x & 0x7fff7fffu, u[2 * p + 1].y & 0x7fff7fffu);
+    m[p] = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+  }
+  // even lanes go on with the first pair, odd ones with the second (of one pair: all with it)
+  uint32_t top = __vmaxu2(NP == 2 && odd ? m[NP - 1] : m[0], __shfl_xor_sync(0xffffffffu, NP == 2 && !odd ? m[NP - 1] : m[0], 1));
+  top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 4));
+  auto both = [&](uint32_t mine, uint32_t (&w)[NP]) {      // this lane's pair and its neighbour's
+    if constexpr (NP == 2) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
+      w[0] = odd ? other : mine; w[1] = odd ? mine : other;
     } else {
-      // Quotients by one Newton step, so that nothing depends on the build's fast-math setting.  amax / 7 comes out correctly
-      // rounded (the reciprocal of 7 is).  x / s comes out exact where it is half way between two whole numbers: then the
-      // residual is exact and the correction off by less than a last place; elsewhere it is at least 2^-12 of itself away from
-      // half way (x and s have 8 significant bits each), a thousand times what is left of the error.  An infinity or a NaN in the
-      // group gives a NaN scale by itself (inf - inf).
-      constexpr float R7 = 1.f / 7.f;
-      const float q7 = amax * R7;
-      sf = __bfloat162float(__float2bfloat16_rn(fmaf(fmaf(-7.f, q7, amax), R7, q7)));
-      float r;
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(sf));
+      w[0] = mine;
+    }
+  };
+  auto plain = [](uint32_t t) { return t == 0u || t - 0x1100u <= 0x7f7fu - 0x1100u; };      // zero, or 2^-93 and more, and finite
+  if (__any_sync(0xffffffffu, !plain(top & 0xffffu) || !plain(top >> 16))) {
+    // Below 2^-93 (in any of the warp's groups) the steps of the other branch would underflow.  A scale below the smallest
+    // normal number counts as zero; an infinity or a NaN makes the scale a NaN.
+    uint32_t all[NP];
+    both(top, all);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float q = v[i] * r;
-        c[i] = nearest(fmaf(fmaf(-sf, q, v[i]), r, q));
+    for (int p = 0; p < NP; ++p) {
+      code[p] = scale[p] = 0u;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint2 w = u[2 * p + h];
+        const uint32_t t = h ? all[p] >> 16 : all[p] & 0xffffu;
+        float sf = __bfloat162float(__float2bfloat16_rn(divide(__uint_as_float(t << 16), 7.f)));
+        if (sf < 1.17549435e-38f) sf = 0.f;
+        if (t > 0x7f7fu) sf = __uint_as_float(0x7fc00000u);
+        const float v[4] = {bf_lo(w.x), bf_hi(w.x), bf_lo(w.y), bf_hi(w.y)};
+        int c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = nearest(divide(v[i], sf));
+        const uint32_t two = sf > 0.f ? code_byte(c[0], c[2]) | (code_byte(c[1], c[3]) << 8) : 0u;
+        code[p] |= two << (16 * h);
+        scale[p] |= (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(sf)) << (16 * h);
       }
     }
-    scale[grp] = __float2bfloat16_rn(sf);
-    const uint32_t two = sf > 0.f ? code_byte(c[0], c[2]) | (code_byte(c[1], c[3]) << 8) : 0u;
-    code[2 * grp] = (uint8_t)two;
-    code[2 * grp + 1] = (uint8_t)(two >> 8);
+    return;
+  }
+  // Quotients by one Newton step, so that nothing depends on the build's fast-math setting.  A maximum / 7 comes out correctly
+  // rounded (the reciprocal of 7 is).  |x| / s comes out exact where it is half way between two whole numbers: then the
+  // residual is exact and the correction off by less than a last place; elsewhere it is at least 2^-12 of itself away from
+  // half way (x and s have 8 significant bits each), a thousand times what is left of the error.
+  constexpr float R7 = 1.f / 7.f;
+  auto seventh = [&](uint32_t t) {
+    const float a = __uint_as_float(t), q = a * R7;
+    return fmaf(fmaf(-7.f, q, a), R7, q);
+  };
+  both(pack_bf16x2(seventh(top << 16), seventh(top & 0xffff0000u)), scale);
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    uint32_t c[2][4];                                      // |code| in the low bits of each
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint2 w = u[2 * p + h];
+      const float v[4] = {bf_lo(w.x), bf_hi(w.x), bf_lo(w.y), bf_hi(w.y)};
+      const float s = h ? bf_hi(scale[p]) : bf_lo(scale[p]);
+      float r;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+      r = fminf(r, 3.402823466e38f);                       // a group of zeros: 0 r must be 0
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = fabsf(v[i]), q = a * r;
+        c[h][i] = __float_as_uint(__fadd_rn(fmaf(fmaf(-s, q, a), r, q), 12582912.f));
+      }
+    }
+    // four bytes at a time; a sign counts where the magnitude is not 0, that is where adding 127 carries into bit 7
+    const uint32_t e0 = __byte_perm(__byte_perm(c[0][0], c[0][1], 0x0040), __byte_perm(c[1][0], c[1][1], 0x0040), 0x5410);
+    const uint32_t e1 = __byte_perm(__byte_perm(c[0][2], c[0][3], 0x0040), __byte_perm(c[1][2], c[1][3], 0x0040), 0x5410);
+    const uint32_t s0 = __byte_perm(u[2 * p].x, u[2 * p + 1].x, 0x7531) & (e0 + 0x7f7f7f7fu) & 0x80808080u;
+    const uint32_t s1 = __byte_perm(u[2 * p].y, u[2 * p + 1].y, 0x7531) & (e1 + 0x7f7f7f7fu) & 0x80808080u;
+    code[p] = e0 | s0 | (e1 << 3) | (s1 >> 1);
   }
 }
 

@@ -25,19 +25,13 @@ __global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
     const long long tile = u >> 4;
     const int kb = (int)(tile % a.k128);
     const long long row = tile / a.k128 * 16 + r;
-    uint8_t code[8];
-    bf16 scale[4];
+    uint32_t code[2], scale[2];
     quantise_block<4>([&](int grp) {
       const int col = kb * 128 + grp * GROUP;
       return row < a.N && col < a.K ? __ldcs(reinterpret_cast<const uint2*>(a.w + (size_t)row * a.K + col + lane8 * 4)) : make_uint2(0, 0);
     }, code, scale);
-    uint2 w;
-    w.x = code[0] | (code[1] << 8) | (code[2] << 16) | ((uint32_t)code[3] << 24);
-    w.y = code[4] | (code[5] << 8) | (code[6] << 16) | ((uint32_t)code[7] << 24);
-    *reinterpret_cast<uint2*>(a.codes + (size_t)u * 64 + lane8 * 8) = w;
-#pragma unroll
-    for (int grp = 0; grp < 4; ++grp)
-      if (lane8 == grp) a.scales[(size_t)u * 4 + grp] = scale[grp];
+    *reinterpret_cast<uint2*>(a.codes + (size_t)u * 64 + lane8 * 8) = make_uint2(code[0], code[1]);
+    if (lane8 == 0) *reinterpret_cast<uint2*>(a.scales + (size_t)u * 4) = make_uint2(scale[0], scale[1]);
   }
 }
 
