@@ -21,6 +21,7 @@
 #include "pdl.cuh"
 #include "qcache.cuh"
 #include "qlinear.cuh"
+#include "qrow.cuh"
 
 namespace {
 
@@ -138,13 +139,13 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) decode_proj_kernel(ProjArgs a) 
 // ------------------------------------------------------------------------------------------------ transforms
 // Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
 // the history for the next token and the input the next step's value shift needs.
-// Where a step's new key and value go: row pos[b] of the bf16 caches or, on a 4-bit cache (qlen set), row b of a staging area
-// from which they are quantised.  False: this sequence's position or length does not fit its cache.
+// Where a step's new key and value go: row pos[b] of the bf16 caches or, on a 4-bit cache (qlen set), row qlen[b].  False: this
+// sequence's position or length does not fit its cache.
 CCA_DEVINL bool new_row(const int* pos, const int* qlen, long long S_max, int max_len, int b, int& t, size_t& row) {
   t = pos[b];
   if (qlen != nullptr) {
     const int n = qlen[b];
-    row = (size_t)b;
+    row = (size_t)n;
     return t >= 0 && n >= 0 && n < S_max && n < max_len;
   }
   row = (size_t)b * S_max + t;
@@ -207,14 +208,15 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
     for (int r = 0; r < 7; ++r)
       if (r < pad) a.hist[((size_t)b * pad + r) * d.L + ch] = win[r + 1];
   }
-  for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256)
-    a.v_cache[row * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
+  if (a.v_cache)                                            // null: the value is quantised beside the key
+    for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256)
+      a.v_cache[row * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
   for (int c = blockIdx.x * 256 + tid; c < d.E / 8; c += gridDim.x * 256)
     reinterpret_cast<uint4*>(a.x_prev + (size_t)b * d.E)[c] = reinterpret_cast<const uint4*>(a.x + (size_t)b * d.E)[c];
 }
 
 // Eq. 9 (q-k-mean) and Eq. 11 (norm, temperature, RoPE at the sequence's own position) for one (sequence, head);
-// the query goes to the workspace, the key into the cache.
+// the query goes to the workspace, the key into the cache; on a 4-bit cache (Q4) key and value are quantised into it here.
 struct FnArgs {
   CcaDims d;
   const float* lat;
@@ -226,9 +228,10 @@ struct FnArgs {
   const int* qlen;       // as in C1Args
   long long S_max;
   int max_len;
+  QCache cache;          // Q4 alone
 };
 
-template <int DH>
+template <int DH, bool Q4>
 __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(FnArgs a) {
   pdl_enter();
   constexpr int NW = (DH < 128 ? 128 : DH) / 32;      // warps per block
@@ -274,16 +277,41 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
   }
   if (c < DH) xh[c] = v;
   __syncthreads();
-  if (c >= DH) return;
-  if (d.flags & F_ROPE) {
+  if constexpr (!Q4)
+    if (c >= DH) return;
+  if (c < DH && (d.flags & F_ROPE)) {
     const int cc = c % (DH / 2);
     const double theta = exp2(-2.0 * (double)cc / (double)DH * log2((double)d.rope_base));
     double sn, cs;
     sincos((double)t * theta, &sn, &cs);
     v = c < DH / 2 ? xh[c] * (float)cs - xh[c + DH / 2] * (float)sn : xh[c] * (float)cs + xh[c - DH / 2] * (float)sn;
   }
-  if (is_q) a.q[(size_t)b * d.Lq + ch0 + c] = v;
-  else a.k_cache[row * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
+  if constexpr (Q4) {
+    if (is_q) {
+      if (c < DH) a.q[(size_t)b * d.Lq + ch0 + c] = v;
+      return;
+    }
+    // the head's key and value, rounded to bf16 as the other cache holds them, quantised by one warp: eight lanes a block
+    using R = q4::Row<DH>;
+    __shared__ __align__(16) bf16 kv_row[2][DH];
+    const int j = head - d.hq;
+    if (c < DH) {
+      kv_row[0][c] = __float2bfloat16(v);
+      kv_row[1][c] = __float2bfloat16(lat_b[d.L + j * DH + c]);
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    const int kv = (lane >> 3) & 1, blk = lane >> 4, lane8 = lane & 7;
+    uint32_t code[(R::NG + 1) / 2], scale[(R::NG + 1) / 2];
+    q4::quantise_block<R::NG>(
+        [&](int grp) {
+          return blk < R::NB ? *reinterpret_cast<const uint2*>(&kv_row[kv][blk * R::BLK + grp * q4::GROUP + lane8 * 4]) : make_uint2(0, 0);
+        }, code, scale);
+    if (blk < R::NB) q4::store_block<DH>(a.cache, ((size_t)b * d.hk + j) * a.S_max + row, kv, blk, lane8, t, code, scale);
+  } else {
+    if (is_q) a.q[(size_t)b * d.Lq + ch0 + c] = v;
+    else a.k_cache[row * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -573,13 +601,14 @@ cudaError_t launch_attn_dh(const AtArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+template <bool Q4>
 cudaError_t launch_finalize_dh(const FnArgs& fa, cudaStream_t st) {
   const dim3 grid((unsigned)(fa.d.hq + fa.d.hk), (unsigned)fa.d.B);
   switch (fa.d.dh) {
-    case 32: return launch_pdl(decode_finalize_kernel<32>, grid, dim3(128), st, fa);
-    case 64: return launch_pdl(decode_finalize_kernel<64>, grid, dim3(128), st, fa);
-    case 128: return launch_pdl(decode_finalize_kernel<128>, grid, dim3(128), st, fa);
-    default: return launch_pdl(decode_finalize_kernel<256>, grid, dim3(256), st, fa);
+    case 32: return launch_pdl(decode_finalize_kernel<32, Q4>, grid, dim3(128), st, fa);
+    case 64: return launch_pdl(decode_finalize_kernel<64, Q4>, grid, dim3(128), st, fa);
+    case 128: return launch_pdl(decode_finalize_kernel<128, Q4>, grid, dim3(128), st, fa);
+    default: return launch_pdl(decode_finalize_kernel<256, Q4>, grid, dim3(256), st, fa);
   }
 }
 
@@ -667,8 +696,8 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   }
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = s.k_cache; fa.pos = s.pos;
-  fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len;
-  if ((e = launch_finalize_dh(fa, st)) != cudaSuccess) return -(int)e;
+  fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len; fa.cache = QCache{};
+  if ((e = launch_finalize_dh<false>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
   AtArgs aa;
   aa.d = d; aa.q = q; aa.k_cache = s.k_cache; aa.v_cache = s.v_cache;
@@ -713,15 +742,13 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
 }
 
 namespace {
-struct QStepLayout { size_t lat, q, k_new, v_new, o, y1s, y2, cache, end; };
+struct QStepLayout { size_t lat, q, o, y1s, y2, cache, end; };
 QStepLayout qstep_layout(const CcaDims& d, int max_len, int sm_count) {
   QStepLayout l;
   size_t off = 0;
   auto take = [&](size_t n) { const size_t o = off; off += (n + 255) / 256 * 256; return o; };
   l.lat = take((size_t)d.B * (d.L + d.Lk) * 4);
   l.q = take((size_t)d.B * d.Lq * 4);
-  l.k_new = take((size_t)d.B * d.Lk * 2);
-  l.v_new = take((size_t)d.B * d.Lk * 2);
   l.o = take((size_t)d.B * d.Lq * 2);
   l.y1s = take((size_t)d.B * d.L * d.k_ch * 2);
   l.y2 = take((size_t)d.B * d.L * 4);
@@ -740,7 +767,6 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   const QStepLayout l = qstep_layout(d, max_len, sm_count);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   float *lat = reinterpret_cast<float*>(ws + l.lat), *q = reinterpret_cast<float*>(ws + l.q), *y2 = reinterpret_cast<float*>(ws + l.y2);
-  bf16 *k_new = reinterpret_cast<bf16*>(ws + l.k_new), *v_new = reinterpret_cast<bf16*>(ws + l.v_new);
   bf16 *o = reinterpret_cast<bf16*>(ws + l.o), *y1s = reinterpret_cast<bf16*>(ws + l.y1s);
   cudaError_t e;
   int r;
@@ -753,7 +779,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   if ((r = launch_qlinear(pa, tc, status, launches, st)) != 0) return r;
   const int kc = (d.flags & F_CONV2) ? d.k_ch : 1;
   C1Args c1;
-  c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = v_new; c1.hist = hist; c1.x_prev = x_prev;
+  c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = nullptr; c1.hist = hist; c1.x_prev = x_prev;
   c1.pos = pos; c1.qlen = cache.len; c1.S_max = cache.S_max; c1.max_len = max_len; c1.status = status;
   if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
@@ -768,11 +794,10 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
     ++*launches;
   }
   FnArgs fa;
-  fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = k_new; fa.pos = pos; fa.qlen = cache.len;
+  fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = nullptr; fa.pos = pos; fa.qlen = cache.len; fa.cache = cache;
   fa.S_max = cache.S_max; fa.max_len = max_len;
-  if ((e = launch_finalize_dh(fa, st)) != cudaSuccess) return -(int)e;
+  if ((e = launch_finalize_dh<true>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
-  if ((r = launch_qcache_append(d, k_new, v_new, pos, nullptr, cache, 1, max_len, status, launches, st)) != 0) return r;
   if ((r = launch_qcache_attention(d, nullptr, q, o, cache, pos, 1, max_len, cache.weight != nullptr, ws + l.cache, sm_count, status,
                                    launches, ev_attn_begin, ev_attn_end, st)) != 0)
     return r;

@@ -6,24 +6,13 @@
 #include <cstring>
 
 #include "pdl.cuh"
-#include "qcache.cuh"
-#include "qformat.cuh"
+#include "qrow.cuh"
 
 namespace {
 
 using namespace q4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int MAX_DEVICES = 64;
-
-template <int DH>
-struct Row {                                       // a cache row of one head
-  static constexpr int BLK = DH < 128 ? DH : 128;  // channels of a block
-  static constexpr int NB = DH / BLK;              // blocks
-  static constexpr int NG = BLK / GROUP;           // scale groups of a block
-  static constexpr int CODES = DH / 2;             // bytes of codes
-  static constexpr int SCALES = DH / GROUP;        // scales
-  static constexpr int SW = (SCALES + 1) / 2;      // 32-bit words that hold the scales
-};
 
 // A row's scales as words; d_h = 32 has a single 16-bit scale.
 template <int DH>
@@ -96,22 +85,7 @@ __global__ void __launch_bounds__(256) qcache_append_kernel(IoArgs a) {
     if (u0 < units) fetch(u0 + mine);
     if (!ok) continue;
     const size_t row = ((size_t)b * a.hk + o.h) * a.c.S_max + len + o.i;
-    uint8_t* dst = (o.kv ? a.c.v_codes : a.c.k_codes) + row * R::CODES + o.blk * (R::BLK / 2) + lane8 * 2 * NG;
-    bf16* sc = (o.kv ? a.c.v_scales : a.c.k_scales) + row * R::SCALES + o.blk * NG;
-    if constexpr (NG == 4) {
-      *reinterpret_cast<uint2*>(dst) = make_uint2(code[0], code[1]);
-      if (lane8 == 0) *reinterpret_cast<uint2*>(sc) = make_uint2(scale[0], scale[1]);
-    } else if constexpr (NG == 2) {
-      *reinterpret_cast<uint32_t*>(dst) = code[0];
-      if (lane8 == 0) *reinterpret_cast<uint32_t*>(sc) = scale[0];
-    } else {
-      *reinterpret_cast<uint16_t*>(dst) = (uint16_t)code[0];
-      if (lane8 == 0) *reinterpret_cast<uint16_t*>(sc) = (uint16_t)scale[0];
-    }
-    if (o.kv == 0 && o.blk == 0 && lane8 == 0) {
-      if (a.c.weight) a.c.weight[row] = 0.f;
-      if (a.c.position) a.c.position[row] = (a.position ? first_pos : len) + o.i;
-    }
+    store_block<DH>(a.c, row, o.kv, o.blk, lane8, (a.position ? first_pos : len) + o.i, code, scale);
   }
 }
 
