@@ -58,10 +58,14 @@ void* need(PyObject* o, const char* name, at::ScalarType type, std::initializer_
   return need(tensor_of(o, name), name, type, shape, h);
 }
 bool absent(PyObject* o) { return !o || o == Py_None; }
-PyObject* item(PyObject* dict, const char* key) {          // borrowed, null if there is none
-  if (!PyDict_Check(dict)) refuse(std::string("wants a dict that holds \"") + key + "\"");
-  return PyDict_GetItemString(dict, key);
+PyObject* item_of(PyObject* dict, PyObject* key, const char* name) {       // borrowed, null if there is none
+  if (!PyDict_Check(dict)) refuse(std::string("wants a dict that holds \"") + name + "\"");
+  PyObject* o = PyDict_GetItemWithError(dict, key);
+  if (!o && PyErr_Occurred()) throw Raised();
+  return o;
 }
+// The key is made once, with its hash.
+#define ITEM(dict, name) item_of(dict, [] { static PyObject* k = PyUnicode_InternFromString(name); return k; }(), name)
 int64_t whole(PyObject* o) {
   const long long v = PyLong_AsLongLong(o);
   if (v == -1 && PyErr_Occurred()) throw Raised();
@@ -90,14 +94,14 @@ Workspace workspace_of(PyObject* o, const Handle* h) {
 // The dict of tensors that new_qcache makes; "weight" and "position" may be absent.
 cca_qcache qcache_of(PyObject* d, const Handle* h, int64_t* B) {
   cca_qcache c;
-  const at::Tensor &len = tensor_of(item(d, "len"), "len"), &codes = tensor_of(item(d, "k_codes"), "k_codes");
+  const at::Tensor &len = tensor_of(ITEM(d, "len"), "len"), &codes = tensor_of(ITEM(d, "k_codes"), "k_codes");
   if (len.dim() != 1 || codes.dim() != 4) refuse("len: wants one dimension, k_codes: four");
   const int64_t b = len.size(0), S = codes.size(2), hk = h->hk, dh = h->dh;
   c.k_codes = need(codes, "k_codes", at::kByte, {b, hk, S, dh / 2}, h);
-  c.v_codes = need(item(d, "v_codes"), "v_codes", at::kByte, {b, hk, S, dh / 2}, h);
-  c.k_scales = need(item(d, "k_scales"), "k_scales", at::kBFloat16, {b, hk, S, dh / 32}, h);
-  c.v_scales = need(item(d, "v_scales"), "v_scales", at::kBFloat16, {b, hk, S, dh / 32}, h);
-  PyObject *w = item(d, "weight"), *p = item(d, "position");
+  c.v_codes = need(ITEM(d, "v_codes"), "v_codes", at::kByte, {b, hk, S, dh / 2}, h);
+  c.k_scales = need(ITEM(d, "k_scales"), "k_scales", at::kBFloat16, {b, hk, S, dh / 32}, h);
+  c.v_scales = need(ITEM(d, "v_scales"), "v_scales", at::kBFloat16, {b, hk, S, dh / 32}, h);
+  PyObject *w = ITEM(d, "weight"), *p = ITEM(d, "position");
   c.weight = absent(w) ? nullptr : static_cast<float*>(need(w, "weight", at::kFloat, {b, hk, S}, h));
   c.position = absent(p) ? nullptr : static_cast<int32_t*>(need(p, "position", at::kInt, {b, hk, S}, h));
   c.len = static_cast<int32_t*>(need(len, "len", at::kInt, {b}, h));
@@ -106,21 +110,21 @@ cca_qcache qcache_of(PyObject* d, const Handle* h, int64_t* B) {
   return c;
 }
 cca_qlinear_weights qlinear_of(PyObject* d, const Handle* h) {
-  PyObject *n = item(d, "N"), *k = item(d, "K");
+  PyObject *n = ITEM(d, "N"), *k = ITEM(d, "K");
   if (!n || !k) refuse("wants a dict that holds \"N\" and \"K\"");
   const int64_t N = whole(n), K = whole(k), n16 = (N + 15) / 16, k128 = (K + 127) / 128;
-  return {need(item(d, "codes"), "codes", at::kByte, {n16, k128, 16, 64}, h),
-          need(item(d, "scales"), "scales", at::kBFloat16, {n16, k128, 16, 4}, h), N, K};
+  return {need(ITEM(d, "codes"), "codes", at::kByte, {n16, k128, 16, 64}, h),
+          need(ITEM(d, "scales"), "scales", at::kBFloat16, {n16, k128, 16, 4}, h), N, K};
 }
 cca_q_decode_state state_of(PyObject* d, const Handle* h, int64_t* B) {
   cca_q_decode_state s;
-  PyObject* cache = item(d, "cache");
+  PyObject* cache = ITEM(d, "cache");
   if (!cache) refuse("state: wants \"cache\"");
   s.cache = qcache_of(cache, h, B);
   const int64_t pad = h->k_seq + h->k_ch - 2, L = (h->hq + h->hk) * h->dh;
-  s.qk0_hist = pad > 0 ? need(item(d, "qk0_hist"), "qk0_hist", at::kFloat, {*B, pad, L}, h) : nullptr;
-  s.x_prev = need(item(d, "x_prev"), "x_prev", at::kBFloat16, {*B, h->E}, h);
-  s.pos = static_cast<int32_t*>(need(item(d, "pos"), "pos", at::kInt, {*B}, h));
+  s.qk0_hist = pad > 0 ? need(ITEM(d, "qk0_hist"), "qk0_hist", at::kFloat, {*B, pad, L}, h) : nullptr;
+  s.x_prev = need(ITEM(d, "x_prev"), "x_prev", at::kBFloat16, {*B, h->E}, h);
+  s.pos = static_cast<int32_t*>(need(ITEM(d, "pos"), "pos", at::kInt, {*B}, h));
   return s;
 }
 
@@ -273,15 +277,13 @@ PyObject* decode_step_q(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t B;
     const cca_q_decode_state s = state_of(a[3], h, &B);
     cca_q_weights w;
-    cca_qlinear_weights* lin[] = {&w.w_qkv, &w.w_vp, &w.w_o};
-    const char* names[] = {"w_qkv", "w_vp", "w_o"};
-    for (int i = 0; i < 3; ++i) {
-      PyObject* d = item(a[1], names[i]);
-      if (!d) refuse(std::string("weights: wants \"") + names[i] + "\"");
-      *lin[i] = qlinear_of(d, h);
-    }
+    PyObject *qkv = ITEM(a[1], "w_qkv"), *vp = ITEM(a[1], "w_vp"), *up = ITEM(a[1], "w_o");
+    if (!qkv || !vp || !up) refuse("weights: wants \"w_qkv\", \"w_vp\" and \"w_o\"");
+    w.w_qkv = qlinear_of(qkv, h);
+    w.w_vp = qlinear_of(vp, h);
+    w.w_o = qlinear_of(up, h);
     const int64_t L = (h->hq + h->hk) * h->dh;
-    PyObject *c0 = item(a[1], "conv0_w"), *c1 = item(a[1], "conv1_w"), *t = item(a[1], "temp");
+    PyObject *c0 = ITEM(a[1], "conv0_w"), *c1 = ITEM(a[1], "conv1_w"), *t = ITEM(a[1], "temp");
     w.conv0_w = absent(c0) ? nullptr : need(c0, "conv0_w", at::kBFloat16, {L, h->k_seq}, h);
     w.conv1_w = absent(c1) ? nullptr : need(c1, "conv1_w", at::kBFloat16, {L, h->dh, h->k_ch}, h);
     w.temp = absent(t) ? nullptr : static_cast<float*>(need(t, "temp", at::kFloat, {h->hk}, h));

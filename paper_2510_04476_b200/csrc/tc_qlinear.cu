@@ -319,8 +319,9 @@ int tc_qlinear(TcState* tc, const QLinArgs& a, int* status, cudaStream_t st) {
   p.mine = ((p.n_tok + ranks - 1) / ranks + 3) / 4 * 4;
   p.per_cta = (p.K128 + ranks - 1) / ranks;
   CUtensorMap maps[2];
-  for (int s = 0; s < 2; ++s)
-    if (!tc_make_map_2d(tc, &maps[s], a.seg[s < a.n_seg ? s : 0].X, (uint64_t)a.K, (uint64_t)a.M, (uint64_t)a.K, 64, (uint32_t)p.n_tok)) return 1;
+  for (int s = 0; s < a.n_seg; ++s)
+    if (!tc_make_map_2d(tc, &maps[s], a.seg[s].X, (uint64_t)a.K, (uint64_t)a.M, (uint64_t)a.K, 64, (uint32_t)p.n_tok)) return 1;
+  if (a.n_seg == 1) maps[1] = maps[0];
   static bool done[TC_MAX_DEVICES];
   if (!done[tc->device]) {
     const cudaError_t e = cudaFuncSetAttribute(tc_qlinear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TQ_SMEM);
