@@ -267,11 +267,14 @@ struct Rows {
     }
   }
   template <int ROW>
-  CCA_DEVINL void read_values(const Places& p, int r0, int last, const bf16* vsc, int g) {
+  CCA_DEVINL void read_values(const Places& p) {
     take_v<ROW * R::CODES>(v[0], p.v0);                    // operand rows 2t, 2t + 1, 2t + 8, 2t + 9
     take_v<ROW * R::CODES>(v[1], p.v1);
     take_v<(ROW + 8) * R::CODES>(v[2], p.v0);
     take_v<(ROW + 8) * R::CODES>(v[3], p.v1);
+  }
+  template <int ROW>
+  CCA_DEVINL void read_value_scales(const Places& p, int r0, int last, const bf16* vsc, int g) {
     if constexpr (DH == 32) single_scales(vs, r0, last, vsc, g);
     else { take<R::SW, S::VS - S::KS + ROW * S::SB>(vs[0], p.s); take<R::SW, S::VS - S::KS + (ROW + 8) * S::SB>(vs[1], p.s); }
   }
@@ -324,7 +327,9 @@ __host__ __device__ constexpr int qa_resident(int dh, int nht) {
 // turn.  S^T = K Q^T has the rows as the 16 and the heads as the 8 of m16n8k16, so that up to 8 heads cost one instruction per
 // 256 codes; O^T = V^T P^T has the channels as the 16.  Both read the codes from the registers that they were loaded into.  A
 // group's scale multiplies the group's partial logit in fp32; a value row's scale is multiplied into the probability, once
-// per group, before that is rounded to bf16 as the operand (the only rounding of the probabilities; the sums are taken before it).
+// per group, before that is rounded to fp16 as the operand (the only rounding of the probabilities; the sums are taken before it).  fp16
+// has 11 significant bits, so that the output's own rounding to bf16 is what its error comes from (bf16 operands: 0.0023 to 0.0026
+// relative to 64 bits instead of 0.0017); its range takes a maximum that knows the values' scales (see below).
 //
 // FUSED: a cluster is all of a (sequence, kv head)'s chunks (8 at most); its CTAs join their results through each other's shared
 // memory, keep their logits in their own, and finish the whole call: one launch instead of two.
@@ -367,8 +372,11 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   }
   const float c_scale = rsqrtf((float)DH) * LOG2E * TWO_69;
 
-  // softmax state of heads 2t, 2t + 1 (+ 8 ht): off = 64 - maximum, the same in all lanes of a column; the sums are per lane.
-  // Probabilities carry 2^64, which the bf16 subnormals of the value codes need, and may pass that by 2^8 before the maximum is moved.
+  // softmax state of heads 2t, 2t + 1 (+ 8 ht): off = TOP - maximum, the same in all lanes of a column; the sums are per lane.  The
+  // maximum is one of logit + log2(largest value scale of the row), so that the product of probability and scale, the fp16 operand, is
+  // 2^TOP at most when the maximum has just been moved.  It may pass that by 2^8 before it is moved again.  Scales count as 2^-30
+  // at least: values below that have no bearing on the maximum, and the sums stay in range.
+  constexpr float TOP = 7.f, SLACK = 8.f;
   float off[NHT][2], sum[NHT][2];
   float o[NHT][MT][4];
 #pragma unroll
@@ -457,22 +465,27 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         for (int c = 0; c < 4; ++c)
           if ((c < 2 ? r_lo : r_hi) > last) s[ht][c] = -INFINITY;
     }
+    cur.template read_value_scales<ROW>(at, r0, last, vsc, g);
+    uint32_t top2 = max_bf16x2(cur.vs[0][0], cur.vs[1][0]);  // a NaN's group is one by itself: it does not count
+#pragma unroll
+    for (int x = 1; x < R::SW; ++x) top2 = max_bf16x2(top2, max_bf16x2(cur.vs[0][x], cur.vs[1][x]));
+    const float e = fmaxf(__log2f(fmaxf(bf_lo(top2), bf_hi(top2))), -30.f);
     bool grow = false;
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) grow = grow || s[ht][c] + off[ht][c & 1] > 72.f;
+      for (int c = 0; c < 2; ++c) grow = grow || fmaxf(s[ht][c], s[ht][2 + c]) + (e + off[ht][c]) > TOP + SLACK;
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float m = fmaxf(s[ht][c], s[ht][2 + c]);
+          float m = fmaxf(s[ht][c], s[ht][2 + c]) + e;
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-          if (m + off[ht][c] > 64.f) {
-            const float al = exp2f(64.f - off[ht][c] - m); // 0 while nothing has been seen
-            off[ht][c] = 64.f - m;
+          if (m + off[ht][c] > TOP) {
+            const float al = exp2f(TOP - off[ht][c] - m);  // 0 while nothing has been seen
+            off[ht][c] = TOP - m;
             sum[ht][c] *= al;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) { o[ht][mt][c] *= al; o[ht][mt][2 + c] *= al; }
@@ -487,15 +500,15 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         sum[ht][c & 1] += s[ht][c];
       }
     // ---- O^T += V^T P^T
-    cur.template read_values<ROW>(at, r0, last, vsc, g);
+    cur.template read_values<ROW>(at);
 #pragma unroll
     for (int gi = 0; gi < R::NB * R::NG; ++gi) {
       const float s_lo = scale_at(cur.vs[0], gi), s_hi = scale_at(cur.vs[1], gi);
       uint32_t pb[NHT][2];
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht) {
-        pb[ht][0] = transpose_8x8(pack_bf16x2(s[ht][0] * s_lo, s[ht][1] * s_lo));
-        pb[ht][1] = transpose_8x8(pack_bf16x2(s[ht][2] * s_hi, s[ht][3] * s_hi));
+        pb[ht][0] = transpose_8x8(pack_f16x2(s[ht][0] * s_lo, s[ht][1] * s_lo));
+        pb[ht][1] = transpose_8x8(pack_f16x2(s[ht][2] * s_hi, s[ht][3] * s_hi));
       }
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
@@ -504,7 +517,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         const uint32_t p0 = __byte_perm(cur.v[0][w], cur.v[1][w], sel), p1 = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
         const uint32_t va[4] = {code_e0(p0), code_e1(p0), code_e0(p1), code_e1(p1)};
 #pragma unroll
-        for (int ht = 0; ht < NHT; ++ht) mma_16816(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
+        for (int ht = 0; ht < NHT; ++ht) mma_16816_f16(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
       }
     }
   };
@@ -565,14 +578,14 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         my_o[(8 * ht + 2 * t + (c & 1)) * (DH + 1) + (mt >> 1) * GROUP + 4 * g + (mt & 1) + 2 * (c >> 1)] =
-            o[ht][mt][c] * (c < 2 ? TWO_69 : TWO_65);
+            o[ht][mt][c] * (c < 2 ? 131072.f : 8192.f);    // 2^24 or 2^20 for the codes, 2^-TOP
   if (g == 0) {
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        sm_ml[warp][8 * ht + 2 * t + c][0] = 64.f - off[ht][c];
-        sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c] * TWO_M64;
+        sm_ml[warp][8 * ht + 2 * t + c][0] = TOP - off[ht][c];
+        sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c] * (1.f / 128.f);
       }
   }
   __syncthreads();
