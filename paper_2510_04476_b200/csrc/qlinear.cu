@@ -143,7 +143,7 @@ int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int 
 }
 
 int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st) {
-  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.6 us against 7.7, 64 x 8192 x 8192: 21.3
+  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.7 us against 7.7, 64 x 8192 x 8192: 22.9
   // against 95.6), unless the handle has the tensor-core kernels switched off
   if (tc && a.M > 8) {
     const int r = tc_qlinear(tc, a, status, st);

@@ -6,13 +6,13 @@
 //                  memory, as the MMA's A operand; the groups take the blocks in turn
 //
 // A weight c * s has up to 11 significant bits, which one bf16 operand cannot hold.  It becomes two, c * s' and c * (s - s'), with
-// s' the scale's first four significant bits: both products are exact (3 + 4 bits), so that the only roundings are the
-// accumulator's.  One operand alone would add an error of up to 2^-8 of each weight to a result that is rounded once.
-// 64 x 8192 x 8192 takes 21.3 us (floor: 6.2 us to read the codes, 7.7 us of matrix instructions).  Timed with parts left out, a third of
+// s' the scale's first four significant bits: both products are exact (3 + 4 bits), so that the only roundings are those
+// of adds.  One operand alone would add an error of up to 2^-8 of each weight to a result that is rounded once.
+// 64 x 8192 x 8192 takes 22.9 us (floor: 6.2 us to read the codes, 7.7 us of matrix instructions).  Timed with parts left out, a third of
 // it is a CTA's way to its first block and from its last, 8.4 us the matrix unit, which the dequantisation (2 instructions a code,
 // 3.4 us by itself, 3.4 more for its loads) does not overlap well: three groups of warps are what tensor memory has room for.
 // The inner dimension is split over the CTAs of a cluster where there are fewer row blocks than SMs; each rank adds up its share of the
-// tokens, in rank order, from parts that the others write into its shared memory (four tokens a store: 21.3 us, 23.1 with one).
+// tokens, in rank order, from parts that the others write into its shared memory (four tokens a store: 1.8 us less than one).
 #include "pdl.cuh"
 #include "qformat.cuh"
 #include "qlinear.cuh"
@@ -28,8 +28,12 @@ constexpr int TQ_GROUPS = 3, TQ_WARPS = 2 + 4 * TQ_GROUPS, TQ_THREADS = 32 * TQ_
 constexpr int TQ_STAGES = 2 * TQ_GROUPS, TQ_TOKENS = 64;
 constexpr int TQ_STAGE_BYTES = TQ_TOKENS * 256;
 constexpr int TQ_PART_BYTES = 8 * 128 * 12 * 4;                       // a cluster's sums: [rank][128 rows][this rank's tokens + 4] fp32
-constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + 256 + 1024;      // barriers, slack for the 1024-byte alignment
-constexpr int TQ_A_COL = 64;                                          // accumulator columns, then the groups' operands
+constexpr int TQ_SUM_BYTES = 128 * TQ_TOKENS * 4;                     // sums of the chunks so far: [16 quads of tokens][128 rows] float4
+constexpr int TQ_SMEM = TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + TQ_SUM_BYTES + 256 + 1024;      // barriers, 1024-byte alignment
+constexpr int TQ_CHUNK = 4;                                           // blocks of a chain of adds; each group has one of them at least
+static_assert(TQ_CHUNK >= TQ_GROUPS, "a group takes a chunk over behind its first block of the next");
+constexpr int TQ_A_COL = 64;                                          // accumulator columns, then the groups' operands,
+constexpr int TQ_ACC1 = TQ_A_COL + TQ_GROUPS * 128;                   // then the other accumulator's
 constexpr uint32_t MUL_104 = 0x73807380u, MUL_100 = 0x71807180u;      // bf16x2 2^104, 2^100: operands become c s 2^-29
 constexpr float TWO_29 = 536870912.f;                                 // exact for scales from 2^-90 to 2^22
 
@@ -76,11 +80,14 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* smem = smem_align1024(smem_dyn);
   float* part = reinterpret_cast<float*>(smem + TQ_STAGES * TQ_STAGE_BYTES);
-  uint64_t* b_full = reinterpret_cast<uint64_t*>(smem + TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES);
+  float4* sums = reinterpret_cast<float4*>(smem + TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES);
+  uint64_t* b_full = reinterpret_cast<uint64_t*>(smem + TQ_STAGES * TQ_STAGE_BYTES + TQ_PART_BYTES + TQ_SUM_BYTES);
   uint64_t* b_empty = b_full + TQ_STAGES;
   uint64_t* a_full = b_empty + TQ_STAGES;
   uint64_t* a_empty = a_full + TQ_GROUPS;
-  uint64_t* done_bar = a_empty + TQ_GROUPS;
+  uint64_t* acc_full = a_empty + TQ_GROUPS;
+  uint64_t* acc_empty = acc_full + 2;
+  uint64_t* done_bar = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done_bar + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -122,6 +129,7 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
   if (threadIdx.x == 0) {
     for (int s = 0; s < TQ_STAGES; ++s) { mbar_init(&b_full[s], 1); mbar_init(&b_empty[s], 1); }
     for (int s = 0; s < TQ_GROUPS; ++s) { mbar_init(&a_full[s], 4); mbar_init(&a_empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 4 * min(TQ_GROUPS, p.n_tok / 16)); }
     mbar_init(done_bar, 1);
     fence_barrier_init();
     for (int i = 0; i < min(n_kb, TQ_STAGES); ++i) load_x(i, i);
@@ -159,6 +167,9 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
         if (i >= n_kb) break;
         ok = __all_sync(0xffffffffu, mbar_wait(&b_full[st], sph, abort_flag)) &&
              __all_sync(0xffffffffu, mbar_wait(&a_full[gr], (st / TQ_GROUPS) & 1, abort_flag));
+        const int chunk = i / TQ_CHUNK, in_chunk = i - chunk * TQ_CHUNK;
+        if (ok && in_chunk == 0)
+          ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty[chunk & 1], ((chunk >> 1) & 1) ^ 1, abort_flag));
         if (!ok) { fail(abort_flag, p.status, ST_TIMEOUT_MMA); break; }
         tc_fence_after();
         const uint32_t a = tmem + TQ_A_COL + gr * 128;
@@ -168,9 +179,11 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
           for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
-              mma_ts_w(tmem, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi, idesc, (i | part | ks) != 0);
+              mma_ts_w(tmem + (chunk & 1) * TQ_ACC1, a + part * 64 + ks * 8, b + (ks >> 2) * (sub >> 4) + (ks & 3) * 2, desc_hi, idesc,
+                       (in_chunk | part | ks) != 0);
           mma_commit(&a_empty[gr]);
           mma_commit(&b_empty[st]);
+          if (in_chunk == TQ_CHUNK - 1) mma_commit(&acc_full[chunk & 1]);
           if (i == n_kb - 1) mma_commit(done_bar);
         }
       }
@@ -180,7 +193,7 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
     // two blocks of the group ahead are on their way while one is worked on
     uint32_t phase = 1;
     auto work = [&](const Block& w) -> bool {
-      if (!mbar_wait(&a_empty[gr], phase, abort_flag)) { fail(abort_flag, p.status, ST_TIMEOUT_EPI); return false; }
+      if (!__all_sync(0xffffffffu, mbar_wait(&a_empty[gr], phase, abort_flag))) { fail(abort_flag, p.status, ST_TIMEOUT_EPI); return false; }
       phase ^= 1;
       tc_fence_after();
 #pragma unroll
@@ -208,35 +221,76 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
       if (lane == 0) mbar_arrive(&a_full[gr]);
       return true;
     };
+    const int r = q * 32 + lane;
+    // The tensor cores cut off what an add shifts out, always towards the same side, so that a chain's error grows with its length (64 x 8192
+    // x 8192 in chains of 512 adds: 4.6e-6 relative to 64 bits, of 1024 9.7e-6).  So a chain is TQ_CHUNK blocks, 64 adds; its sum is added to
+    // those before it in fp32 by the warps that have its rows, while the other accumulator takes the next chunk.  4.8e-7 for any K,
+    // 22.9 us (one chain: 21.3; chunks of 3: 3.6e-7, 23.9; of 6: 7.0e-7, 22.5).
+    int next = 0;                                          // the chunk to be taken over next
+    auto take_over = [&](int end) -> bool {
+      for (; next < end; ++next) {
+        if (gr >= p.n_tok / 16) continue;
+        const int buf = next & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(&acc_full[buf], (next >> 1) & 1, abort_flag))) { fail(abort_flag, p.status, ST_TIMEOUT_EPI); return false; }
+        tc_fence_after();
+        for (int c = gr; c < p.n_tok / 16; c += TQ_GROUPS) {
+          uint32_t v[16];
+          tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + buf * TQ_ACC1 + c * 16, v);
+          tmem_ld_wait();
+          float4* at = sums + c * 4 * 128 + r;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float4 o = next ? at[x * 128] : make_float4(0.f, 0.f, 0.f, 0.f);
+            o.x += __uint_as_float(v[4 * x]); o.y += __uint_as_float(v[4 * x + 1]);
+            o.z += __uint_as_float(v[4 * x + 2]); o.w += __uint_as_float(v[4 * x + 3]);
+            at[x * 128] = o;
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&acc_empty[buf]);
+      }
+      return true;
+    };
+    // A chunk is taken over behind the group's first block of the next one, so that the tensor cores have work meanwhile.
     for (int i = gr; i < n_kb; i += 3 * TQ_GROUPS) {
       load(w2, i + 2 * TQ_GROUPS);
-      if (!work(w0)) break;
+      if (!work(w0) || !take_over(i / TQ_CHUNK)) break;
       if (i + TQ_GROUPS >= n_kb) break;
       load(w0, i + 3 * TQ_GROUPS);
-      if (!work(w1)) break;
+      if (!work(w1) || !take_over((i + TQ_GROUPS) / TQ_CHUNK)) break;
       if (i + 2 * TQ_GROUPS >= n_kb) break;
       load(w1, i + 4 * TQ_GROUPS);
-      if (!work(w2)) break;
+      if (!work(w2) || !take_over((i + 2 * TQ_GROUPS) / TQ_CHUNK)) break;
     }
+    const int last_chunk = max(n_kb - 1, 0) / TQ_CHUNK;
     // ---- sums: thread = row, one column per token.  In a cluster a rank adds up `mine` neighbouring tokens: every CTA writes its part
     // of them into that rank's shared memory, four at a time (rows 16 bytes further apart than they are long, so that the lanes' pieces
     // fall into different banks).
-    bool ok = true;
-    if (n_kb > 0) {
+    bool ok = take_over(last_chunk);
+    if (ok && n_kb > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag));
       if (!ok) fail(abort_flag, p.status, ST_TIMEOUT_EPI);
       tc_fence_after();
     }
     if (ranks > 1) cluster_wait();
-    const int r = q * 32 + lane;
     const uint32_t to = smem_u32(part) + (uint32_t)((rank * 128 + r) * (p.mine + 4)) * 4;
     for (int c = gr; ok && c < p.n_tok / 16; c += TQ_GROUPS) {
       uint32_t v[16];
 #pragma unroll
       for (int x = 0; x < 16; ++x) v[x] = 0u;
       if (n_kb > 0) {
-        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c * 16, v);
+        tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (last_chunk & 1) * TQ_ACC1 + c * 16, v);
         tmem_ld_wait();
+        if (last_chunk > 0) {
+          const float4* at = sums + c * 4 * 128 + r;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float4 o = at[x * 128];
+            v[4 * x] = __float_as_uint(__uint_as_float(v[4 * x]) + o.x); v[4 * x + 1] = __float_as_uint(__uint_as_float(v[4 * x + 1]) + o.y);
+            v[4 * x + 2] = __float_as_uint(__uint_as_float(v[4 * x + 2]) + o.z); v[4 * x + 3] = __float_as_uint(__uint_as_float(v[4 * x + 3]) + o.w);
+          }
+        }
       }
       if (ranks > 1) {
         int owner = c * 16 / p.mine, at = c * 16 - owner * p.mine;       // of the chunk's first token; mine is a multiple of 4

@@ -4,11 +4,10 @@ Tolerance of a product: the codes are exact operands and every product of one wi
 products per group, one scaling per group, and a chain of at most K / 256 + 1 groups per warp and 8 warps, each add off by at
 most 2^-23 of the terms' magnitudes (adds may truncate): |err| <= 2^-23 (K / 256 + 48) sum |x w|, plus 2^-8 |y| for a bf16 output.
 
-From 9 tokens on an output is one chain of 2 K / 16 adds (two exact parts of each weight, 16 products an add), each off by at most
-2^-23 of the sum so far.  With inputs of random signs that sum is a random walk: products of standard deviation d have, four
-deviations out, |sum after i of the K / 8 adds| <= 4 d sqrt(8 i), so all adds together are off by at most
-2^-23 * 4 d sqrt(8) (2/3) (K / 8)^(3/2) = 2^-23 K^(3/2) d / 3; with sum |x w| = (2 / pi) d K for normal numbers that is
-2^-23 * 0.53 sqrt(K) sum |x w|, and 0.53 sqrt(K) < K / 256 + 48 for every K (K / 256 + 48 >= 2 sqrt(48 K / 256) = 0.86 sqrt(K))."""
+From 9 tokens on the products of 512 columns are a chain of 64 adds on the tensor cores (two exact parts of each weight, 16 products an
+add), each off by at most 2^-23 of the sum so far, which after i adds has i / 64 of the chunk's sum |x w| (terms of one distribution): 33 times
+2^-23 of that in all.  The K / 512 chunks and 8 ranks are added in fp32, 2^-24 of the sum |x w| an add:
+|err| <= 2^-23 (33 + K / 1024 + 4) sum |x w|, below the bound above."""
 import pytest
 import torch
 
@@ -107,6 +106,18 @@ def test_product_without_the_tensor_core_kernels(cca, M):
         _check(cca.qlinear(packed, x.cuda(), out_dtype=torch.float32), x, Q.values(*Q.quantise(w)), 1056)
     finally:
         cca.set_impl(before)
+
+
+@pytest.mark.parametrize("M,N,K", [(9, 150, 32768), (64, 40, 65536), (33, 9500, 8192)])
+def test_product_of_numbers_of_one_sign_in_long_rows(cca, M, N, K):
+    """Every add of a chain is cut off to the same side: the bound of chunks of 64 adds, with 8 more for terms that are not all alike."""
+    gen = torch.Generator().manual_seed(K)
+    w = (0.05 * torch.rand(N, K, generator=gen)).bfloat16()
+    x = torch.rand(M, K, generator=gen).bfloat16()
+    y = cca.qlinear(cca.qlinear_pack(w.cuda()), x.cuda(), out_dtype=torch.float32).cpu().double()
+    ref = x.double() @ Q.values(*Q.quantise(w)).t()
+    assert ((y - ref).abs() <= 2.0 ** -23 * (45 + K / 1024) * ref).all(), float(((y - ref).abs() / ref).max() * 2 ** 23)
+    assert cca.last_status() == 0
 
 
 def test_product_of_more_rows_than_a_grid_dimension_has_blocks(cca):
