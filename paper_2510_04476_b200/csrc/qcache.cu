@@ -35,7 +35,7 @@ struct IoArgs {
 
 // Eight neighbouring lanes take one block of one row (quantise_block); units run over (sequence, new row, head, block, key | value)
 // with the last fastest, so that a warp reads whole token rows.  1 x 16384 rows of 2 heads x 128 and their reading back take 13.9 us
-// (8.6 us of traffic, the rest two launches; 16.9 with the groups quantised one by one: 503 instructions a warp instead of 342), one row
+// (8.6 us of traffic, the rest two launches; 16.9 with the groups quantised one by one: 503 instructions a warp instead of 362), one row
 // of each of 32 sequences and its reading back 3.0.
 struct IoUnit { int kv, blk, i, h; };
 template <int DH>
