@@ -327,9 +327,10 @@ __host__ __device__ constexpr int qa_resident(int dh, int nht) {
 // turn.  S^T = K Q^T has the rows as the 16 and the heads as the 8 of m16n8k16, so that up to 8 heads cost one instruction per
 // 256 codes; O^T = V^T P^T has the channels as the 16.  Both read the codes from the registers that they were loaded into.  A
 // group's scale multiplies the group's partial logit in fp32; a value row's scale is multiplied into the probability, once
-// per group, before that is rounded to fp16 as the operand (the only rounding of the probabilities; the sums are taken before it).  fp16
-// has 11 significant bits, so that the output's own rounding to bf16 is what its error comes from (bf16 operands: 0.0023 to 0.0026
-// relative to 64 bits instead of 0.0017); its range takes a maximum that knows the values' scales (see below).
+// per group, and goes to the tensor cores as two bf16 numbers: its first 8 significant bits, cut off, and the rest, rounded to 8 (the
+// only rounding of the probabilities, 2^-15 at most; the sums are taken before it).  A single bf16 operand adds to the error of the
+// output (0.0023 to 0.0026 relative to 64 bits instead of the output's own 0.0017), and a single fp16 one has too few exponents for
+// values of different sizes side by side.  32 x 16384 rows: 47.2 us; with a single operand 41.1 to 42.6.
 //
 // FUSED: a cluster is all of a (sequence, kv head)'s chunks (8 at most); its CTAs join their results through each other's shared
 // memory, keep their logits in their own, and finish the whole call: one launch instead of two.
@@ -372,17 +373,18 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   }
   const float c_scale = rsqrtf((float)DH) * LOG2E * TWO_69;
 
-  // softmax state of heads 2t, 2t + 1 (+ 8 ht): off = TOP - maximum, the same in all lanes of a column; the sums are per lane.  The
-  // maximum is one of logit + log2(largest value scale of the row), so that the product of probability and scale, the fp16 operand, is
-  // 2^TOP at most when the maximum has just been moved.  It may pass that by 2^8 before it is moved again.  Scales count as 2^-30
-  // at least: values below that have no bearing on the maximum, and the sums stay in range.
-  constexpr float TOP = 7.f, SLACK = 8.f;
-  float off[NHT][2], sum[NHT][2];
+  // softmax state of heads 2t, 2t + 1 (+ 8 ht): a reference that no logit passes by more than 2^SLACK (the maximum of when it was last
+  // moved), the same in all lanes of a column, and sums per lane.  Nothing is ever added to a logit but another logit, so that large ones
+  // keep their differences.  The values' scales carry 2^70, which the bf16 subnormals of their codes need: scales of up to 2^48 stay
+  // in range, and so do products of probability and scale down to 2^-63.
+  constexpr float SLACK = 8.f;
+  constexpr uint32_t TWO_70 = 0x62806280u;                 // bf16x2
+  float ref[NHT][2], sum[NHT][2];
   float o[NHT][MT][4];
 #pragma unroll
   for (int ht = 0; ht < NHT; ++ht) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) { off[ht][c] = INFINITY; sum[ht][c] = 0.f; }
+    for (int c = 0; c < 2; ++c) { ref[ht][c] = -INFINITY; sum[ht][c] = 0.f; }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -465,27 +467,22 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         for (int c = 0; c < 4; ++c)
           if ((c < 2 ? r_lo : r_hi) > last) s[ht][c] = -INFINITY;
     }
-    cur.template read_value_scales<ROW>(at, r0, last, vsc, g);
-    uint32_t top2 = max_bf16x2(cur.vs[0][0], cur.vs[1][0]);  // a NaN's group is one by itself: it does not count
-#pragma unroll
-    for (int x = 1; x < R::SW; ++x) top2 = max_bf16x2(top2, max_bf16x2(cur.vs[0][x], cur.vs[1][x]));
-    const float e = fmaxf(__log2f(fmaxf(bf_lo(top2), bf_hi(top2))), -30.f);
     bool grow = false;
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) grow = grow || fmaxf(s[ht][c], s[ht][2 + c]) + (e + off[ht][c]) > TOP + SLACK;
+      for (int c = 0; c < 2; ++c) grow = grow || fmaxf(s[ht][c], s[ht][2 + c]) - ref[ht][c] > SLACK;
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float m = fmaxf(s[ht][c], s[ht][2 + c]) + e;
+          float m = fmaxf(s[ht][c], s[ht][2 + c]);
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-          if (m + off[ht][c] > TOP) {
-            const float al = exp2f(TOP - off[ht][c] - m);  // 0 while nothing has been seen
-            off[ht][c] = TOP - m;
+          if (m > ref[ht][c]) {
+            const float al = exp2f(ref[ht][c] - m);        // 0 while nothing has been seen
+            ref[ht][c] = m;
             sum[ht][c] *= al;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) { o[ht][mt][c] *= al; o[ht][mt][2 + c] *= al; }
@@ -496,19 +493,25 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[ht][c] = exp2f(s[ht][c] + off[ht][c & 1]);
+        s[ht][c] = exp2f(s[ht][c] - ref[ht][c & 1]);
         sum[ht][c & 1] += s[ht][c];
       }
+    cur.template read_value_scales<ROW>(at, r0, last, vsc, g);
+#pragma unroll
+    for (int x = 0; x < R::SW; ++x) { cur.vs[0][x] = mul_bf16x2(cur.vs[0][x], TWO_70); cur.vs[1][x] = mul_bf16x2(cur.vs[1][x], TWO_70); }
     // ---- O^T += V^T P^T
     cur.template read_values<ROW>(at);
 #pragma unroll
     for (int gi = 0; gi < R::NB * R::NG; ++gi) {
       const float s_lo = scale_at(cur.vs[0], gi), s_hi = scale_at(cur.vs[1], gi);
-      uint32_t pb[NHT][2];
+      uint32_t pb[NHT][4];                                 // first parts of both rows, second parts
 #pragma unroll
       for (int ht = 0; ht < NHT; ++ht) {
-        pb[ht][0] = transpose_8x8(pack_f16x2(s[ht][0] * s_lo, s[ht][1] * s_lo));
-        pb[ht][1] = transpose_8x8(pack_f16x2(s[ht][2] * s_hi, s[ht][3] * s_hi));
+        uint32_t rest[2];
+        pb[ht][0] = transpose_8x8(split_bf16x2(s[ht][0] * s_lo, s[ht][1] * s_lo, rest[0]));
+        pb[ht][1] = transpose_8x8(split_bf16x2(s[ht][2] * s_hi, s[ht][3] * s_hi, rest[1]));
+        pb[ht][2] = transpose_8x8(rest[0]);
+        pb[ht][3] = transpose_8x8(rest[1]);
       }
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
@@ -517,7 +520,10 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
         const uint32_t p0 = __byte_perm(cur.v[0][w], cur.v[1][w], sel), p1 = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
         const uint32_t va[4] = {code_e0(p0), code_e1(p0), code_e0(p1), code_e1(p1)};
 #pragma unroll
-        for (int ht = 0; ht < NHT; ++ht) mma_16816_f16(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
+        for (int ht = 0; ht < NHT; ++ht) {
+          mma_16816(o[ht][2 * gi + jj], va, pb[ht][0], pb[ht][1]);
+          mma_16816(o[ht][2 * gi + jj], va, pb[ht][2], pb[ht][3]);
+        }
       }
     }
   };
@@ -578,14 +584,14 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         my_o[(8 * ht + 2 * t + (c & 1)) * (DH + 1) + (mt >> 1) * GROUP + 4 * g + (mt & 1) + 2 * (c >> 1)] =
-            o[ht][mt][c] * (c < 2 ? 131072.f : 8192.f);    // 2^24 or 2^20 for the codes, 2^-TOP
+            o[ht][mt][c] * (c < 2 ? 9.223372036854775808e18f : 5.76460752303423488e17f);    // 2^63, 2^59: 2^133 or 2^129 for the codes, 2^-70
   if (g == 0) {
 #pragma unroll
     for (int ht = 0; ht < NHT; ++ht)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        sm_ml[warp][8 * ht + 2 * t + c][0] = TOP - off[ht][c];
-        sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c] * (1.f / 128.f);
+        sm_ml[warp][8 * ht + 2 * t + c][0] = ref[ht][c];
+        sm_ml[warp][8 * ht + 2 * t + c][1] = sum[ht][c];
       }
   }
   __syncthreads();

@@ -4,8 +4,7 @@
 // sign and magnitude: e0 = sign in bit 7, magnitude in bits 0-2; e1 = sign in bit 6, magnitude in bits 3-5.  With the byte
 // copied into both bytes of a 16-bit lane, (lane & 0x8007) IS the bf16 number e0 * 2^-133 and ((lane << 1) & 0x8070) IS
 // e1 * 2^-129: bf16 subnormals, which mma.sync multiplies exactly.  So a code needs no conversion and leaves no offset to take
-// off; the other operand carries 2^64 (for e0) and 2^60 (for e1), and sums come out times 2^-69.  The same bits are the fp16 numbers
-// e0 * 2^-24 and e1 * 2^-20, subnormals too, where the other operand is fp16.
+// off; the other operand carries 2^64 (for e0) and 2^60 (for e1), and sums come out times 2^-69.
 //
 // A row is cut into blocks of min(d, 128) channels with NG = block / 32 groups; in a block, byte g * 2 NG + grp * 2 + j
 // (g = 0..7, j = 0, 1) holds channels grp * 32 + 4 g + j (e0) and grp * 32 + 4 g + 2 + j (e1).  That order serves both ways a
@@ -13,8 +12,6 @@
 // 2t + 1, whichever group each pair is in) and over the rows (lane group g takes its own 2 NG bytes, byte i being one 16-channel
 // output tile).
 #pragma once
-#include <cuda_fp16.h>
-
 #include "common.cuh"
 
 namespace q4 {
@@ -26,11 +23,6 @@ constexpr float TWO_69 = 590295810358705651712.f;
 
 CCA_DEVINL void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-CCA_DEVINL void mma_16816_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -49,14 +41,11 @@ CCA_DEVINL uint32_t pack_bf16x2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
-CCA_DEVINL uint32_t pack_f16x2(float lo, float hi) {
-  __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&v);
-}
-CCA_DEVINL uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // of a number and a NaN the number
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+// Two numbers as two bf16 pairs that add up to them: the first 8 significant bits, cut off (returned), and the rest, rounded.
+CCA_DEVINL uint32_t split_bf16x2(float lo, float hi, uint32_t& rest) {
+  const uint32_t l = __float_as_uint(lo), h = __float_as_uint(hi);
+  rest = pack_bf16x2(lo - __uint_as_float(l & 0xffff0000u), hi - __uint_as_float(h & 0xffff0000u));
+  return __byte_perm(l, h, 0x7632);
 }
 CCA_DEVINL uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
