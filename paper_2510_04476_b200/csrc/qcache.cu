@@ -316,7 +316,8 @@ template <int DH, int H>
 struct FusedShare {                                        // what the CTAs of a cluster read of each other, and what they make of it
   float o[H * DH];
   float2 ml[H];
-  float fac[H][8], lse[H];
+  float fac[H][8];
+  float2 norm[H];                                          // maximum, reciprocal of the sum
 };
 // CTAs of the attention kernel that an SM holds; registers are given out accordingly.
 __host__ __device__ constexpr int qa_resident(int dh, int nht) {
@@ -629,8 +630,9 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
       float l = ml.y * f;
 #pragma unroll
       for (int x = 4; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-      if (lane < 8) fz.fac[h][lane] = n_rows > 0 ? f / l : 0.f;
-      if (lane == 0) fz.lse[h] = m + __log2f(l);
+      const float inv = n_rows > 0 ? 1.f / l : 0.f;
+      if (lane < 8) fz.fac[h][lane] = f * inv;
+      if (lane == 0) fz.norm[h] = make_float2(m, inv);
     }
     __syncthreads();
     // the output's channels are shared out among the CTAs
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
       float* w = a.c.weight + ((size_t)b * d.hk + j) * a.c.S_max;
       for (int r = r_begin + threadIdx.x; r < r_end; r += QA_WARPS * 32) {
         float acc = 0.f;
-        for (int h = 0; h < d.g; ++h) acc += exp2f(sco[r * d.g + h] - fz.lse[h]);
+        for (int h = 0; h < d.g; ++h) acc = fmaf(exp2f(sco[r * d.g + h] - fz.norm[h].x), fz.norm[h].y, acc);
         atomicAdd(w + r, acc);                             // the row's only one: no order to depend on, and nothing to wait for
       }
     }
@@ -656,14 +658,14 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 }
 
 // Joins the chunks' partial results of one (sequence, kv head) and, where the weights are gathered, adds to every row what its
-// heads gave it: 2^(logit - logsumexp), from the logits that the first kernel left (exact in fp32 whatever maximum a chunk used).
-// Its time is latency: the logits and weights of its rows are asked for before the logsumexps that they wait for are formed, and a head's
+// heads gave it: 2^(logit - maximum) / sum, from the logits that the first kernel left.  Maximum and sum stay apart: a large maximum would
+// swallow the logarithm of the sum.  Its time is latency: the logits and weights of its rows are asked for before the sums that they wait for are formed, and a head's
 // channels are shared out so that no thread adds up more than four chunks (1 x 16384 rows, both kernels: 7.1 us, 8.0 with a CTA a head).
 constexpr int QJ_ROWS = 4;                                 // rows of a thread, where the weights are gathered
 template <int DH>
 __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
   pdl_enter();
-  __shared__ float sm_lse[64], sm_inv[64], fac[QA_MAX_SPLITS];
+  __shared__ float sm_max[64], sm_inv[64], fac[QA_MAX_SPLITS];
   __shared__ float4 red[64];
   constexpr int PIECES = DH / 32;                          // CTAs that share a head's channels
   const CcaDims& d = a.d;
@@ -709,7 +711,7 @@ __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    if (lane == 0) { sm_lse[h] = m + __log2f(l); sm_inv[h] = n_rows > 0 ? 1.f / l : 0.f; }
+    if (lane == 0) { sm_max[h] = m; sm_inv[h] = n_rows > 0 ? 1.f / l : 0.f; }
   }
   __syncthreads();
   if ((int)blockIdx.x < d.g * PIECES) {                    // a CTA joins 32 channels of a head: 32 threads share 4 of them
@@ -740,19 +742,20 @@ __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
     }
   }
   if (!a.gather) return;
+  auto given = [&](float logit, int h) { return exp2f(logit - sm_max[h]) * sm_inv[h]; };
 #pragma unroll
   for (int i = 0; i < QJ_ROWS; ++i) {
     const int r = r_first + i * 256;
     if (r >= n_rows) break;
     float acc = 0.f;
     if (d.g % 4 == 0) {
-      acc = exp2f(s4[i].x - sm_lse[0]) + exp2f(s4[i].y - sm_lse[1]) + exp2f(s4[i].z - sm_lse[2]) + exp2f(s4[i].w - sm_lse[3]);
+      acc = given(s4[i].x, 0) + given(s4[i].y, 1) + given(s4[i].z, 2) + given(s4[i].w, 3);
       for (int h = 4; h < d.g; h += 4) {
         const float4 v = *reinterpret_cast<const float4*>(sc + (size_t)r * d.g + h);
-        acc += exp2f(v.x - sm_lse[h]) + exp2f(v.y - sm_lse[h + 1]) + exp2f(v.z - sm_lse[h + 2]) + exp2f(v.w - sm_lse[h + 3]);
+        acc += given(v.x, h) + given(v.y, h + 1) + given(v.z, h + 2) + given(v.w, h + 3);
       }
     } else {
-      for (int h = 0; h < d.g; ++h) acc += exp2f(sc[(size_t)r * d.g + h] - sm_lse[h]);
+      for (int h = 0; h < d.g; ++h) acc += given(sc[(size_t)r * d.g + h], h);
     }
     w[r] = wr[i] + acc;
   }
