@@ -309,7 +309,7 @@ int cca_qcache_read(cca_handle* h, const cca_qcache* cache, const int32_t* first
                     void* cuda_stream);
 
 /* Bytes of device workspace that one cca_qcache_attention or cca_qcache_evict call needs (one size for both) for caches of at most
- * max_len rows.  Depends on the device's SM count as cca_decode_workspace_size does.  B <= 65535, B * max_len <= 2^30. */
+ * max_len rows, of B sequences or fewer.  Depends on the device's SM count as cca_decode_workspace_size does.  B <= 65535, B * max_len <= 2^30. */
 int cca_qcache_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
 
 /* softmax(q k^T / sqrt(d_h)) v (Eq. 11, third line) of one query token per sequence over its len[b] rows: q, o device bf16
@@ -360,6 +360,7 @@ typedef struct {
   const int32_t* pos;   /* int32 [B], device: position of each sequence's new token.  After an eviction it is larger than the
                            number of cached rows, and may be larger than S_max                                       */
 } cca_q_decode_state;
+/* For caches of at most max_len rows, the new one included, of B sequences or fewer. */
 int cca_decode_workspace_size_q(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
 /* cca_decode_step with the new key and value quantised into row len[b] and attention over len[b] + 1 rows (the new one as it is
  * cached); the weights are gathered where cache.weight is set.  The caller advances pos and len after the step.  max_len: len[b] + 1

@@ -783,6 +783,16 @@ void attn_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* spl
   }
 }
 
+// Chunks that the plan above makes at most, over all sequences, for any number of rows up to max_len and any batch up to d.B: what a
+// workspace holds, so that one made for the longest caches serves shorter ones, which the plan may cut into more chunks.
+size_t attn_parts(const CcaDims& d, int max_len, int sm_count) {
+  const int n_grp = (d.g + heads_per_cta(d) - 1) / heads_per_cta(d);
+  const long long most = 4LL * sm_count * qa_resident(d.dh, heads_per_cta(d) / 8) / (d.hk * n_grp);      // four waves of CTAs
+  const long long by_rows = (max_len + 63) / 64 < QA_MAX_SPLITS ? (max_len + 63) / 64 : QA_MAX_SPLITS;
+  const long long all = by_rows * d.B;
+  return (size_t)(all < most ? all : most > d.B ? most : d.B);
+}
+
 // One launch does where 8 chunks hold the sequence that have no more rows than 256 or than the plan above gives a chunk (d_h 128, h_q 8,
 // h_k 2, in a graph: 1 x 1024 rows 5.1 us against 6.2 in two launches, 1 x 2048 6.3 against 6.0, 1 x 4096 8.4 against 6.5, 32 x 4096
 // 16.9 against 18.3; called one by one, 5.7 against 8.5 us of host time), one CTA has all of a kv head's query heads, and a chunk's logits
@@ -1231,9 +1241,8 @@ int launch_qcache_read(const CcaDims& d, const QCache& c, const int* first, floa
 }
 
 size_t qcache_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
-  int chunk, splits;
-  attn_plan(d, max_len, sm_count, &chunk, &splits);
-  const size_t attn = up256((size_t)d.B * d.hq * splits * d.dh * 4) + up256((size_t)d.B * d.hq * splits * 2 * 4) +
+  const size_t parts = d.hq * attn_parts(d, max_len, sm_count);
+  const size_t attn = up256(parts * d.dh * 4) + up256(parts * 2 * 4) +
                       up256((size_t)d.B * d.hq * max_len * 4);
   const size_t ev = up256((size_t)d.B * 8) + up256((size_t)d.B * d.hk * 4) + up256((size_t)d.B * d.hk * 2 * (max_len / 2 + 1) * 4);
   return attn > ev ? attn : ev;
