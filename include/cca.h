@@ -217,7 +217,7 @@ typedef struct {
   int64_t S_max;        /* capacity of both caches in tokens                                                    */
 } cca_decode_state;
 
-/* Bytes of device workspace one decode step needs for B sequences of at most max_len tokens (the new
+/* Bytes of device workspace one decode step needs for B sequences, or fewer, of at most max_len tokens (the new
  * token included).  The size depends on the device's SM count (the key range is split over the SMs); a
  * host-only handle assumes 148. */
 int cca_decode_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);

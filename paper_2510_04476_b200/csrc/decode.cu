@@ -614,18 +614,34 @@ cudaError_t launch_finalize_dh(const FnArgs& fa, cudaStream_t st) {
 
 }  // namespace
 
-void decode_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
-  const int n_grp = d.g <= 8 ? 1 : (d.g + 15) / 16;
-  const long long base = (long long)d.B * d.hk * n_grp;
-  static int per_sm = 0;                                       // CTAs per SM to aim for (CCA_DECODE_CTAS_PER_SM overrides)
+namespace {
+constexpr int DC_MAX_SPLITS = 128;
+int decode_groups(const CcaDims& d) { return d.hk * (d.g <= 8 ? 1 : (d.g + 15) / 16); }      // CTAs of a chunk
+int decode_ctas_per_sm() {                                     // to aim for (CCA_DECODE_CTAS_PER_SM overrides)
+  static int per_sm = 0;
   if (per_sm == 0) {
     const char* e = getenv("CCA_DECODE_CTAS_PER_SM");
-    per_sm = e ? atoi(e) : 12;
-    if (per_sm < 1 || per_sm > 64) per_sm = 12;
+    int n = e ? atoi(e) : 12;
+    if (n < 1 || n > 64) n = 12;
+    per_sm = n;
   }
-  long long want = ((long long)per_sm * sm_count + base - 1) / base;
+  return per_sm;
+}
+// Chunks that decode_plan makes at most, over all sequences, for any length up to max_len and any batch up to d.B: what a workspace
+// holds, so that one made for the longest caches serves shorter ones, which the plan may cut into more chunks.
+size_t decode_parts(const CcaDims& d, int max_len, int sm_count) {
+  const long long ctas = (long long)decode_ctas_per_sm() * sm_count, grp = decode_groups(d);
+  const long long most = (ctas + grp - 1) / grp + d.B;         // the plan rounds a sequence's share up
+  const long long by_rows = ((long long)max_len + 63) / 64 < DC_MAX_SPLITS ? ((long long)max_len + 63) / 64 : DC_MAX_SPLITS;
+  return (size_t)(by_rows * d.B < most ? by_rows * d.B : most);
+}
+}  // namespace
+
+void decode_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits) {
+  const long long base = (long long)d.B * decode_groups(d);
+  long long want = ((long long)decode_ctas_per_sm() * sm_count + base - 1) / base;
   if (want < 1) want = 1;
-  if (want > 128) want = 128;
+  if (want > DC_MAX_SPLITS) want = DC_MAX_SPLITS;
   int ch = (int)((max_len + want - 1) / want);
   ch = (ch + 63) / 64 * 64;                                    // the four warps of a CTA take 16 keys each per round
   if (ch < 64) ch = 64;
@@ -634,14 +650,13 @@ void decode_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* s
 }
 
 size_t decode_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
-  int chunk, splits;
-  decode_plan(d, max_len, sm_count, &chunk, &splits);
+  const size_t parts = d.hq * decode_parts(d, max_len, sm_count);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t n = 0;
   n += up((size_t)d.B * (d.L + d.Lk) * 4);             // lat
   n += up((size_t)d.B * d.Lq * 4);                     // q
-  n += up((size_t)d.B * d.hq * splits * d.dh * 4);     // partial o
-  n += up((size_t)d.B * d.hq * splits * 2 * 4);        // partial (m, l)
+  n += up(parts * d.dh * 4);                           // partial o
+  n += up(parts * 2 * 4);                              // partial (m, l)
   n += up((size_t)d.B * d.Lq * 2);                     // o
   n += up((size_t)d.B * d.L * d.k_ch * 2);             // conv1 output at the taps conv2 reads
   n += up((size_t)d.B * d.L * 4);                      // conv output

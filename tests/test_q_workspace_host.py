@@ -46,3 +46,16 @@ def test_size_never_falls_with_the_batch(name, hq, hk, dh):
         sizes = [_sizes(getattr(lib, name), h, B, [max_len])[0] for B in range(1, 200)]
         assert sizes == sorted(sizes), max_len
     lib.cca_destroy(h)
+
+
+@pytest.mark.parametrize("hq,hk,dh", SHAPES)
+def test_size_of_the_bf16_step_never_falls(hq, hk, dh):
+    lib = binding.load_library()
+    h = _handle(lib, hq, hk, dh)
+    for B in (1, 2, 3, 4, 32, 150):
+        sizes = _sizes(lib.cca_decode_workspace_size, h, B, range(1, 20000 if B < 5 else 6000))
+        assert sizes == sorted(sizes), B
+    for max_len in (1, 64, 1000, 8192, 16385, 1 << 20):
+        sizes = [_sizes(lib.cca_decode_workspace_size, h, B, [max_len])[0] for B in range(1, 200)]
+        assert sizes == sorted(sizes), max_len
+    lib.cca_destroy(h)
