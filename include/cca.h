@@ -278,7 +278,8 @@ int cca_mla_forward(cca_handle* h, const cca_mla_dims* m, const cca_mla_weights*
  * zeros, or one whose s would be below the smallest normal number).  An infinity or NaN makes its whole group NaN.  The format
  * holds any bf16 number; the kernels that compute with it keep their accuracy for queries and inputs of magnitude 2^-30 .. 2^60,
  * cached numbers of 2^-45 .. 2^50 (or 0; of any sizes side by side, whatever the logits) and weights whose groups' largest magnitude is
- * 2^-87 .. 2^24 (or 0); above that results overflow, below it they lose bits as numbers do that underflow.  A code is 4 bits in sign and magnitude, two to a byte: bit 7 | bits 0-2 and bit 6 | bits 3-5.
+ * 2^-87 .. 2^24 (or 0) with |x| times that of 2^-90 or more where x is not 0; above that results overflow, below it they lose bits as numbers
+ * do that underflow.  What an infinite input gives is not a number or infinite.  A code is 4 bits in sign and magnitude, two to a byte: bit 7 | bits 0-2 and bit 6 | bits 3-5.
  * A row of d channels is cut into blocks of min(d, 128) channels = G groups, 16 G bytes: byte 2 G i + 2 grp + j (i < 8, j < 2) holds
  * channel 32 grp + 4 i + j (bits 7, 0-2) and channel 32 grp + 4 i + 2 + j (bits 6, 3-5).
  *

@@ -19,6 +19,7 @@ namespace q4 {
 constexpr int GROUP = 32;
 constexpr uint32_t MUL_E0 = 0x5f805f80u;   // bf16x2 {2^64, 2^64}
 constexpr uint32_t MUL_E1 = 0x5d805d80u;   // bf16x2 {2^60, 2^60}
+constexpr uint32_t MUL_69 = 0x62006200u;   // bf16x2 {2^69, 2^69}
 constexpr float TWO_69 = 590295810358705651712.f;
 
 CCA_DEVINL void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {

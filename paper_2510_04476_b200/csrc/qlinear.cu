@@ -37,7 +37,8 @@ __global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
 
 // 16 weight rows per CTA, 8 NT tokens, the inner dimension split over the 8 warps and summed through shared memory in a fixed
 // order.  A lane's 16 bytes of a weight row are 8 channels of each of 4 groups: two instructions per group, whose sum is multiplied
-// by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.
+// by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.  A group's sum comes out times 2^-69, which
+// its scale takes off before the groups are added: sums of small weights would fall below the smallest normal number.
 // At few tokens it is bound by the 200 instructions that a block of 16 rows by 128 columns takes, and what hides their latency is
 // warps: four CTAs per SM with one block of each warp on its way take 18.7 us for 5 x 16383 x 8192 (75 MB: 64 % of the measured copy
 // rate), three with two or three 20.1 to 21.2, two with four 21.1; rings of asynchronous copies under CTAs that stay (16 or 32 warps, x in
@@ -77,6 +78,8 @@ __global__ void __launch_bounds__(QL_WARPS * 32, NT == 1 ? 4 : 1) qlinear_kernel
     load_words<2>(sl, scales + (size_t)kb * 64);
     load_words<2>(sh, scales + (size_t)kb * 64 + 32);
 #pragma unroll
+    for (int i = 0; i < 2; ++i) { sl[i] = mul_bf16x2(sl[i], MUL_69); sh[i] = mul_bf16x2(sh[i], MUL_69); }
+#pragma unroll
     for (int gi = 0; gi < 4; ++gi) {
       const int col = kb * 128 + gi * GROUP;
       uint32_t ka[2][4];
@@ -110,7 +113,6 @@ __global__ void __launch_bounds__(QL_WARPS * 32, NT == 1 ? 4 : 1) qlinear_kernel
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < QL_WARPS; ++w) v += red[w][row][tok];
-    v *= TWO_69;
     const int r = tile * 16 + row;
     if (r < sg.N && tok0 + tok < a.M) {
       const size_t o = (size_t)(tok0 + tok) * a.ldo + sg.out_off + r;
