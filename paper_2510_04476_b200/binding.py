@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import subprocess
 from typing import Dict, Optional
 
 import torch
@@ -21,6 +22,29 @@ _BIND = None
 
 class CcaError(RuntimeError):
     pass
+
+
+class _NoExtension:
+    """In the extension's place where it cannot be used: every 4-bit call raises, the others do not need it."""
+
+    def __init__(self, why: str):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise CcaError(f"the 4-bit entry points need the extension _bind.so (python -m paper_2510_04476_b200.build): {self._why}")
+
+
+def _load_extension(build_if_missing: bool):
+    try:
+        if build_if_missing:
+            _build.build_bind()
+        elif not _build.bind_fits():
+            raise ImportError("it is missing or was built for another Python or torch")
+        from . import _bind
+    except (ImportError, OSError, RuntimeError, subprocess.SubprocessError) as e:
+        return _NoExtension(f"{type(e).__name__}: {e}")
+    _bind.set_error(CcaError)
+    return _bind
 
 
 class cca_config(C.Structure):
@@ -145,7 +169,7 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     global _LIB
     if _LIB is not None:
         return _LIB
-    path = _build.build() if build_if_missing else _build.LIB
+    path = _build.build_library() if build_if_missing else _build.LIB
     if not os.path.exists(path):
         raise CcaError(f"{path} is missing: build the CUDA library first (python -m paper_2510_04476_b200.build)")
     lib = C.CDLL(path)
@@ -154,9 +178,7 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
         fn.restype = res
         fn.argtypes = args
     global _BIND
-    from . import _bind
-    _bind.set_error(CcaError)
-    _BIND = _bind
+    _BIND = _load_extension(build_if_missing)
     _LIB = lib
     return lib
 
@@ -197,7 +219,9 @@ class CCA:
         self.device = torch.device("cuda", device)
         self.handle = C.c_void_p()
         _check(self.lib, self.lib.cca_init(C.byref(self.cfg), device, C.byref(self.handle)), None, "cca_init")
-        self._native = _BIND.new_handle(self.handle.value, d_model, n_q_heads, n_kv_heads, head_dim, k_seq, k_ch, device)
+        self._native = None
+        if not isinstance(_BIND, _NoExtension):
+            self._native = _BIND.new_handle(self.handle.value, d_model, n_q_heads, n_kv_heads, head_dim, k_seq, k_ch, device)
 
     @classmethod
     def from_shape(cls, sh, device=0) -> "CCA":

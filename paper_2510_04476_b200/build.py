@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcca.so")
+HEADER = os.path.join(HERE, "..", "include", "cca.h")
 BIND = os.path.join(HERE, "_bind.so")          # CPython extension: argument marshalling of the 4-bit entry points
 SOURCES = ["cca_api.cu", "gemm_simt.cu", "transform.cu", "attn_simt.cu", "tc_kernels.cu", "tc_gemm2.cu", "tc_attn.cu", "tc_attn_bwd.cu", "tc_attn_bwd_fused.cu", "tc_transform.cu", "tc_transform2.cu", "tc_transform_bwd.cu", "decode.cu", "tc_attn256.cu", "transform_unfused.cu", "bwd_unfused.cu", "mla.cu", "qcache.cu", "qlinear.cu", "tc_qlinear.cu"]
 NVCC_FLAGS = [
@@ -16,12 +17,36 @@ NVCC_FLAGS = [
 ]
 
 
+def _older(path: str, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
+
+
+def _lib_stale() -> bool:
+    return _older(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [HEADER])
+
+
+def _built_for() -> str:
+    """The Python and the torch that the extension is compiled against; it carries this text."""
+    import sysconfig
+
+    import torch
+    return f"built for {sysconfig.get_config_var('SOABI')}, torch {torch.__version__}"
+
+
+def bind_fits() -> bool:
+    """Whether there is an extension and it was compiled against this Python and this torch."""
+    if not os.path.exists(BIND):
+        return False
+    with open(BIND, "rb") as f:
+        return _built_for().encode() + b"\0" in f.read()
+
+
+def _bind_stale() -> bool:
+    return _older(BIND, [os.path.join(CSRC, "bind.cpp"), HEADER]) or not bind_fits()
+
+
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(BIND):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BIND))
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "cca.h")]
-    return any(os.path.getmtime(p) > t for p in deps)
+    return _lib_stale() or _bind_stale()
 
 
 def _bind_commands(bdir: str):
@@ -34,6 +59,7 @@ def _bind_commands(bdir: str):
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"))), "include")
     cxx = os.environ.get("CXX", "g++")
     compile_ = [cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                f'-DCCA_BUILT_FOR="{_built_for()}"',
                 "-I" + os.path.join(root, "include"), "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I" + cuda,
                 "-I" + sysconfig.get_paths()["include"], "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
     link = [cxx, "-shared", "-o", BIND, obj, "-L" + HERE, "-l:libcca.so", "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda",
@@ -41,9 +67,21 @@ def _bind_commands(bdir: str):
     return compile_, link
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu into objects (in parallel) and link libcca.so next to this file, then the Python extension over it."""
-    if not force and not _stale():
+def _finish(src: str, p, log) -> None:
+    out, _ = p.communicate()
+    log.append(f"== {src}\n{out}")
+    if p.returncode != 0:
+        sys.stderr.write(out)
+        raise RuntimeError(f"the compiler failed on {src}")
+
+
+def _start(cmd):
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """Compile every .cu into objects (in parallel) and link libcca.so next to this file."""
+    if not force and not _lib_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     bdir = os.path.join(HERE, "_build")
@@ -53,24 +91,34 @@ def build(force: bool = False, verbose: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(bdir, src.replace(".cu", ".o"))
         objs.append(obj)
-        cmd = [nvcc, *NVCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
-        procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    bind_compile, bind_link = _bind_commands(bdir)
-    procs.append(("bind.cpp", subprocess.Popen(bind_compile, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        procs.append((src, _start([nvcc, *NVCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])))
     log = []
     for src, p in procs:
-        out, _ = p.communicate()
-        log.append(f"== {src}\n{out}")
-        if p.returncode != 0:
-            sys.stderr.write(out)
-            raise RuntimeError(f"the compiler failed on {src}")
+        _finish(src, p, log)
     with open(os.path.join(bdir, "ptxas.log"), "w") as f:
         f.write("\n".join(log))
     if verbose:
         print("\n".join(log))
-    cmd = [nvcc, "-shared", "-o", LIB, *objs, "-lcudart"]
-    subprocess.run(cmd, check=True)
-    subprocess.run(bind_link, check=True)
+    subprocess.run([nvcc, "-shared", "-o", LIB, *objs, "-lcudart"], check=True)
+    return LIB
+
+
+def build_bind(force: bool = False) -> str:
+    """Compile the Python extension and link it over libcca.so, which has to be there."""
+    if not force and not _bind_stale():
+        return BIND
+    bdir = os.path.join(HERE, "_build")
+    os.makedirs(bdir, exist_ok=True)
+    compile_, link = _bind_commands(bdir)
+    _finish("bind.cpp", _start(compile_), [])
+    subprocess.run(link, check=True)
+    return BIND
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """The library, then the Python extension over it."""
+    build_library(force, verbose)
+    build_bind(force)
     return LIB
 
 

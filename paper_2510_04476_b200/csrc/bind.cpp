@@ -24,11 +24,14 @@ struct Handle {                      // what the methods need of a CCA object
   int device;
 };
 
-PyObject* cca_error = nullptr;
+// The Python and the torch that this was compiled against, for the build to compare.
+__attribute__((used)) const char built_for[] = CCA_BUILT_FOR;
+
+PyObject* cca_error = nullptr;       // the package's CcaError once it has been set
 struct Raised {};                    // a Python exception is set
 
 [[noreturn]] void refuse(const std::string& msg) {
-  PyErr_SetString(cca_error, msg.c_str());
+  PyErr_SetString(cca_error ? cca_error : PyExc_RuntimeError, msg.c_str());
   throw Raised();
 }
 Handle* handle_of(PyObject* o) {
