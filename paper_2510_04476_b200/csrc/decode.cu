@@ -137,8 +137,6 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) decode_proj_kernel(ProjArgs a) 
 }
 
 // ------------------------------------------------------------------------------------------------ transforms
-// Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
-// the history for the next token and the input the next step's value shift needs.
 // Where a step's new key and value go: row pos[b] of the bf16 caches or, on a 4-bit cache (qlen set), row qlen[b].  False: this
 // sequence's position or length does not fit its cache.
 CCA_DEVINL bool new_row(const int* pos, const int* qlen, long long S_max, int max_len, int b, int& t, size_t& row) {
@@ -169,6 +167,8 @@ struct C1Args {
   int* status;
 };
 
+// Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
+// the history for the next token and the input the next step's value shift needs.
 __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
   pdl_enter();
   const CcaDims& d = a.d;

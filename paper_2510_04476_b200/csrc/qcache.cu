@@ -14,13 +14,6 @@ using namespace q4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int MAX_DEVICES = 64;
 
-// A row's scales as words; d_h = 32 has a single 16-bit scale.
-template <int DH>
-CCA_DEVINL void load_scales(uint32_t (&w)[Row<DH>::SW], const bf16* p) {
-  if constexpr (DH == 32) w[0] = __ldcs(reinterpret_cast<const unsigned short*>(p));
-  else load_words<Row<DH>::SW>(w, p);
-}
-
 // ------------------------------------------------------------------------------------------------ rows in and out
 struct IoArgs {
   const bf16 *k, *v;             // [B, n, hk, dh]

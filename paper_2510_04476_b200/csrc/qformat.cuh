@@ -66,26 +66,16 @@ CCA_DEVINL float scale_at(const uint32_t (&w)[NW], int i) {
   return (i & 1) ? bf_hi(w[i >> 1]) : bf_lo(w[i >> 1]);
 }
 
-// NW consecutive 32-bit words (NW = 1, 2, 4, 8; the address is a multiple of min(16, 4 NW) bytes), read once: streamed.
+// NW = 2 or 4 consecutive 32-bit words (the address is a multiple of their size), read once: streamed.
 template <int NW>
 CCA_DEVINL void load_words(uint32_t (&w)[NW], const void* p) {
-  if constexpr (NW == 1) {
-    w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
-  } else if constexpr (NW == 2) {
+  if constexpr (NW == 2) {
     const uint2 u = __ldcs(reinterpret_cast<const uint2*>(p));
     w[0] = u.x; w[1] = u.y;
   } else {
-#pragma unroll
-    for (int i = 0; i < NW / 4; ++i) {
-      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-      w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
-    }
+    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
   }
-}
-template <int NW>
-CCA_DEVINL void zero_words(uint32_t (&w)[NW]) {
-#pragma unroll
-  for (int i = 0; i < NW; ++i) w[i] = 0u;
 }
 
 CCA_DEVINL float divide(float a, float b) {                // to nearest, subnormal numbers as they are whatever the build's setting
