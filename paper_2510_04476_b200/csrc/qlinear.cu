@@ -2,6 +2,7 @@
 #include "pdl.cuh"
 #include "qformat.cuh"
 #include "qlinear.cuh"
+#include "tc_state.cuh"
 
 namespace {
 
@@ -122,11 +123,27 @@ __global__ void __launch_bounds__(QL_WARPS * 32, NT == 1 ? 4 : 1) qlinear_kernel
   }
 }
 
-template <int NT>
-cudaError_t run_nt(const QLinArgs& a, cudaStream_t st) {
+int row_tiles(const QLinArgs& a) {
   int tiles = 0;
   for (int s = 0; s < a.n_seg; ++s) tiles += (a.seg[s].N + 15) / 16;
-  return launch_pdl(qlinear_kernel<NT>, dim3((unsigned)tiles, (unsigned)((a.M + NT * 8 - 1) / (NT * 8))), dim3(QL_WARPS * 32), st, a);
+  return tiles;
+}
+template <int NT>
+cudaError_t run_nt(const QLinArgs& a, cudaStream_t st) {
+  return launch_pdl(qlinear_kernel<NT>, dim3((unsigned)row_tiles(a), (unsigned)((a.M + NT * 8 - 1) / (NT * 8))), dim3(QL_WARPS * 32), st, a);
+}
+
+// Whether more than 8 tokens go to the tcgen05 kernel.  The kernel here takes 32 of them at a time, one CTA an SM, in 1 us and 1 more for
+// every 1024 columns a wave of CTAs; the other one takes 4 to 9 us however small the matrix is.  They cross at two waves or 4096
+// columns in all.  us, this one | tcgen05, at 9, 32 and 64 tokens:
+//   1000 x 1024   2.2  2.9  2.7 |  4.9  5.5  6.3        4096 x 2048    5.9  7.4 13.2 |  6.4  7.0  9.1
+//   4096 x 1024   4.1  4.9  8.7 |  5.1  5.6  7.7        8192 x 1024    6.8  8.5 15.0 |  6.2  6.8  8.0
+//   2368 x 2048   3.4  4.6  7.7 |  6.1  6.7  8.7         960 x 8192    8.5 10.4      |  8.2  8.9
+//   1536 x 4096   5.3  6.5 11.4 |  6.7  7.1  9.0        4096 x 4096   11.2 13.1 23.0 |  8.8  9.6 11.8
+//   2368 x 4096   5.4  6.8 12.5 |  8.0  8.8 11.2       16383 x 8192   64.2 74.3  136 | 29.2 31.0 36.5
+bool tcgen05_pays(const QLinArgs& a, int sm_count) {
+  const long long ctas = (long long)row_tiles(a) * ((a.M + 31) / 32), waves = (ctas + sm_count - 1) / sm_count;
+  return waves > 2 || waves * a.K > 4096;
 }
 
 }  // namespace
@@ -145,9 +162,9 @@ int launch_qlinear_pack(const bf16* w, uint8_t* codes, bf16* scales, int N, int 
 }
 
 int launch_qlinear(const QLinArgs& a, TcState* tc, int* status, long long* launches, cudaStream_t st) {
-  // 8 tokens cost here what 1 costs; from 9 on the tcgen05 kernel takes over (32 x 4096 x 1024: 5.7 us against 7.7, 64 x 8192 x 8192: 22.9
-  // against 95.6), unless the handle has the tensor-core kernels switched off
-  if (tc && a.M > 8) {
+  // 8 tokens cost here what 1 costs (on a tall matrix two passes of 8 take longer than the tcgen05 kernel: 16 x 16383 x 8192 38.0 us against
+  // 29.3), unless the handle has the tensor-core kernels switched off
+  if (tc && a.M > 8 && tcgen05_pays(a, tc->sm_count)) {
     const int r = tc_qlinear(tc, a, status, st);
     if (r < 0) return r;
     if (r == 0) { ++*launches; return 0; }

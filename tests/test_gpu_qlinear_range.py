@@ -32,3 +32,17 @@ def test_product_of_weights_of_any_size(cca, M, w_exp, x_exp):
     err = (y - ref).abs() / mag
     assert float(err.max()) <= 2.0 ** -23 * (K / 256 + 48), float(err.max() * 2 ** 23)
     assert cca.last_status() == 0
+
+
+@pytest.mark.parametrize("N,K", [(1000, 1024), (2368, 4096), (2369, 4096), (2368, 4128), (4736, 2048), (4737, 2048), (4736, 2080), (1180, 4096)])
+@pytest.mark.parametrize("M", [8, 9, 32, 33, 64, 65, 97])
+def test_product_on_both_sides_of_the_change_of_kernel(cca, M, N, K):
+    """16 x 148 and 32 x 148 rows, 4096 columns in all: where one kernel takes over from the other."""
+    gen = torch.Generator(device="cuda").manual_seed(M + N + K)
+    w = (0.05 * torch.randn(N, K, generator=gen, device="cuda")).bfloat16()
+    x = torch.randn(M, K, generator=gen, device="cuda").bfloat16()
+    y = cca.qlinear(cca.qlinear_pack(w), x, out_dtype=torch.float32).double()
+    w64 = Q.values(*Q.quantise(w)).cuda()
+    ref, mag = x.double() @ w64.t(), x.double().abs() @ w64.abs().t()
+    assert ((y - ref).abs() <= 2.0 ** -23 * (K / 256 + 48) * mag).all(), float(((y - ref).abs() / mag).max() * 2 ** 23)
+    assert cca.last_status() == 0
