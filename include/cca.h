@@ -284,13 +284,17 @@ int cca_mla_forward(cca_handle* h, const cca_mla_dims* m, const cca_mla_weights*
  * channel 32 grp + 4 i + j (bits 7, 0-2) and channel 32 grp + 4 i + 2 + j (bits 6, 3-5).
  *
  * No call here allocates or synchronises; every call may be captured into a graph.  Calls that share a cache or a workspace are
- * ordered by the caller.  The caller's current device is left as it was. */
+ * ordered by the caller.  The caller's current device is left as it was.  Limits, UNSUPPORTED beyond them: B <= 65535, S_max <= 2^24,
+ * B n <= 2^30 new or read rows, B max_len <= 2^30, weights of N <= 2^24 rows and K <= 2^20 columns. */
 typedef struct {
   void* k_codes;        /* uint8 [B, h_k, S_max, d_h / 2]: keys after norm, temperature and RoPE (Eq. 11)            */
   void* v_codes;        /* uint8 [B, h_k, S_max, d_h / 2]: values (Eq. 10)                                           */
   void* k_scales;       /* bf16 [B, h_k, S_max, d_h / 32]                                                            */
   void* v_scales;       /* bf16 [B, h_k, S_max, d_h / 32]                                                            */
-  float* weight;        /* fp32 [B, h_k, S_max]: attention weight each row has gathered; may be null (then no eviction) */
+  float* weight;        /* fp32 [B, h_k, S_max]: attention weight each row has gathered; may be null (then no eviction).
+                           Attention of later tokens alone gives weight: rows that a prefill or an append put in start
+                           from 0, whatever the prompt's own tokens attended to, and until tokens have been decoded an
+                           eviction goes by position and row                                                       */
   int32_t* position;    /* int32 [B, h_k, S_max]: position of each row's token; may be null (then no eviction)       */
   int32_t* len;         /* int32 [B]: rows held, the same for every head; cca_qcache_evict alone writes it           */
   int64_t S_max;        /* capacity in rows                                                                          */

@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
 // Joins the chunks' partial results of one (sequence, kv head) and, where the weights are gathered, adds to every row what its
 // heads gave it: 2^(logit - maximum) / sum, from the logits that the first kernel left.  Maximum and sum stay apart: a large maximum would
 // swallow the logarithm of the sum.  Its time is latency: the logits and weights of its rows are asked for before the sums that they wait for are formed, and a head's
-// channels are shared out so that no thread adds up more than four chunks (1 x 16384 rows, both kernels: 7.1 us, 8.0 with a CTA a head).
+// channels are shared out so that no thread adds up more than four chunks (1 x 16384 rows, both kernels: 7.4 us, 0.9 more with a CTA a head).
 constexpr int QJ_ROWS = 4;                                 // rows of a thread, where the weights are gathered
 template <int DH>
 __global__ void __launch_bounds__(256) qcache_join_kernel(QaArgs a) {
@@ -787,8 +787,8 @@ size_t attn_parts(const CcaDims& d, int max_len, int sm_count) {
 }
 
 // One launch does where 8 chunks hold the sequence that have no more rows than 256 or than the plan above gives a chunk (d_h 128, h_q 8,
-// h_k 2, in a graph: 1 x 1024 rows 5.1 us against 6.2 in two launches, 1 x 2048 6.3 against 6.0, 1 x 4096 8.4 against 6.5, 32 x 4096
-// 16.9 against 18.3; called one by one, 5.7 against 8.5 us of host time), one CTA has all of a kv head's query heads, and a chunk's logits
+// h_k 2, in a graph: 1 x 1024 rows 5.1 us against 6.0 in two launches, 1 x 2048 6.3 against 6.2, 1 x 4096 8.6 against 6.3, 32 x 4096
+// 17.7 against 20.8; called one by one, 5.7 against 8.5 us of host time), one CTA has all of a kv head's query heads, and a chunk's logits
 // find room.  Chunks of 128 rows: a stage for each warp.
 bool attn_fused(const CcaDims& d, int max_len, int sm_count, int gather, int plan_chunk, int* chunk, int* splits) {
   if (d.g > heads_per_cta(d)) return false;

@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256) qlinear_pack_kernel(PackArgs a) {
 // order.  A lane's 16 bytes of a weight row are 8 channels of each of 4 groups: two instructions per group, whose sum is multiplied
 // by the group's scale in fp32.  The codes are exact operands, so the only roundings are fp32's.  A group's sum comes out times 2^-69, which
 // its scale takes off before the groups are added: sums of small weights would fall below the smallest normal number.
-// At few tokens it is bound by the 200 instructions that a block of 16 rows by 128 columns takes, and what hides their latency is
+// At few tokens it is bound by the 204 instructions that a block of 16 rows by 128 columns takes, and what hides their latency is
 // warps: four CTAs per SM with one block of each warp on its way take 18.7 us for 5 x 16383 x 8192 (75 MB: 64 % of the measured copy
 // rate), three with two or three 20.1 to 21.2, two with four 21.1; rings of asynchronous copies under CTAs that stay (16 or 32 warps, x in
 // registers or in shared memory, one row tile or two) 22.6 to 24.3.

@@ -224,8 +224,8 @@ tc_qlinear_kernel(const __grid_constant__ CUtensorMap tm0, const __grid_constant
     const int r = q * 32 + lane;
     // The tensor cores cut off what an add shifts out, always towards the same side, so that a chain's error grows with its length (64 x 8192
     // x 8192 in chains of 512 adds: 4.6e-6 relative to 64 bits, of 1024 9.7e-6).  So a chain is TQ_CHUNK blocks, 64 adds; its sum is added to
-    // those before it in fp32 by the warps that have its rows, while the other accumulator takes the next chunk.  4.8e-7 for any K,
-    // 22.9 us (one chain: 21.3; chunks of 3: 3.6e-7, 23.9; of 6: 7.0e-7, 22.5).
+    // those before it in fp32 by the warps that have its rows, while the other accumulator takes the next chunk: 4.8e-7,
+    // and for longer rows one fp32 add more for every 64; 22.9 us (one chain: 21.3; chunks of 3: 3.6e-7, 23.9; of 6: 7.0e-7, 22.5).
     int next = 0;                                          // the chunk to be taken over next
     auto take_over = [&](int end) -> bool {
       for (; next < end; ++next) {
