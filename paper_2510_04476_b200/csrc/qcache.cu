@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(QA_WARPS * 32, qa_resident(DH, NHT)) qcache_at
   }
   const float c_scale = rsqrtf((float)DH) * LOG2E * TWO_69;
 
-  // softmax state of heads 2t, 2t + 1 (+ 8 ht): a reference that no logit passes by more than 2^SLACK (the maximum of when it was last
+  // softmax state of heads 2t, 2t + 1 (+ 8 ht): a reference that no logit passes by more than SLACK (the maximum of when it was last
   // moved), the same in all lanes of a column, and sums per lane.  Nothing is ever added to a logit but another logit, so that large ones
   // keep their differences.  The values' scales carry 2^70, which the bf16 subnormals of their codes need: scales of up to 2^48 stay
   // in range, and so do products of probability and scale down to 2^-63.
