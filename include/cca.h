@@ -379,6 +379,102 @@ int cca_decode_step_q(cca_handle* h, const cca_q_weights* w, const void* x, void
 int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B,
                                     int64_t S, const cca_q_decode_state* state, void* cuda_stream);
 
+/* ---- Cache in pages (serving) ----------------------------------------------------------------------
+ * The bf16 latent cache for many sequences of unknown length, or several continuations of one prompt: a pool of pages, each page_size
+ * rows of every kv head, and for each sequence a row of page numbers.  Row r of sequence b is place r % page_size of page
+ * table[b, r / page_size].  refs[p] counts the table entries that name page p; 0: it is free.  A page that several sequences hold is
+ * only read: cca_pages_reserve gives each its own copy before rows are put there.
+ *
+ * No call here allocates device memory or synchronises; every call may be captured into a graph.  Calls that share pages or a workspace
+ * are ordered by the caller.  The caller's current device is left as it was.  Results do not depend on the order in which threads run.
+ * The tables are the caller's to set up (refs 0, table -1, len 0 for an empty pool) and to keep consistent; an entry outside [0, n_pages)
+ * names no page, and no call reads or writes outside the pool whatever the tables hold.
+ * B sequences are rows 0 .. B - 1 of table and len; the rows of some sequences that lie one after the other are a cca_pages of their own,
+ * except for cca_pages_compact, which has to see every sequence that holds a page of the pool.
+ * Limits, UNSUPPORTED beyond them: B <= 65535, page_size <= 65536, max_pages * page_size <= 2^24 rows a sequence, n_pages * h_k * page_size
+ * < 2^31 rows of the pool, B * max_pages <= 2^30, B n <= 2^30 new or read rows. */
+typedef struct {
+  void* k;              /* bf16 [n_pages, h_k, page_size, d_h]: keys after norm, temperature and RoPE (Eq. 11)        */
+  void* v;              /* bf16 [n_pages, h_k, page_size, d_h]: values (Eq. 10)                                       */
+  int32_t* refs;        /* int32 [n_pages]                                                                            */
+  int32_t* table;       /* int32 [B, max_pages]: page numbers, -1 where there is none                                 */
+  int32_t* len;         /* int32 [B]: rows held; cca_pages_fork and cca_pages_free alone write it                     */
+  int64_t n_pages, page_size, max_pages;
+} cca_pages;
+
+/* Bytes of device workspace that one cca_pages_reserve, _fork or _compact call needs (one size for all). */
+int cca_pages_workspace_size(const cca_handle* h, int64_t n_pages, int64_t max_pages, int64_t B, size_t* bytes);
+
+/* Gives every sequence pages that it holds alone for its rows first[b] .. first[b] + n - 1 (len[b] .. where `first` is null; only the
+ * first min(count[b], n) of them where `count`, device int32 [B], is given).  Of the table entries of these rows, those without a page
+ * get a new one, and those whose page others hold too (refs > 1) get a new one with the old one's contents (all of its rows); if all who hold it ask
+ * for it in the same call, the last of them keeps it.  New pages are the free ones with the lowest numbers, ascending, for the sequences in order
+ * and their pages in order.  Rows that have such pages already cost nothing, so the call may come before every step or once for many.
+ * All or nothing: if more pages are needed than are free, nothing changes and the device status word becomes 123.  A sequence whose rows
+ * would pass max_pages * page_size, or whose first row is negative, is left as it is and the status word becomes 122.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE_TOO_SMALL, CUDA. */
+int cca_pages_reserve(cca_handle* h, const cca_pages* pages, int64_t n, const int32_t* count, const int32_t* first, void* workspace,
+                      size_t workspace_bytes, int64_t B, void* cuda_stream);
+
+/* Sequence child[i] becomes what sequence parent[i] was before the call, i < n <= B (device int32 [n]): it holds the pages of the parent's
+ * len rows too (none that were reserved behind them), its own former pages are let go.  A sequence that is its own parent is left as it is; where
+ * several pairs have the same child the last one counts; a pair with an index outside [0, B), or whose parent's length is negative or has no
+ * room in the table, is skipped and the status word becomes 122.  The rest of a decode state (history, previous input) is the caller's to
+ * copy.  Errors as above. */
+int cca_pages_fork(cca_handle* h, const cca_pages* pages, const int32_t* parent, const int32_t* child, int64_t n, void* workspace,
+                   size_t workspace_bytes, int64_t B, void* cuda_stream);
+
+/* Sequence b keeps its first min(keep[b], len[b]) rows (device int32 [B]): len[b] becomes that, and the pages behind these rows are let go, those
+ * reserved behind its length among them.  0 frees the sequence; a negative number leaves it as it is.  Errors as above. */
+int cca_pages_free(cca_handle* h, const cca_pages* pages, const int32_t* keep, int64_t B, void* cuda_stream);
+
+/* Moves the held pages to the front of the pool: with U held pages, those numbered U or more, ascending, move to the free ones below U,
+ * ascending, and the table follows.  used: device int32 [1], becomes U.  What lay in the pages that are free afterwards stays there.
+ * Errors as above. */
+int cca_pages_compact(cca_handle* h, const cca_pages* pages, int32_t* used, void* workspace, size_t workspace_bytes, int64_t B,
+                      void* cuda_stream);
+
+/* Puts n new tokens of every sequence into its pages: k, v device bf16 [B, n, h_k, d_h]; row len[b] + i gets token i; only the first
+ * min(count[b], n) of them where `count` (device int32 [B]) is given.  len is not advanced: the caller does that.  A row whose page is
+ * missing or held by others too, or that passes the table, is not written, and the status word becomes 122.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int cca_paged_append(cca_handle* h, const void* k, const void* v, const int32_t* count, const cca_pages* pages, int64_t B, int64_t n,
+                     void* cuda_stream);
+
+/* Rows first[b] .. first[b] + n - 1 (len[b] .. where `first` is null): k, v device bf16 [B, n, h_k, d_h]; zeros for rows without a page.
+ * Errors as above. */
+int cca_paged_read(cca_handle* h, const cca_pages* pages, const int32_t* first, void* k, void* v, int64_t B, int64_t n, void* cuda_stream);
+
+/* Bytes of device workspace that one cca_paged_attention call needs for sequences of at most max_len rows, of B sequences or fewer.
+ * Depends on the device's SM count as cca_decode_workspace_size does. */
+int cca_paged_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
+
+/* softmax(q k^T / sqrt(d_h)) v (Eq. 11, third line) of one query token per sequence over its len[b] rows: q, o device bf16 [B, h_q, d_h].
+ * lse (device fp32 [B, h_q], may be null): the logarithm of the sum of the exponentials, for joining with attention over other rows.
+ * A sequence without rows gets zeros, and -infinity.  A row whose page is missing is left out and the status word becomes 122.  max_len:
+ * host-side bound, len[b] <= max_len <= max_pages * page_size; a sequence outside it is skipped (its output is left as it is) and the status word
+ * becomes 122.  Places behind len[b] may hold anything.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE_TOO_SMALL, CUDA. */
+int cca_paged_attention(cca_handle* h, const void* q, void* o, float* lse, const cca_pages* pages, int64_t max_len, void* workspace,
+                        size_t workspace_bytes, int64_t B, void* cuda_stream);
+
+/* The decode step on a cache in pages: cca_decode_step with the new key and value put into row len[b], for which the caller has reserved
+ * a page, and attention over len[b] + 1 rows.  A token's position is its row.  The caller advances len after the step.  max_len: len[b] + 1 <=
+ * max_len <= max_pages * page_size.  A sequence outside it, or whose new row has no page of its own, is skipped: nothing of its state
+ * is written, its output row is undefined, and the status word becomes 122.  Limits and errors as cca_decode_step, except that every
+ * number of query heads per kv head is covered. */
+typedef struct {
+  cca_pages pages;
+  void* qk0_hist;       /* as in cca_decode_state                                                                    */
+  void* x_prev;
+} cca_paged_decode_state;
+int cca_decode_workspace_size_paged(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes);
+int cca_decode_step_paged(cca_handle* h, const cca_weights* w, const void* x, void* out, const cca_paged_decode_state* state,
+                          int64_t max_len, void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream);
+/* cca_decode_state_from_prefill for a cache in pages: appends the S keys and values of each sequence, for whose rows pages are reserved and whose len
+ * must be 0 for them to be the tokens' own, and fills the history and previous input.  The caller then sets len = S. */
+int cca_decode_state_from_prefill_paged(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B,
+                                        int64_t S, const cca_paged_decode_state* state, void* cuda_stream);
+
 /* Select kernel implementations: 0 = plain SIMT kernels, 1 = tcgen05/TMA kernels where they
  * exist (default).  Returns the previous value. */
 int cca_set_impl(cca_handle* h, int impl);
@@ -410,7 +506,8 @@ int64_t cca_launch_count(const cca_handle* h);
 
 /* After the caller has synchronised the stream: copies the device status word.  0 = no error;
  * otherwise the code written by a kernel whose bounded wait expired (101..105 by role, 109 from
- * cca_wait_selftest; 120: a decode step met a position outside its cache; 121: a sequence's rows do not fit its 4-bit cache).  Returns
+ * cca_wait_selftest; 120: a decode step met a position outside its cache; 121: a sequence's rows do not fit its 4-bit cache; 122: a
+ * row without a page of its sequence's own, or an index outside its range; 123: more pages asked for than are free).  Returns
  * CCA_ERR_DEVICE_TIMEOUT if it is non-zero, and clears the word. */
 int cca_last_status(cca_handle* h, int* device_status);
 

@@ -1,5 +1,5 @@
-"""Thin binding over libcca.so: argument marshalling only, by ctypes and, for the 4-bit entry points, whose calls are a few
-microseconds long, by a small CPython extension (csrc/bind.cpp).
+"""Thin binding over libcca.so: argument marshalling only, by ctypes and, for the serving entry points (4-bit data,
+pages), whose calls are a few microseconds long, by a small CPython extension (csrc/bind.cpp).
 
 Every step of the block runs inside the library's CUDA kernels; torch is used here for device
 memory and streams.  There is no CPU fallback: if the library cannot be loaded, or a call fails,
@@ -25,13 +25,13 @@ class CcaError(RuntimeError):
 
 
 class _NoExtension:
-    """In the extension's place where it cannot be used: every 4-bit call raises, the others do not need it."""
+    """In the extension's place where it cannot be used: every 4-bit call and every call on pages raises, the others do not need it."""
 
     def __init__(self, why: str):
         self._why = why
 
     def __getattr__(self, name):
-        raise CcaError(f"the 4-bit entry points need the extension _bind.so (python -m paper_2510_04476_b200.build): {self._why}")
+        raise CcaError(f"the 4-bit and the paged entry points need the extension _bind.so (python -m paper_2510_04476_b200.build): {self._why}")
 
 
 def _load_extension(build_if_missing: bool):
@@ -85,6 +85,15 @@ class cca_mla_weights(C.Structure):
 class cca_decode_state(C.Structure):
     _fields_ = [("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("qk0_hist", C.c_void_p), ("x_prev", C.c_void_p),
                 ("pos", C.c_void_p), ("S_max", C.c_int64)]
+
+
+class cca_pages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "refs", "table", "len")] + \
+               [(n, C.c_int64) for n in ("n_pages", "page_size", "max_pages")]
+
+
+class cca_paged_decode_state(C.Structure):
+    _fields_ = [("pages", cca_pages), ("qk0_hist", C.c_void_p), ("x_prev", C.c_void_p)]
 
 
 class cca_qcache(C.Structure):
@@ -148,6 +157,23 @@ SYMBOLS = {
                                     C.c_int64, C.c_void_p, C.c_size_t, C.c_int64, C.c_void_p]),
     "cca_decode_state_from_prefill_q": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64, C.c_int64,
                                                   C.POINTER(cca_q_decode_state), C.c_void_p]),
+    "cca_pages_workspace_size": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "cca_pages_reserve": (C.c_int, [C.c_void_p, C.POINTER(cca_pages), C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64,
+                                    C.c_void_p]),
+    "cca_pages_fork": (C.c_int, [C.c_void_p, C.POINTER(cca_pages), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_int64,
+                                 C.c_void_p]),
+    "cca_pages_free": (C.c_int, [C.c_void_p, C.POINTER(cca_pages), C.c_void_p, C.c_int64, C.c_void_p]),
+    "cca_pages_compact": (C.c_int, [C.c_void_p, C.POINTER(cca_pages), C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_paged_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(cca_pages), C.c_int64, C.c_int64, C.c_void_p]),
+    "cca_paged_read": (C.c_int, [C.c_void_p, C.POINTER(cca_pages), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]),
+    "cca_paged_workspace_size": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "cca_paged_attention": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(cca_pages), C.c_int64, C.c_void_p,
+                                      C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_decode_workspace_size_paged": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
+    "cca_decode_step_paged": (C.c_int, [C.c_void_p, C.POINTER(cca_weights), C.c_void_p, C.c_void_p, C.POINTER(cca_paged_decode_state),
+                                        C.c_int64, C.c_void_p, C.c_size_t, C.c_int64, C.c_void_p]),
+    "cca_decode_state_from_prefill_paged": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int64, C.c_int64,
+                                                      C.POINTER(cca_paged_decode_state), C.c_void_p]),
     "cca_set_impl": (C.c_int, [C.c_void_p, C.c_int]),
     "cca_set_attention_events": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "cca_set_stage_events": (C.c_int, [C.c_void_p, C.POINTER(C.c_void_p), C.c_int]),
@@ -514,6 +540,87 @@ class CCA:
     def decode_state_from_prefill_q(self, x: torch.Tensor, workspace: torch.Tensor, state):
         """cca_decode_state_from_prefill_q: the keys and values a forward of x left in `workspace` go into the 4-bit cache."""
         _BIND.decode_state_from_prefill_q(self._native, x, workspace, state)
+
+    # ---- cache in pages -------------------------------------------------------------------
+    # Tensors are checked (type, shape, device, contiguous) by the extension; what does not fit raises CcaError.
+    def new_pages(self, n_pages: int, page_size: int, B: int, max_pages: int) -> Dict[str, torch.Tensor]:
+        """Caller-owned tensors of cca_pages: an empty pool and B empty sequences of up to max_pages pages.  Some sequences on their
+        own, for a prefill say: the same dict with rows [b : c] of "table" and "len"."""
+        hk, dh, dev = self.cfg.n_kv_heads, self.cfg.head_dim, self.device
+        pages = {n: torch.zeros(n_pages, hk, page_size, dh, dtype=torch.bfloat16, device=dev) for n in ("k", "v")}
+        return {**pages, "refs": torch.zeros(n_pages, dtype=torch.int32, device=dev),
+                "table": torch.full((B, max_pages), -1, dtype=torch.int32, device=dev),
+                "len": torch.zeros(B, dtype=torch.int32, device=dev)}
+
+    def pages_workspace_size(self, n_pages: int, B: int, max_pages: int) -> int:
+        n = C.c_size_t()
+        _check(self.lib, self.lib.cca_pages_workspace_size(self.handle, n_pages, max_pages, B, C.byref(n)), self.handle,
+               "cca_pages_workspace_size")
+        return int(n.value)
+
+    def alloc_pages_workspace(self, n_pages: int, B: int, max_pages: int) -> torch.Tensor:
+        return torch.empty(self.pages_workspace_size(n_pages, B, max_pages) + 256, dtype=torch.uint8, device=self.device)
+
+    def pages_reserve(self, pages, n: int, workspace: torch.Tensor, count: Optional[torch.Tensor] = None,
+                      first: Optional[torch.Tensor] = None):
+        """cca_pages_reserve: pages that each sequence holds alone for its rows first[b] .. (default: len[b] ..)."""
+        _BIND.pages_reserve(self._native, pages, n, workspace, count, first)
+
+    def pages_fork(self, pages, parent: torch.Tensor, child: torch.Tensor, workspace: torch.Tensor):
+        """cca_pages_fork: sequence child[i] becomes what sequence parent[i] is, on the same pages."""
+        _BIND.pages_fork(self._native, pages, parent, child, workspace)
+
+    def pages_free(self, pages, keep: torch.Tensor):
+        """cca_pages_free: every sequence down to its first keep[b] rows (0: frees it, negative: as it is)."""
+        _BIND.pages_free(self._native, pages, keep)
+
+    def pages_compact(self, pages, workspace: torch.Tensor, used: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """cca_pages_compact: held pages to the front of the pool; returns their number, int32 [1] on the device."""
+        return _BIND.pages_compact(self._native, pages, workspace, used)
+
+    def paged_append(self, pages, k: torch.Tensor, v: torch.Tensor, count: Optional[torch.Tensor] = None):
+        """cca_paged_append: k, v [B, n, h_k, d_h] into rows len[b] .. , for which pages are reserved; `len` is the caller's to advance."""
+        _BIND.paged_append(self._native, pages, k, v, count)
+
+    def paged_read(self, pages, n: int, first: Optional[torch.Tensor] = None):
+        """cca_paged_read: (k, v), bf16 [B, n, h_k, d_h], of rows first[b] .. (default: len[b] ..)."""
+        return _BIND.paged_read(self._native, pages, n, first)
+
+    def paged_workspace_size(self, B: int, max_len: int) -> int:
+        n = C.c_size_t()
+        _check(self.lib, self.lib.cca_paged_workspace_size(self.handle, B, max_len, C.byref(n)), self.handle, "cca_paged_workspace_size")
+        return int(n.value)
+
+    def alloc_paged_workspace(self, B: int, max_len: int) -> torch.Tensor:
+        return torch.empty(self.paged_workspace_size(B, max_len) + 256, dtype=torch.uint8, device=self.device)
+
+    def paged_attention(self, q: torch.Tensor, pages, max_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None):
+        """cca_paged_attention: q [B, h_q, d_h] -> o over each sequence's len[b] rows; lse, fp32 [B, h_q], is written where it is given."""
+        return _BIND.paged_attention(self._native, q, pages, max_len, workspace, out, lse)
+
+    def new_decode_state_paged(self, n_pages: int, page_size: int, B: int, max_pages: int) -> Dict[str, object]:
+        """Caller-owned tensors of cca_paged_decode_state for B empty sequences: "pages" (new_pages), history, previous input."""
+        s = self.new_decode_state(B, 1)
+        return {"pages": self.new_pages(n_pages, page_size, B, max_pages), **{n: s[n] for n in ("qk0_hist", "x_prev")}}
+
+    def decode_workspace_size_paged(self, B: int, max_len: int) -> int:
+        n = C.c_size_t()
+        _check(self.lib, self.lib.cca_decode_workspace_size_paged(self.handle, B, max_len, C.byref(n)), self.handle,
+               "cca_decode_workspace_size_paged")
+        return int(n.value)
+
+    def alloc_decode_workspace_paged(self, B: int, max_len: int) -> torch.Tensor:
+        return torch.empty(self.decode_workspace_size_paged(B, max_len) + 256, dtype=torch.uint8, device=self.device)
+
+    def decode_step_paged(self, w, x: torch.Tensor, state, max_len: int, workspace: torch.Tensor, out: Optional[torch.Tensor] = None):
+        """cca_decode_step_paged: x [B, E] -> out [B, E]; pages for the new row are reserved before it, and `len` is the caller's to
+        advance after it."""
+        return _BIND.decode_step_paged(self._native, w, x, state, max_len, workspace, out)
+
+    def decode_state_from_prefill_paged(self, x: torch.Tensor, workspace: torch.Tensor, state):
+        """cca_decode_state_from_prefill_paged: the keys and values a forward of x left in `workspace` go into the reserved pages."""
+        _BIND.decode_state_from_prefill_paged(self._native, x, workspace, state)
 
     def backward(self, w, x: torch.Tensor, d_out: torch.Tensor, workspace: torch.Tensor, separate_grads: bool = False):
         """Returns (d_x bf16, dict of fp32 parameter gradients).  separate_grads: give every gradient a buffer of

@@ -1,4 +1,4 @@
-// Argument marshalling of the 4-bit entry points for Python, natively: at a decode step's sizes a call is bound by what the host
+// Argument marshalling of the entry points on 4-bit data and on pages for Python, natively: at a decode step's sizes a call is bound by what the host
 // does for it, and checking a dozen tensors and filling the C structs takes longer in Python than the launches do.  Nothing is kept
 // between calls.  Every check that fails raises the package's CcaError.
 #define PY_SSIZE_T_CLEAN
@@ -129,6 +129,27 @@ cca_q_decode_state state_of(PyObject* d, const Handle* h, int64_t* B) {
   s.x_prev = need(ITEM(d, "x_prev"), "x_prev", at::kBFloat16, {*B, h->E}, h);
   s.pos = static_cast<int32_t*>(need(ITEM(d, "pos"), "pos", at::kInt, {*B}, h));
   return s;
+}
+
+// The dict of tensors that new_pages makes.
+cca_pages pages_of(PyObject* d, const Handle* h, int64_t* B) {
+  cca_pages c;
+  const at::Tensor &k = tensor_of(ITEM(d, "k"), "k"), &table = tensor_of(ITEM(d, "table"), "table");
+  if (k.dim() != 4 || table.dim() != 2) refuse("k: wants four dimensions, table: two");
+  const int64_t n = k.size(0), P = k.size(2), b = table.size(0), wide = table.size(1);
+  c.k = need(k, "k", at::kBFloat16, {n, h->hk, P, h->dh}, h);
+  c.v = need(ITEM(d, "v"), "v", at::kBFloat16, {n, h->hk, P, h->dh}, h);
+  c.refs = static_cast<int32_t*>(need(ITEM(d, "refs"), "refs", at::kInt, {n}, h));
+  c.table = static_cast<int32_t*>(need(table, "table", at::kInt, {b, wide}, h));
+  c.len = static_cast<int32_t*>(need(ITEM(d, "len"), "len", at::kInt, {b}, h));
+  c.n_pages = n;
+  c.page_size = P;
+  c.max_pages = wide;
+  *B = b;
+  return c;
+}
+int32_t* optional_ints(PyObject* o, const char* name, std::initializer_list<int64_t> shape, const Handle* h) {
+  return absent(o) ? nullptr : static_cast<int32_t*>(need(o, name, at::kInt, shape, h));
 }
 
 // A method: refuses the wrong number of arguments, turns C++ exceptions into Python's.
@@ -322,9 +343,179 @@ PyObject* decode_state_from_prefill_q(PyObject*, PyObject* const* a, Py_ssize_t 
   });
 }
 
+// (handle, pages, n, workspace, count | None, first | None)
+PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<6>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    const Workspace ws = workspace_of(a[3], h);
+    const int32_t *count = optional_ints(a[4], "count", {B}, h), *first = optional_ints(a[5], "first", {B}, h);
+    check(cca_pages_reserve(h->h, &c, whole(a[2]), count, first, ws.p, ws.n, B, stream(h)), h, "cca_pages_reserve");
+    return none();
+  });
+}
+// (handle, pages, parent, child, workspace)
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<5>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    const at::Tensor& child = tensor_of(a[3], "child");
+    const int64_t pairs = child.dim() == 1 ? child.size(0) : 0;
+    auto* cp = static_cast<int32_t*>(need(child, "child", at::kInt, {pairs}, h));
+    auto* pp = static_cast<int32_t*>(need(a[2], "parent", at::kInt, {pairs}, h));
+    const Workspace ws = workspace_of(a[4], h);
+    check(cca_pages_fork(h->h, &c, pp, cp, pairs, ws.p, ws.n, B, stream(h)), h, "cca_pages_fork");
+    return none();
+  });
+}
+// (handle, pages, keep)
+PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<3>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    auto* keep = static_cast<int32_t*>(need(a[2], "keep", at::kInt, {B}, h));
+    check(cca_pages_free(h->h, &c, keep, B, stream(h)), h, "cca_pages_free");
+    return none();
+  });
+}
+// (handle, pages, workspace, used | None) -> used
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<4>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    const Workspace ws = workspace_of(a[2], h);
+    at::Tensor made;
+    int32_t* used = optional_ints(a[3], "used", {1}, h);
+    if (!used) {
+      made = fresh({1}, at::kInt, h);
+      used = static_cast<int32_t*>(made.data_ptr());
+    }
+    check(cca_pages_compact(h->h, &c, used, ws.p, ws.n, B, stream(h)), h, "cca_pages_compact");
+    if (made.defined()) return THPVariable_Wrap(std::move(made));
+    Py_INCREF(a[3]);
+    return a[3];
+  });
+}
+// (handle, pages, k, v, count | None)
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<5>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    const at::Tensor& k = tensor_of(a[2], "k");
+    const int64_t rows = k.dim() == 4 ? k.size(1) : 0;
+    const void* kp = need(k, "k", at::kBFloat16, {B, rows, h->hk, h->dh}, h);
+    const void* vp = need(a[3], "v", at::kBFloat16, {B, rows, h->hk, h->dh}, h);
+    const int32_t* count = optional_ints(a[4], "count", {B}, h);
+    check(cca_paged_append(h->h, kp, vp, count, &c, B, rows, stream(h)), h, "cca_paged_append");
+    return none();
+  });
+}
+// (handle, pages, n, first | None) -> (k, v)
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<4>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[1], h, &B);
+    const int64_t rows = whole(a[2]);
+    if (rows < 0) refuse("cca_paged_read: invalid argument");
+    const int32_t* first = optional_ints(a[3], "first", {B}, h);
+    at::Tensor k = fresh({B, rows, h->hk, h->dh}, at::kBFloat16, h), v = fresh({B, rows, h->hk, h->dh}, at::kBFloat16, h);
+    check(cca_paged_read(h->h, &c, first, k.data_ptr(), v.data_ptr(), B, rows, stream(h)), h, "cca_paged_read");
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(k)), THPVariable_Wrap(std::move(v)));
+  });
+}
+// (handle, q, pages, max_len, workspace, out | None, lse | None) -> out
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<7>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_pages c = pages_of(a[2], h, &B);
+    const void* q = need(a[1], "q", at::kBFloat16, {B, h->hq, h->dh}, h);
+    const Workspace ws = workspace_of(a[4], h);
+    const int64_t max_len = whole(a[3]);
+    auto* lse = absent(a[6]) ? nullptr : static_cast<float*>(need(a[6], "lse", at::kFloat, {B, h->hq}, h));
+    at::Tensor made;
+    void* out;
+    if (absent(a[5])) {
+      made = fresh({B, h->hq, h->dh}, at::kBFloat16, h);
+      out = made.data_ptr();
+    } else {
+      out = need(a[5], "out", at::kBFloat16, {B, h->hq, h->dh}, h);
+    }
+    check(cca_paged_attention(h->h, q, out, lse, &c, max_len, ws.p, ws.n, B, stream(h)), h, "cca_paged_attention");
+    if (made.defined()) return THPVariable_Wrap(std::move(made));
+    Py_INCREF(a[5]);
+    return a[5];
+  });
+}
+cca_paged_decode_state paged_state_of(PyObject* d, const Handle* h, int64_t* B) {
+  cca_paged_decode_state s;
+  PyObject* pages = ITEM(d, "pages");
+  if (!pages) refuse("state: wants \"pages\"");
+  s.pages = pages_of(pages, h, B);
+  const int64_t pad = h->k_seq + h->k_ch - 2, L = (h->hq + h->hk) * h->dh;
+  s.qk0_hist = pad > 0 ? need(ITEM(d, "qk0_hist"), "qk0_hist", at::kFloat, {*B, pad, L}, h) : nullptr;
+  s.x_prev = need(ITEM(d, "x_prev"), "x_prev", at::kBFloat16, {*B, h->E}, h);
+  return s;
+}
+// (handle, weights, x, state, max_len, workspace, out | None) -> out
+PyObject* decode_step_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<7>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_paged_decode_state s = paged_state_of(a[3], h, &B);
+    const int64_t Lq = h->hq * h->dh, Lk = h->hk * h->dh, L = Lq + Lk;
+    cca_weights w;
+    w.w_qk = need(ITEM(a[1], "w_qk"), "w_qk", at::kBFloat16, {L, h->E}, h);
+    w.w_v1 = need(ITEM(a[1], "w_v1"), "w_v1", at::kBFloat16, {Lk / 2, h->E}, h);
+    w.w_v2 = need(ITEM(a[1], "w_v2"), "w_v2", at::kBFloat16, {Lk / 2, h->E}, h);
+    w.w_o = need(ITEM(a[1], "w_o"), "w_o", at::kBFloat16, {h->E, Lq}, h);
+    PyObject *c0 = ITEM(a[1], "conv0_w"), *c1 = ITEM(a[1], "conv1_w"), *t = ITEM(a[1], "temp");
+    w.conv0_w = absent(c0) ? nullptr : need(c0, "conv0_w", at::kBFloat16, {L, h->k_seq}, h);
+    w.conv1_w = absent(c1) ? nullptr : need(c1, "conv1_w", at::kBFloat16, {L, h->dh, h->k_ch}, h);
+    w.temp = absent(t) ? nullptr : static_cast<float*>(need(t, "temp", at::kFloat, {h->hk}, h));
+    const void* x = need(a[2], "x", at::kBFloat16, {B, h->E}, h);
+    const int64_t max_len = whole(a[4]);
+    const Workspace ws = workspace_of(a[5], h);
+    at::Tensor made;
+    void* out;
+    if (absent(a[6])) {
+      made = fresh({B, h->E}, at::kBFloat16, h);
+      out = made.data_ptr();
+    } else {
+      out = need(a[6], "out", at::kBFloat16, {B, h->E}, h);
+    }
+    check(cca_decode_step_paged(h->h, &w, x, out, &s, max_len, ws.p, ws.n, B, stream(h)), h, "cca_decode_step_paged");
+    if (made.defined()) return THPVariable_Wrap(std::move(made));
+    Py_INCREF(a[6]);
+    return a[6];
+  });
+}
+// (handle, x, workspace, state)
+PyObject* decode_state_from_prefill_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return method<4>(a, n, [&] {
+    const Handle* h = handle_of(a[0]);
+    int64_t B;
+    const cca_paged_decode_state s = paged_state_of(a[3], h, &B);
+    const at::Tensor& x = tensor_of(a[1], "x");
+    const int64_t S = x.dim() == 3 ? x.size(1) : 0;
+    const void* xp = need(x, "x", at::kBFloat16, {B, S, h->E}, h);
+    const Workspace ws = workspace_of(a[2], h);
+    check(cca_decode_state_from_prefill_paged(h->h, xp, ws.p, ws.n, B, S, &s, stream(h)), h, "cca_decode_state_from_prefill_paged");
+    return none();
+  });
+}
+
 #define M(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {M(new_handle), M(close_handle), M(set_error), M(qcache_append), M(qcache_read), M(qcache_attention),
                          M(qcache_evict), M(qlinear), M(qlinear_pack), M(decode_step_q), M(decode_state_from_prefill_q),
+                         M(pages_reserve), M(pages_fork), M(pages_free), M(pages_compact), M(paged_append), M(paged_read),
+                         M(paged_attention), M(decode_step_paged), M(decode_state_from_prefill_paged),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -7,6 +7,7 @@
 #include "../../include/cca.h"
 #include "common.cuh"
 #include "decode.cuh"
+#include "paged.cuh"
 #include "qcache.cuh"
 #include "qlinear.cuh"
 #include "tc_kernels.cuh"
@@ -434,7 +435,7 @@ int cca_decode_step(cca_handle* h, const cca_weights* w, const void* x, void* ou
   CU(cudaSetDevice(h->device));
   DecodeWeights dw{(const bf16*)w->w_qk, (const bf16*)w->w_v1, (const bf16*)w->w_v2, (const bf16*)w->w_o,
                    (const bf16*)w->conv0_w, (const bf16*)w->conv1_w, (const float*)w->temp};
-  DecodeState ds{(bf16*)s->k_cache, (bf16*)s->v_cache, (float*)s->qk0_hist, (bf16*)s->x_prev, s->pos, s->S_max};
+  DecodeState ds{(bf16*)s->k_cache, (bf16*)s->v_cache, (float*)s->qk0_hist, (bf16*)s->x_prev, s->pos, s->S_max, Paged{}};
   int rr = launch_decode_step(d, dw, (const bf16*)x, (bf16*)out, ds, (int)max_len, workspace, h->sm_count, h->d_status,
                               &h->launches, h->ev_attn_begin, h->ev_attn_end, (cudaStream_t)cuda_stream);
   if (rr < 0) { h->last_cuda = -rr; return CCA_ERR_CUDA; }
@@ -1368,6 +1369,193 @@ int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* wo
   r = enqueued(h, launch_qcache_append(make_dims(c, B, 1), (const bf16*)(ws + l.k), (const bf16*)(ws + l.v), nullptr, nullptr,
                                        make_qcache(&s->cache), S, s->cache.S_max, h->d_status, &h->launches,
                                        (cudaStream_t)cuda_stream));
+  if (r != CCA_OK) return r;
+  return copy_token_state(h, d, l, x, ws, B, S, s->x_prev, s->qk0_hist, (cudaStream_t)cuda_stream);
+}
+
+namespace {
+constexpr int64_t PG_MAX_ROWS = (int64_t)1 << 24;
+int check_pool(const cca_handle* h, int64_t n_pages, int64_t page_size, int64_t max_pages, int64_t B) {
+  if (n_pages < 1 || page_size < 1 || max_pages < 1 || B < 1) return CCA_ERR_INVALID_ARG;
+  if (B > Q_MAX_BATCH || page_size > 65536 || max_pages > PG_MAX_ROWS / page_size || B * max_pages > (int64_t)1 << 30 ||
+      n_pages > (((int64_t)1 << 31) - 1) / (page_size * h->cfg.n_kv_heads))
+    return CCA_ERR_UNSUPPORTED;
+  return CCA_OK;
+}
+int check_pages(const cca_handle* h, const cca_pages* c, int64_t B) {
+  if (!h || !c || h->device < 0) return CCA_ERR_INVALID_ARG;
+  if (!c->k || !c->v || !c->refs || !c->table || !c->len) return CCA_ERR_INVALID_ARG;
+  const int r = check_pool(h, c->n_pages, c->page_size, c->max_pages, B);
+  if (r != CCA_OK) return r;
+  if (!aligned16(c->k) || !aligned16(c->v)) return CCA_ERR_ALIGNMENT;
+  return CCA_OK;
+}
+Paged make_pages(const cca_pages* c) {
+  return Paged{(bf16*)c->k, (bf16*)c->v, c->refs, c->table, c->len, (int)c->n_pages, (int)c->page_size, (int)c->max_pages,
+               (((unsigned long long)1 << 40) + c->page_size - 1) / c->page_size};
+}
+int check_pages_workspace(const cca_pages* c, const void* workspace, size_t bytes, int64_t B) {
+  if (!workspace) return CCA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return CCA_ERR_ALIGNMENT;
+  return bytes < pages_workspace_bytes(c->n_pages, c->max_pages, B) ? CCA_ERR_WORKSPACE_TOO_SMALL : CCA_OK;
+}
+}  // namespace
+
+int cca_pages_workspace_size(const cca_handle* h, int64_t n_pages, int64_t max_pages, int64_t B, size_t* bytes) {
+  if (!h || !bytes) return CCA_ERR_INVALID_ARG;
+  const int r = check_pool(h, n_pages, 1, max_pages, B);
+  if (r != CCA_OK) return r;
+  *bytes = pages_workspace_bytes(n_pages, max_pages, B);
+  return CCA_OK;
+}
+
+int cca_pages_reserve(cca_handle* h, const cca_pages* c, int64_t n, const int32_t* count, const int32_t* first, void* workspace,
+                      size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (n < 1) return CCA_ERR_INVALID_ARG;
+  if (n > PG_MAX_ROWS) return CCA_ERR_UNSUPPORTED;
+  if ((r = check_pages_workspace(c, workspace, workspace_bytes, B)) != CCA_OK) return r;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_pages_reserve(make_dims(h->cfg, B, 1), make_pages(c), n, count, first, workspace, h->sm_count, h->d_status,
+                                          &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_pages_fork(cca_handle* h, const cca_pages* c, const int32_t* parent, const int32_t* child, int64_t n, void* workspace,
+                   size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!parent || !child || n < 1 || n > B) return CCA_ERR_INVALID_ARG;
+  if ((r = check_pages_workspace(c, workspace, workspace_bytes, B)) != CCA_OK) return r;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_pages_fork(make_dims(h->cfg, B, 1), make_pages(c), parent, child, (int)n, workspace, h->d_status, &h->launches,
+                                       (cudaStream_t)cuda_stream));
+}
+
+int cca_pages_free(cca_handle* h, const cca_pages* c, const int32_t* keep, int64_t B, void* cuda_stream) {
+  const int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!keep) return CCA_ERR_INVALID_ARG;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_pages_free(make_dims(h->cfg, B, 1), make_pages(c), keep, h->d_status, &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_pages_compact(cca_handle* h, const cca_pages* c, int32_t* used, void* workspace, size_t workspace_bytes, int64_t B,
+                      void* cuda_stream) {
+  int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!used) return CCA_ERR_INVALID_ARG;
+  if ((r = check_pages_workspace(c, workspace, workspace_bytes, B)) != CCA_OK) return r;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_pages_compact(make_dims(h->cfg, B, 1), make_pages(c), used, workspace, h->sm_count, &h->launches,
+                                          (cudaStream_t)cuda_stream));
+}
+
+int cca_paged_append(cca_handle* h, const void* k, const void* v, const int32_t* count, const cca_pages* c, int64_t B, int64_t n,
+                     void* cuda_stream) {
+  const int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!k || !v || n < 1 || n > c->max_pages * c->page_size) return CCA_ERR_INVALID_ARG;
+  if (B * n > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v)) return CCA_ERR_ALIGNMENT;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_paged_append(make_dims(h->cfg, B, 1), (const bf16*)k, (const bf16*)v, count, make_pages(c), n, h->d_status,
+                                         &h->launches, (cudaStream_t)cuda_stream));
+}
+
+int cca_paged_read(cca_handle* h, const cca_pages* c, const int32_t* first, void* k, void* v, int64_t B, int64_t n, void* cuda_stream) {
+  const int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!k || !v || n < 1) return CCA_ERR_INVALID_ARG;
+  if (n > PG_MAX_ROWS || B * n > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(k) || !aligned16(v)) return CCA_ERR_ALIGNMENT;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_paged_read(make_dims(h->cfg, B, 1), make_pages(c), first, (bf16*)k, (bf16*)v, n, &h->launches,
+                                       (cudaStream_t)cuda_stream));
+}
+
+int cca_paged_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
+  if (!h || !bytes || B < 1 || max_len < 1) return CCA_ERR_INVALID_ARG;
+  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS) return CCA_ERR_UNSUPPORTED;
+  *bytes = paged_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
+  return CCA_OK;
+}
+
+int cca_paged_attention(cca_handle* h, const void* q, void* o, float* lse, const cca_pages* c, int64_t max_len, void* workspace,
+                        size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  const int r = check_pages(h, c, B);
+  if (r != CCA_OK) return r;
+  if (!q || !o || !workspace || max_len < 1 || max_len > c->max_pages * c->page_size) return CCA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(o) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CCA_ERR_ALIGNMENT;
+  const CcaDims d = make_dims(h->cfg, B, 1);
+  if (workspace_bytes < paged_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_paged_attention(d, (const bf16*)q, nullptr, (bf16*)o, lse, make_pages(c), 0, (int)max_len, workspace,
+                                            h->sm_count, h->d_status, &h->launches, h->ev_attn_begin, h->ev_attn_end,
+                                            (cudaStream_t)cuda_stream));
+}
+
+int cca_decode_workspace_size_paged(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
+  if (!h || !bytes || B < 1 || max_len < 1) return CCA_ERR_INVALID_ARG;
+  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS) return CCA_ERR_UNSUPPORTED;
+  *bytes = decode_paged_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
+  return CCA_OK;
+}
+
+int cca_decode_step_paged(cca_handle* h, const cca_weights* w, const void* x, void* out, const cca_paged_decode_state* s,
+                          int64_t max_len, void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream) {
+  if (!w || !s) return CCA_ERR_INVALID_ARG;
+  const int r = check_pages(h, &s->pages, B);
+  if (r != CCA_OK) return r;
+  const cca_config& c = h->cfg;
+  const int pad = c.k_seq + c.k_ch - 2;
+  if (!x || !out || !workspace || !w->w_qk || !w->w_v1 || !w->w_v2 || !w->w_o) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_CONV1) && !w->conv0_w) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_CONV2) && !w->conv1_w) return CCA_ERR_INVALID_ARG;
+  if ((c.flags & CCA_QK_NORM) && !w->temp) return CCA_ERR_INVALID_ARG;
+  if (!s->x_prev || (pad > 0 && !s->qk0_hist)) return CCA_ERR_INVALID_ARG;
+  if (max_len < 1 || max_len > s->pages.max_pages * s->pages.page_size) return CCA_ERR_INVALID_ARG;
+  const CcaDims d = make_dims(c, B, 1);
+  if (!c.causal || d.Lk % 8 || d.E % 32 || d.Lq % 32) return CCA_ERR_UNSUPPORTED;
+  if (!aligned16(x) || !aligned16(out) || !aligned16(w->w_qk) || !aligned16(w->w_v1) || !aligned16(w->w_v2) || !aligned16(w->w_o) ||
+      !aligned16(s->x_prev) || ((c.flags & CCA_CONV2) && !aligned16(w->conv1_w)) || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return CCA_ERR_ALIGNMENT;
+  if (workspace_bytes < decode_paged_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  const DecodeWeights dw{(const bf16*)w->w_qk, (const bf16*)w->w_v1, (const bf16*)w->w_v2, (const bf16*)w->w_o,
+                         (const bf16*)w->conv0_w, (const bf16*)w->conv1_w, (const float*)w->temp};
+  const DecodeState ds{nullptr, nullptr, (float*)s->qk0_hist, (bf16*)s->x_prev, nullptr, 0, make_pages(&s->pages)};
+  OnDevice on;
+  CU(on.enter(h->device));
+  return enqueued(h, launch_decode_step(d, dw, (const bf16*)x, (bf16*)out, ds, (int)max_len, workspace, h->sm_count, h->d_status,
+                                        &h->launches, h->ev_attn_begin, h->ev_attn_end, (cudaStream_t)cuda_stream));
+}
+
+int cca_decode_state_from_prefill_paged(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B, int64_t S,
+                                        const cca_paged_decode_state* s, void* cuda_stream) {
+  if (!s) return CCA_ERR_INVALID_ARG;
+  int r = check_pages(h, &s->pages, B);
+  if (r != CCA_OK) return r;
+  if ((r = check_sizes(h, B, S, true)) != CCA_OK) return r;
+  const cca_config& c = h->cfg;
+  const int pad = c.k_seq + c.k_ch - 2;
+  if (!x || !workspace || !s->x_prev || (pad > 0 && !s->qk0_hist) || S > s->pages.max_pages * s->pages.page_size) return CCA_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(s->x_prev) || (pad > 0 && !aligned16(s->qk0_hist)) || (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return CCA_ERR_ALIGNMENT;
+  const Layout l = make_layout(c, B, S);
+  if (workspace_bytes < l.saved_end) return CCA_ERR_WORKSPACE_TOO_SMALL;
+  OnDevice on;
+  CU(on.enter(h->device));
+  const CcaDims d = make_dims(c, B, S);
+  const char* ws = (const char*)workspace;
+  r = enqueued(h, launch_paged_append(make_dims(c, B, 1), (const bf16*)(ws + l.k), (const bf16*)(ws + l.v), nullptr, make_pages(&s->pages), S,
+                                      h->d_status, &h->launches, (cudaStream_t)cuda_stream));
   if (r != CCA_OK) return r;
   return copy_token_state(h, d, l, x, ws, B, S, s->x_prev, s->qk0_hist, (cudaStream_t)cuda_stream);
 }

@@ -1,0 +1,73 @@
+// Thread-block clusters: each other's shared memory, barriers, and what a launch of them needs.
+#pragma once
+#include "common.cuh"
+
+constexpr int MAX_DEVICES = 64;
+
+CCA_DEVINL uint32_t cluster_place(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return r;
+}
+CCA_DEVINL float cluster_float(const float* p, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL float2 cluster_float2(const float2* p, int rank) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+CCA_DEVINL void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+CCA_DEVINL void cluster_barrier() { cluster_arrive(); cluster_wait(); }
+CCA_DEVINL int cluster_load(const int* p, int rank) {
+  int v;
+  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL int2 cluster_load2(const int* p, int rank) {
+  int2 v;
+  asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
+CCA_DEVINL void all_sync(int ranks) {                      // `ranks` CTAs; one alone has no cluster to wait for
+  if (ranks == 1) __syncthreads();
+  else cluster_barrier();
+}
+
+// The opt-in to more than 48 KB of dynamic shared memory, per device and kernel (`done`: one flag per device).
+template <typename K>
+cudaError_t opt_in(K kernel, int bytes, bool* done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < MAX_DEVICES && done[dev])) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < MAX_DEVICES) done[dev] = true;
+  return e;
+}
+
+// Launched as a dependent of the kernel before it, in clusters of `ranks` CTAs.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int ranks, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)ranks; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}

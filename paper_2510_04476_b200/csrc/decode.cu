@@ -18,6 +18,7 @@
 
 #include "common.cuh"
 #include "decode.cuh"
+#include "paged.cuh"
 #include "pdl.cuh"
 #include "qcache.cuh"
 #include "qlinear.cuh"
@@ -150,6 +151,16 @@ CCA_DEVINL bool new_row(const int* pos, const int* qlen, long long S_max, int ma
   return t >= 0 && t < S_max && t < max_len;
 }
 
+// The same on a cache in pages: row len[b], whose page the sequence has to hold alone; `row`: its place in the pool, kv head 0.
+CCA_DEVINL bool new_paged_row(const Paged& c, int hk, int max_len, int b, int& t, size_t& row) {
+  t = c.len[b];
+  if (t < 0 || t >= max_len || t >= (long long)c.max_pages * c.P) return false;
+  const int i = page_index(c, t), page = page_at(c, b, i);
+  if (page < 0 || c.refs[page] != 1) return false;
+  row = (size_t)pool_row(c, hk, page, 0, t - i * c.P);
+  return true;
+}
+
 struct C1Args {
   CcaDims d;
   const float* lat;      // [B, L + Lk]: q0 | k0 | v1 | v2 of the new token
@@ -165,6 +176,7 @@ struct C1Args {
   long long S_max;
   int max_len;
   int* status;
+  Paged pages;           // k null: no pages
 };
 
 // Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
@@ -175,8 +187,9 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
   const int b = blockIdx.y, tid = threadIdx.x;
   int t;
   size_t row;
-  if (!new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)) {
-    if (tid == 0 && blockIdx.x == 0) atomicCAS(a.status, 0, a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
+  const bool paged = a.pages.k != nullptr;
+  if (!(paged ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row))) {
+    if (tid == 0 && blockIdx.x == 0) atomicCAS(a.status, 0, paged ? ST_PAGE_MISSING : a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
     return;
   }
   const int ld_lat = d.L + d.Lk;
@@ -208,9 +221,14 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
     for (int r = 0; r < 7; ++r)
       if (r < pad) a.hist[((size_t)b * pad + r) * d.L + ch] = win[r + 1];
   }
-  if (a.v_cache)                                            // null: the value is quantised beside the key
+  if (a.v_cache)                                            // null: pages, or the value is quantised beside the key
     for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256)
       a.v_cache[row * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
+  if (paged)
+    for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256) {
+      const int j = c / d.dh;
+      a.pages.v[(row + (size_t)j * a.pages.P) * d.dh + c - j * d.dh] = __float2bfloat16(lat_b[d.L + c]);
+    }
   for (int c = blockIdx.x * 256 + tid; c < d.E / 8; c += gridDim.x * 256)
     reinterpret_cast<uint4*>(a.x_prev + (size_t)b * d.E)[c] = reinterpret_cast<const uint4*>(a.x + (size_t)b * d.E)[c];
 }
@@ -229,6 +247,7 @@ struct FnArgs {
   long long S_max;
   int max_len;
   QCache cache;          // Q4 alone
+  Paged pages;           // k null: no pages
 };
 
 template <int DH, bool Q4>
@@ -242,7 +261,9 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int t;
   size_t row;
-  if (!new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)) return;      // reported by the conv1 kernel
+  const bool paged = !Q4 && a.pages.k != nullptr;
+  if (!(paged ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)))
+    return;                                                                // reported by the conv1 kernel
   const bool is_q = head < d.hq;
   const int ch0 = head * DH;                   // first channel of the head in the q0|k0 latent
   const float* lat_b = a.lat + (size_t)b * (d.L + d.Lk);
@@ -310,6 +331,7 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
     if (blk < R::NB) q4::store_block<DH>(a.cache, ((size_t)b * d.hk + j) * a.S_max + row, kv, blk, lane8, t, code, scale);
   } else {
     if (is_q) a.q[(size_t)b * d.Lq + ch0 + c] = v;
+    else if (paged) a.pages.k[(row + (size_t)(head - d.hq) * a.pages.P) * DH + c] = __float2bfloat16(v);
     else a.k_cache[row * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
   }
 }
@@ -663,6 +685,12 @@ size_t decode_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
   return n;
 }
 
+size_t decode_paged_workspace_bytes(const CcaDims& d, int max_len, int sm_count) {
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  return up((size_t)d.B * (d.L + d.Lk) * 4) + up((size_t)d.B * d.Lq * 4) + up((size_t)d.B * d.Lq * 2) + up((size_t)d.B * d.L * d.k_ch * 2) +
+         up((size_t)d.B * d.L * 4) + paged_workspace_bytes(d, max_len, sm_count);
+}
+
 int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, bf16* out, const DecodeState& s,
                        int max_len, void* workspace, int sm_count, int* status, long long* launches, cudaEvent_t ev_attn_begin,
                        cudaEvent_t ev_attn_end, cudaStream_t st) {
@@ -672,15 +700,16 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   unsigned char* p = static_cast<unsigned char*>(workspace);
   float* lat = reinterpret_cast<float*>(p); p += up((size_t)d.B * (d.L + d.Lk) * 4);
   float* q = reinterpret_cast<float*>(p); p += up((size_t)d.B * d.Lq * 4);
-  float* part_o = reinterpret_cast<float*>(p); p += up((size_t)d.B * d.hq * splits * d.dh * 4);
-  float* part_ml = reinterpret_cast<float*>(p); p += up((size_t)d.B * d.hq * splits * 2 * 4);
+  const bool paged = s.pages.k != nullptr;
+  float* part_o = reinterpret_cast<float*>(p); p += paged ? 0 : up((size_t)d.B * d.hq * splits * d.dh * 4);
+  float* part_ml = reinterpret_cast<float*>(p); p += paged ? 0 : up((size_t)d.B * d.hq * splits * 2 * 4);
   bf16* o = reinterpret_cast<bf16*>(p); p += up((size_t)d.B * d.Lq * 2);
   bf16* y1s = reinterpret_cast<bf16*>(p); p += up((size_t)d.B * d.L * d.k_ch * 2);
-  float* y2 = reinterpret_cast<float*>(p);
+  float* y2 = reinterpret_cast<float*>(p); p += up((size_t)d.B * d.L * 4);
   cudaError_t e;
   if (d.dh != 32 && d.dh != 64 && d.dh != 128 && d.dh != 256) return 1;
   if (d.E % 32 || d.Lq % 32) return 1;
-  if (d.dh == 256 && d.g > 8) return 1;
+  if (d.dh == 256 && d.g > 8 && !paged) return 1;
   // Eq. 7 and Eq. 10: q0 | k0 | v1 from x_t, v2 from x_{t-1}
   ProjArgs pa;
   memset(&pa, 0, sizeof(pa));
@@ -697,6 +726,7 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   C1Args c1;
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = s.v_cache;
   c1.hist = s.qk0_hist; c1.x_prev = s.x_prev; c1.pos = s.pos; c1.qlen = nullptr; c1.S_max = s.S_max; c1.max_len = max_len; c1.status = status;
+  c1.pages = s.pages;
   if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
   ++*launches;
@@ -711,39 +741,45 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   }
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = s.k_cache; fa.pos = s.pos;
-  fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len; fa.cache = QCache{};
+  fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len; fa.cache = QCache{}; fa.pages = s.pages;
   if ((e = launch_finalize_dh<false>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
-  AtArgs aa;
-  aa.d = d; aa.q = q; aa.k_cache = s.k_cache; aa.v_cache = s.v_cache;
-  aa.temp = (d.flags & F_QK_NORM) ? w.temp : nullptr;
-  aa.pos = s.pos; aa.S_max = s.S_max; aa.max_len = max_len; aa.chunk = chunk; aa.splits = splits;
-  aa.part_o = part_o; aa.part_ml = part_ml;
-  if (ev_attn_begin && (e = cudaEventRecord(ev_attn_begin, st)) != cudaSuccess) return -(int)e;
-  switch (d.dh) {
-    case 32: e = launch_attn_dh<32>(aa, st); break;
-    case 64: e = launch_attn_dh<64>(aa, st); break;
-    case 128: e = launch_attn_dh<128>(aa, st); break;
-    case 256: e = launch_attn_dh<256>(aa, st); break;
-    default: return 1;
-  }
-  if (e != cudaSuccess) return -(int)e;
-  ++*launches;
-  if (ev_attn_end && (e = cudaEventRecord(ev_attn_end, st)) != cudaSuccess) return -(int)e;
-  CbArgs ca;
-  ca.d = d; ca.part_o = part_o; ca.part_ml = part_ml; ca.pos = s.pos; ca.S_max = s.S_max; ca.max_len = max_len;
-  ca.splits = splits; ca.o = o;
-  {
-    dim3 grid((unsigned)d.hq, (unsigned)d.B);
+  if (paged) {
+    const int r = launch_paged_attention(d, nullptr, q, o, nullptr, s.pages, 1, max_len, p, sm_count, status, launches, ev_attn_begin,
+                                         ev_attn_end, st);
+    if (r != 0) return r;
+  } else {
+    AtArgs aa;
+    aa.d = d; aa.q = q; aa.k_cache = s.k_cache; aa.v_cache = s.v_cache;
+    aa.temp = (d.flags & F_QK_NORM) ? w.temp : nullptr;
+    aa.pos = s.pos; aa.S_max = s.S_max; aa.max_len = max_len; aa.chunk = chunk; aa.splits = splits;
+    aa.part_o = part_o; aa.part_ml = part_ml;
+    if (ev_attn_begin && (e = cudaEventRecord(ev_attn_begin, st)) != cudaSuccess) return -(int)e;
     switch (d.dh) {
-      case 32: e = launch_pdl(decode_combine_kernel<32>, grid, dim3(64), st, ca); break;
-      case 64: e = launch_pdl(decode_combine_kernel<64>, grid, dim3(64), st, ca); break;
-      case 128: e = launch_pdl(decode_combine_kernel<128>, grid, dim3(128), st, ca); break;
-      case 256: e = launch_pdl(decode_combine_kernel<256>, grid, dim3(256), st, ca); break;
+      case 32: e = launch_attn_dh<32>(aa, st); break;
+      case 64: e = launch_attn_dh<64>(aa, st); break;
+      case 128: e = launch_attn_dh<128>(aa, st); break;
+      case 256: e = launch_attn_dh<256>(aa, st); break;
       default: return 1;
     }
     if (e != cudaSuccess) return -(int)e;
     ++*launches;
+    if (ev_attn_end && (e = cudaEventRecord(ev_attn_end, st)) != cudaSuccess) return -(int)e;
+    CbArgs ca;
+    ca.d = d; ca.part_o = part_o; ca.part_ml = part_ml; ca.pos = s.pos; ca.S_max = s.S_max; ca.max_len = max_len;
+    ca.splits = splits; ca.o = o;
+    {
+      dim3 grid((unsigned)d.hq, (unsigned)d.B);
+      switch (d.dh) {
+        case 32: e = launch_pdl(decode_combine_kernel<32>, grid, dim3(64), st, ca); break;
+        case 64: e = launch_pdl(decode_combine_kernel<64>, grid, dim3(64), st, ca); break;
+        case 128: e = launch_pdl(decode_combine_kernel<128>, grid, dim3(128), st, ca); break;
+        case 256: e = launch_pdl(decode_combine_kernel<256>, grid, dim3(256), st, ca); break;
+        default: return 1;
+      }
+      if (e != cudaSuccess) return -(int)e;
+      ++*launches;
+    }
   }
   // Eq. 11, up-projection
   ProjArgs pb;
@@ -795,7 +831,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   const int kc = (d.flags & F_CONV2) ? d.k_ch : 1;
   C1Args c1;
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = nullptr; c1.hist = hist; c1.x_prev = x_prev;
-  c1.pos = pos; c1.qlen = cache.len; c1.S_max = cache.S_max; c1.max_len = max_len; c1.status = status;
+  c1.pos = pos; c1.qlen = cache.len; c1.S_max = cache.S_max; c1.max_len = max_len; c1.status = status; c1.pages = Paged{};
   if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
   ++*launches;
@@ -810,7 +846,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   }
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = nullptr; fa.pos = pos; fa.qlen = cache.len; fa.cache = cache;
-  fa.S_max = cache.S_max; fa.max_len = max_len;
+  fa.S_max = cache.S_max; fa.max_len = max_len; fa.pages = Paged{};
   if ((e = launch_finalize_dh<true>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
   if ((r = launch_qcache_attention(d, nullptr, q, o, cache, pos, 1, max_len, cache.weight != nullptr, ws + l.cache, sm_count, status,

@@ -1,6 +1,7 @@
 // Decode step against the latent KV cache: host-side launcher interface.
 #pragma once
 #include "common.cuh"
+#include "paged.cuh"
 #include "qcache.cuh"
 #include "tc_kernels.cuh"
 
@@ -16,11 +17,13 @@ struct DecodeState {
   bf16* x_prev;       // [B, E]
   const int* pos;     // [B]
   long long S_max;
+  Paged pages;        // k set: in place of the two caches, pos and S_max
 };
 
 // Key chunk per CTA and number of chunks for sequences of up to max_len tokens.
 void decode_plan(const CcaDims& d, int max_len, int sm_count, int* chunk, int* splits);
 size_t decode_workspace_bytes(const CcaDims& d, int max_len, int sm_count);
+size_t decode_paged_workspace_bytes(const CcaDims& d, int max_len, int sm_count);
 // 0 = enqueued, 1 = shape not covered, < 0 = minus a cudaError_t.  *launches is advanced by the kernels enqueued.
 // The two events (may be null) are recorded around the attention kernel.
 int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, bf16* out, const DecodeState& s,

@@ -5,6 +5,7 @@
 // stream as whole lines and a row moves without touching its neighbours' heads.
 #include <cstring>
 
+#include "cluster.cuh"
 #include "pdl.cuh"
 #include "qrow.cuh"
 
@@ -12,7 +13,6 @@ namespace {
 
 using namespace q4;
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int MAX_DEVICES = 64;
 
 // ------------------------------------------------------------------------------------------------ rows in and out
 struct IoArgs {
@@ -279,31 +279,6 @@ struct Rows {
 
 constexpr int QA_WARPS = 4, QA_MAX_SPLITS = 128, QA_FIXED = 192;
 constexpr int QA_FUSED_SPLITS = 8, QA_FUSED_ROWS = 256, QA_FUSED_LOGITS = 32 * 1024;    // chunks, rows of one, bytes of its logits
-
-CCA_DEVINL uint32_t cluster_place(const void* p, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-  return r;
-}
-CCA_DEVINL float cluster_float(const float* p, int rank) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_place(p, rank)) : "memory");
-  return v;
-}
-CCA_DEVINL float2 cluster_float2(const float2* p, int rank) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_place(p, rank)) : "memory");
-  return v;
-}
-CCA_DEVINL void cluster_arrive() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-CCA_DEVINL void cluster_wait() {
-  __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-CCA_DEVINL void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 
 template <int DH, int H>
 struct FusedShare {                                        // what the CTAs of a cluster read of each other, and what they make of it
@@ -803,17 +778,6 @@ bool attn_fused(const CcaDims& d, int max_len, int sm_count, int gather, int pla
   return best >= 0;
 }
 
-// The opt-in to more than 48 KB of dynamic shared memory, per device and kernel (`done`: one flag per device).
-template <typename K>
-cudaError_t opt_in(K kernel, int bytes, bool* done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || (dev < MAX_DEVICES && done[dev])) return e;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev < MAX_DEVICES) done[dev] = true;
-  return e;
-}
-
 template <int DH, int NHT>
 cudaError_t attn_run(const QaArgs& a, dim3 grid, bool fused, cudaStream_t st) {
   constexpr int smem = QA_WARPS * Stage<DH>::N * Stage<DH>::BYTES;
@@ -871,21 +835,6 @@ CCA_DEVINL uint32_t keep_key(float w, int pos, long long first_recent) {
   if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
   if ((u << 1) == 0u) u = 0u;
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
-CCA_DEVINL int cluster_load(const int* p, int rank) {
-  int v;
-  asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(cluster_place(p, rank)) : "memory");
-  return v;
-}
-CCA_DEVINL int2 cluster_load2(const int* p, int rank) {
-  int2 v;
-  asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_place(p, rank)) : "memory");
-  return v;
-}
-CCA_DEVINL void all_sync(int ranks) {                      // the CTAs that share a head
-  if (ranks == 1) __syncthreads();
-  else cluster_barrier();
 }
 
 // Exclusive sum over the 32 warps of a value that is the same in a warp's lanes; `total`: over all of them.
