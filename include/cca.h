@@ -392,7 +392,7 @@ int cca_decode_state_from_prefill_q(cca_handle* h, const void* x, const void* wo
  * B sequences are rows 0 .. B - 1 of table and len; the rows of some sequences that lie one after the other are a cca_pages of their own,
  * except for cca_pages_compact, which has to see every sequence that holds a page of the pool.
  * Limits, UNSUPPORTED beyond them: B <= 65535, page_size <= 65536, max_pages * page_size <= 2^24 rows a sequence, n_pages * h_k * page_size
- * < 2^31 rows of the pool, B * max_pages <= 2^30, B n <= 2^30 new or read rows. */
+ * < 2^31 rows of the pool, B * max_pages <= 2^30, B n <= 2^30 new or read rows, B * max_len <= 2^30 in attention and the step. */
 typedef struct {
   void* k;              /* bf16 [n_pages, h_k, page_size, d_h]: keys after norm, temperature and RoPE (Eq. 11)        */
   void* v;              /* bf16 [n_pages, h_k, page_size, d_h]: values (Eq. 10)                                       */

@@ -1482,7 +1482,7 @@ int cca_paged_read(cca_handle* h, const cca_pages* c, const int32_t* first, void
 
 int cca_paged_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
   if (!h || !bytes || B < 1 || max_len < 1) return CCA_ERR_INVALID_ARG;
-  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS) return CCA_ERR_UNSUPPORTED;
+  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS || B * max_len > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
   *bytes = paged_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
   return CCA_OK;
 }
@@ -1492,6 +1492,7 @@ int cca_paged_attention(cca_handle* h, const void* q, void* o, float* lse, const
   const int r = check_pages(h, c, B);
   if (r != CCA_OK) return r;
   if (!q || !o || !workspace || max_len < 1 || max_len > c->max_pages * c->page_size) return CCA_ERR_INVALID_ARG;
+  if (B * max_len > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
   if (!aligned16(q) || !aligned16(o) || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CCA_ERR_ALIGNMENT;
   const CcaDims d = make_dims(h->cfg, B, 1);
   if (workspace_bytes < paged_workspace_bytes(d, (int)max_len, h->sm_count)) return CCA_ERR_WORKSPACE_TOO_SMALL;
@@ -1504,7 +1505,7 @@ int cca_paged_attention(cca_handle* h, const void* q, void* o, float* lse, const
 
 int cca_decode_workspace_size_paged(const cca_handle* h, int64_t B, int64_t max_len, size_t* bytes) {
   if (!h || !bytes || B < 1 || max_len < 1) return CCA_ERR_INVALID_ARG;
-  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS) return CCA_ERR_UNSUPPORTED;
+  if (B > Q_MAX_BATCH || max_len > PG_MAX_ROWS || B * max_len > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
   *bytes = decode_paged_workspace_bytes(make_dims(h->cfg, B, 1), (int)max_len, h->sm_count > 0 ? h->sm_count : 148);
   return CCA_OK;
 }
@@ -1523,7 +1524,7 @@ int cca_decode_step_paged(cca_handle* h, const cca_weights* w, const void* x, vo
   if (!s->x_prev || (pad > 0 && !s->qk0_hist)) return CCA_ERR_INVALID_ARG;
   if (max_len < 1 || max_len > s->pages.max_pages * s->pages.page_size) return CCA_ERR_INVALID_ARG;
   const CcaDims d = make_dims(c, B, 1);
-  if (!c.causal || d.Lk % 8 || d.E % 32 || d.Lq % 32) return CCA_ERR_UNSUPPORTED;
+  if (!c.causal || d.Lk % 8 || d.E % 32 || d.Lq % 32 || B * max_len > (int64_t)1 << 30) return CCA_ERR_UNSUPPORTED;
   if (!aligned16(x) || !aligned16(out) || !aligned16(w->w_qk) || !aligned16(w->w_v1) || !aligned16(w->w_v2) || !aligned16(w->w_o) ||
       !aligned16(s->x_prev) || ((c.flags & CCA_CONV2) && !aligned16(w->conv1_w)) || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return CCA_ERR_ALIGNMENT;

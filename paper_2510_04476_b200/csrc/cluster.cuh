@@ -19,6 +19,12 @@ CCA_DEVINL float2 cluster_float2(const float2* p, int rank) {
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_place(p, rank)) : "memory");
   return v;
 }
+CCA_DEVINL float4 cluster_float4(const float* p, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_place(p, rank)) : "memory");
+  return v;
+}
 CCA_DEVINL void cluster_arrive() {
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");

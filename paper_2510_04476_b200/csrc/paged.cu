@@ -113,9 +113,9 @@ struct PaArgs {
   int B, hk, g, hq;
   int heads, n_grp;       // query heads per pass over a kv head's rows, passes
   int extra, max_len;
-  float* part_o;          // [2 G][8][DH]
-  float2* part_ml;        // [2 G][8]
-  int4* desc;             // [G]: what the join has to do: sequence, kv head and pass, last CTA
+  int ctas;               // of the attention kernel that shares its units out
+  float* part_o;          // [2 ctas][8][DH]
+  float2* part_ml;        // [2 ctas][8]
   int* status;
 };
 
@@ -137,11 +137,76 @@ struct At {
 };
 
 CCA_DEVINL int rows_of(const PaArgs& a, int b) {              // -1: does not fit
-  const int n = a.c.len[b];
+  const int n = __ldcg(a.c.len + b);
   return n >= 0 && n <= a.max_len - a.extra && n + a.extra <= (long long)a.c.max_pages * a.c.P ? n + a.extra : -1;
 }
 
-// Where a CTA is in the list of units: sequences in order, in each its kv heads (and passes), in each its units of rows.
+// The list of units: sequences in order, in each its kv heads (and passes over them), in each its units of rows.  It is cut into `used`
+// parts, one for each CTA that has something to do, the first `more` of them one unit longer than the others.  (B max_len <= 2^30: less
+// than 2^31 units.)
+struct Plan {
+  unsigned units, used, each, more, groups;
+  CCA_DEVINL unsigned begin(unsigned cta) const { return cta * each + min(cta, more); }
+  CCA_DEVINL int owner(unsigned unit) const {
+    const unsigned longer = more * (each + 1);
+    return (int)(unit < longer ? unit / (each + 1) : more + (unit - longer) / each);
+  }
+};
+
+CCA_DEVINL unsigned warp_upto(unsigned v, int lane) {         // sum over the lanes up to this one
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const unsigned x = __shfl_up_sync(0xffffffffu, v, s);
+    if (lane >= s) v += x;
+  }
+  return v;
+}
+template <int UNIT>
+CCA_DEVINL unsigned tiles_of(int rows) { return (unsigned)(max(rows, 0) + UNIT - 1) / UNIT; }
+
+// Every warp for itself, from the lengths: the plan, and the sequence that `pick(plan)`, a tile of the sequences laid end to end (each taken
+// once, not once a kv head), belongs to, with its rows and the tiles before it.  seq = -1: there is no such tile.
+template <int UNIT, typename Pick>
+CCA_DEVINL Plan make_plan(const PaArgs& a, int lane, Pick pick, int& seq, int& rows, unsigned& before) {
+  constexpr int KEPT = 4;                                      // rows of the first 128 sequences stay in registers
+  int n[KEPT];
+  unsigned total = 0;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) n[i] = i * 32 + lane < a.B ? rows_of(a, i * 32 + lane) : 0;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) total += tiles_of<UNIT>(n[i]);
+  for (int b = KEPT * 32 + lane; b < a.B; b += 32) total += tiles_of<UNIT>(rows_of(a, b));
+  total = __reduce_add_sync(0xffffffffu, total);
+  Plan p;
+  p.groups = a.hk * a.n_grp;
+  p.units = total * p.groups;
+  p.used = min((unsigned)a.ctas, p.units);
+  p.each = p.used > 0 ? p.units / p.used : 0;
+  p.more = p.units - p.each * p.used;
+  seq = -1;
+  before = 0;
+  const unsigned want = pick(p);
+  if (want >= total) return p;
+  for (int i = 0; seq < 0; ++i) {
+    int here = 0;
+#pragma unroll
+    for (int x = 0; x < KEPT; ++x)
+      if (i == x) here = n[x];
+    if (i >= KEPT) here = i * 32 + lane < a.B ? rows_of(a, i * 32 + lane) : 0;
+    const unsigned tiles = tiles_of<UNIT>(here), upto = warp_upto(tiles, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, want < before + upto);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      seq = i * 32 + l;
+      rows = __shfl_sync(0xffffffffu, here, l);
+      before += __shfl_sync(0xffffffffu, upto - tiles, l);
+    } else {
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+  }
+  return p;
+}
+
 template <int DH>
 struct Cursor {
   int b, j, tile, tiles, rows;
@@ -158,110 +223,96 @@ struct Cursor {
   }
 };
 
-template <int DH, int HG>
+// JOINED: the CTAs of a cluster share the rows of one (sequence, kv head) and join their results through each other's shared memory.
+// Otherwise every CTA takes its part of the list of units, and paged_join_kernel joins what several CTAs had part in.
+template <int DH, int HG, bool JOINED>
 __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_kernel(PaArgs a) {
   using S = At<DH>;
   constexpr int NT = S::WARPS * 32, MT = DH / 16, R = S::R, NB = R / 16, RL = R > 32 ? 2 : 1;
   constexpr int PARTS = HG == 4 ? 1 : 2;                       // accumulator tiles of the weights' two parts
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ long long scan[S::WARPS];
-  __shared__ long long found[2];
   __shared__ float2 sm_ml[S::WARPS][8];
+  __shared__ float2 cta_ml[8];                                 // JOINED: what the others of the cluster read
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int cta = blockIdx.x, n_cta = gridDim.x;
   float* sm_o = reinterpret_cast<float*>(smem + S::RING);      // [WARPS][HG][OLD]
   pdl_enter();
 
-  // ---- this CTA's share of the units: all rows there are, in equal parts
-  const int groups = a.hk * a.n_grp;
-  long long total = 0, mine = 0;
-  for (int b = tid; b < a.B; b += NT) mine += (max(rows_of(a, b), 0) + S::UNIT - 1) / S::UNIT;
-#pragma unroll
-  for (int s = 16; s > 0; s >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, s);
-  if (lane == 0) scan[warp] = mine;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < S::WARPS; ++w) total += scan[w];
-  const long long units = total * groups;
-  const int used = (int)min((long long)n_cta, units);          // CTAs that have something to do
-  // sequences without rows
-  for (int b = cta; b < a.B; b += n_cta) {
-    const int n = rows_of(a, b);
-    if (n > 0) continue;
-    if (n < 0) {
-      if (tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
-      continue;
+  // ---- this CTA's units
+  const int ranks = JOINED ? gridDim.x : 1, cta = blockIdx.x;
+  Cursor<DH> cur = {0, 0, 0, 1, 0}, ld;                        // (no rows: a CTA without units)
+  int to_load = 0;
+  if (JOINED) {
+    cur.b = blockIdx.z;
+    cur.j = blockIdx.y;
+    cur.rows = rows_of(a, cur.b);
+    cur.tiles = tiles_of<S::UNIT>(cur.rows);
+    cur.tile = cur.tiles * cta / ranks;
+    to_load = cur.tiles * (cta + 1) / ranks - cur.tile;
+  } else {
+    unsigned before;
+    int seq, rows;
+    const Plan plan = make_plan<S::UNIT>(a, lane, [&](const Plan& p) { return cta < p.used ? p.begin(cta) / p.groups : 0xffffffffu; },
+                                         seq, rows, before);
+    if (seq >= 0) {
+      cur.b = seq;
+      cur.rows = rows;
+      cur.tiles = tiles_of<S::UNIT>(rows);
+      const unsigned u0 = plan.begin(cta), rem = u0 - before * plan.groups;
+      cur.j = rem / cur.tiles;
+      cur.tile = rem - cur.j * cur.tiles;
+      to_load = plan.begin(cta + 1) - u0;
     }
-    for (int i = tid; i < a.hq * DH; i += NT) a.o[(size_t)b * a.hq * DH + i] = __float2bfloat16(0.f);
-    if (a.lse)
-      for (int i = tid; i < a.hq; i += NT) a.lse[(size_t)b * a.hq + i] = -INFINITY;
   }
-  if (cta >= used) {
-    if (tid == 0) a.desc[cta] = make_int4(-1, 0, 0, 0);
+  // sequences without rows
+  auto no_rows = [&](int b, int h0, int n) {
+    const int rows = rows_of(a, b);
+    if (rows > 0) return;
+    if (rows < 0) {
+      if (tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+      return;
+    }
+    const size_t head = (size_t)b * a.hq + h0;
+    for (int i = tid; i < n * DH; i += NT) a.o[head * DH + i] = __float2bfloat16(0.f);
+    if (a.lse)
+      for (int i = tid; i < n; i += NT) a.lse[head + i] = -INFINITY;
+  };
+  if (JOINED && cur.rows <= 0) {                               // the same in the whole cluster
+    const int j = cur.j / a.n_grp, h0 = (cur.j - j * a.n_grp) * a.heads;
+    if (cta == 0) no_rows(cur.b, j * a.g + h0, min(a.heads, a.g - h0));
     return;
   }
-  const long long u0 = cta * units / used, u1 = (cta + 1) * units / used;
-  const long long want = u0 / groups;
-  {
-    long long base = 0;
-    for (int b0 = 0; b0 < a.B; b0 += NT) {                     // the sequence whose units hold `want`
-      const int b = b0 + tid;
-      const long long n = b < a.B ? (max(rows_of(a, b), 0) + S::UNIT - 1) / S::UNIT : 0;
-      long long upto = n;
-#pragma unroll
-      for (int s = 1; s < 32; s <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, upto, s);
-        if (lane >= s) upto += v;
-      }
-      __syncthreads();
-      if (lane == 31) scan[warp] = upto;
-      __syncthreads();
-      long long before = base;
-#pragma unroll
-      for (int w = 0; w < S::WARPS; ++w) {
-        if (w < warp) before += scan[w];
-        base += scan[w];
-      }
-      if (want >= before + upto - n && want < before + upto) { found[0] = b; found[1] = before + upto - n; }
-      if (want < base) break;
-    }
-    __syncthreads();
-  }
-  Cursor<DH> cur, ld;
-  cur.b = (int)found[0];
-  cur.rows = rows_of(a, cur.b);
-  cur.tiles = (cur.rows + S::UNIT - 1) / S::UNIT;
-  {
-    const long long rem = u0 - found[1] * groups;
-    cur.j = (int)(rem / cur.tiles);
-    cur.tile = (int)(rem - (long long)cur.j * cur.tiles);
-  }
-  ld = cur;
-  int to_load = (int)(u1 - u0), to_do = to_load;
 
   // ---- loads: a lane knows the pool row of its row of the warp's next stage, looked up one stage ahead
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE);
-  int entry[RL];
-  auto look_up = [&] {
-#pragma unroll
-    for (int x = 0; x < RL; ++x) {
-      const int row = ld.tile * S::UNIT + warp * R + x * 32 + (R < 32 ? lane % R : lane);
-      entry[x] = -1;
-      if (to_load > 0 && row < ld.rows) {
-        entry[x] = a.c.table[(size_t)ld.b * a.c.max_pages + page_index(a.c, row)];
-        if ((unsigned)entry[x] >= (unsigned)a.c.n_pages) entry[x] = -2;
-      }
-    }
+  struct Stage {                                               // one to be loaded: its rows (below `rows` where there is one) and their pages
+    int j, row, rows, entry[RL];
   };
-  auto issue = [&](int slot, uint32_t* mask) {
-    const int j = ld.j / a.n_grp;
+  int ahead = to_load;                                         // units that have not been looked up
+  ld = cur;
+  auto look_up = [&] {
+    Stage x;
+    x.j = ld.j;
+    x.row = ld.tile * S::UNIT + warp * R + (R < 32 ? lane % R : lane);
+    x.rows = ahead > 0 ? ld.rows : 0;
+#pragma unroll
+    for (int i = 0; i < RL; ++i)                               // (nothing is done with an entry before its stage's turn: it is on its way)
+      x.entry[i] = x.row + i * 32 < x.rows ? a.c.table[(size_t)ld.b * a.c.max_pages + page_index(a.c, x.row + i * 32)] : -1;
+    if (--ahead > 0) {
+      if (JOINED) ++ld.tile;
+      else ld.next(a);
+    }
+    return x;
+  };
+  auto issue = [&](const Stage& x, int slot, uint32_t* mask) {
+    const int j = x.j / a.n_grp;
     int at[RL];
 #pragma unroll
-    for (int x = 0; x < RL; ++x) {
-      const int row = ld.tile * S::UNIT + warp * R + x * 32 + (R < 32 ? lane % R : lane);
-      at[x] = entry[x] >= 0 ? pool_row(a.c, a.hk, entry[x], j, row - page_index(a.c, row) * a.c.P) : -1;
-      if (entry[x] == -2) atomicCAS(a.status, 0, ST_PAGE_MISSING);
-      mask[x] = __ballot_sync(0xffffffffu, at[x] >= 0);
+    for (int i = 0; i < RL; ++i) {
+      const int row = x.row + i * 32;
+      at[i] = -1;
+      if ((unsigned)x.entry[i] < (unsigned)a.c.n_pages) at[i] = pool_row(a.c, a.hk, x.entry[i], j, row - page_index(a.c, row) * a.c.P);
+      else if (row < x.rows) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+      mask[i] = __ballot_sync(0xffffffffu, at[i] >= 0);
     }
     bool any = mask[0] != 0;
     if (RL > 1) any = any || mask[RL - 1] != 0;
@@ -277,22 +328,28 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
         copy_async(to + S::HALF + S::place(row, piece), a.c.v + off, from >= 0);
       }
     }
-    if (to_load > 0) {
-      --to_load;
-      if (to_load > 0) ld.next(a);
-    }
-    look_up();
   };
   uint32_t masks[S::STAGES - 1][RL];                           // rows there are, of the stages on their way
-  look_up();
+  Stage next;
+  {
+    Stage first[S::STAGES - 1];
 #pragma unroll
-  for (int s = 0; s < S::STAGES - 1; ++s) {
-    issue(s, masks[s]);
-    copies_commit();
+    for (int s = 0; s < S::STAGES - 1; ++s) first[s] = look_up();
+    next = look_up();
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s) {
+      issue(first[s], s, masks[s]);
+      copies_commit();
+    }
   }
+  if (!JOINED) {
+    for (int b = cta; b < a.B; b += gridDim.x) no_rows(b, 0, a.hq);
+    if (to_load == 0) return;
+  }
+  int to_do = to_load;
 
   // ---- queries: row r of the 16-row operand is head r (HG = 4: r % 4), rows 8 to 15 are zero
-  uint32_t qa[MT][4];
+  uint32_t qa[MT][2];
   int nh = 0, h0 = 0;
   auto load_q = [&] {
     const int j = cur.j / a.n_grp;
@@ -302,15 +359,15 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
     const size_t at = ((size_t)cur.b * a.hq + j * a.g + h0 + head) * DH + 2 * t;
 #pragma unroll
     for (int ks = 0; ks < MT; ++ks) {
-      qa[ks][0] = qa[ks][1] = qa[ks][2] = qa[ks][3] = 0;
+      qa[ks][0] = qa[ks][1] = 0;
       if (head < nh) {
         if (a.q32) {
           const float2 lo = *reinterpret_cast<const float2*>(a.q32 + at + ks * 16), hi = *reinterpret_cast<const float2*>(a.q32 + at + ks * 16 + 8);
           qa[ks][0] = pack_bf16x2(lo.x, lo.y);
-          qa[ks][2] = pack_bf16x2(hi.x, hi.y);
+          qa[ks][1] = pack_bf16x2(hi.x, hi.y);
         } else {
           qa[ks][0] = *reinterpret_cast<const uint32_t*>(a.q + at + ks * 16);
-          qa[ks][2] = *reinterpret_cast<const uint32_t*>(a.q + at + ks * 16 + 8);
+          qa[ks][1] = *reinterpret_cast<const uint32_t*>(a.q + at + ks * 16 + 8);
         }
       }
     }
@@ -330,9 +387,54 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
   load_q();
   fresh();
   bool from_start = cur.tile == 0;
-  int which = 0;                                               // slot of this CTA's partial results: 1 for a run that begins here
-  bool desc_set = false;
   const float scale = rsqrtf((float)DH) * LOG2E;
+
+  // The CTA's result for channels c .. c + 3 of head h from its warps' (which lie in shared memory): sums under the maximum mx.
+  auto of_warps = [&](int h, int c, float& mx, float& l) {
+    float2 ml[S::WARPS];
+    mx = -INFINITY;
+    l = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < S::WARPS; ++w) {
+      ml[w] = sm_ml[w][h];
+      mx = fmaxf(mx, ml[w].x);
+    }
+#pragma unroll
+    for (int w = 0; w < S::WARPS; ++w) {
+      const float f = mx == -INFINITY ? 1.f : exp2f(ml[w].x - mx);
+      const float4 x = *reinterpret_cast<const float4*>(&sm_o[(w * HG + h) * S::OLD + c]);
+      l += ml[w].y * f;
+      v.x += x.x * f; v.y += x.y * f; v.z += x.z * f; v.w += x.w * f;
+    }
+    return v;
+  };
+  auto put = [&](int h, int c, float4 v, float mx, float l) {
+    const size_t head = (size_t)cur.b * a.hq + (cur.j / a.n_grp) * a.g + h0 + h;
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint2*>(a.o + head * DH + c) = make_uint2(pack_bf16x2(v.x * f, v.y * f), pack_bf16x2(v.z * f, v.w * f));
+    if (c == 0 && a.lse) a.lse[head] = (mx + log2f(l)) * LN2;
+  };
+  auto leave_warps = [&] {                                     // this warp's result into shared memory
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    float* so = sm_o + warp * HG * S::OLD;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float v = o[0][mt][c];
+        const int ch = mt * 16 + g + 8 * (c >> 1);
+        if (HG == 4) {
+          v += __shfl_xor_sync(0xffffffffu, v, 2);
+          if (t < 2) so[(2 * t + (c & 1)) * S::OLD + ch] = v;
+        } else {
+          so[(2 * t + (c & 1)) * S::OLD + ch] = v + o[PARTS - 1][mt][c];
+        }
+      }
+    if (t == 0) sm_ml[warp][g] = make_float2(top, sum);
+    __syncthreads();
+  };
 
   for (int slot = 0; to_do > 0; --to_do, slot = slot + 1 == S::STAGES ? 0 : slot + 1) {
     copies_wait<S::STAGES - 2>();
@@ -344,8 +446,9 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
 #pragma unroll
       for (int s = 0; s + 1 < S::STAGES - 1; ++s) masks[s][x] = masks[s + 1][x];
     }
-    issue(slot == 0 ? S::STAGES - 1 : slot - 1, masks[S::STAGES - 2]);
+    issue(next, slot == 0 ? S::STAGES - 1 : slot - 1, masks[S::STAGES - 2]);
     copies_commit();
+    next = look_up();
     bool any = mask[0] != 0, all = mask[0] == 0xffffffffu;
     if (RL > 1) { any = any || mask[RL - 1] != 0; all = all && mask[RL - 1] == 0xffffffffu; }
     if (any) {
@@ -359,9 +462,10 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
 #pragma unroll
         for (int ks = 0; ks < MT; ++ks) {
           uint32_t kf[4];
+          const uint32_t qf[4] = {qa[ks][0], 0u, qa[ks][1], 0u};
           ldmatrix_x4(kf, kb + S::place(nb * 16 + lrow, 2 * ks + lpiece));
-          mma_16816(s[2 * nb], qa[ks], kf[0], kf[1]);
-          mma_16816(s[2 * nb + 1], qa[ks], kf[2], kf[3]);
+          mma_16816(s[2 * nb], qf, kf[0], kf[1]);
+          mma_16816(s[2 * nb + 1], qf, kf[2], kf[3]);
         }
       }
       float most = -INFINITY;
@@ -416,57 +520,25 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
         }
       }
     }
+    if (JOINED) continue;
     // ---- the end of a run of units of one (sequence, kv head): the warps' results are joined
     const bool ends = cur.tile + 1 == cur.tiles;
     if (ends || to_do == 1) {
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      float* so = sm_o + warp * HG * S::OLD;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v = o[0][mt][c];
-          const int ch = mt * 16 + g + 8 * (c >> 1);
-          if (HG == 4) {
-            v += __shfl_xor_sync(0xffffffffu, v, 2);
-            if (t < 2) so[(2 * t + (c & 1)) * S::OLD + ch] = v;
-          } else {
-            so[(2 * t + (c & 1)) * S::OLD + ch] = v + o[PARTS - 1][mt][c];
-          }
-        }
-      if (t == 0) sm_ml[warp][g] = make_float2(top, sum);
-      __syncthreads();
+      leave_warps();
       const bool whole = from_start && ends;
-      const int j = cur.j / a.n_grp;
-      which = from_start ? 1 : 0;
-      for (int i = tid; i < nh * DH; i += NT) {
-        const int h = i / DH, c = i % DH;
-        float mx = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < S::WARPS; ++w) mx = fmaxf(mx, sm_ml[w][h].x);
-        float l = 0.f, v = 0.f;
-#pragma unroll
-        for (int w = 0; w < S::WARPS; ++w) {
-          const float f = mx == -INFINITY ? 1.f : exp2f(sm_ml[w][h].x - mx);
-          l += sm_ml[w][h].y * f;
-          v += sm_o[(w * HG + h) * S::OLD + c] * f;
-        }
-        const size_t head = (size_t)cur.b * a.hq + j * a.g + h0 + h;
+      const int slot_of = cta * 2 + (from_start ? 1 : 0);      // a run that begins here and one that began before
+      for (int i = tid; i < nh * DH / 4; i += NT) {
+        const int h = i / (DH / 4), c = i % (DH / 4) * 4;
+        float mx, l;
+        const float4 v = of_warps(h, c, mx, l);
         if (whole) {
-          a.o[head * DH + c] = __float2bfloat16(l == 0.f ? 0.f : v / l);
-          if (c == 0 && a.lse) a.lse[head] = (mx + log2f(l)) * LN2;
+          put(h, c, v, mx, l);
         } else {
-          const size_t p = ((size_t)(cta * 2 + which) * 8 + h);
-          a.part_o[p * DH + c] = v;
-          if (c == 0) a.part_ml[p] = make_float2(mx, l);
+          const size_t p = (size_t)slot_of * 8 + h;
+          __stcg(reinterpret_cast<float4*>(a.part_o + p * DH + c), v);
+          if (c == 0) __stcg(a.part_ml + p, make_float2(mx, l));
         }
       }
-      if (from_start && !ends && tid == 0) {                   // the rest of this run is other CTAs': they join it up to the last one
-        const long long end = u1 + (cur.tiles - 1 - cur.tile);  // unit behind the run's last
-        a.desc[cta] = make_int4(cur.b, cur.j, (int)((end * used - 1) / units), 0);
-      }
-      if (from_start && !ends) desc_set = true;
       if (to_do > 1) {
         cur.next(a);
         from_start = true;
@@ -478,89 +550,215 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
       ++cur.tile;
     }
   }
-  if (!desc_set && tid == 0) a.desc[cta] = make_int4(-1, 0, 0, 0);
+  if (!JOINED) return;
+
+  // ---- the cluster's results
+  leave_warps();
+  if (ranks == 1) {
+    for (int i = tid; i < nh * DH / 4; i += NT) {
+      const int h = i / (DH / 4), c = i % (DH / 4) * 4;
+      float mx, l;
+      const float4 v = of_warps(h, c, mx, l);
+      put(h, c, v, mx, l);
+    }
+    return;
+  }
+  float* cta_o = reinterpret_cast<float*>(smem);               // [nh][DH], where the loads are over
+  copies_wait<0>();
+  __syncthreads();
+  for (int i = tid; i < nh * DH / 4; i += NT) {
+    const int h = i / (DH / 4), c = i % (DH / 4) * 4;
+    float mx, l;
+    *reinterpret_cast<float4*>(&cta_o[h * DH + c]) = of_warps(h, c, mx, l);
+    if (c == 0) cta_ml[h] = make_float2(mx, l);
+  }
+  cluster_barrier();
+  const int share = nh * DH / 4 / ranks;                       // (DH / 4 is a multiple of 8)
+  for (int i = cta * share + tid; i < (cta + 1) * share; i += NT) {
+    const int h = i / (DH / 4), c = i % (DH / 4) * 4;
+    float mx = -INFINITY, l = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f), part[8];
+    float2 ml[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      ml[x] = x < ranks ? cluster_float2(&cta_ml[h], x) : make_float2(-INFINITY, 0.f);
+      part[x] = x < ranks ? cluster_float4(&cta_o[h * DH + c], x) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) mx = fmaxf(mx, ml[x].x);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float f = mx == -INFINITY ? 1.f : exp2f(ml[x].x - mx);
+      l += ml[x].y * f;
+      v.x += part[x].x * f; v.y += part[x].y * f; v.z += part[x].z * f; v.w += part[x].w * f;
+    }
+    put(h, c, v, mx, l);
+  }
+  cluster_barrier();                                           // nobody leaves while its memory may be read
 }
 
-// Joins the partial results of a run of units that several CTAs shared: CTA x is about the run that begins in CTA x of the attention
-// and is not over there, 32 channels of it.  In the order of the CTAs, so the same every time.
-constexpr int PJ_THREADS = 512, PJ_WARPS = PJ_THREADS / 32;
-template <int DH>
-__global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a) {
-  extern __shared__ float factor[];                            // [8][parts]
-  __shared__ float red[PJ_WARPS][8][32];
-  __shared__ float total[8];
+// Joins the partial results of a run of units that several CTAs shared, 4 CL channels of it, in the order of the CTAs, so the same every
+// time.  Which run: the x-th (sequence, kv head) or, where there are more of those than CTAs, the one that begins in CTA x of the attention
+// and is not over there.  That is worked out from the lengths while the attention is still running; it wrote none of them.  A slice of
+// CL lanes takes one part at a time, four channels a lane.
+constexpr int PJ_WARPS = 4, PJ_THREADS = PJ_WARPS * 32;
+template <int DH, int CL, int NH>
+__global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a, int by_run) {
+  constexpr int UNIT = At<DH>::UNIT, SLICES = PJ_THREADS / CL;
+  __shared__ float4 red[PJ_WARPS][NH][CL];
+  __shared__ float2 red_ml[PJ_WARPS][NH];
+  const int x = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int b, rows = 0, j = 0, first = 0, last = 0;
+  unsigned before;
+  const Plan p = make_plan<UNIT>(a, lane, [&](const Plan& pl) {
+    return by_run || x + 1 >= pl.used ? 0xffffffffu : (pl.begin(x + 1) - 1) / pl.groups;
+  }, b, rows, before);
+  if (by_run) {
+    b = x / p.groups;
+    j = x - b * p.groups;
+    unsigned sum = 0;
+    for (int i = lane; i < b; i += 32) sum += tiles_of<UNIT>(rows_of(a, i));
+    before = __reduce_add_sync(0xffffffffu, sum);
+    rows = rows_of(a, b);
+  }
+  const unsigned tiles = tiles_of<UNIT>(rows);
+  bool work = b >= 0 && tiles > 0;
+  if (work) {
+    if (!by_run) j = (p.begin(x + 1) - 1 - before * p.groups) / tiles;
+    const unsigned s0 = before * p.groups + j * tiles;
+    first = p.owner(s0);
+    last = p.owner(s0 + tiles - 1);
+    work = last > first && (by_run || first == x);
+  }
   pdl_enter();
-  const int first = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int4 d = a.desc[first];
-  if (d.x < 0) return;
-  const int parts = d.z - first + 1;
-  const int j = d.y / a.n_grp, h0 = (d.y - j * a.n_grp) * a.heads, nh = min(a.heads, a.g - h0);
-  auto slot = [&](int p) { return (size_t)((first + p) * 2 + (p == 0 ? 1 : 0)) * 8; };
-  if (warp < nh) {
-    float mx = -INFINITY, l = 0.f;
-    for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, a.part_ml[slot(p) + warp].x);
+  if (!work) return;
+  const int parts = last - first + 1;
+  const int kv = j / a.n_grp, h0 = (j - kv * a.n_grp) * a.heads, nh = min(a.heads, a.g - h0);
+  float mx[NH], l[NH];
+  float4 acc[NH];
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-    for (int p = lane; p < parts; p += 32) {
-      const float2 ml = a.part_ml[slot(p) + warp];
-      const float f = mx == -INFINITY ? 1.f : exp2f(ml.x - mx);
-      factor[warp * parts + p] = f;
-      l += ml.y * f;
-    }
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-    if (lane == 0) {
-      total[warp] = l;
-      if (a.lse && blockIdx.y == 0) a.lse[(size_t)d.x * a.hq + j * a.g + h0 + warp] = (mx + log2f(l)) * LN2;
-    }
-  }
-  __syncthreads();
-  float acc[8];
-#pragma unroll
-  for (int h = 0; h < 8; ++h) acc[h] = 0.f;
-  const int c = blockIdx.y * 32 + lane;
+  for (int h = 0; h < NH; ++h) { mx[h] = -INFINITY; l[h] = 0.f; acc[h] = make_float4(0.f, 0.f, 0.f, 0.f); }
+  auto factor = [](float m, float to) { return to == -INFINITY ? 1.f : exp2f(m - to); };
+  const int c = (blockIdx.y * CL + lane % CL) * 4;
 #pragma unroll 2
-  for (int p = warp; p < parts; p += PJ_WARPS) {
-    const float* po = a.part_o + slot(p) * DH + c;
+  for (int q = tid / CL; q < parts; q += SLICES) {
+    const size_t slot = (size_t)((first + q) * 2 + (q == 0 ? 1 : 0)) * 8;
+    float4 v[NH];                                              // (heads behind the pass's last hold anything and are not used)
+    float2 ml[NH];
 #pragma unroll
-    for (int h = 0; h < 8; ++h)
-      if (h < nh) acc[h] += po[h * DH] * factor[h * parts + p];
+    for (int h = 0; h < NH; ++h) {
+      v[h] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (slot + h) * DH + c));
+      ml[h] = __ldcg(a.part_ml + slot + h);
+    }
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const float now = fmaxf(mx[h], ml[h].x), f0 = factor(mx[h], now), f1 = factor(ml[h].x, now);
+      acc[h].x = acc[h].x * f0 + v[h].x * f1; acc[h].y = acc[h].y * f0 + v[h].y * f1;
+      acc[h].z = acc[h].z * f0 + v[h].z * f1; acc[h].w = acc[h].w * f0 + v[h].w * f1;
+      l[h] = l[h] * f0 + ml[h].y * f1;
+      mx[h] = now;
+    }
   }
 #pragma unroll
-  for (int h = 0; h < 8; ++h) red[warp][h][lane] = acc[h];
-  __syncthreads();
-  if (warp < nh) {
-    float v = 0.f;
+  for (int h = 0; h < NH; ++h) {
 #pragma unroll
-    for (int w = 0; w < PJ_WARPS; ++w) v += red[w][warp][lane];
-    const float l = total[warp];
-    a.o[((size_t)d.x * a.hq + j * a.g + h0 + warp) * DH + c] = __float2bfloat16(l == 0.f ? 0.f : v / l);
+    for (int s = CL; s < 32; s <<= 1) {
+      const float m2 = __shfl_xor_sync(0xffffffffu, mx[h], s), l2 = __shfl_xor_sync(0xffffffffu, l[h], s);
+      const float now = fmaxf(mx[h], m2), f0 = factor(mx[h], now), f1 = factor(m2, now);
+      acc[h].x = acc[h].x * f0 + __shfl_xor_sync(0xffffffffu, acc[h].x, s) * f1;
+      acc[h].y = acc[h].y * f0 + __shfl_xor_sync(0xffffffffu, acc[h].y, s) * f1;
+      acc[h].z = acc[h].z * f0 + __shfl_xor_sync(0xffffffffu, acc[h].z, s) * f1;
+      acc[h].w = acc[h].w * f0 + __shfl_xor_sync(0xffffffffu, acc[h].w, s) * f1;
+      l[h] = l[h] * f0 + l2 * f1;
+      mx[h] = now;
+    }
+    if (lane < CL) red[warp][h][lane] = acc[h];
+    if (lane == 0) red_ml[warp][h] = make_float2(mx[h], l[h]);
+  }
+  __syncthreads();
+  for (int i = tid; i < nh * CL; i += PJ_THREADS) {
+    const int h = i / CL;
+    float m = -INFINITY, lt = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < PJ_WARPS; ++w) m = fmaxf(m, red_ml[w][h].x);
+#pragma unroll
+    for (int w = 0; w < PJ_WARPS; ++w) {
+      const float f = factor(red_ml[w][h].x, m);
+      const float4 r = red[w][h][i % CL];
+      lt += red_ml[w][h].y * f;
+      v.x += r.x * f; v.y += r.y * f; v.z += r.z * f; v.w += r.w * f;
+    }
+    const size_t head = (size_t)b * a.hq + kv * a.g + h0 + h;
+    const float f = lt == 0.f ? 0.f : 1.f / lt;
+    *reinterpret_cast<uint2*>(a.o + head * DH + (blockIdx.y * CL + i % CL) * 4) =
+        make_uint2(pack_bf16x2(v.x * f, v.y * f), pack_bf16x2(v.z * f, v.w * f));
+    if (a.lse && blockIdx.y == 0 && i % CL == 0) a.lse[head] = (m + log2f(lt)) * LN2;
   }
 }
 
 int attn_ctas(int dh, int sm_count) { return sm_count * (dh == 256 ? 1 : 2); }
 
-template <int DH, int HG>
-cudaError_t launch_attn(const PaArgs& a, int ctas, cudaStream_t st) {
+template <int DH, int HG, bool JOINED>
+cudaError_t launch_attn(const PaArgs& a, dim3 grid, int ranks, cudaStream_t st) {
   const size_t smem = At<DH>::smem(HG);
   static bool done[MAX_DEVICES];
-  const cudaError_t e = opt_in(paged_attn_kernel<DH, HG>, (int)smem, done);
+  const cudaError_t e = opt_in(paged_attn_kernel<DH, HG, JOINED>, (int)smem, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl_smem(paged_attn_kernel<DH, HG>, dim3((unsigned)ctas), dim3(At<DH>::WARPS * 32), smem, st, a);
+  if (JOINED) return launch_clusters(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), smem, ranks, st, a);
+  return launch_pdl_smem(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), smem, st, a);
+}
+
+// CTAs of a cluster that share a (sequence, kv head), 0: the units are shared out over all CTAs and joined in a second launch.  The cheaper
+// by a count of the units that follow one another: a CTA's own, as many times as there are turns of CTAs, or those that memory delivers in that
+// time, whichever is more; 4 for a launch and 8 for two; a 128th for each CTA in a cluster, which are started one after the other; and of
+// clusters of 8 three quarters find room.  Measured (us, caches of one length, clusters of 8 / the best smaller one / shared out):
+// 8/2 x 128: 1 x 1024 4.4 / 5.5 / 5.9, 1 x 8192 14 / 25 / 8.0, 16 x 2048 7.3 / 8.3 / 11.8, 64 x 512 17 / 6.7 / 11.1, 256 x 2048 120 / 79 / 90.
+template <int DH>
+int join_ranks(const PaArgs& a, int sm_count) {
+  const long long groups = (long long)a.hk * a.n_grp, runs = groups * a.B, resident = attn_ctas(DH, sm_count);
+  const long long tiles = (a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT;
+  const long long flow = runs * tiles / (DH == 256 ? 80 : 160);             // (a unit is 64 KB at 256 channels, else 32 KB)
+  auto larger = [](long long x, long long y) { return x > y ? x : y; };
+  long long best = 128 * (8 + larger((runs * tiles + resident - 1) / resident, flow));
+  int ranks = 0;
+  for (int n = 1; n <= 8; n *= 2) {
+    const long long room = n == 8 ? resident * 3 / 4 : resident, turns = (runs * n + room - 1) / room;
+    const long long cost = 128 * (4 + larger(turns * ((tiles + n - 1) / n), flow)) + (n > 1 ? runs * n : 0);
+    if (cost < best) { best = cost; ranks = n; }
+  }
+  return ranks;
+}
+
+// Slices for as many parts as a run twice as long as the mean one has: 16 of 32 channels, or 64 of 8.
+template <int DH, int NH>
+cudaError_t launch_join(const PaArgs& a, long long runs, cudaStream_t st) {
+  const int by_run = runs <= a.ctas;
+  const unsigned x = (unsigned)(by_run ? runs : a.ctas);
+  if (a.ctas / runs <= 8) return launch_pdl(paged_join_kernel<DH, 8, NH>, dim3(x, DH / 32), dim3(PJ_THREADS), st, a, by_run);
+  return launch_pdl(paged_join_kernel<DH, 2, NH>, dim3(x, DH / 8), dim3(PJ_THREADS), st, a, by_run);
 }
 
 template <int DH>
 int launch_attention_dh(PaArgs a, int sm_count, long long* launches, cudaEvent_t ev_begin, cudaEvent_t ev_end, cudaStream_t st) {
-  const long long units = (long long)a.B * a.hk * a.n_grp * ((a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT);
-  const long long most = attn_ctas(DH, sm_count);
-  const int ctas = (int)(units < most ? units : most);
   cudaError_t e;
   if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
-  e = a.heads <= 4 ? launch_attn<DH, 4>(a, ctas, st) : launch_attn<DH, 8>(a, ctas, st);
+  const long long runs = (long long)a.B * a.hk * a.n_grp;
+  const int ranks = join_ranks<DH>(a, sm_count);
+  if (ranks > 0) {
+    const dim3 grid((unsigned)ranks, (unsigned)(a.hk * a.n_grp), (unsigned)a.B);
+    e = a.heads <= 4 ? launch_attn<DH, 4, true>(a, grid, ranks, st) : launch_attn<DH, 8, true>(a, grid, ranks, st);
+  } else {
+    const long long units = runs * ((a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT), most = attn_ctas(DH, sm_count);
+    a.ctas = (int)(units < most ? units : most);
+    const dim3 grid((unsigned)a.ctas);
+    e = a.heads <= 4 ? launch_attn<DH, 4, false>(a, grid, 0, st) : launch_attn<DH, 8, false>(a, grid, 0, st);
+  }
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   if (ev_end && (e = cudaEventRecord(ev_end, st)) != cudaSuccess) return -(int)e;
-  e = launch_pdl_smem(paged_join_kernel<DH>, dim3((unsigned)ctas, DH / 32), dim3(PJ_THREADS), (size_t)8 * ctas * 4, st, a);
+  if (ranks > 0) return 0;
+  e = a.heads <= 4 ? launch_join<DH, 4>(a, runs, st) : launch_join<DH, 8>(a, runs, st);
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
@@ -593,7 +791,7 @@ int launch_paged_read(const CcaDims& d, const Paged& c, const int* first, bf16* 
 }
 
 namespace {
-struct PagedLayout { size_t part_o, part_ml, desc, end; };
+struct PagedLayout { size_t part_o, part_ml, end; };
 PagedLayout paged_layout(const CcaDims& d, int sm_count) {
   const size_t ctas = attn_ctas(d.dh, sm_count);
   PagedLayout l;
@@ -601,7 +799,6 @@ PagedLayout paged_layout(const CcaDims& d, int sm_count) {
   auto take = [&](size_t n) { const size_t o = off; off += (n + 255) / 256 * 256; return o; };
   l.part_o = take(ctas * 2 * 8 * d.dh * 4);
   l.part_ml = take(ctas * 2 * 8 * 8);
-  l.desc = take(ctas * 16);
   l.end = off;
   return l;
 }
@@ -625,7 +822,6 @@ int launch_paged_attention(const CcaDims& d, const bf16* q, const float* q32, bf
   a.extra = extra; a.max_len = max_len; a.status = status;
   a.part_o = reinterpret_cast<float*>(ws + l.part_o);
   a.part_ml = reinterpret_cast<float2*>(ws + l.part_ml);
-  a.desc = reinterpret_cast<int4*>(ws + l.desc);
   switch (d.dh) {
     case 32: return launch_attention_dh<32>(a, sm_count, launches, ev_begin, ev_end, st);
     case 64: return launch_attention_dh<64>(a, sm_count, launches, ev_begin, ev_end, st);
