@@ -1451,7 +1451,7 @@ int cca_pages_compact(cca_handle* h, const cca_pages* c, int32_t* used, void* wo
   if ((r = check_pages_workspace(c, workspace, workspace_bytes, B)) != CCA_OK) return r;
   OnDevice on;
   CU(on.enter(h->device));
-  return enqueued(h, launch_pages_compact(make_dims(h->cfg, B, 1), make_pages(c), used, workspace, h->sm_count, &h->launches,
+  return enqueued(h, launch_pages_compact(make_dims(h->cfg, B, 1), make_pages(c), used, workspace, h->sm_count, h->d_status, &h->launches,
                                           (cudaStream_t)cuda_stream));
 }
 

@@ -44,4 +44,5 @@ int launch_pages_reserve(const CcaDims& d, const Paged& c, long long n, const in
 int launch_pages_fork(const CcaDims& d, const Paged& c, const int* parent, const int* child, int n, void* workspace, int* status,
                       long long* launches, cudaStream_t st);
 int launch_pages_free(const CcaDims& d, const Paged& c, const int* keep, int* status, long long* launches, cudaStream_t st);
-int launch_pages_compact(const CcaDims& d, const Paged& c, int* used, void* workspace, int sm_count, long long* launches, cudaStream_t st);
+int launch_pages_compact(const CcaDims& d, const Paged& c, int* used, void* workspace, int sm_count, int* status, long long* launches,
+                         cudaStream_t st);

@@ -6,10 +6,12 @@
 #include "common.cuh"
 #include "paged.cuh"
 #include "pdl.cuh"
+#include "tc_ptx.cuh"
 
 namespace {
 
 constexpr int PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
+constexpr int RANKS = 8;                                       // CTAs of a cluster
 
 // Sum of `v` over the block, and of the threads before this one (`before`).
 CCA_DEVINL int block_scan(int v, int* sm, int& before) {
@@ -34,100 +36,318 @@ CCA_DEVINL int block_scan(int v, int* sm, int& before) {
   return __shfl_sync(0xffffffffu, wu, 31);
 }
 
+// ------------------------------------------------------------------------------------------------ copies
+// Pages are copied by the bulk copy engine, 16 KB at a time through a ring in shared memory: one warp a CTA, whose first lane starts the
+// copies in and out.  A stage is filled again two steps after its copy out began, so four loads are on their way while two stages drain.
+constexpr int EN_STAGES = 6, EN_BYTES = 16384, EN_CTAS = 2;    // CTAs of an SM
+constexpr size_t EN_RING = (size_t)EN_STAGES * EN_BYTES;
+struct EngineShare {
+  uint64_t bar[EN_STAGES];
+  void* to[EN_STAGES];
+  uint32_t bytes[EN_STAGES];
+  int ctl[2];
+};
+CCA_DEVINL void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(tc::smem_u32(to)), "l"(from), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
+}
+CCA_DEVINL void bulk_store(void* to, const void* from, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(tc::smem_u32(from)), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+// Copies of one warp: item x of `items` (from, to, bytes: multiples of 16, at most EN_BYTES, for any lane's x) for x = first, first + step, ...
+template <typename Item>
+CCA_DEVINL void engine(unsigned char* ring, EngineShare& sh, long long first, long long step, long long items, Item item, int* status) {
+  const int lane = threadIdx.x & 31;
+  constexpr int LAG = EN_STAGES - 2;
+  if (lane == 0) {
+    for (int i = 0; i < EN_STAGES; ++i) tc::mbar_init(&sh.bar[i], 1);
+    tc::fence_barrier_init();
+    tc::wait_ctl_init(sh.ctl, status);
+    asm volatile("fence.proxy.async.global;" ::: "memory");    // the pages were written by ordinary stores of earlier kernels
+  }
+  __syncwarp();
+  const long long mine = items > first ? (items - first + step - 1) / step : 0;
+  const void* from = nullptr;
+  void* to = nullptr;
+  uint32_t bytes = 0;
+  bool ok = true;
+  long long i = 0;
+  for (; i < mine + LAG && ok; ++i) {
+    if (i < mine) {
+      if (i % 32 == 0 && i + lane < mine) item(first + (i + lane) * step, from, to, bytes);      // 32 items ahead, one a lane
+      const int l = (int)(i % 32), s = (int)(i % EN_STAGES);
+      const unsigned long long f = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), l);
+      const unsigned long long t = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), l);
+      const uint32_t n = __shfl_sync(0xffffffffu, bytes, l);
+      if (lane == 0) {
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        sh.to[s] = reinterpret_cast<void*>(t);
+        sh.bytes[s] = n;
+        tc::mbar_expect_tx(&sh.bar[s], n);
+        bulk_load(ring + (size_t)s * EN_BYTES, reinterpret_cast<const void*>(f), n, &sh.bar[s]);
+      }
+    }
+    if (i >= LAG) {
+      const long long k = i - LAG;
+      const int s = (int)(k % EN_STAGES);
+      if (lane == 0) {
+        ok = tc::mbar_wait(&sh.bar[s], (uint32_t)(k / EN_STAGES) & 1, sh.ctl);
+        if (ok) bulk_store(sh.to[s], ring + (size_t)s * EN_BYTES, sh.bytes[s]);
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    }
+  }
+  if (lane == 0) {
+    if (!ok) {                                                 // a load never came: the others are waited for before the CTA ends
+      atomicCAS(status, 0, tc::ST_TIMEOUT_TMA);
+      for (long long k = i - 1 - LAG; k < i && k < mine; ++k) tc::mbar_wait(&sh.bar[k % EN_STAGES], (uint32_t)(k / EN_STAGES) & 1, sh.ctl);
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  __syncwarp();
+}
+
+// The CTA's share of the copies of n pairs of pages, pair(m) for m < n: keys and values in parts of EN_BYTES.
+template <typename Pair>
+CCA_DEVINL void copy_pages(const Paged& c, int hk, int dh, int n, unsigned char* ring, EngineShare& sh, Pair pair, int* status) {
+  const long long page_bytes = (long long)hk * c.P * dh * 2;
+  const int half = (int)((page_bytes + EN_BYTES - 1) / EN_BYTES), parts = 2 * half;
+  engine(ring, sh, blockIdx.x, gridDim.x, (long long)n * parts, [&](long long x, const void*& from, void*& to, uint32_t& bytes) {
+    const int m = (int)(x / parts), part = (int)(x - (long long)m * parts);
+    const int2 ft = pair(m);
+    const long long at = (long long)(part < half ? part : part - half) * EN_BYTES;
+    unsigned char* base = reinterpret_cast<unsigned char*>(part < half ? c.k : c.v) + at;
+    from = base + ft.x * page_bytes;
+    to = base + ft.y * page_bytes;
+    bytes = (uint32_t)min((long long)EN_BYTES, page_bytes - at);
+  }, status);
+}
+
+// The same by the threads of a cluster, where few bytes can be meant.
+template <typename Pair>
+CCA_DEVINL void copy_by_threads(const Paged& c, int hk, int dh, int n, int rank, Pair pair) {
+  const unsigned pieces = (unsigned)(hk * c.P * dh / 8), all = 2 * pieces * n;              // 16 bytes each
+#pragma unroll 4
+  for (unsigned x = rank * PG_THREADS + threadIdx.x; x < all; x += RANKS * PG_THREADS) {
+    const unsigned half = x / pieces, piece = x - half * pieces;
+    const int2 ft = pair(half >> 1);
+    uint4* at = reinterpret_cast<uint4*>(half & 1 ? c.v : c.k) + piece;
+    at[(size_t)ft.y * pieces] = __ldcg(at + (size_t)ft.x * pieces);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ reserve
 struct RsArgs {
   Paged c;
   int B;
+  int width;                      // page indexes that n rows reach into at most
   long long n;
   const int *count, *first;
   int *asked, *last;              // [n_pages]: of a shared page, how many of its holders ask for it, and the last of them
   int* fresh;                     // [n_pages]: the pages handed out
   int2* pairs;                    // [n_pages]: pages to copy, from and to
-  int* need;                      // [B]: pages a sequence needs, then its place in `fresh`
   int* n_pairs;
   int hk, dh;
   int* status;
 };
 
-// Page indexes [i0, i1) of the rows that sequence b is to hold alone.
-CCA_DEVINL void window(const RsArgs& a, int b, int& i0, int& i1) {
-  i0 = i1 = 0;
+// Entry x of the list of all sequences' page indexes, `width` for each: its sequence and index; false where the sequence has fewer.
+CCA_DEVINL bool entry_of(const RsArgs& a, int x, int& b, int& i) {
+  b = x / a.width;
+  const int k = x - b * a.width;
+  if (b >= a.B) return false;
   long long n = a.n;
-  if (a.count) n = min(n, (long long)max(a.count[b], 0));
   const int from = a.first ? a.first[b] : a.c.len[b];
-  if (n == 0) return;
+  if (a.count) n = min(n, (long long)max(a.count[b], 0));
+  if (n == 0) return false;
   if (from < 0 || from + n > (long long)a.c.max_pages * a.c.P) {
-    if ((threadIdx.x & 31) == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
-    return;
+    if (k == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+    return false;
   }
-  i0 = page_index(a.c, from);
-  i1 = page_index(a.c, (int)(from + n - 1)) + 1;
+  i = page_index(a.c, from) + k;
+  return i <= page_index(a.c, (int)(from + n - 1));
 }
-// What becomes of entry e of sequence b: whether it gets a new page.
+
+// Few entries: one cluster.  The first CTA looks at the entries, of shared pages in a hash table in shared memory, while the others
+// list the free pages of a part of the pool each; then it hands these out.  HERE: all of them copy what is to be copied, otherwise
+// pages_copy_kernel does.
+constexpr int RV_ENTRIES = 4096, RV_SLOTS = 2 * RV_ENTRIES, RV_ROUNDS = RV_ENTRIES / PG_THREADS;
+struct ReserveShare {
+  int page[RV_SLOTS], asked[RV_SLOTS], last[RV_SLOTS];         // first CTA: shared pages that are asked for
+  int2 pairs[RV_ENTRIES];
+  int fresh[RV_ENTRIES];                                       // others: free pages, ascending
+  int n_fresh, n_pairs;
+  int counts[RANKS];
+  int scan[PG_WARPS];
+};
+template <bool HERE>
+__global__ void __launch_bounds__(PG_THREADS) pages_reserve_few_kernel(RsArgs a) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  ReserveShare& sh = *reinterpret_cast<ReserveShare*>(smem);
+  const int rank = blockIdx.x, tid = threadIdx.x;
+  const int entries = a.B * a.width, rounds = (entries + PG_THREADS - 1) / PG_THREADS;
+  int slots = 64;                                              // at least twice as many as entries
+  while (slots < 2 * entries) slots *= 2;
+  if (rank == 0)
+    for (int x = tid; x < slots; x += PG_THREADS) { sh.page[x] = -1; sh.asked[x] = 0; sh.last[x] = -1; }
+  if (tid == 0) sh.n_pairs = sh.n_fresh = 0;
+  __syncthreads();
+  pdl_enter();
+  int seq[RV_ROUNDS], index[RV_ROUNDS], page[RV_ROUNDS], slot[RV_ROUNDS], place[RV_ROUNDS];
+  bool wants[RV_ROUNDS];
+  int total = 0;
+  if (rank == 0) {
+    int refs[RV_ROUNDS];
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r) {
+      wants[r] = false;
+      page[r] = -1;
+      refs[r] = 0;
+      if (r < rounds) wants[r] = entry_of(a, r * PG_THREADS + tid, seq[r], index[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r)
+      if (wants[r]) page[r] = page_at(a.c, seq[r], index[r]);
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r)
+      if (page[r] >= 0) refs[r] = a.c.refs[page[r]];
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r)
+      if (refs[r] > 1) {
+        unsigned at = (unsigned)page[r] * 2654435761u;         // (multiplicative hashing)
+        for (int tries = 0; tries < slots; ++tries, ++at) {
+          slot[r] = at & (slots - 1);
+          const int was = atomicCAS(&sh.page[slot[r]], -1, page[r]);
+          if (was == -1 || was == page[r]) break;
+        }
+        atomicAdd(&sh.asked[slot[r]], 1);
+        atomicMax(&sh.last[slot[r]], seq[r]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r)
+      if (page[r] >= 0) wants[r] = refs[r] > 1 && !(sh.asked[slot[r]] == refs[r] && sh.last[slot[r]] == seq[r]);
+#pragma unroll
+    for (int r = 0; r < RV_ROUNDS; ++r)
+      if (r < rounds) {
+        const int all = block_scan(wants[r], sh.scan, place[r]);
+        place[r] += total;
+        total += all;
+      }
+  } else {
+    const int parts = RANKS - 1;
+    const int p0 = (int)((long long)a.c.n_pages * (rank - 1) / parts), p1 = (int)((long long)a.c.n_pages * rank / parts);
+    constexpr int EACH = 8;                                    // neighbouring pages a thread looks at
+    int n = 0;
+    for (int p = p0; p < p1 && n < entries; p += EACH * PG_THREADS) {
+      unsigned free = 0;
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        const int at = p + tid * EACH + k;
+        if (at < p1 && a.c.refs[at] <= 0) free |= 1u << k;
+      }
+      int before;
+      const int all = block_scan(__popc(free), sh.scan, before);
+      before += n;
+      for (; free; free &= free - 1, ++before)
+        if (before < RV_ENTRIES) sh.fresh[before] = p + tid * EACH + __ffs(free) - 1;
+      n += all;
+    }
+    if (tid == 0) sh.n_fresh = min(n, RV_ENTRIES);
+  }
+  cluster_barrier();
+  if (rank == 0) {
+    if (tid < RANKS) sh.counts[tid] = tid > 0 ? cluster_load(&sh.n_fresh, tid) : 0;
+    __syncthreads();
+    int there = 0;
+#pragma unroll
+    for (int x = 1; x < RANKS; ++x) there += sh.counts[x];
+    if (total > there && tid == 0) atomicCAS(a.status, 0, ST_PAGES_SHORT);
+    if (total <= there) {
+#pragma unroll
+      for (int r = 0; r < RV_ROUNDS; ++r)
+        if (r < rounds && wants[r]) {
+          int at = place[r], x = 1;
+          while (at >= sh.counts[x]) at -= sh.counts[x++];
+          const int fresh = cluster_load(&sh.fresh[at], x);
+          a.c.table[(size_t)seq[r] * a.c.max_pages + index[r]] = fresh;
+          a.c.refs[fresh] = 1;
+          if (page[r] >= 0) {
+            atomicSub(a.c.refs + page[r], 1);
+            sh.pairs[atomicAdd(&sh.n_pairs, 1)] = make_int2(page[r], fresh);
+          }
+        }
+    }
+    if (!HERE) {
+      __syncthreads();
+      for (int x = tid; x < sh.n_pairs; x += PG_THREADS) a.pairs[x] = sh.pairs[x];
+      if (tid == 0) *a.n_pairs = sh.n_pairs;
+    }
+  }
+  cluster_barrier();                                           // (nobody leaves while its shared memory may be read)
+  if (HERE) {
+    const int n = cluster_load(&sh.n_pairs, 0);
+    copy_by_threads(a.c, a.hk, a.dh, n, rank, [&](int x) { return cluster_load2(&sh.pairs[x].x, 0); });
+    cluster_barrier();
+  }
+}
+
+// Whether the entry gets a new page, by what has been counted in global memory.
 CCA_DEVINL bool wants_page(const RsArgs& a, int b, int e) {
   if (e < 0) return true;
   const int refs = __ldcg(a.c.refs + e);
   return refs > 1 && !(__ldcg(a.asked + e) == refs && __ldcg(a.last + e) == b);
 }
 
-// One cluster.  Its CTAs share out the sequences and the pool, both in contiguous runs, and learn each other's counts through shared memory.
-__global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(RsArgs a, int ranks) {
+// Any number of entries: one cluster whose CTAs share out the entries and the pool, both in contiguous runs.
+__global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(RsArgs a) {
   __shared__ int sm[PG_WARPS];
   __shared__ int mine[2];                                      // pages needed and pages free in this CTA's runs
-  const int rank = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int s0 = (int)((long long)a.B * rank / ranks), s1 = (int)((long long)a.B * (rank + 1) / ranks);
-  const int p0 = (int)((long long)a.c.n_pages * rank / ranks), p1 = (int)((long long)a.c.n_pages * (rank + 1) / ranks);
+  const int rank = blockIdx.x, tid = threadIdx.x;
+  const long long entries = (long long)a.B * a.width;
+  const int x0 = (int)(entries * rank / RANKS), x1 = (int)(entries * (rank + 1) / RANKS);
+  const int p0 = (int)((long long)a.c.n_pages * rank / RANKS), p1 = (int)((long long)a.c.n_pages * (rank + 1) / RANKS);
   pdl_enter();
   if (rank == 0 && tid == 0) *a.n_pairs = 0;
+  auto look = [&](int x, int& b, int& i, int& e) {             // false: no entry
+    if (x >= x1 || !entry_of(a, x, b, i)) return false;
+    e = page_at(a.c, b, i);
+    return true;
+  };
   // ---- who asks for shared pages
-  for (int b = s0 + warp; b < s1; b += PG_WARPS) {
-    int i0, i1;
-    window(a, b, i0, i1);
-    for (int i = i0 + lane; i < i1; i += 32) {
-      const int e = page_at(a.c, b, i);
-      if (e >= 0 && a.c.refs[e] > 1) { __stcg(a.asked + e, 0); __stcg(a.last + e, -1); }
-    }
+#pragma unroll 4
+  for (int x = x0 + tid; x < x1; x += PG_THREADS) {
+    int b, i, e;
+    if (look(x, b, i, e) && e >= 0 && a.c.refs[e] > 1) { __stcg(a.asked + e, 0); __stcg(a.last + e, -1); }
   }
-  all_sync(ranks);
-  for (int b = s0 + warp; b < s1; b += PG_WARPS) {
-    int i0, i1;
-    window(a, b, i0, i1);
-    for (int i = i0 + lane; i < i1; i += 32) {
-      const int e = page_at(a.c, b, i);
-      if (e >= 0 && a.c.refs[e] > 1) { atomicAdd(a.asked + e, 1); atomicMax(a.last + e, b); }
-    }
+  cluster_barrier();
+#pragma unroll 4
+  for (int x = x0 + tid; x < x1; x += PG_THREADS) {
+    int b, i, e;
+    if (look(x, b, i, e) && e >= 0 && a.c.refs[e] > 1) { atomicAdd(a.asked + e, 1); atomicMax(a.last + e, b); }
   }
-  all_sync(ranks);
-  // ---- pages needed, by sequence and in all
-  for (int b = s0 + warp; b < s1; b += PG_WARPS) {
-    int i0, i1, n = 0;
-    window(a, b, i0, i1);
-    for (int i = i0; i < i1; i += 32) {
-      const bool wants = i + lane < i1 && wants_page(a, b, page_at(a.c, b, i + lane));
-      n += __popc(__ballot_sync(0xffffffffu, wants));
-    }
-    if (lane == 0) __stcg(a.need + b, n);
+  cluster_barrier();
+  // ---- pages needed and pages free
+  int n = 0, free_here = 0;
+#pragma unroll 4
+  for (int x = x0 + tid; x < x1; x += PG_THREADS) {
+    int b, i, e;
+    n += look(x, b, i, e) && wants_page(a, b, e);
   }
-  __syncthreads();
-  int needed = 0;
-  for (int b = s0; b < s1; b += PG_THREADS) {
-    int before;
-    const int n = b + tid < s1 ? __ldcg(a.need + b + tid) : 0;
-    const int all = block_scan(n, sm, before);
-    if (b + tid < s1) __stcg(a.need + b + tid, needed + before);
-    needed += all;
-  }
-  int free_here = 0;
-  for (int p = p0; p < p1; p += PG_THREADS) {
-    free_here += __syncthreads_count(p + tid < p1 && a.c.refs[p + tid] <= 0);
-  }
-  if (tid == 0) { mine[0] = needed; mine[1] = free_here; }
-  all_sync(ranks);
-  int total = 0, free_all = 0, seq_base = 0, page_base = 0;
-  for (int x = 0; x < ranks; ++x) {
-    const int n = ranks == 1 ? mine[0] : cluster_load(&mine[0], x), f = ranks == 1 ? mine[1] : cluster_load(&mine[1], x);
-    if (x < rank) { seq_base += n; page_base += f; }
-    total += n;
+#pragma unroll 4
+  for (int p = p0 + tid; p < p1; p += PG_THREADS) free_here += a.c.refs[p] <= 0;
+  int before;
+  n = block_scan(n, sm, before);
+  free_here = block_scan(free_here, sm, before);
+  if (tid == 0) { mine[0] = n; mine[1] = free_here; }
+  cluster_barrier();
+  int total = 0, free_all = 0, need_base = 0, page_base = 0;
+  for (int x = 0; x < RANKS; ++x) {
+    const int need = cluster_load(&mine[0], x), f = cluster_load(&mine[1], x);
+    if (x < rank) { need_base += need; page_base += f; }
+    total += need;
     free_all += f;
   }
   if (total > free_all && rank == 0 && tid == 0) atomicCAS(a.status, 0, ST_PAGES_SHORT);
@@ -135,60 +355,40 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(RsArgs a, int
   // ---- the free pages, ascending, as many as are needed
   if (go)
     for (int p = p0, at = page_base; p < p1 && at < total; p += PG_THREADS) {
-      int before;
       const bool is_free = p + tid < p1 && a.c.refs[p + tid] <= 0;
       const int all = block_scan(is_free, sm, before);
       if (is_free && at + before < total) __stcg(a.fresh + at + before, p + tid);
       at += all;
     }
-  all_sync(ranks);                                             // (nobody leaves while its shared memory may be read)
+  cluster_barrier();                                             // (nobody leaves while its shared memory may be read)
   if (!go) return;
-  // ---- handed out in the order of the sequences and their pages
-  for (int b = s0 + warp; b < s1; b += PG_WARPS) {
-    int i0, i1, at = seq_base + __ldcg(a.need + b);
-    window(a, b, i0, i1);
-    for (int i = i0; i < i1; i += 32) {
-      const int e = i + lane < i1 ? page_at(a.c, b, i + lane) : -1;
-      const bool wants = i + lane < i1 && wants_page(a, b, e);
-      const unsigned all = __ballot_sync(0xffffffffu, wants);
-      if (wants) {
-        const int page = __ldcg(a.fresh + at + __popc(all & ((1u << lane) - 1)));
-        a.c.table[(size_t)b * a.c.max_pages + i + lane] = page;
-        a.c.refs[page] = 1;
-        if (e >= 0) a.pairs[atomicAdd(a.n_pairs, 1)] = make_int2(e, page);     // refs[e] falls with the copy
-      }
-      at += __popc(all);
+  // ---- handed out in the order of the entries
+  for (int x = x0, at = need_base; x < x1; x += PG_THREADS) {
+    int b, i, e;
+    const bool wants = look(x + tid, b, i, e) && wants_page(a, b, e);
+    const int all = block_scan(wants, sm, before);
+    if (wants) {
+      const int page = __ldcg(a.fresh + at + before);
+      a.c.table[(size_t)b * a.c.max_pages + i] = page;
+      a.c.refs[page] = 1;
+      if (e >= 0) a.pairs[atomicAdd(a.n_pairs, 1)] = make_int2(e, page);       // refs[e] falls with the copy: it is still read here
     }
+    at += all;
   }
 }
 
-constexpr int CP_THREADS = 256, CP_PIECES = 1024;              // 16-byte pieces a block copies at once
-
-CCA_DEVINL void copy_pieces(const Paged& c, int from, int to, long long page_pieces, int part, int tid) {
-  const long long parts = (page_pieces + CP_PIECES - 1) / CP_PIECES;
-  const bool v = part >= parts;
-  const long long p0 = (long long)(v ? part - parts : part) * CP_PIECES;
-  const uint4* src = reinterpret_cast<const uint4*>(v ? c.v : c.k) + (size_t)from * page_pieces;
-  uint4* dst = reinterpret_cast<uint4*>(v ? c.v : c.k) + (size_t)to * page_pieces;
-  uint4 x[CP_PIECES / CP_THREADS];
-#pragma unroll
-  for (int i = 0; i < CP_PIECES / CP_THREADS; ++i)
-    if (p0 + i * CP_THREADS + tid < page_pieces) x[i] = __ldcs(src + p0 + i * CP_THREADS + tid);
-#pragma unroll
-  for (int i = 0; i < CP_PIECES / CP_THREADS; ++i)
-    if (p0 + i * CP_THREADS + tid < page_pieces) dst[p0 + i * CP_THREADS + tid] = x[i];
-}
-
-__global__ void __launch_bounds__(CP_THREADS) pages_copy_kernel(RsArgs a) {
+// What has been paired, copied; `let_go`: the old pages' counts fall here.
+constexpr int CP_THREADS = 256;
+__global__ void __launch_bounds__(CP_THREADS) pages_copy_kernel(RsArgs a, int let_go) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ EngineShare sh;
   pdl_enter();
-  const long long page_pieces = (long long)a.hk * a.c.P * a.dh / 8;
-  const int parts = 2 * (int)((page_pieces + CP_PIECES - 1) / CP_PIECES);
-  const long long items = (long long)*a.n_pairs * parts;
-  for (long long x = blockIdx.x; x < items; x += gridDim.x) {
-    const int pair = (int)(x / parts), part = (int)(x - (long long)pair * parts);
-    const int2 ft = a.pairs[pair];
-    copy_pieces(a.c, ft.x, ft.y, page_pieces, part, threadIdx.x);
-    if (part == 0 && threadIdx.x == 0) atomicSub(a.c.refs + ft.x, 1);
+  const int n = *a.n_pairs;
+  if (threadIdx.x < 32) {
+    copy_pages(a.c, a.hk, a.dh, n, ring, sh, [&](int x) { return a.pairs[x]; }, a.status);
+  } else if (let_go) {
+    for (long long x = (long long)blockIdx.x * (CP_THREADS - 32) + threadIdx.x - 32; x < n; x += (long long)gridDim.x * (CP_THREADS - 32))
+      atomicSub(a.c.refs + a.pairs[x].x, 1);
   }
 }
 
@@ -201,51 +401,104 @@ struct FkArgs {
   int* lens;                      // [n]: their lengths, -1: nothing to do
   int* status;
 };
-constexpr int FK_THREADS = 256;
+constexpr int FK_THREADS = 256, FK_EACH = 4;                   // table entries that a thread has on their way at once
 
-CCA_DEVINL void let_go(const Paged& c, int page, int* status) {
-  if (atomicSub(c.refs + page, 1) <= 0) {                      // held by nobody: the table and the counts do not agree
-    atomicAdd(c.refs + page, 1);
-    atomicCAS(status, 0, ST_PAGE_MISSING);
-  }
+CCA_DEVINL void let_go(const Paged& c, const int* page, int* status) {     // FK_EACH pages, -1: none
+  int held[FK_EACH];
+#pragma unroll
+  for (int k = 0; k < FK_EACH; ++k) held[k] = page[k] >= 0 ? atomicSub(c.refs + page[k], 1) : 1;
+#pragma unroll
+  for (int k = 0; k < FK_EACH; ++k)
+    if (held[k] <= 0) {                                        // held by nobody: the table and the counts do not agree
+      atomicAdd(c.refs + page[k], 1);
+      atomicCAS(status, 0, ST_PAGE_MISSING);
+    }
 }
 
-// Everything that is read of the state before the call: the parents' rows, kept aside; the counts change here, in any order.
-__global__ void __launch_bounds__(FK_THREADS) pages_fork_read_kernel(FkArgs a) {
-  pdl_enter();
-  const int x = blockIdx.x, tid = threadIdx.x;
+struct AnyOfBlock {
+  static constexpr int threads = FK_THREADS;
+  CCA_DEVINL bool operator()(bool v) const { return __syncthreads_or(v) != 0; }
+};
+struct AnyOfWarp {
+  static constexpr int threads = 32;
+  CCA_DEVINL bool operator()(bool v) const { return __any_sync(0xffffffffu, v) != 0; }
+};
+// Pair x, by `threads` threads: everything that is read of the state before the call.  The parent's row is kept aside; the counts change
+// here, in any order.  Returns the child's new length, -1: nothing to do.  any(v): whether one of its
+// group of threads, which look at all later pairs together, has v.
+template <typename Any>
+CCA_DEVINL int fork_read(const FkArgs& a, int x, int tid, int threads, Any any) {
   const int p = a.parent[x], c = a.child[x];
   const bool inside = (unsigned)p < (unsigned)a.B && (unsigned)c < (unsigned)a.B;
-  int len = inside ? a.c.len[p] : -1;
+  int len = inside ? __ldcg(a.c.len + p) : -1;
   bool later = false;                                          // another pair has the same child: the last one counts
-  for (int y = x + 1 + tid; y < a.n; y += FK_THREADS)
+  const int group = any.threads;
+  for (int y = x + 1 + tid % group; y < a.n; y += group)
     if (a.child[y] == c && (unsigned)a.parent[y] < (unsigned)a.B) later = true;
-  later = __syncthreads_or(later);
+  later = any(later);
   const long long held = len < 0 ? 0 : ((long long)len + a.c.P - 1) / a.c.P;
   if (len < 0 || held > a.c.max_pages) {
     if (tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
     len = -1;
   }
   const bool go = len >= 0 && !later && p != c;
-  if (tid == 0) a.lens[x] = go ? len : -1;
-  if (!go) return;
-  for (int i = tid; i < a.c.max_pages; i += FK_THREADS) {
-    const int e = i < held ? page_at(a.c, p, i) : -1, old = page_at(a.c, c, i);
-    a.rows[(size_t)x * a.c.max_pages + i] = e;
-    if (e == old) continue;
-    if (e >= 0) atomicAdd(a.c.refs + e, 1);
-    if (old >= 0) let_go(a.c, old, a.status);
+  if (!go) return -1;
+  for (int i0 = tid; i0 < a.c.max_pages; i0 += FK_EACH * threads) {
+    int e[FK_EACH], old[FK_EACH];
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) {
+      const int i = i0 + k * threads;
+      e[k] = i < held ? page_at(a.c, p, i) : -1;
+      old[k] = i < a.c.max_pages ? page_at(a.c, c, i) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) {
+      const int i = i0 + k * threads;
+      if (i < a.c.max_pages) __stcg(a.rows + (size_t)x * a.c.max_pages + i, e[k]);
+      if (e[k] == old[k]) e[k] = old[k] = -1;
+      if (e[k] >= 0) atomicAdd(a.c.refs + e[k], 1);
+    }
+    let_go(a.c, old, a.status);
   }
+  return len;
+}
+CCA_DEVINL void fork_write(const FkArgs& a, int x, int len, int tid, int threads) {
+  if (len < 0) return;
+  const int c = a.child[x];
+  for (int i0 = tid; i0 < a.c.max_pages; i0 += FK_EACH * threads) {
+    int e[FK_EACH];
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) {
+      const int i = i0 + k * threads;
+      if (i < a.c.max_pages) e[k] = __ldcg(a.rows + (size_t)x * a.c.max_pages + i);
+    }
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) {
+      const int i = i0 + k * threads;
+      if (i < a.c.max_pages) a.c.table[(size_t)c * a.c.max_pages + i] = e[k];
+    }
+  }
+  if (tid == 0) a.c.len[c] = len;
+}
+__global__ void __launch_bounds__(FK_THREADS) pages_fork_read_kernel(FkArgs a) {
+  pdl_enter();
+  const int len = fork_read(a, blockIdx.x, threadIdx.x, FK_THREADS, AnyOfBlock{});
+  if (threadIdx.x == 0) a.lens[blockIdx.x] = len;
 }
 __global__ void __launch_bounds__(FK_THREADS) pages_fork_write_kernel(FkArgs a) {
   pdl_enter();
-  const int x = blockIdx.x, tid = threadIdx.x;
-  const int len = a.lens[x];
-  if (len < 0) return;
-  const int c = a.child[x];
-  for (int i = tid; i < a.c.max_pages; i += FK_THREADS)
-    a.c.table[(size_t)c * a.c.max_pages + i] = a.rows[(size_t)x * a.c.max_pages + i];
-  if (tid == 0) a.c.len[c] = len;
+  fork_write(a, blockIdx.x, a.lens[blockIdx.x], threadIdx.x, FK_THREADS);
+}
+// Both in one launch: a cluster of 8, a pair by some of its warps.
+__global__ void __launch_bounds__(PG_THREADS) pages_fork_few_kernel(FkArgs a) {
+  pdl_enter();
+  const int each = gridDim.x * PG_WARPS / a.n;                 // warps of a pair
+  const int w = blockIdx.x * PG_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int x = w / each, t = w % each * 32 + lane, threads = each * 32;
+  int len = -1;
+  if (x < a.n) len = fork_read(a, x, t, threads, AnyOfWarp{});
+  cluster_barrier();
+  if (x < a.n) fork_write(a, x, len, t, threads);
 }
 
 struct FrArgs {
@@ -261,13 +514,18 @@ __global__ void __launch_bounds__(FK_THREADS) pages_free_kernel(FrArgs a) {
   const int left = max(min(keep, len), 0);
   __syncthreads();                                             // everybody has read the length
   if (tid == 0) a.c.len[b] = left;
+  int* row = a.c.table + (size_t)b * a.c.max_pages;
   const long long held = ((long long)left + a.c.P - 1) / a.c.P;
-  for (long long i = held + tid; i < a.c.max_pages; i += FK_THREADS) {
-    int* at = a.c.table + (size_t)b * a.c.max_pages + i;
-    const int e = *at;
-    if (e == -1) continue;
-    *at = -1;
-    if ((unsigned)e < (unsigned)a.c.n_pages) let_go(a.c, e, a.status);
+  for (long long i0 = held + tid; i0 < a.c.max_pages; i0 += FK_EACH * FK_THREADS) {
+    int e[FK_EACH];
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) e[k] = i0 + k * FK_THREADS < a.c.max_pages ? row[i0 + k * FK_THREADS] : -1;
+#pragma unroll
+    for (int k = 0; k < FK_EACH; ++k) {
+      if (e[k] != -1) row[i0 + k * FK_THREADS] = -1;
+      if ((unsigned)e[k] >= (unsigned)a.c.n_pages) e[k] = -1;
+    }
+    let_go(a.c, e, a.status);
   }
 }
 
@@ -280,66 +538,81 @@ struct CmArgs {
   int* number;                    // [n_pages]: a page's number among the held ones, -1 where it is free (behind the held ones' count)
   int* counts;                    // held pages, moving pages
   int* used;                      // the caller's
+  int* status;
 };
 
-// One cluster, as in pages_reserve_kernel: held pages are counted, then those that move and the places they go to are listed.
-__global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(CmArgs a, int ranks) {
+// One cluster: held pages are counted, then those that move and the places they go to are listed, each CTA a contiguous run of the pool.
+__global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(CmArgs a) {
   __shared__ int sm[PG_WARPS];
-  __shared__ int mine[1];
+  __shared__ int mine;                                         // held pages of this CTA's run
   const int rank = blockIdx.x, tid = threadIdx.x;
-  const int p0 = (int)((long long)a.c.n_pages * rank / ranks), p1 = (int)((long long)a.c.n_pages * (rank + 1) / ranks);
+  const int p0 = (int)((long long)a.c.n_pages * rank / RANKS), p1 = (int)((long long)a.c.n_pages * (rank + 1) / RANKS);
+  constexpr int EACH = 4;                                      // neighbouring pages of a thread
   pdl_enter();
   if (rank == 0 && tid == 0) a.counts[1] = 0;
-  int held = 0;
-  for (int p = p0; p < p1; p += PG_THREADS) held += __syncthreads_count(p + tid < p1 && a.c.refs[p + tid] > 0);
-  if (tid == 0) mine[0] = held;
-  all_sync(ranks);
+  int held = 0, before;
+#pragma unroll 4
+  for (int p = p0 + tid; p < p1; p += PG_THREADS) held += a.c.refs[p] > 0;
+  held = block_scan(held, sm, before);
+  if (tid == 0) mine = held;
+  cluster_barrier();
   int total = 0, at = 0;
-  for (int x = 0; x < ranks; ++x) {
-    const int n = ranks == 1 ? mine[0] : cluster_load(&mine[0], x);
+  for (int x = 0; x < RANKS; ++x) {
+    const int n = cluster_load(&mine, x);
     if (x < rank) at += n;
     total += n;
   }
-  all_sync(ranks);                                             // (nobody leaves while its shared memory may be read)
   if (rank == 0 && tid == 0) { a.counts[0] = total; *a.used = total; }
   int holes = 0;
-  for (int p = p0; p < p1; p += PG_THREADS) {
-    const int page = p + tid;
-    const bool is_held = page < p1 && a.c.refs[page] > 0;
-    int before;
-    const int all = block_scan(is_held, sm, before);
-    const int number = at + before;
-    if (page < p1) {
-      if (page >= total) {
-        a.number[page] = is_held ? number : -1;
-        if (is_held) a.src[number] = page;
-      } else if (!is_held) {
-        a.dst[page - number] = page;
+  for (int p = p0; p < p1; p += EACH * PG_THREADS) {
+    int refs[EACH], n = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int page = p + tid * EACH + k;
+      refs[k] = page < p1 ? a.c.refs[page] : 0;
+      n += refs[k] > 0;
+    }
+    const int all = block_scan(n, sm, before);
+    int number = at + before;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int page = p + tid * EACH + k;
+      if (page < p1) {
+        if (page >= total) {
+          a.number[page] = refs[k] > 0 ? number : -1;
+          if (refs[k] > 0) a.src[number] = page;
+        } else if (refs[k] <= 0) {
+          a.dst[page - number] = page;
+          ++holes;
+        }
+        number += refs[k] > 0;
       }
     }
-    holes += __syncthreads_count(page < p1 && page < total && !is_held);
     at += all;
   }
+  holes = block_scan(holes, sm, before);
   if (tid == 0 && holes) atomicAdd(a.counts + 1, holes);
+  cluster_barrier();                                           // (nobody leaves while its shared memory may be read)
 }
 __global__ void __launch_bounds__(CP_THREADS) pages_move_kernel(CmArgs a) {
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ EngineShare sh;
   pdl_enter();
-  const int total = a.counts[0], moves = a.counts[1], stay = total - moves;      // number of the first held page that moves
+  const int total = a.counts[0], moves = a.counts[1], stay = total - moves;
   if (moves == 0) return;
-  const long long page_pieces = (long long)a.hk * a.c.P * a.dh / 8;
-  const int parts = 2 * (int)((page_pieces + CP_PIECES - 1) / CP_PIECES);
-  const long long items = (long long)moves * parts;
-  for (long long x = blockIdx.x; x < items; x += gridDim.x) {
-    const int m = (int)(x / parts), part = (int)(x - (long long)m * parts);
+  if (threadIdx.x < 32) {
+    copy_pages(a.c, a.hk, a.dh, moves, ring, sh, [&](int m) { return make_int2(a.src[stay + m], a.dst[m]); }, a.status);
+    return;
+  }
+  const long long t = (long long)blockIdx.x * (CP_THREADS - 32) + threadIdx.x - 32, threads = (long long)gridDim.x * (CP_THREADS - 32);
+  for (long long m = t; m < moves; m += threads) {
     const int from = a.src[stay + m], to = a.dst[m];
-    copy_pieces(a.c, from, to, page_pieces, part, threadIdx.x);
-    if (part == 0 && threadIdx.x == 0) {
-      a.c.refs[to] = a.c.refs[from];
-      a.c.refs[from] = 0;
-    }
+    a.c.refs[to] = a.c.refs[from];
+    a.c.refs[from] = 0;
   }
   const long long entries = (long long)a.B * a.c.max_pages;
-  for (long long i = (long long)blockIdx.x * CP_THREADS + threadIdx.x; i < entries; i += (long long)gridDim.x * CP_THREADS) {
+#pragma unroll 4
+  for (long long i = t; i < entries; i += threads) {
     const int e = a.c.table[i];
     if (e >= total && e < a.c.n_pages) {
       const int number = a.number[e];
@@ -348,10 +621,19 @@ __global__ void __launch_bounds__(CP_THREADS) pages_move_kernel(CmArgs a) {
   }
 }
 
-int cluster_ranks(long long) { return 8; }
-int copy_blocks(int sm_count) { return sm_count * 8; }         // what is resident at 256 threads
+constexpr int FK_FEW = 64;                                     // pairs that one cluster forks, a few warps each
+constexpr long long FEW_BYTES = 256 << 10;                     // that the threads of one cluster copy before all SMs pay for a second launch
 
-struct PagesLayout { size_t asked, last, fresh, pairs, need, counts, rows, lens, end; };
+template <typename... KArgs, typename... Args>
+int launch_copies(void (*kernel)(KArgs...), bool* done, int sm_count, long long* launches, cudaStream_t st, Args... args) {
+  cudaError_t e = opt_in(kernel, (int)EN_RING, done);
+  if (e == cudaSuccess) e = launch_pdl_smem(kernel, dim3((unsigned)(sm_count * EN_CTAS)), dim3(CP_THREADS), EN_RING, st, args...);
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+struct PagesLayout { size_t asked, last, fresh, pairs, counts, rows, lens, end; };
 PagesLayout pages_layout(long long n_pages, long long max_pages, long long B) {
   PagesLayout l;
   size_t off = 0, fork = 0;
@@ -360,7 +642,6 @@ PagesLayout pages_layout(long long n_pages, long long max_pages, long long B) {
   l.last = take(off, (size_t)n_pages * 4);
   l.fresh = take(off, (size_t)n_pages * 4);
   l.pairs = take(off, (size_t)n_pages * 8);
-  l.need = take(off, (size_t)B * 4);
   l.counts = take(off, 8);
   l.rows = take(fork, (size_t)B * max_pages * 4);
   l.lens = take(fork, (size_t)B * 4);
@@ -380,15 +661,25 @@ int launch_pages_reserve(const CcaDims& d, const Paged& c, long long n, const in
   RsArgs a;
   memset(&a, 0, sizeof(a));
   a.c = c; a.B = d.B; a.n = n; a.count = count; a.first = first; a.asked = at(l.asked); a.last = at(l.last); a.fresh = at(l.fresh);
-  a.pairs = reinterpret_cast<int2*>(ws + l.pairs); a.need = at(l.need); a.n_pairs = at(l.counts); a.hk = d.hk; a.dh = d.dh; a.status = status;
-  const int ranks = cluster_ranks(c.n_pages);
-  cudaError_t e = launch_clusters(pages_reserve_kernel, dim3((unsigned)ranks), dim3(PG_THREADS), 0, ranks, st, a, ranks);
+  a.pairs = reinterpret_cast<int2*>(ws + l.pairs); a.n_pairs = at(l.counts); a.hk = d.hk; a.dh = d.dh; a.status = status;
+  const long long width = (n + c.P - 2) / c.P + 1, page_bytes = 4ll * d.hk * c.P * d.dh;
+  a.width = (int)(width < c.max_pages ? width : c.max_pages);
+  const long long entries = (long long)d.B * a.width;
+  const bool few = entries <= RV_ENTRIES, here = few && entries * page_bytes <= FEW_BYTES;
+  static bool done[3][MAX_DEVICES];
+  cudaError_t e = cudaSuccess;
+  if (few) {
+    e = here ? opt_in(pages_reserve_few_kernel<true>, (int)sizeof(ReserveShare), done[0])
+             : opt_in(pages_reserve_few_kernel<false>, (int)sizeof(ReserveShare), done[1]);
+    if (e == cudaSuccess)
+      e = launch_clusters(here ? pages_reserve_few_kernel<true> : pages_reserve_few_kernel<false>, dim3(RANKS), dim3(PG_THREADS),
+                          sizeof(ReserveShare), RANKS, st, a);
+  } else {
+    e = launch_clusters(pages_reserve_kernel, dim3(RANKS), dim3(PG_THREADS), 0, RANKS, st, a);
+  }
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
-  e = launch_pdl(pages_copy_kernel, dim3((unsigned)copy_blocks(sm_count)), dim3(CP_THREADS), st, a);
-  if (e != cudaSuccess) return -(int)e;
-  ++*launches;
-  return 0;
+  return here ? 0 : launch_copies(pages_copy_kernel, done[2], sm_count, launches, st, a, (int)!few);
 }
 
 int launch_pages_fork(const CcaDims& d, const Paged& c, const int* parent, const int* child, int n, void* workspace, int* status,
@@ -399,8 +690,13 @@ int launch_pages_fork(const CcaDims& d, const Paged& c, const int* parent, const
   memset(&a, 0, sizeof(a));
   a.c = c; a.B = d.B; a.n = n; a.parent = parent; a.child = child; a.rows = reinterpret_cast<int*>(ws + l.rows);
   a.lens = reinterpret_cast<int*>(ws + l.lens); a.status = status;
-  cudaError_t e = launch_pdl(pages_fork_read_kernel, dim3((unsigned)n), dim3(FK_THREADS), st, a);
-  if (e != cudaSuccess) return -(int)e;
+  cudaError_t e;
+  if (n <= FK_FEW) {
+    if ((e = launch_clusters(pages_fork_few_kernel, dim3(RANKS), dim3(PG_THREADS), 0, RANKS, st, a)) != cudaSuccess) return -(int)e;
+    ++*launches;
+    return 0;
+  }
+  if ((e = launch_pdl(pages_fork_read_kernel, dim3((unsigned)n), dim3(FK_THREADS), st, a)) != cudaSuccess) return -(int)e;
   ++*launches;
   if ((e = launch_pdl(pages_fork_write_kernel, dim3((unsigned)n), dim3(FK_THREADS), st, a)) != cudaSuccess) return -(int)e;
   ++*launches;
@@ -414,19 +710,18 @@ int launch_pages_free(const CcaDims& d, const Paged& c, const int* keep, int* st
   return 0;
 }
 
-int launch_pages_compact(const CcaDims& d, const Paged& c, int* used, void* workspace, int sm_count, long long* launches, cudaStream_t st) {
+int launch_pages_compact(const CcaDims& d, const Paged& c, int* used, void* workspace, int sm_count, int* status, long long* launches,
+                         cudaStream_t st) {
   const PagesLayout l = pages_layout(c.n_pages, c.max_pages, d.B);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   auto at = [&](size_t o) { return reinterpret_cast<int*>(ws + o); };
   CmArgs a;
   memset(&a, 0, sizeof(a));
   a.c = c; a.B = d.B; a.hk = d.hk; a.dh = d.dh; a.src = at(l.asked); a.dst = at(l.last); a.number = at(l.fresh); a.counts = at(l.counts);
-  a.used = used;
-  const int ranks = cluster_ranks(c.n_pages);
-  cudaError_t e = launch_clusters(pages_compact_kernel, dim3((unsigned)ranks), dim3(PG_THREADS), 0, ranks, st, a, ranks);
+  a.used = used; a.status = status;
+  const cudaError_t e = launch_clusters(pages_compact_kernel, dim3(RANKS), dim3(PG_THREADS), 0, RANKS, st, a);
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
-  if ((e = launch_pdl(pages_move_kernel, dim3((unsigned)copy_blocks(sm_count)), dim3(CP_THREADS), st, a)) != cudaSuccess) return -(int)e;
-  ++*launches;
-  return 0;
+  static bool done[MAX_DEVICES];
+  return launch_copies(pages_move_kernel, done, sm_count, launches, st, a);
 }
