@@ -597,17 +597,18 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
   cluster_barrier();                                           // nobody leaves while its memory may be read
 }
 
-// Joins the partial results of a run of units that several CTAs shared, 4 CL channels of it, in the order of the CTAs, so the same every
+// Joins the partial results of a run of units that several CTAs shared, 4 CL channels of one head, in a fixed order, so the same every
 // time.  Which run: the x-th (sequence, kv head) or, where there are more of those than CTAs, the one that begins in CTA x of the attention
 // and is not over there.  That is worked out from the lengths while the attention is still running; it wrote none of them.  A slice of
-// CL lanes takes one part at a time, four channels a lane.
+// CL lanes takes one part at a time, four channels a lane; a head's slices are those of a warp (ONE) or of the CTA.
 constexpr int PJ_WARPS = 4, PJ_THREADS = PJ_WARPS * 32;
-template <int DH, int CL, int NH>
+template <int DH, int CL, bool ONE>
 __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a, int by_run) {
-  constexpr int UNIT = At<DH>::UNIT, SLICES = PJ_THREADS / CL;
-  __shared__ float4 red[PJ_WARPS][NH][CL];
-  __shared__ float2 red_ml[PJ_WARPS][NH];
+  constexpr int UNIT = At<DH>::UNIT, SLICES = (ONE ? 32 : PJ_THREADS) / CL;
+  __shared__ float4 red[PJ_WARPS][CL];
+  __shared__ float2 red_ml[PJ_WARPS];
   const int x = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int h = ONE ? blockIdx.z * PJ_WARPS + warp : blockIdx.z;
   int b, rows = 0, j = 0, first = 0, last = 0;
   unsigned before;
   const Plan p = make_plan<UNIT>(a, lane, [&](const Plan& pl) {
@@ -633,68 +634,56 @@ __global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(PaArgs a, int by
   pdl_enter();
   if (!work) return;
   const int parts = last - first + 1;
-  const int kv = j / a.n_grp, h0 = (j - kv * a.n_grp) * a.heads, nh = min(a.heads, a.g - h0);
-  float mx[NH], l[NH];
-  float4 acc[NH];
-#pragma unroll
-  for (int h = 0; h < NH; ++h) { mx[h] = -INFINITY; l[h] = 0.f; acc[h] = make_float4(0.f, 0.f, 0.f, 0.f); }
+  const int kv = j / a.n_grp, h0 = (j - kv * a.n_grp) * a.heads;
+  if (h >= min(a.heads, a.g - h0)) return;                     // (ONE: a warp alone; otherwise the whole CTA)
+  float mx = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   auto factor = [](float m, float to) { return to == -INFINITY ? 1.f : exp2f(m - to); };
+  auto add = [&](float4 v, float2 ml) {
+    const float now = fmaxf(mx, ml.x), f0 = factor(mx, now), f1 = factor(ml.x, now);
+    acc.x = acc.x * f0 + v.x * f1; acc.y = acc.y * f0 + v.y * f1;
+    acc.z = acc.z * f0 + v.z * f1; acc.w = acc.w * f0 + v.w * f1;
+    l = l * f0 + ml.y * f1;
+    mx = now;
+  };
   const int c = (blockIdx.y * CL + lane % CL) * 4;
-#pragma unroll 2
-  for (int q = tid / CL; q < parts; q += SLICES) {
-    const size_t slot = (size_t)((first + q) * 2 + (q == 0 ? 1 : 0)) * 8;
-    float4 v[NH];                                              // (heads behind the pass's last hold anything and are not used)
-    float2 ml[NH];
+  constexpr int AHEAD = 4;                                     // parts of a slice on their way
+  for (int q0 = (ONE ? lane : tid) / CL; q0 < parts; q0 += AHEAD * SLICES) {
+    float4 v[AHEAD];
+    float2 ml[AHEAD];
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      v[h] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (slot + h) * DH + c));
-      ml[h] = __ldcg(a.part_ml + slot + h);
+    for (int k = 0; k < AHEAD; ++k) {
+      const int q = q0 + k * SLICES;
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      ml[k] = make_float2(-INFINITY, 0.f);
+      if (q < parts) {
+        const size_t slot = (size_t)((first + q) * 2 + (q == 0 ? 1 : 0)) * 8 + h;
+        v[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + slot * DH + c));
+        ml[k] = __ldcg(a.part_ml + slot);
+      }
     }
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      const float now = fmaxf(mx[h], ml[h].x), f0 = factor(mx[h], now), f1 = factor(ml[h].x, now);
-      acc[h].x = acc[h].x * f0 + v[h].x * f1; acc[h].y = acc[h].y * f0 + v[h].y * f1;
-      acc[h].z = acc[h].z * f0 + v[h].z * f1; acc[h].w = acc[h].w * f0 + v[h].w * f1;
-      l[h] = l[h] * f0 + ml[h].y * f1;
-      mx[h] = now;
-    }
+    for (int k = 0; k < AHEAD; ++k) add(v[k], ml[k]);
   }
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
-#pragma unroll
-    for (int s = CL; s < 32; s <<= 1) {
-      const float m2 = __shfl_xor_sync(0xffffffffu, mx[h], s), l2 = __shfl_xor_sync(0xffffffffu, l[h], s);
-      const float now = fmaxf(mx[h], m2), f0 = factor(mx[h], now), f1 = factor(m2, now);
-      acc[h].x = acc[h].x * f0 + __shfl_xor_sync(0xffffffffu, acc[h].x, s) * f1;
-      acc[h].y = acc[h].y * f0 + __shfl_xor_sync(0xffffffffu, acc[h].y, s) * f1;
-      acc[h].z = acc[h].z * f0 + __shfl_xor_sync(0xffffffffu, acc[h].z, s) * f1;
-      acc[h].w = acc[h].w * f0 + __shfl_xor_sync(0xffffffffu, acc[h].w, s) * f1;
-      l[h] = l[h] * f0 + l2 * f1;
-      mx[h] = now;
-    }
-    if (lane < CL) red[warp][h][lane] = acc[h];
-    if (lane == 0) red_ml[warp][h] = make_float2(mx[h], l[h]);
+  for (int s = CL; s < 32; s <<= 1) {
+    const float2 ml = make_float2(__shfl_xor_sync(0xffffffffu, mx, s), __shfl_xor_sync(0xffffffffu, l, s));
+    add(make_float4(__shfl_xor_sync(0xffffffffu, acc.x, s), __shfl_xor_sync(0xffffffffu, acc.y, s),
+                    __shfl_xor_sync(0xffffffffu, acc.z, s), __shfl_xor_sync(0xffffffffu, acc.w, s)), ml);
   }
-  __syncthreads();
-  for (int i = tid; i < nh * CL; i += PJ_THREADS) {
-    const int h = i / CL;
-    float m = -INFINITY, lt = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!ONE) {
+    if (lane < CL) red[warp][lane] = acc;
+    if (lane == 0) red_ml[warp] = make_float2(mx, l);
+    __syncthreads();
+    if (tid >= CL) return;
 #pragma unroll
-    for (int w = 0; w < PJ_WARPS; ++w) m = fmaxf(m, red_ml[w][h].x);
-#pragma unroll
-    for (int w = 0; w < PJ_WARPS; ++w) {
-      const float f = factor(red_ml[w][h].x, m);
-      const float4 r = red[w][h][i % CL];
-      lt += red_ml[w][h].y * f;
-      v.x += r.x * f; v.y += r.y * f; v.z += r.z * f; v.w += r.w * f;
-    }
-    const size_t head = (size_t)b * a.hq + kv * a.g + h0 + h;
-    const float f = lt == 0.f ? 0.f : 1.f / lt;
-    *reinterpret_cast<uint2*>(a.o + head * DH + (blockIdx.y * CL + i % CL) * 4) =
-        make_uint2(pack_bf16x2(v.x * f, v.y * f), pack_bf16x2(v.z * f, v.w * f));
-    if (a.lse && blockIdx.y == 0 && i % CL == 0) a.lse[head] = (m + log2f(lt)) * LN2;
+    for (int w = 1; w < PJ_WARPS; ++w) add(red[w][tid], red_ml[w]);
   }
+  if (lane >= CL) return;
+  const size_t head = (size_t)b * a.hq + kv * a.g + h0 + h;
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<uint2*>(a.o + head * DH + c) = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+  if (a.lse && blockIdx.y == 0 && lane == 0) a.lse[head] = (mx + log2f(l)) * LN2;
 }
 
 int attn_ctas(int dh, int sm_count) { return sm_count * (dh == 256 ? 1 : 2); }
@@ -730,13 +719,13 @@ int join_ranks(const PaArgs& a, int sm_count) {
   return ranks;
 }
 
-// Slices for as many parts as a run twice as long as the mean one has: 16 of 32 channels, or 64 of 8.
-template <int DH, int NH>
+// Few parts a run: a warp for a head, 16 parts of 32 channels at once.  Many: a CTA for a head, 256 parts of 8 channels.
+template <int DH>
 cudaError_t launch_join(const PaArgs& a, long long runs, cudaStream_t st) {
   const int by_run = runs <= a.ctas;
-  const unsigned x = (unsigned)(by_run ? runs : a.ctas);
-  if (a.ctas / runs <= 8) return launch_pdl(paged_join_kernel<DH, 8, NH>, dim3(x, DH / 32), dim3(PJ_THREADS), st, a, by_run);
-  return launch_pdl(paged_join_kernel<DH, 2, NH>, dim3(x, DH / 8), dim3(PJ_THREADS), st, a, by_run);
+  const unsigned x = (unsigned)(by_run ? runs : a.ctas), z = (unsigned)a.heads;
+  if (a.ctas / runs <= 8) return launch_pdl(paged_join_kernel<DH, 8, true>, dim3(x, DH / 32, (z + 3) / 4), dim3(PJ_THREADS), st, a, by_run);
+  return launch_pdl(paged_join_kernel<DH, 2, false>, dim3(x, DH / 8, z), dim3(PJ_THREADS), st, a, by_run);
 }
 
 template <int DH>
@@ -758,7 +747,7 @@ int launch_attention_dh(PaArgs a, int sm_count, long long* launches, cudaEvent_t
   ++*launches;
   if (ev_end && (e = cudaEventRecord(ev_end, st)) != cudaSuccess) return -(int)e;
   if (ranks > 0) return 0;
-  e = a.heads <= 4 ? launch_join<DH, 4>(a, runs, st) : launch_join<DH, 8>(a, runs, st);
+  e = launch_join<DH>(a, runs, st);
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;
