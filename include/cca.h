@@ -435,7 +435,7 @@ int cca_pages_compact(cca_handle* h, const cca_pages* pages, int32_t* used, void
                       void* cuda_stream);
 
 /* Puts n new tokens of every sequence into its pages: k, v device bf16 [B, n, h_k, d_h]; row len[b] + i gets token i; only the first
- * min(count[b], n) of them where `count` (device int32 [B]) is given.  len is not advanced: the caller does that.  A row whose page is
+ * min(count[b], n) of them where `count` (device int32 [B]) is given; n <= max_pages * page_size.  len is not advanced: the caller does that.  A row whose page is
  * missing or held by others too, or that passes the table, is not written, and the status word becomes 122.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
 int cca_paged_append(cca_handle* h, const void* k, const void* v, const int32_t* count, const cca_pages* pages, int64_t B, int64_t n,

@@ -38,7 +38,7 @@ template <int N>
 CCA_DEVINL void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // ------------------------------------------------------------------------------------------------ rows in and out
-constexpr int RW_TOKENS = 16, RW_THREADS = 256;
+constexpr int RW_TOKENS = 16, RW_THREADS = 256, RW_AHEAD = 2;   // tokens of a block; 16-byte pieces of k and of v that a thread has on their way
 
 struct RowsArgs {
   Paged c;
@@ -52,13 +52,30 @@ struct RowsArgs {
 };
 
 // A block moves 16 tokens of one sequence.  The rows of a token lie together on the dense side and hk * P rows apart in its page; both
-// are whole 64-byte pieces or more, so the kernel is bound by its traffic (each byte once in and once out).
+// are whole 64-byte pieces or more, so the kernel is bound by its traffic (each byte once in and once out).  New rows are on their way while
+// their places are looked up.
 template <bool APPEND>
 __global__ void __launch_bounds__(RW_THREADS) paged_rows_kernel(RowsArgs a) {
   __shared__ int at[RW_TOKENS];                             // pool row of kv head 0, -1: none
   const int b = blockIdx.y, tid = threadIdx.x;
   const long long t0 = (long long)blockIdx.x * RW_TOKENS;
+  const int per_token = a.hk * a.row_chunks;
+  const int here = (int)min((long long)RW_TOKENS, a.n - t0) * per_token;
+  const size_t dense0 = ((size_t)b * a.n + t0) * per_token;
+  const uint4 *kd = reinterpret_cast<const uint4*>(a.k_in) + dense0, *vd = reinterpret_cast<const uint4*>(a.v_in) + dense0;
+  uint4 *ko = reinterpret_cast<uint4*>(a.k_out) + dense0, *vo = reinterpret_cast<uint4*>(a.v_out) + dense0;
+  uint4 *kp = reinterpret_cast<uint4*>(a.c.k), *vp = reinterpret_cast<uint4*>(a.c.v);
+  uint4 k[RW_AHEAD], v[RW_AHEAD];
+  auto fetch = [&](int x0) {
+#pragma unroll
+    for (int i = 0; i < RW_AHEAD; ++i)
+      if (x0 + i * RW_THREADS < here) {
+        k[i] = __ldcs(kd + x0 + i * RW_THREADS);
+        v[i] = __ldcs(vd + x0 + i * RW_THREADS);
+      }
+  };
   pdl_enter();
+  if (APPEND) fetch(tid);
   if (tid < RW_TOKENS) {
     int to = -1;
     const long long i = t0 + tid;
@@ -67,38 +84,42 @@ __global__ void __launch_bounds__(RW_THREADS) paged_rows_kernel(RowsArgs a) {
     if (APPEND && a.count) n = min(n, (long long)max(a.count[b], 0));
     if (i < n) {
       const long long row = held + i, most = (long long)a.c.max_pages * a.c.P;
-      if (held >= 0 || !APPEND) {
-        if (row >= 0 && row < most) {
-          const int pi = page_index(a.c, (int)row), page = page_at(a.c, b, pi);
-          if (page >= 0 && (!APPEND || a.c.refs[page] == 1)) to = pool_row(a.c, a.hk, page, 0, (int)row - pi * a.c.P);
-        }
+      if (row >= 0 && row < most && (held >= 0 || !APPEND)) {
+        const int pi = page_index(a.c, (int)row), page = page_at(a.c, b, pi);
+        if (page >= 0 && (!APPEND || a.c.refs[page] == 1)) to = pool_row(a.c, a.hk, page, 0, (int)row - pi * a.c.P);
       }
       if (APPEND && to < 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
     }
     at[tid] = to;
   }
   __syncthreads();
-  const int per_token = a.hk * a.row_chunks;
-  const int here = (int)min((long long)RW_TOKENS, a.n - t0) * per_token;
-  const uint4 *kd = reinterpret_cast<const uint4*>(a.k_in), *vd = reinterpret_cast<const uint4*>(a.v_in);
-  uint4 *ko = reinterpret_cast<uint4*>(a.k_out), *vo = reinterpret_cast<uint4*>(a.v_out);
-  uint4 *kp = reinterpret_cast<uint4*>(a.c.k), *vp = reinterpret_cast<uint4*>(a.c.v);
-  const size_t dense0 = ((size_t)b * a.n + t0) * per_token;
-#pragma unroll 2
-  for (int x = tid; x < here; x += RW_THREADS) {
+  auto place = [&](int x, bool& there) {                    // of the block's x-th piece in the pool
     const int token = x / per_token, in = x - token * per_token;
     const int j = in / a.row_chunks, piece = in - j * a.row_chunks;
-    const size_t pool = (size_t)(at[token] + j * a.c.P) * a.row_chunks + piece;
-    if (APPEND) {
-      if (at[token] < 0) continue;
-      const uint4 kx = __ldcs(kd + dense0 + x), vx = __ldcs(vd + dense0 + x);
-      kp[pool] = kx;
-      vp[pool] = vx;
-    } else {
-      uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
-      if (at[token] >= 0) { kx = kp[pool]; vx = vp[pool]; }
-      ko[dense0 + x] = kx;
-      vo[dense0 + x] = vx;
+    there = at[token] >= 0;
+    return (size_t)(at[token] + j * a.c.P) * a.row_chunks + piece;
+  };
+  for (int x0 = tid; x0 < here; x0 += RW_AHEAD * RW_THREADS) {
+    if (APPEND && x0 != tid) fetch(x0);
+#pragma unroll
+    for (int i = 0; i < RW_AHEAD; ++i) {
+      const int x = x0 + i * RW_THREADS;
+      bool there = false;
+      const size_t pool = x < here ? place(x, there) : 0;
+      if (APPEND) {
+        if (there) { kp[pool] = k[i]; vp[pool] = v[i]; }
+      } else {
+        k[i] = v[i] = make_uint4(0, 0, 0, 0);
+        if (there) { k[i] = kp[pool]; v[i] = vp[pool]; }
+      }
+    }
+    if (!APPEND) {
+#pragma unroll
+      for (int i = 0; i < RW_AHEAD; ++i)
+        if (x0 + i * RW_THREADS < here) {
+          ko[x0 + i * RW_THREADS] = k[i];
+          vo[x0 + i * RW_THREADS] = v[i];
+        }
     }
   }
 }
@@ -187,7 +208,7 @@ CCA_DEVINL Plan make_plan(const PaArgs& a, int lane, Pick pick, int& seq, int& r
   before = 0;
   const unsigned want = pick(p);
   if (want >= total) return p;
-  for (int i = 0; seq < 0; ++i) {
+  for (int i = 0; seq < 0 && i * 32 < a.B; ++i) {
     int here = 0;
 #pragma unroll
     for (int x = 0; x < KEPT; ++x)

@@ -401,7 +401,7 @@ struct FkArgs {
   int* lens;                      // [n]: their lengths, -1: nothing to do
   int* status;
 };
-constexpr int FK_THREADS = 256, FK_EACH = 4;                   // table entries that a thread has on their way at once
+constexpr int FK_THREADS = 512, FK_EACH = 4;                   // table entries that a thread has on their way at once
 
 CCA_DEVINL void let_go(const Paged& c, const int* page, int* status) {     // FK_EACH pages, -1: none
   int held[FK_EACH];

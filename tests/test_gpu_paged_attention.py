@@ -116,6 +116,9 @@ def test_any_number_of_heads_per_group(g, dh):
     (2, 1, 64, 16, [(37 * b) % 91 for b in range(700)], 91),   # more sequences than a CTA has threads, empty ones among them
     (8, 1, 128, 48, [5000, 0, 0, 0, 0, 64, 3000], 5000),
     (8, 2, 128, 64, [16384], 16384),
+    (4, 1, 128, 64, [9000 if b == 7 else (53 * b) % 200 for b in range(150)], 16384),      # a bound far above most lengths: units shared out
+    (2, 1, 128, 32, [9000 if b == 290 else (53 * b) % 70 for b in range(300)], 16384),     # and more sequences than CTAs
+    (12, 2, 64, 16, [3000] * 70, 16384),
 ])
 def test_long_and_ragged(hq, hk, dh, size, lens, max_len):
     cca = make(hk, dh, hq)
