@@ -39,6 +39,8 @@ CCA_DEVINL int block_scan(int v, int* sm, int& before) {
 // ------------------------------------------------------------------------------------------------ copies
 // Pages are copied by the bulk copy engine, 16 KB at a time through a ring in shared memory: one warp a CTA, whose first lane starts the
 // copies in and out.  A stage is filled again two steps after its copy out began, so four loads are on their way while two stages drain.
+// Bound by memory: 1792 pages of 64 KB copied from 256 (the sources stay in the L2) in 27 us, 4096 moved from all over a pool of a gigabyte in
+// 92 us = 5.8 TB/s in and out.  Stages of 8 or 32 KB, three CTAs an SM: the same.  By threads, 16 bytes a load, the first took 50 us.
 constexpr int EN_STAGES = 6, EN_BYTES = 16384, EN_CTAS = 2;    // CTAs of an SM
 constexpr size_t EN_RING = (size_t)EN_STAGES * EN_BYTES;
 struct EngineShare {
@@ -170,9 +172,10 @@ CCA_DEVINL bool entry_of(const RsArgs& a, int x, int& b, int& i) {
   return i <= page_index(a.c, (int)(from + n - 1));
 }
 
-// Few entries: one cluster.  The first CTA looks at the entries, of shared pages in a hash table in shared memory, while the others
-// list the free pages of a part of the pool each; then it hands these out.  HERE: all of them copy what is to be copied, otherwise
-// pages_copy_kernel does.
+// Few entries: one cluster.  The first CTA looks at the entries, counting who asks for a shared page in a hash table in shared memory, while the
+// others list the free pages of a part of the pool each; then it hands these out.  HERE: all of them copy what is to be copied, otherwise
+// pages_copy_kernel does.  Bound by the latency of three loads that follow one another (length, table, count), two barriers of the cluster and
+// what is copied: 32 entries without copies 5.9 us, 1024 6.3, 3000 8.5 (the other kernel 9.5, 9.6, 10.1, with 16 pages copied 14.4 against 7.5).
 constexpr int RV_ENTRIES = 4096, RV_SLOTS = 2 * RV_ENTRIES, RV_ROUNDS = RV_ENTRIES / PG_THREADS;
 struct ReserveShare {
   int page[RV_SLOTS], asked[RV_SLOTS], last[RV_SLOTS];         // first CTA: shared pages that are asked for
@@ -301,7 +304,8 @@ CCA_DEVINL bool wants_page(const RsArgs& a, int b, int e) {
   return refs > 1 && !(__ldcg(a.asked + e) == refs && __ldcg(a.last + e) == b);
 }
 
-// Any number of entries: one cluster whose CTAs share out the entries and the pool, both in contiguous runs.
+// Any number of entries: one cluster whose CTAs share out the entries and the pool, both in contiguous runs, and count in global memory.  Bound by
+// the loads' latency and its five barriers: 8192 entries 17 us, 65536 (a pool of 78651 pages) 41.
 __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(RsArgs a) {
   __shared__ int sm[PG_WARPS];
   __shared__ int mine[2];                                      // pages needed and pages free in this CTA's runs
@@ -506,6 +510,7 @@ struct FrArgs {
   const int* keep;
   int* status;
 };
+// A block a sequence.  Bound by latency: length, row, counts one after the other (256 rows of 1026 pages, half of them let go: 5.5 us).
 __global__ void __launch_bounds__(FK_THREADS) pages_free_kernel(FrArgs a) {
   pdl_enter();
   const int b = blockIdx.x, tid = threadIdx.x;
@@ -541,7 +546,8 @@ struct CmArgs {
   int* status;
 };
 
-// One cluster: held pages are counted, then those that move and the places they go to are listed, each CTA a contiguous run of the pool.
+// One cluster: held pages are counted, then those that move and the places they go to are listed, each CTA a contiguous run of the pool.  Bound by
+// latency up to 10^5 pages (5.2 us with the launch behind it where nothing moves, 9.9 at 78651 pages), then by what 8 SMs read (46 at 629153).
 __global__ void __launch_bounds__(PG_THREADS) pages_compact_kernel(CmArgs a) {
   __shared__ int sm[PG_WARPS];
   __shared__ int mine;                                         // held pages of this CTA's run
@@ -621,8 +627,12 @@ __global__ void __launch_bounds__(CP_THREADS) pages_move_kernel(CmArgs a) {
   }
 }
 
-constexpr int FK_FEW = 64;                                     // pairs that one cluster forks, a few warps each
-constexpr long long FEW_BYTES = 256 << 10;                     // that the threads of one cluster copy before all SMs pay for a second launch
+// One launch or two (us on the device; a launch costs the host 2.5 more).  Reserving: what could have to be copied, 16 pages of 64 KB: 4.3
+// where nothing is, 7.5 where 8 pages are, against 5.9 and 7.4 with a launch for the copies; 32 pages: 4.2 and 9.3 against 5.9 and 7.5.
+constexpr long long FEW_BYTES = 1 << 20;
+// Forking: 32 pairs of rows of 64 pages 4.3 against 3.6, 64 of 256 5.2 against 4.0, 64 of 1024 7.1 against 4.3.
+constexpr int FK_FEW = 64;
+constexpr long long FK_FEW_ENTRIES = 64 * 256;
 
 template <typename... KArgs, typename... Args>
 int launch_copies(void (*kernel)(KArgs...), bool* done, int sm_count, long long* launches, cudaStream_t st, Args... args) {
@@ -691,7 +701,7 @@ int launch_pages_fork(const CcaDims& d, const Paged& c, const int* parent, const
   a.c = c; a.B = d.B; a.n = n; a.parent = parent; a.child = child; a.rows = reinterpret_cast<int*>(ws + l.rows);
   a.lens = reinterpret_cast<int*>(ws + l.lens); a.status = status;
   cudaError_t e;
-  if (n <= FK_FEW) {
+  if (n <= FK_FEW && (long long)n * c.max_pages <= FK_FEW_ENTRIES) {
     if ((e = launch_clusters(pages_fork_few_kernel, dim3(RANKS), dim3(PG_THREADS), 0, RANKS, st, a)) != cudaSuccess) return -(int)e;
     ++*launches;
     return 0;
