@@ -506,8 +506,7 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
         }
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      // the maximum moves only when a logit passes it by a factor of 2^8: weights stay below 2^8 and nothing is lost in fp32
-      if (__any_sync(0xffffffffu, most > top + 8.f || (top == -INFINITY && most != -INFINITY))) {
+      if (__any_sync(0xffffffffu, most > top)) {
         const float now = fmaxf(top, most);
         const float alpha = now == -INFINITY ? 1.f : exp2f(top - now);
         top = now;

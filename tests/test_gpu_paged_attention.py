@@ -152,6 +152,21 @@ def test_rising_and_falling_logits():
     cca.close()
 
 
+def test_values_near_the_end_of_the_range():
+    """A value of 2^127 in a row that a few later ones outweigh by a little: nothing overflows on the way."""
+    cca = make(1, 64, 4)
+    pages = cached(cca, 16, [200], 1)
+    pool = pages["table"][0].long()
+    pages["v"][pool[1], 0, 3, 5] = 2.0 ** 127
+    q = torch.zeros(1, 4, 64)
+    q[..., 0] = 1.0
+    pages["k"][pool, 0, :, 0] = (torch.arange(13 * 16, device="cuda").view(13, 16) // 8).bfloat16()      # logits rise by 1/8 every 8 rows
+    o = cca.paged_attention(q.bfloat16().cuda(), pages, 200, cca.alloc_paged_workspace(1, 200))
+    assert bool(torch.isfinite(o).all()) and float(o[0, 0, 5]) > 2.0 ** 110
+    check(cca, pages, q.bfloat16(), [200], o, None)
+    cca.close()
+
+
 def test_shared_pages():
     cca = make(2, 64, 8)
     pages = cached(cca, 16, [100, 40], 3, junk=False)
@@ -276,6 +291,50 @@ def test_a_pool_of_more_than_2_to_the_32_elements():
     cca.close()
 
 
+def test_the_largest_batch():
+    """65535 sequences, most of them short or empty."""
+    cca = make(1, 32, 2)
+    B = 65535
+    lens = torch.arange(B) * 7919 % 23
+    lens[::5] = 0
+    pages = {n: torch.randn(4096, 1, 8, 32, device="cuda").bfloat16() for n in ("k", "v")}
+    gen = torch.Generator().manual_seed(3)
+    pages.update(refs=torch.ones(4096, dtype=torch.int32, device="cuda"), len=lens.int().cuda(),
+                 table=torch.randint(0, 4096, (B, 3), generator=gen).int().cuda())
+    q = torch.randn(B, 2, 32, generator=gen).bfloat16()
+    for max_len in (22, 24):
+        lse = torch.full((B, 2), 7.0, device="cuda")
+        o = cca.paged_attention(q.cuda(), pages, max_len, cca.alloc_paged_workspace(B, max_len), lse=lse)
+        torch.cuda.synchronize()
+        assert cca.last_status() == 0
+        for b in [*range(40), *range(30000, 30040), *range(B - 40, B)]:
+            one = {**pages, "table": pages["table"][b:b + 1], "len": pages["len"][b:b + 1]}
+            check(cca, one, q[b:b + 1], [int(lens[b])], o[b:b + 1], lse[b:b + 1])
+        assert not o[(lens == 0).cuda()].any() and bool(torch.isinf(lse[(lens == 0).cuda()]).all())
+    cca.close()
+
+
+def test_two_streams_at_once():
+    """Calls of one handle side by side, each stream with its own pages and workspace: the same as one after the other."""
+    cca = make(2, 128, 8)
+    sides = []
+    for seed, lens in ((1, [5000, 300]), (2, [700, 16, 2200])):
+        pages = cached(cca, 16, lens, seed)
+        q = torch.randn(len(lens), 8, 128, generator=torch.Generator().manual_seed(seed)).bfloat16().cuda()
+        ws = cca.alloc_paged_workspace(len(lens), 5000)
+        sides.append((torch.cuda.Stream(), pages, q, ws, max(lens), cca.paged_attention(q, pages, max(lens), ws)))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for i, (stream, pages, q, ws, n, _) in enumerate(sides):
+            with torch.cuda.stream(stream):
+                outs[i].append(cca.paged_attention(q, pages, n, ws))
+    torch.cuda.synchronize()
+    for got, side in zip(outs, sides):
+        assert all(torch.equal(o, side[5]) for o in got)
+    cca.close()
+
+
 def test_refusals():
     from paper_2510_04476_b200.binding import CcaError
     cca = make(2, 64, 8)
@@ -285,6 +344,8 @@ def test_refusals():
     for match, call in [
         ("invalid", lambda: cca.paged_attention(q, pages, 0, ws)),
         ("invalid", lambda: cca.paged_attention(q, pages, 33, ws)),
+        ("unsupported", lambda: cca.alloc_paged_workspace(1025, 1 << 20)),
+        ("align", lambda: cca.paged_attention(torch.zeros(2 * 8 * 64 + 4, dtype=torch.bfloat16, device="cuda")[4:].view(2, 8, 64), pages, 32, ws)),
         ("workspace too small", lambda: cca.paged_attention(q, pages, 32, ws[:1000])),
         ("workspace", lambda: cca.paged_attention(q, pages, 32, ws.float())),
         ("q: wants", lambda: cca.paged_attention(q[:1], pages, 32, ws)),

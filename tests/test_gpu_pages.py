@@ -70,6 +70,39 @@ def test_append_and_read(hk, dh, size, n):
     cca.close()
 
 
+@pytest.mark.parametrize("size", [50001, 65536, 4097, 3])
+def test_rows_far_into_a_sequence(size):
+    """Up to the last of 2^24 rows: which page a row lies in, and where."""
+    cca = make(1, 32)
+    wide = (1 << 24) // size
+    at = [0, wide // 2, wide - 2, wide - 1]
+    n_pages = min(len(at) + 1, (1 << 31) // size - 1)
+    pages = filled(cca, n_pages, size, 4, wide)
+    for b, i in enumerate(at):
+        pages["table"][:, i] = b
+    pages["refs"].copy_(ints([1] * 4 + [0]))
+    k, v = (torch.randn(4, 5, 1, 32).bfloat16() for _ in range(2))
+    lens = [at[0] * size, at[1] * size + 1, at[2] * size + size - 3, at[3] * size + size - 5]       # the third runs on from one page to the next
+    if size == 3:
+        lens = [0, at[1] * size, at[2] * size + 1, at[3] * size - 2]
+    pages["len"].copy_(ints(lens))
+    pool = P.Pool.of({n: t if n != "table" else t[:1] for n, t in pages.items()})
+    pool.table = pool.table * 4
+    for b in range(4):                                         # one after the other, the sequences share their pages here
+        one = {**pages, "table": pages["table"][b:b + 1], "len": pages["len"][b:b + 1]}
+        cca.paged_append(one, k[b:b + 1].cuda(), v[b:b + 1].cuda())
+        for i in range(5):
+            place = pool.place(b, lens[b] + i)
+            if place is not None:
+                pool.k[place[0], :, place[1]], pool.v[place[0], :, place[1]] = k[b, i], v[b, i]
+    torch.cuda.synchronize()
+    for n in ("k", "v"):
+        assert torch.equal(bits(pages[n]), getattr(pool, n).view(torch.int16))
+    for got, want in zip(cca.paged_read(pages, 7, ints([n - 1 for n in lens])), pool.read(7, [n - 1 for n in lens])):
+        assert torch.equal(bits(got), bits(want))
+    cca.close()
+
+
 def test_append_leaves_out_what_it_may_not_write():
     """Counts of a padded batch; rows on shared pages, without a page, on a page that is none of the pool's, behind the table, behind a
     negative length."""
