@@ -398,7 +398,9 @@ typedef struct {
   void* v;              /* bf16 [n_pages, h_k, page_size, d_h]: values (Eq. 10)                                       */
   int32_t* refs;        /* int32 [n_pages]                                                                            */
   int32_t* table;       /* int32 [B, max_pages]: page numbers, -1 where there is none                                 */
-  int32_t* len;         /* int32 [B]: rows held; cca_pages_fork and cca_pages_free alone write it                     */
+  int32_t* len;         /* int32 [B]: rows held; cca_pages_fork and cca_pages_free alone write it.  Negative: the sequence is not in use,
+                           and calls that go by its length skip it: nothing of it is written, its output is left as it is (the
+                           step's: undefined), and that is no error                                                   */
   int64_t n_pages, page_size, max_pages;
 } cca_pages;
 
@@ -411,7 +413,7 @@ int cca_pages_workspace_size(const cca_handle* h, int64_t n_pages, int64_t max_p
  * for it in the same call, the last of them keeps it.  New pages are the free ones with the lowest numbers, ascending, for the sequences in order
  * and their pages in order.  Rows that have such pages already cost nothing, so the call may come before every step or once for many.
  * All or nothing: if more pages are needed than are free, nothing changes and the device status word becomes 123.  A sequence whose rows
- * would pass max_pages * page_size, or whose first row is negative, is left as it is and the status word becomes 122.
+ * would pass max_pages * page_size, or whose first[b] is negative, is left as it is and the status word becomes 122.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE_TOO_SMALL, CUDA. */
 int cca_pages_reserve(cca_handle* h, const cca_pages* pages, int64_t n, const int32_t* count, const int32_t* first, void* workspace,
                       size_t workspace_bytes, int64_t B, void* cuda_stream);
@@ -425,7 +427,8 @@ int cca_pages_fork(cca_handle* h, const cca_pages* pages, const int32_t* parent,
                    size_t workspace_bytes, int64_t B, void* cuda_stream);
 
 /* Sequence b keeps its first min(keep[b], len[b]) rows (device int32 [B]): len[b] becomes that, and the pages behind these rows are let go, those
- * reserved behind its length among them.  0 frees the sequence; a negative number leaves it as it is.  Errors as above. */
+ * reserved behind its length among them.  0 frees the sequence (a negative length stays); a negative number leaves it as it is.  Errors as
+ * above. */
 int cca_pages_free(cca_handle* h, const cca_pages* pages, const int32_t* keep, int64_t B, void* cuda_stream);
 
 /* Moves the held pages to the front of the pool: with U held pages, those numbered U or more, ascending, move to the free ones below U,

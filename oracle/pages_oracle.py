@@ -41,8 +41,8 @@ class Pool:
         status = 0
         for b in range(len(self.table)):
             n = k.shape[1] if count is None else min(max(count[b], 0), k.shape[1])
-            for i in range(n):
-                at = self.place(b, self.len[b] + i) if self.len[b] >= 0 else None
+            for i in range(n if self.len[b] >= 0 else 0):
+                at = self.place(b, self.len[b] + i)
                 if at is None or self.refs[at[0]] != 1:
                     status = MISSING
                 else:
@@ -63,6 +63,8 @@ class Pool:
         for b in range(len(self.table)):
             m = n if count is None else min(max(count[b], 0), n)
             r = (self.len if first is None else first)[b]
+            if m and first is None and r < 0:
+                m = 0
             if m and (r < 0 or r + m > self.wide * self.P):
                 status, m = MISSING, 0
             window.append(range(r // self.P, (r + m - 1) // self.P + 1) if m else range(0))
@@ -122,8 +124,9 @@ class Pool:
         for b, m in enumerate(keep):
             if m < 0:
                 continue
-            self.len[b] = max(min(self.len[b], m), 0)
-            for i in range(-(-self.len[b] // self.P), self.wide):
+            left = min(m, max(self.len[b], 0))
+            self.len[b] = left if self.len[b] >= 0 else self.len[b]
+            for i in range(-(-left // self.P), self.wide):
                 p = self.page(b, i)
                 self.table[b][i] = -1
                 if p is not None:

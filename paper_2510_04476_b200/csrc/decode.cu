@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
   size_t row;
   const bool paged = a.pages.k != nullptr;
   if (!(paged ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row))) {
-    if (tid == 0 && blockIdx.x == 0) atomicCAS(a.status, 0, paged ? ST_PAGE_MISSING : a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
+    if (tid == 0 && blockIdx.x == 0 && !(paged && t < 0))      // (a negative length: not in use)
+      atomicCAS(a.status, 0, paged ? ST_PAGE_MISSING : a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
     return;
   }
   const int ld_lat = d.L + d.Lk;

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(RW_THREADS) paged_rows_kernel(RowsArgs a) {
         const int pi = page_index(a.c, (int)row), page = page_at(a.c, b, pi);
         if (page >= 0 && (!APPEND || a.c.refs[page] == 1)) to = pool_row(a.c, a.hk, page, 0, (int)row - pi * a.c.P);
       }
-      if (APPEND && to < 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+      if (APPEND && to < 0 && held >= 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
     }
     at[tid] = to;
   }
@@ -157,7 +157,7 @@ struct At {
   }
 };
 
-CCA_DEVINL int rows_of(const PaArgs& a, int b) {              // -1: does not fit
+CCA_DEVINL int rows_of(const PaArgs& a, int b) {              // -1: does not fit, or is not in use
   const int n = __ldcg(a.c.len + b);
   return n >= 0 && n <= a.max_len - a.extra && n + a.extra <= (long long)a.c.max_pages * a.c.P ? n + a.extra : -1;
 }
@@ -294,8 +294,8 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
   auto no_rows = [&](int b, int h0, int n) {
     const int rows = rows_of(a, b);
     if (rows > 0) return;
-    if (rows < 0) {
-      if (tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+    if (rows < 0) {                                            // too long; not in use if the length is negative
+      if (tid == 0 && a.c.len[b] >= 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
       return;
     }
     const size_t head = (size_t)b * a.hq + h0;

@@ -165,7 +165,7 @@ CCA_DEVINL bool entry_of(const RsArgs& a, int x, int& b, int& i) {
   if (a.count) n = min(n, (long long)max(a.count[b], 0));
   if (n == 0) return false;
   if (from < 0 || from + n > (long long)a.c.max_pages * a.c.P) {
-    if (k == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+    if (k == 0 && (a.first || from >= 0)) atomicCAS(a.status, 0, ST_PAGE_MISSING);         // (a negative length: not in use)
     return false;
   }
   i = page_index(a.c, from) + k;
@@ -516,9 +516,9 @@ __global__ void __launch_bounds__(FK_THREADS) pages_free_kernel(FrArgs a) {
   const int b = blockIdx.x, tid = threadIdx.x;
   const int keep = a.keep[b], len = a.c.len[b];
   if (keep < 0) return;
-  const int left = max(min(keep, len), 0);
+  const int left = min(keep, max(len, 0));
   __syncthreads();                                             // everybody has read the length
-  if (tid == 0) a.c.len[b] = left;
+  if (tid == 0 && len >= 0) a.c.len[b] = left;
   int* row = a.c.table + (size_t)b * a.c.max_pages;
   const long long held = ((long long)left + a.c.P - 1) / a.c.P;
   for (long long i0 = held + tid; i0 < a.c.max_pages; i0 += FK_EACH * FK_THREADS) {

@@ -200,6 +200,30 @@ def test_lengths_outside_the_bound_are_skipped():
     assert cca.last_status() == 122
     assert bool((out[1:3] == 7).all()) and bool((lse[1:3] == 7).all())
     check(cca, pages, q, [50, 61, 0, 20], out, lse, only=(0, 3))
+    # one that is not in use is no error, whichever way the rows are shared out
+    for lens, max_len in (([50, 60, -1, 20], 60), ([50, 60, -7, 20], 64)):
+        pages["len"].copy_(ints(lens))
+        out.fill_(7)
+        ws = cca.alloc_paged_workspace(4, max_len)
+        cca.paged_attention(q.cuda(), pages, max_len, ws, out=out, lse=lse)
+        torch.cuda.synchronize()
+        assert cca.last_status() == 0 and bool((out[2] == 7).all())
+        check(cca, pages, q, [50, 60, 0, 20], out, lse, only=(0, 1, 3))
+    cca.close()
+
+
+def test_sequences_not_in_use_among_long_ones():
+    cca = make(1, 128, 4)
+    lens = [9000 if b == 7 else (53 * b) % 200 for b in range(150)]
+    pages = cached(cca, 64, lens, 5, wide=256)
+    for b in range(0, 150, 3):
+        pages["len"][b] = -1 - b
+    q = torch.randn(150, 4, 128, generator=torch.Generator().manual_seed(1)).bfloat16()
+    out = torch.full((150, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    cca.paged_attention(q.cuda(), pages, 16384, cca.alloc_paged_workspace(150, 16384), out=out)
+    torch.cuda.synchronize()
+    assert cca.last_status() == 0 and bool((out[::3] == 7).all())
+    check(cca, pages, q, lens, out, None, only=[b for b in range(150) if b % 3])
     cca.close()
 
 

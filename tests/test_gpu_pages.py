@@ -215,6 +215,29 @@ def test_reserve_takes_all_or_nothing():
     cca.close()
 
 
+def test_sequences_not_in_use():
+    """A negative length: skipped by every call that goes by it, without a word."""
+    cca = make(1, 32)
+    pages = filled(cca, 9, 2, 4, 3)
+    ws = cca.alloc_pages_workspace(9, 4, 3)
+    cca.pages_reserve(pages, 5, ws, ints(5, 3, 0, 5))
+    pages["len"].copy_(ints(3, -1, -5, 2))
+    pool = P.Pool.of(pages)
+    k, v = (torch.randn(4, 2, 1, 32).bfloat16() for _ in range(2))
+    cca.pages_reserve(pages, 2, ws)
+    cca.paged_append(pages, k.cuda(), v.cuda())
+    cca.pages_free(pages, ints(9, 1, 0, -1))
+    assert pool.reserve(2) == 0 and pool.append(k, v) == 0 and pool.free([9, 1, 0, -1]) == 0
+    same(pages, pool)
+    assert cca.last_status() == 0 and pages["len"].tolist() == [3, -1, -5, 2]
+    cca.pages_fork(pages, ints(1), ints(0), ws)
+    cca.pages_reserve(pages, 1, ws, first=ints(0, -1, 0, 0))
+    assert pool.fork([1], [0]) == 122 and pool.reserve(1, first=[0, -1, 0, 0]) == 122
+    same(pages, pool)
+    assert cca.last_status() == 122
+    cca.close()
+
+
 def test_tables_that_name_no_page_of_the_pool():
     """Entries outside the pool, counts that do not agree with the table: no access outside, and what is held stays in order."""
     cca = make(1, 32)

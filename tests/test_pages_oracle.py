@@ -30,6 +30,16 @@ def test_reserve_by_hand():
     assert s.reserve(13) == P.MISSING and s.table[2] == [5, 6, -1]
 
 
+def test_sequences_not_in_use():
+    s = pool(6, 4, [[0, 1], [2, -1], [-1, -1]], [5, -1, -3])
+    before = s.k.clone()
+    assert s.reserve(2) == 0 and s.table == [[0, 1], [2, -1], [-1, -1]]
+    assert s.append(*[torch.ones(3, 1, 2, 4, dtype=torch.bfloat16)] * 2) == 0
+    assert torch.equal(s.k[2:], before[2:]) and bool((s.k[1, :, 1] == 1).all())
+    assert s.fork([1], [2]) == P.MISSING
+    assert s.free([5, 3, 0]) == 0 and s.len == [5, -1, -3] and s.table == [[0, 1], [-1, -1], [-1, -1]] and s.refs == [1, 1, 0, 0, 0, 0]
+
+
 def test_fork_and_free_by_hand():
     s = pool(6, 4, [[0, 1, 2], [3, -1, -1], [-1, -1, -1]], [5, 2, 0])                    # page 2 is reserved ahead
     assert s.fork([0, 1], [1, 2]) == 0                                                   # the second takes what the first pair overwrites
