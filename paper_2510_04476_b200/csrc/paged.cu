@@ -244,7 +244,7 @@ struct Cursor {
   }
 };
 
-// Flash attention of the query heads that share a kv head, over rows that pages scatter.  Of a unit each warp takes R rows: lanes look their
+// Softmax and both products in one pass, for the query heads that share a kv head, over rows that pages scatter.  Of a unit each warp takes R rows: lanes look their
 // pages up one stage ahead and bring the rows by cp.async, 16 bytes a lane, into places from which ldmatrix reads without conflicts (a page may
 // begin and end anywhere; a row is whole); S = Q K^T and O^T += V^T P^T by mma.sync, heads being 8 of its rows, then its 8 columns.  With 4
 // heads or fewer the columns hold the weights' two bf16 parts, with more there are two products.  (tcgen05 would want 128 rows in its M: heads
