@@ -176,21 +176,21 @@ struct C1Args {
   long long S_max;
   int max_len;
   int* status;
-  Paged pages;           // k null: no pages
+  Paged pages;           // PAGED
 };
 
 // Eq. 8, conv1 at the k_ch tokens conv2 reads, for every channel of one sequence; also the value row (Eq. 10),
 // the history for the next token and the input the next step's value shift needs.
+template <bool PAGED>
 __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
   pdl_enter();
   const CcaDims& d = a.d;
   const int b = blockIdx.y, tid = threadIdx.x;
   int t;
   size_t row;
-  const bool paged = a.pages.k != nullptr;
-  if (!(paged ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row))) {
-    if (tid == 0 && blockIdx.x == 0 && !(paged && t < 0))      // (a negative length: not in use)
-      atomicCAS(a.status, 0, paged ? ST_PAGE_MISSING : a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
+  if (!(PAGED ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row))) {
+    if (tid == 0 && blockIdx.x == 0 && !(PAGED && t < 0))      // (a negative length: not in use)
+      atomicCAS(a.status, 0, PAGED ? ST_PAGE_MISSING : a.qlen ? ST_QCACHE_BAD_LEN : ST_DECODE_BAD_POSITION);
     return;
   }
   const int ld_lat = d.L + d.Lk;
@@ -222,10 +222,10 @@ __global__ void __launch_bounds__(256) decode_conv1_kernel(C1Args a) {
     for (int r = 0; r < 7; ++r)
       if (r < pad) a.hist[((size_t)b * pad + r) * d.L + ch] = win[r + 1];
   }
-  if (a.v_cache)                                            // null: pages, or the value is quantised beside the key
+  if (!PAGED && a.v_cache)                                  // null: the value is quantised beside the key
     for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256)
       a.v_cache[row * d.Lk + c] = __float2bfloat16(lat_b[d.L + c]);
-  if (paged)
+  if (PAGED)
     for (int c = blockIdx.x * 256 + tid; c < d.Lk; c += gridDim.x * 256) {
       const int j = c / d.dh;
       a.pages.v[(row + (size_t)j * a.pages.P) * d.dh + c - j * d.dh] = __float2bfloat16(lat_b[d.L + c]);
@@ -248,10 +248,10 @@ struct FnArgs {
   long long S_max;
   int max_len;
   QCache cache;          // Q4 alone
-  Paged pages;           // k null: no pages
+  Paged pages;           // PAGED
 };
 
-template <int DH, bool Q4>
+template <int DH, bool Q4, bool PAGED>
 __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(FnArgs a) {
   pdl_enter();
   constexpr int NW = (DH < 128 ? 128 : DH) / 32;      // warps per block
@@ -262,8 +262,7 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int t;
   size_t row;
-  const bool paged = !Q4 && a.pages.k != nullptr;
-  if (!(paged ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)))
+  if (!(PAGED ? new_paged_row(a.pages, d.hk, a.max_len, b, t, row) : new_row(a.pos, a.qlen, a.S_max, a.max_len, b, t, row)))
     return;                                                                // reported by the conv1 kernel
   const bool is_q = head < d.hq;
   const int ch0 = head * DH;                   // first channel of the head in the q0|k0 latent
@@ -332,7 +331,7 @@ __global__ void __launch_bounds__(DH < 128 ? 128 : DH) decode_finalize_kernel(Fn
     if (blk < R::NB) q4::store_block<DH>(a.cache, ((size_t)b * d.hk + j) * a.S_max + row, kv, blk, lane8, t, code, scale);
   } else {
     if (is_q) a.q[(size_t)b * d.Lq + ch0 + c] = v;
-    else if (paged) a.pages.k[(row + (size_t)(head - d.hq) * a.pages.P) * DH + c] = __float2bfloat16(v);
+    else if (PAGED) a.pages.k[(row + (size_t)(head - d.hq) * a.pages.P) * DH + c] = __float2bfloat16(v);
     else a.k_cache[row * d.Lk + (ch0 - d.Lq) + c] = __float2bfloat16(v);
   }
 }
@@ -624,14 +623,14 @@ cudaError_t launch_attn_dh(const AtArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-template <bool Q4>
+template <bool Q4, bool PAGED>
 cudaError_t launch_finalize_dh(const FnArgs& fa, cudaStream_t st) {
   const dim3 grid((unsigned)(fa.d.hq + fa.d.hk), (unsigned)fa.d.B);
   switch (fa.d.dh) {
-    case 32: return launch_pdl(decode_finalize_kernel<32, Q4>, grid, dim3(128), st, fa);
-    case 64: return launch_pdl(decode_finalize_kernel<64, Q4>, grid, dim3(128), st, fa);
-    case 128: return launch_pdl(decode_finalize_kernel<128, Q4>, grid, dim3(128), st, fa);
-    default: return launch_pdl(decode_finalize_kernel<256, Q4>, grid, dim3(256), st, fa);
+    case 32: return launch_pdl(decode_finalize_kernel<32, Q4, PAGED>, grid, dim3(128), st, fa);
+    case 64: return launch_pdl(decode_finalize_kernel<64, Q4, PAGED>, grid, dim3(128), st, fa);
+    case 128: return launch_pdl(decode_finalize_kernel<128, Q4, PAGED>, grid, dim3(128), st, fa);
+    default: return launch_pdl(decode_finalize_kernel<256, Q4, PAGED>, grid, dim3(256), st, fa);
   }
 }
 
@@ -728,7 +727,7 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = s.v_cache;
   c1.hist = s.qk0_hist; c1.x_prev = s.x_prev; c1.pos = s.pos; c1.qlen = nullptr; c1.S_max = s.S_max; c1.max_len = max_len; c1.status = status;
   c1.pages = s.pages;
-  if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
+  if ((e = launch_pdl(paged ? decode_conv1_kernel<true> : decode_conv1_kernel<false>, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
   ++*launches;
   if (d.flags & F_CONV2) {
@@ -743,7 +742,7 @@ int launch_decode_step(const CcaDims& d, const DecodeWeights& w, const bf16* x, 
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = s.k_cache; fa.pos = s.pos;
   fa.qlen = nullptr; fa.S_max = s.S_max; fa.max_len = max_len; fa.cache = QCache{}; fa.pages = s.pages;
-  if ((e = launch_finalize_dh<false>(fa, st)) != cudaSuccess) return -(int)e;
+  if ((e = paged ? launch_finalize_dh<false, true>(fa, st) : launch_finalize_dh<false, false>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
   if (paged) {
     const int r = launch_paged_attention(d, nullptr, q, o, nullptr, s.pages, 1, max_len, p, sm_count, status, launches, ev_attn_begin,
@@ -833,7 +832,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   C1Args c1;
   c1.d = d; c1.lat = lat; c1.x = x; c1.w0 = w.conv0_w; c1.y1s = y1s; c1.y2 = y2; c1.v_cache = nullptr; c1.hist = hist; c1.x_prev = x_prev;
   c1.pos = pos; c1.qlen = cache.len; c1.S_max = cache.S_max; c1.max_len = max_len; c1.status = status; c1.pages = Paged{};
-  if ((e = launch_pdl(decode_conv1_kernel, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
+  if ((e = launch_pdl(decode_conv1_kernel<false>, dim3((unsigned)((d.L + 255) / 256), (unsigned)d.B), dim3(256), st, c1)) != cudaSuccess)
     return -(int)e;
   ++*launches;
   if (d.flags & F_CONV2) {
@@ -848,7 +847,7 @@ int launch_decode_step_q(const CcaDims& d, const DecodeQWeights& w, const bf16* 
   FnArgs fa;
   fa.d = d; fa.lat = lat; fa.y2 = y2; fa.temp = w.temp; fa.q = q; fa.k_cache = nullptr; fa.pos = pos; fa.qlen = cache.len; fa.cache = cache;
   fa.S_max = cache.S_max; fa.max_len = max_len; fa.pages = Paged{};
-  if ((e = launch_finalize_dh<true>(fa, st)) != cudaSuccess) return -(int)e;
+  if ((e = launch_finalize_dh<true, false>(fa, st)) != cudaSuccess) return -(int)e;
   ++*launches;
   if ((r = launch_qcache_attention(d, nullptr, q, o, cache, pos, 1, max_len, cache.weight != nullptr, ws + l.cache, sm_count, status,
                                    launches, ev_attn_begin, ev_attn_end, st)) != 0)
