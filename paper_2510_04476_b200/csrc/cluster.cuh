@@ -60,6 +60,21 @@ cudaError_t opt_in(K kernel, int bytes, bool* done) {
   return e;
 }
 
+// Clusters of `ranks` CTAs that are resident at once.
+template <typename K>
+inline cudaError_t clusters_at_once(K kernel, dim3 block, size_t smem, int ranks, int* n) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ranks);
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)ranks; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaOccupancyMaxActiveClusters(n, kernel, &cfg);
+}
+
 // Launched as a dependent of the kernel before it, in clusters of `ranks` CTAs.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_clusters(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int ranks, cudaStream_t st, Args... args) {

@@ -716,31 +716,52 @@ int attn_ctas(int dh, int sm_count) { return sm_count * (dh == 256 ? 1 : 2); }
 
 template <int DH, int HG, bool JOINED>
 cudaError_t launch_attn(const PaArgs& a, dim3 grid, int ranks, cudaStream_t st) {
-  const size_t smem = At<DH>::smem(HG);
   static bool done[MAX_DEVICES];
-  const cudaError_t e = opt_in(paged_attn_kernel<DH, HG, JOINED>, (int)smem, done);
+  const cudaError_t e = opt_in(paged_attn_kernel<DH, HG, JOINED>, (int)At<DH>::smem(HG), done);
   if (e != cudaSuccess) return e;
-  if (JOINED) return launch_clusters(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), smem, ranks, st, a);
-  return launch_pdl_smem(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), smem, st, a);
+  if (JOINED) return launch_clusters(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), At<DH>::smem(HG), ranks, st, a);
+  return launch_pdl_smem(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), At<DH>::smem(HG), st, a);
+}
+
+// CTAs of clusters of 1, 2, 4 and 8 that find room on the device at once (a cluster lies within a part of it), asked for once a device.
+constexpr int PA_SIZES = 4;
+template <int DH, int HG>
+cudaError_t cluster_room(int sm_count, int* room) {
+  static int known[MAX_DEVICES][PA_SIZES];                     // 0: not asked
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  static bool done[MAX_DEVICES];
+  for (int i = 0; i < PA_SIZES; ++i) {
+    room[i] = dev < MAX_DEVICES ? known[dev][i] : 0;
+    if (room[i] > 0) continue;
+    if ((e = opt_in(paged_attn_kernel<DH, HG, true>, (int)At<DH>::smem(HG), done)) != cudaSuccess) return e;
+    int n = 0;
+    if ((e = clusters_at_once(paged_attn_kernel<DH, HG, true>, dim3(At<DH>::WARPS * 32), At<DH>::smem(HG), 1 << i, &n)) != cudaSuccess) return e;
+    room[i] = n > 0 ? n << i : attn_ctas(DH, sm_count);
+    if (dev < MAX_DEVICES) known[dev][i] = room[i];
+  }
+  return cudaSuccess;
 }
 
 // CTAs of a cluster that share a (sequence, kv head), 0: the units are shared out over all CTAs and joined in a second launch.  The cheaper
 // by a count of the units that follow one another: a CTA's own, as many times as there are turns of CTAs, or those that memory delivers in that
-// time, whichever is more; 4 for a launch and 8 for two; a 128th for each CTA in a cluster, which are started one after the other; and of
-// clusters of 8 three quarters find room.  Measured (us, caches of one length, clusters of 8 / the best smaller one / shared out):
-// 8/2 x 128: 1 x 1024 4.4 / 5.5 / 5.9, 1 x 8192 14 / 25 / 8.0, 16 x 2048 7.3 / 8.3 / 11.8, 64 x 512 17 / 6.7 / 11.1, 256 x 2048 120 / 79 / 90.
+// time, whichever is more; 4 for a launch and 8 for two; and a 128th for each CTA in a cluster, which are started one after the other.
+// Measured (us, caches of one length, clusters of 8 / the best smaller one / shared out), 8/2 x 128: 1 x 1024 4.4 / 5.5 / 5.9, 1 x 8192 14 / 25 / 8.0,
+// 16 x 2048 7.3 / 8.3 / 11.8, 64 x 512 17 / 6.7 / 11.1, 256 x 2048 120 / 79 / 90; from memory 12 x 16384 35 / 41 / 39, 16 x 16384 43 / 48 / 49,
+// 18 x 16384 (288 CTAs in clusters of 8 are more than find room) 61 / 52 / 53, 32 x 16384 83 / 80 / 85.
 template <int DH>
-int join_ranks(const PaArgs& a, int sm_count) {
+int join_ranks(const PaArgs& a, int sm_count, const int* room) {
   const long long groups = (long long)a.hk * a.n_grp, runs = groups * a.B, resident = attn_ctas(DH, sm_count);
   const long long tiles = (a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT;
   const long long flow = runs * tiles / (DH == 256 ? 80 : 160);             // (a unit is 64 KB at 256 channels, else 32 KB)
   auto larger = [](long long x, long long y) { return x > y ? x : y; };
   long long best = 128 * (8 + larger((runs * tiles + resident - 1) / resident, flow));
   int ranks = 0;
-  for (int n = 1; n <= 8; n *= 2) {
-    const long long room = n == 8 ? resident * 3 / 4 : resident, turns = (runs * n + room - 1) / room;
+  for (int i = 0; i < PA_SIZES; ++i) {
+    const long long n = 1 << i, turns = (runs * n + room[i] - 1) / room[i];
     const long long cost = 128 * (4 + larger(turns * ((tiles + n - 1) / n), flow)) + (n > 1 ? runs * n : 0);
-    if (cost < best) { best = cost; ranks = n; }
+    if (cost < best) { best = cost; ranks = (int)n; }
   }
   return ranks;
 }
@@ -759,7 +780,9 @@ int launch_attention_dh(PaArgs a, int sm_count, long long* launches, cudaEvent_t
   cudaError_t e;
   if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
   const long long runs = (long long)a.B * a.hk * a.n_grp;
-  const int ranks = join_ranks<DH>(a, sm_count);
+  int room[PA_SIZES];
+  if ((e = a.heads <= 4 ? cluster_room<DH, 4>(sm_count, room) : cluster_room<DH, 8>(sm_count, room)) != cudaSuccess) return -(int)e;
+  const int ranks = join_ranks<DH>(a, sm_count, room);
   if (ranks > 0) {
     const dim3 grid((unsigned)ranks, (unsigned)(a.hk * a.n_grp), (unsigned)a.B);
     e = a.heads <= 4 ? launch_attn<DH, 4, true>(a, grid, ranks, st) : launch_attn<DH, 8, true>(a, grid, ranks, st);
