@@ -456,7 +456,9 @@ int cca_paged_workspace_size(const cca_handle* h, int64_t B, int64_t max_len, si
  * lse (device fp32 [B, h_q], may be null): the logarithm of the sum of the exponentials, for joining with attention over other rows.
  * A sequence without rows gets zeros, and -infinity.  A row whose page is missing is left out and the status word becomes 122.  max_len:
  * host-side bound, len[b] <= max_len <= max_pages * page_size; a sequence outside it is skipped (its output is left as it is) and the status word
- * becomes 122.  Places behind len[b] may hold anything.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE_TOO_SMALL, CUDA. */
+ * becomes 122.  Places behind len[b] may hold anything.  An infinite value makes its channel infinite, as long as its row's weight is not below
+ * 2^-126 of the largest: a smaller one may be 0, and the channel then no number.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT,
+ * WORKSPACE_TOO_SMALL, CUDA. */
 int cca_paged_attention(cca_handle* h, const void* q, void* o, float* lse, const cca_pages* pages, int64_t max_len, void* workspace,
                         size_t workspace_bytes, int64_t B, void* cuda_stream);
 

@@ -16,6 +16,9 @@ CCA_DEVINL uint32_t pack_bf16x2(float lo, float hi) {
 }
 CCA_DEVINL float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 CCA_DEVINL float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// A sum of weighted values from the weights' first parts and from what these left over: an infinite value makes the first infinite, and the second
+// no number wherever nothing, or less than nothing, was left over.
+CCA_DEVINL float both_parts(float first, float rest) { return fabsf(first) == INFINITY ? first : first + rest; }
 CCA_DEVINL void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -453,10 +456,10 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
         float v = o[0][mt][c];
         const int ch = mt * 16 + g + 8 * (c >> 1);
         if (HG == 4) {
-          v += __shfl_xor_sync(0xffffffffu, v, 2);
+          v = both_parts(v, __shfl_xor_sync(0xffffffffu, v, 2));      // (used where t < 2, whose columns are the first parts)
           if (t < 2) so[(2 * t + (c & 1)) * S::OLD + ch] = v;
         } else {
-          so[(2 * t + (c & 1)) * S::OLD + ch] = v + o[PARTS - 1][mt][c];
+          so[(2 * t + (c & 1)) * S::OLD + ch] = both_parts(v, o[PARTS - 1][mt][c]);
         }
       }
     if (t == 0) sm_ml[warp][g] = make_float2(top, sum);
