@@ -400,7 +400,7 @@ typedef struct {
   int32_t* table;       /* int32 [B, max_pages]: page numbers, -1 where there is none                                 */
   int32_t* len;         /* int32 [B]: rows held; cca_pages_fork and cca_pages_free alone write it.  Negative: the sequence is not in use,
                            and calls that go by its length skip it: nothing of it is written, its output is left as it is (the
-                           step's: undefined), and that is no error                                                   */
+                           step's: undefined, rows read: zeros), and that is no error                                  */
   int64_t n_pages, page_size, max_pages;
 } cca_pages;
 
@@ -444,8 +444,8 @@ int cca_pages_compact(cca_handle* h, const cca_pages* pages, int32_t* used, void
 int cca_paged_append(cca_handle* h, const void* k, const void* v, const int32_t* count, const cca_pages* pages, int64_t B, int64_t n,
                      void* cuda_stream);
 
-/* Rows first[b] .. first[b] + n - 1 (len[b] .. where `first` is null): k, v device bf16 [B, n, h_k, d_h]; zeros for rows without a page.
- * Errors as above. */
+/* Rows first[b] .. first[b] + n - 1 (len[b] .. where `first` is null): k, v device bf16 [B, n, h_k, d_h]; zeros for rows without a page and,
+ * where `first` is null, for all n of a sequence that is not in use.  Errors as above. */
 int cca_paged_read(cca_handle* h, const cca_pages* pages, const int32_t* first, void* k, void* v, int64_t B, int64_t n, void* cuda_stream);
 
 /* Bytes of device workspace that one cca_paged_attention call needs for sequences of at most max_len rows, of B sequences or fewer.

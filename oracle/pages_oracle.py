@@ -52,7 +52,7 @@ class Pool:
     def read(self, n, first=None):
         out = torch.zeros(2, len(self.table), n, self.k.shape[1], self.k.shape[3], dtype=torch.bfloat16)
         for b in range(len(self.table)):
-            for i in range(n):
+            for i in range(n if first is not None or self.len[b] >= 0 else 0):       # (not in use: zeros)
                 at = self.place(b, (self.len if first is None else first)[b] + i)
                 if at is not None:
                     out[0, b, i], out[1, b, i] = self.k[at[0], :, at[1]], self.v[at[0], :, at[1]]

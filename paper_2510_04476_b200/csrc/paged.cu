@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(RW_THREADS) paged_rows_kernel(RowsArgs a) {
     if (APPEND && a.count) n = min(n, (long long)max(a.count[b], 0));
     if (i < n) {
       const long long row = held + i, most = (long long)a.c.max_pages * a.c.P;
-      if (row >= 0 && row < most && (held >= 0 || !APPEND)) {
+      if (row >= 0 && row < most && (held >= 0 || a.first)) {      // (a negative length: not in use; a negative start is one like others)
         const int pi = page_index(a.c, (int)row), page = page_at(a.c, b, pi);
         if (page >= 0 && (!APPEND || a.c.refs[page] == 1)) to = pool_row(a.c, a.hk, page, 0, (int)row - pi * a.c.P);
       }
