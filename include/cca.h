@@ -476,7 +476,8 @@ int cca_decode_workspace_size_paged(const cca_handle* h, int64_t B, int64_t max_
 int cca_decode_step_paged(cca_handle* h, const cca_weights* w, const void* x, void* out, const cca_paged_decode_state* state,
                           int64_t max_len, void* workspace, size_t workspace_bytes, int64_t B, void* cuda_stream);
 /* cca_decode_state_from_prefill for a cache in pages: appends the S keys and values of each sequence, for whose rows pages are reserved and whose len
- * must be 0 for them to be the tokens' own, and fills the history and previous input.  The caller then sets len = S. */
+ * must be 0 for them to be the tokens' own, and fills the history and previous input.  The caller then sets len = S.  Nothing is written of a
+ * sequence whose len is negative, no history either. */
 int cca_decode_state_from_prefill_paged(cca_handle* h, const void* x, const void* workspace, size_t workspace_bytes, int64_t B,
                                         int64_t S, const cca_paged_decode_state* state, void* cuda_stream);
 

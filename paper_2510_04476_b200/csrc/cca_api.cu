@@ -1558,7 +1558,8 @@ int cca_decode_state_from_prefill_paged(cca_handle* h, const void* x, const void
   r = enqueued(h, launch_paged_append(make_dims(c, B, 1), (const bf16*)(ws + l.k), (const bf16*)(ws + l.v), nullptr, make_pages(&s->pages), S,
                                       h->d_status, &h->launches, (cudaStream_t)cuda_stream));
   if (r != CCA_OK) return r;
-  return copy_token_state(h, d, l, x, ws, B, S, s->x_prev, s->qk0_hist, (cudaStream_t)cuda_stream);
+  return enqueued(h, launch_paged_token_state(d, make_pages(&s->pages), (const bf16*)x, (const float*)(ws + l.qk0), (bf16*)s->x_prev,
+                                              (float*)s->qk0_hist, &h->launches, (cudaStream_t)cuda_stream));
 }
 
 }  // extern "C"

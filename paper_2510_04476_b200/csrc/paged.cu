@@ -127,6 +127,26 @@ __global__ void __launch_bounds__(RW_THREADS) paged_rows_kernel(RowsArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------ from a prefill to the first step
+struct TsArgs {
+  const int* len;
+  const uint4 *x, *qk0;           // [B, S] rows of x_chunks and l_chunks 16-byte pieces
+  uint4 *x_prev, *hist;           // [B] and [B, pad] rows
+  int S, pad, x_chunks, l_chunks;
+};
+// A row a block: row r < pad of the history is token S - pad + r's latent, row pad the last token's input.  A few KB a sequence: bound by the launch.
+constexpr int TS_THREADS = 256;
+__global__ void __launch_bounds__(TS_THREADS) paged_token_state_kernel(TsArgs a) {
+  pdl_enter();
+  const int b = blockIdx.y, r = blockIdx.x;
+  if (a.len[b] < 0) return;                                 // not in use
+  const bool input = r == a.pad;
+  const int chunks = input ? a.x_chunks : a.l_chunks, token = input ? a.S - 1 : a.S - a.pad + r;
+  const uint4* from = (input ? a.x : a.qk0) + ((size_t)b * a.S + max(token, 0)) * chunks;
+  uint4* to = input ? a.x_prev + (size_t)b * chunks : a.hist + ((size_t)b * a.pad + r) * chunks;
+  for (int i = threadIdx.x; i < chunks; i += TS_THREADS) to[i] = token >= 0 ? from[i] : make_uint4(0, 0, 0, 0);
+}
+
 // ------------------------------------------------------------------------------------------------ attention
 struct PaArgs {
   Paged c;
@@ -826,6 +846,17 @@ int launch_paged_read(const CcaDims& d, const Paged& c, const int* first, bf16* 
   a.c = c; a.B = d.B; a.hk = d.hk; a.row_chunks = d.dh / 8; a.k_out = k; a.v_out = v; a.first = first; a.n = n;
   const cudaError_t e = launch_pdl(paged_rows_kernel<false>, dim3((unsigned)((n + RW_TOKENS - 1) / RW_TOKENS), (unsigned)d.B),
                                    dim3(RW_THREADS), st, a);
+  if (e != cudaSuccess) return -(int)e;
+  ++*launches;
+  return 0;
+}
+
+int launch_paged_token_state(const CcaDims& d, const Paged& c, const bf16* x, const float* qk0, bf16* x_prev, float* hist, long long* launches,
+                             cudaStream_t st) {
+  const int pad = d.k_seq + d.k_ch - 2;                     // (d_model is a multiple of 8, a latent row of 4)
+  const TsArgs a{c.len, reinterpret_cast<const uint4*>(x), reinterpret_cast<const uint4*>(qk0), reinterpret_cast<uint4*>(x_prev),
+                 reinterpret_cast<uint4*>(hist), d.S, pad, d.E / 8, d.L / 4};
+  const cudaError_t e = launch_pdl(paged_token_state_kernel, dim3((unsigned)(pad + 1), (unsigned)d.B), dim3(TS_THREADS), st, a);
   if (e != cudaSuccess) return -(int)e;
   ++*launches;
   return 0;

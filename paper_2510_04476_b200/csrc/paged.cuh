@@ -31,6 +31,10 @@ int launch_paged_append(const CcaDims& d, const bf16* k, const bf16* v, const in
                         long long* launches, cudaStream_t st);
 int launch_paged_read(const CcaDims& d, const Paged& c, const int* first, bf16* k, bf16* v, long long n, long long* launches,
                       cudaStream_t st);
+// What a decode step needs of the tokens before it besides keys and values, from a forward's input x [B, S, E] and saved q0|k0 latent [B, S, L]: the last
+// input and the last `pad` latent rows (zeros before the first), of the sequences that are in use.
+int launch_paged_token_state(const CcaDims& d, const Paged& c, const bf16* x, const float* qk0, bf16* x_prev, float* hist, long long* launches,
+                             cudaStream_t st);
 size_t paged_workspace_bytes(const CcaDims& d, int max_len, int sm_count);
 // Rows 0 .. len[b] + extra - 1.  q: bf16 or, where q32 is set, fp32 rounded to bf16 on the way in.  lse may be null.
 int launch_paged_attention(const CcaDims& d, const bf16* q, const float* q32, bf16* o, float* lse, const Paged& c, int extra, int max_len,
