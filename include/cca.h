@@ -420,8 +420,8 @@ int cca_pages_reserve(cca_handle* h, const cca_pages* pages, int64_t n, const in
 
 /* Sequence child[i] becomes what sequence parent[i] was before the call, i < n <= B (device int32 [n]): it holds the pages of the parent's
  * len rows too (none that were reserved behind them), its own former pages are let go.  A sequence that is its own parent is left as it is; where
- * several pairs have the same child the last one counts; a pair with an index outside [0, B), or whose parent's length is negative or has no
- * room in the table, is skipped and the status word becomes 122.  The rest of a decode state (history, previous input) is the caller's to
+ * several pairs have the same child the last one counts.  A pair with an index outside [0, B), or whose parent's length is negative or has no
+ * room in the table, is skipped, as if it were not there, and the status word becomes 122.  The rest of a decode state (history, previous input) is the caller's to
  * copy.  Errors as above. */
 int cca_pages_fork(cca_handle* h, const cca_pages* pages, const int32_t* parent, const int32_t* child, int64_t n, void* workspace,
                    size_t workspace_bytes, int64_t B, void* cuda_stream);

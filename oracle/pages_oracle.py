@@ -101,9 +101,10 @@ class Pool:
             if not (0 <= p < B and 0 <= c < B):
                 status = MISSING
                 continue
-            fits = 0 <= self.len[p] <= self.wide * self.P
-            status = status if fits else MISSING
-            todo[c] = p if fits and p != c else None
+            if not 0 <= self.len[p] <= self.wide * self.P:
+                status = MISSING
+                continue
+            todo[c] = p if p != c else None
         held = {p: [e if i * self.P < self.len[p] and 0 <= e < self.n_pages else -1 for i, e in enumerate(self.table[p])]
                 for p in todo.values() if p is not None}
         rows = {c: (held[p], self.len[p]) for c, p in todo.items() if p is not None}

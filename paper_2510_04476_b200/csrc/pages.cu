@@ -433,18 +433,18 @@ struct AnyOfWarp {
 template <typename Any>
 CCA_DEVINL int fork_read(const FkArgs& a, int x, int tid, int threads, Any any) {
   const int p = a.parent[x], c = a.child[x];
-  const bool inside = (unsigned)p < (unsigned)a.B && (unsigned)c < (unsigned)a.B;
-  int len = inside ? __ldcg(a.c.len + p) : -1;
+  auto rows = [&](int parent) {                                // -1: a pair with this parent is skipped
+    const int n = (unsigned)parent < (unsigned)a.B ? __ldcg(a.c.len + parent) : -1;
+    return n <= (long long)a.c.max_pages * a.c.P ? n : -1;
+  };
+  const int len = (unsigned)c < (unsigned)a.B ? rows(p) : -1;
   bool later = false;                                          // another pair has the same child: the last one counts
   const int group = any.threads;
   for (int y = x + 1 + tid % group; y < a.n; y += group)
-    if (a.child[y] == c && (unsigned)a.parent[y] < (unsigned)a.B) later = true;
+    if (a.child[y] == c && rows(a.parent[y]) >= 0) later = true;
   later = any(later);
-  const long long held = len < 0 ? 0 : ((long long)len + a.c.P - 1) / a.c.P;
-  if (len < 0 || held > a.c.max_pages) {
-    if (tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
-    len = -1;
-  }
+  if (len < 0 && tid == 0) atomicCAS(a.status, 0, ST_PAGE_MISSING);
+  const int held = len > 0 ? (len - 1) / a.c.P + 1 : 0;
   const bool go = len >= 0 && !later && p != c;
   if (!go) return -1;
   for (int i0 = tid; i0 < a.c.max_pages; i0 += FK_EACH * threads) {
