@@ -4,6 +4,7 @@
 #include "cluster.cuh"
 #include "common.cuh"
 #include "paged.cuh"
+#include "paged_rule.h"
 #include "pdl.cuh"
 
 namespace {
@@ -746,10 +747,9 @@ cudaError_t launch_attn(const PaArgs& a, dim3 grid, int ranks, cudaStream_t st) 
   return launch_pdl_smem(paged_attn_kernel<DH, HG, JOINED>, grid, dim3(At<DH>::WARPS * 32), At<DH>::smem(HG), st, a);
 }
 
-// CTAs of clusters of 1, 2, 4 and 8 that find room on the device at once (a cluster lies within a part of it), asked for once a device.
-constexpr int PA_SIZES = 4;
+// CTAs of clusters of 1, 2, 4 and 8 that find room on the device at once (a cluster lies within a part of it), asked for once a device; -1: not even one.
 template <int DH, int HG>
-cudaError_t cluster_room(int sm_count, int* room) {
+cudaError_t cluster_room(int* room) {
   static int known[MAX_DEVICES][PA_SIZES];                     // 0: not asked
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -757,36 +757,14 @@ cudaError_t cluster_room(int sm_count, int* room) {
   static bool done[MAX_DEVICES];
   for (int i = 0; i < PA_SIZES; ++i) {
     room[i] = dev < MAX_DEVICES ? known[dev][i] : 0;
-    if (room[i] > 0) continue;
+    if (room[i] != 0) continue;
     if ((e = opt_in(paged_attn_kernel<DH, HG, true>, (int)At<DH>::smem(HG), done)) != cudaSuccess) return e;
     int n = 0;
     if ((e = clusters_at_once(paged_attn_kernel<DH, HG, true>, dim3(At<DH>::WARPS * 32), At<DH>::smem(HG), 1 << i, &n)) != cudaSuccess) return e;
-    room[i] = n > 0 ? n << i : attn_ctas(DH, sm_count);
+    room[i] = cluster_ctas(n, 1 << i);
     if (dev < MAX_DEVICES) known[dev][i] = room[i];
   }
   return cudaSuccess;
-}
-
-// CTAs of a cluster that share a (sequence, kv head), 0: the units are shared out over all CTAs and joined in a second launch.  The cheaper
-// by a count of the units that follow one another: a CTA's own, as many times as there are turns of CTAs, or those that memory delivers in that
-// time, whichever is more; 4 for a launch and 8 for two; and a 128th for each CTA in a cluster, which are started one after the other.
-// Measured (us, caches of one length, clusters of 8 / the best smaller one / shared out), 8/2 x 128: 1 x 1024 4.4 / 5.5 / 5.9, 1 x 8192 14 / 25 / 8.0,
-// 16 x 2048 7.3 / 8.3 / 11.8, 64 x 512 17 / 6.7 / 11.1, 256 x 2048 120 / 79 / 90; from memory 12 x 16384 35 / 41 / 39, 16 x 16384 43 / 48 / 49,
-// 18 x 16384 (288 CTAs in clusters of 8 are more than find room) 61 / 52 / 53, 32 x 16384 83 / 80 / 85.
-template <int DH>
-int join_ranks(const PaArgs& a, int sm_count, const int* room) {
-  const long long groups = (long long)a.hk * a.n_grp, runs = groups * a.B, resident = attn_ctas(DH, sm_count);
-  const long long tiles = (a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT;
-  const long long flow = runs * tiles / (DH == 256 ? 80 : 160);             // (a unit is 64 KB at 256 channels, else 32 KB)
-  auto larger = [](long long x, long long y) { return x > y ? x : y; };
-  long long best = 128 * (8 + larger((runs * tiles + resident - 1) / resident, flow));
-  int ranks = 0;
-  for (int i = 0; i < PA_SIZES; ++i) {
-    const long long n = 1 << i, turns = (runs * n + room[i] - 1) / room[i];
-    const long long cost = 128 * (4 + larger(turns * ((tiles + n - 1) / n), flow)) + (n > 1 ? runs * n : 0);
-    if (cost < best) { best = cost; ranks = (int)n; }
-  }
-  return ranks;
 }
 
 // Few parts a run: a warp for a head, 16 parts of 32 channels at once.  Many: a CTA for a head, 256 parts of 8 channels.
@@ -804,13 +782,14 @@ int launch_attention_dh(PaArgs a, int sm_count, long long* launches, cudaEvent_t
   if (ev_begin && (e = cudaEventRecord(ev_begin, st)) != cudaSuccess) return -(int)e;
   const long long runs = (long long)a.B * a.hk * a.n_grp;
   int room[PA_SIZES];
-  if ((e = a.heads <= 4 ? cluster_room<DH, 4>(sm_count, room) : cluster_room<DH, 8>(sm_count, room)) != cudaSuccess) return -(int)e;
-  const int ranks = join_ranks<DH>(a, sm_count, room);
+  if ((e = a.heads <= 4 ? cluster_room<DH, 4>(room) : cluster_room<DH, 8>(room)) != cudaSuccess) return -(int)e;
+  const long long tiles = (a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT;
+  const int ranks = paged_join_ranks(DH, runs, tiles, attn_ctas(DH, sm_count), room);
   if (ranks > 0) {
     const dim3 grid((unsigned)ranks, (unsigned)(a.hk * a.n_grp), (unsigned)a.B);
     e = a.heads <= 4 ? launch_attn<DH, 4, true>(a, grid, ranks, st) : launch_attn<DH, 8, true>(a, grid, ranks, st);
   } else {
-    const long long units = runs * ((a.max_len + At<DH>::UNIT - 1) / At<DH>::UNIT), most = attn_ctas(DH, sm_count);
+    const long long units = runs * tiles, most = attn_ctas(DH, sm_count);
     a.ctas = (int)(units < most ? units : most);
     const dim3 grid((unsigned)a.ctas);
     e = a.heads <= 4 ? launch_attn<DH, 4, false>(a, grid, 0, st) : launch_attn<DH, 8, false>(a, grid, 0, st);
