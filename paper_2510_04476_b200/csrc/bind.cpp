@@ -423,6 +423,7 @@ PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const cca_pages c = pages_of(a[1], h, &B);
     const int64_t rows = whole(a[2]);
     if (rows < 0) refuse("cca_paged_read: invalid argument");
+    if (rows > (int64_t)1 << 24 || B * rows > (int64_t)1 << 30) check(CCA_ERR_UNSUPPORTED, h, "cca_paged_read");      // (before memory is asked for)
     const int32_t* first = optional_ints(a[3], "first", {B}, h);
     at::Tensor k = fresh({B, rows, h->hk, h->dh}, at::kBFloat16, h), v = fresh({B, rows, h->hk, h->dh}, at::kBFloat16, h);
     check(cca_paged_read(h->h, &c, first, k.data_ptr(), v.data_ptr(), B, rows, stream(h)), h, "cca_paged_read");
