@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(At<DH>::WARPS * 32, At<DH>::CTAS) paged_attn_k
 
 // Joins the partial results of a run of units that several CTAs shared, 4 CL channels of one head, in a fixed order, so the same every
 // time.  Which run: the x-th (sequence, kv head) or, where there are more of those than CTAs, the one that begins in CTA x of the attention
-// and is not over there.  That is worked out from the lengths while the attention is still running; it wrote none of them.  A slice of
+// and is not over there.  That is worked out from the lengths while the attention is still running (pdl.cuh says why they can be read).  A slice of
 // CL lanes takes one part at a time, four channels a lane; a head's slices are those of a warp (ONE) or of the CTA.
 constexpr int PJ_WARPS = 4, PJ_THREADS = PJ_WARPS * 32;
 template <int DH, int CL, bool ONE>

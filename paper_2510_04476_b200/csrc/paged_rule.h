@@ -15,6 +15,8 @@ inline int cluster_ctas(int n, int size) { return n > 0 ? n * size : -1; }
 // Measured (us, caches of one length, clusters of 8 / the best smaller one / shared out), 8/2 x 128: 1 x 1024 4.4 / 5.5 / 5.9, 1 x 8192 14 / 25 / 8.0,
 // 16 x 2048 7.3 / 8.3 / 11.8, 64 x 512 17 / 6.7 / 11.1, 256 x 2048 120 / 79 / 90; from memory 12 x 16384 35 / 41 / 39, 16 x 16384 43 / 48 / 49,
 // 18 x 16384 (288 CTAs in clusters of 8 are more than find room) 61 / 52 / 53, 32 x 16384 83 / 80 / 85.
+// The lengths are on the device: the rule takes the bound for every sequence.  Where one is long and the others are short, a cluster's CTAs work through the
+// long one while the others have nothing left: one of 16384 rows and 31 (63) of 64 to 500 under that bound take 40 (74) us, the long one alone 10.
 inline int paged_join_ranks(int dh, long long runs, long long tiles, long long resident, const int* room) {
   const long long flow = runs * tiles / (dh == 256 ? 80 : 160);             // (a unit is 64 KB at 256 channels, else 32 KB)
   auto larger = [](long long x, long long y) { return x > y ? x : y; };

@@ -6,6 +6,9 @@
 // CTAs have started, and waits for the kernel before it (completion and visibility of its writes) before it touches
 // global memory.  The wait comes first in every CTA, also in those that return early, so that "kernel N complete"
 // always implies "kernel N - 1 complete".
+// One kernel reads before its wait: the join of attention over pages reads the sequences' lengths.  It is always launched behind the attention kernel,
+// which does not write them, and whose CTAs release their dependents only behind their own wait, so whatever wrote the lengths is complete
+// before a CTA of the join starts.  That rests on the order of the two instructions in pdl_enter.
 CCA_DEVINL void pdl_enter() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
